@@ -1,0 +1,267 @@
+// C ABI of the target's operators (include/qlin_target.h): argument checks,
+// plans and launches.
+
+#include "../../include/qlin_target.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+
+#include "qlin_internal.h"
+#include "target_internal.h"
+
+using namespace qlin;
+
+namespace {
+
+constexpr int64_t kMaxSeq = 65536, kMaxRows = (int64_t)1 << 22, kMaxLen = (int64_t)1 << 28, kMaxSlots = (int64_t)1 << 40;
+constexpr int64_t kMaxHeads = 4096, kMaxGroup = 64, kMaxSplits = 256, kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxDraft = 64, kMaxVocab = (int64_t)1 << 24;
+constexpr int64_t kMaxRowStride = (int64_t)1 << 32;
+constexpr int64_t kMaxExtent = (int64_t)1 << 60;      // elements of one strided array
+
+// An address range, in bytes.
+struct Range { uintptr_t lo; size_t bytes; };
+
+bool overlap(const Range &a, const Range &b) { return a.bytes && b.bytes && a.lo < b.lo + b.bytes && b.lo < a.lo + a.bytes; }
+
+Range rows_range(const void *p, int64_t rows, int64_t stride, int64_t width) {
+    return Range{(uintptr_t)p, rows > 0 ? (size_t)((rows - 1) * stride + width) * 2 : 0};
+}
+
+Range cache_range(const void *p, const qlin_kv_cache *c) {
+    return Range{(uintptr_t)p, (size_t)((c->slots - 1) * c->token_stride + (c->heads - 1) * c->head_stride + kHeadDim) * 2};
+}
+
+bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+int check_batch(const qlin_batch *b) {
+    if (!b) return fail(QLIN_ERR_INVALID, "NULL batch");
+    if (b->n_seq < 1 || b->rows < 0 || b->max_new < 0 || b->max_new > b->rows || b->max_len < 0)
+        return fail(QLIN_ERR_INVALID, "n_seq must be positive, rows >= 0, max_new in [0, rows], max_len >= 0");
+    if (b->n_seq > kMaxSeq || b->rows > kMaxRows || b->max_len > kMaxLen)
+        return fail(QLIN_ERR_UNSUPPORTED, "at most 65536 sequences, 2^22 rows and 2^28 cached tokens");
+    return QLIN_OK;
+}
+
+int check_batch_arrays(const qlin_batch *b) {
+    if (!b->new_start || !b->length) return fail(QLIN_ERR_INVALID, "NULL new_start or length");
+    if (!aligned(b->new_start, 4) || !aligned(b->length, 4) || !aligned(b->cache_start, 8))
+        return fail(QLIN_ERR_ALIGN, "new_start and length must be 4-byte aligned, cache_start 8");
+    return QLIN_OK;
+}
+
+int check_heads(int64_t q_heads, int64_t kv_heads, int64_t head_dim) {
+    if (q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads)
+        return fail(QLIN_ERR_INVALID, "query and key/value heads must be positive, the first a multiple of the second");
+    if (head_dim != kHeadDim) return fail(QLIN_ERR_UNSUPPORTED, "head_dim must be 128 (got %lld)", (long long)head_dim);
+    if (q_heads > kMaxHeads) return fail(QLIN_ERR_UNSUPPORTED, "at most 4096 query heads");
+    if (q_heads / kv_heads > kMaxGroup) return fail(QLIN_ERR_UNSUPPORTED, "at most 64 query heads per key/value head");
+    return QLIN_OK;
+}
+
+int check_cache(const qlin_kv_cache *c) {
+    if (!c) return fail(QLIN_ERR_INVALID, "NULL cache");
+    if (c->slots < 1 || c->seq_slots < 0 || c->token_stride < kHeadDim || c->head_stride < kHeadDim)
+        return fail(QLIN_ERR_INVALID, "cache: slots must be positive, seq_slots >= 0, strides >= 128");
+    if (c->token_stride % 8 || c->head_stride % 8) return fail(QLIN_ERR_ALIGN, "cache strides must be multiples of 8");
+    if (c->slots > kMaxSlots || c->seq_slots > kMaxSlots || c->token_stride > kMaxStride || c->head_stride > kMaxStride ||
+        (double)c->slots * (double)c->token_stride + (double)c->heads * (double)c->head_stride > (double)kMaxExtent)
+        return fail(QLIN_ERR_UNSUPPORTED, "cache too large");
+    if (!c->k || !c->v) return fail(QLIN_ERR_INVALID, "NULL cache");
+    if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(QLIN_ERR_ALIGN, "the cache must be 16-byte aligned");
+    return QLIN_OK;
+}
+
+// Row arrays of `width` elements: stride and alignment.
+int check_rows(const void *p, int64_t stride, int64_t width, const char *name) {
+    if (!p) return fail(QLIN_ERR_INVALID, "NULL %s", name);
+    if (stride < width || stride > kMaxRowStride) return fail(QLIN_ERR_INVALID, "%s: stride must be at least %lld", name, (long long)width);
+    if (stride % 8 || !aligned(p, 16)) return fail(QLIN_ERR_ALIGN, "%s must be 16-byte aligned, its stride a multiple of 8", name);
+    return QLIN_OK;
+}
+
+BatchArgs batch_args(const qlin_batch *b, const qlin_kv_cache *c) {
+    BatchArgs a;
+    a.new_start = b->new_start;
+    a.length = b->length;
+    a.cache_start = b->cache_start;
+    a.slots = c->slots;
+    a.seq_slots = c->seq_slots;
+    a.tok = c->token_stride;
+    a.head = c->head_stride;
+    a.n_seq = (int)b->n_seq;
+    a.rows = (int)b->rows;
+    a.max_new = (int)b->max_new;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qlin_norm_rope_append(const qlin_batch *batch, const qlin_kv_cache *cache, int64_t q_heads, int64_t head_dim,
+                          const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride,
+                          const uint16_t *v, int64_t v_stride, const uint16_t *q_norm, const uint16_t *k_norm,
+                          float eps, const double *inv_freq, int64_t rotary_dim, int interleaved, uint16_t *q_out,
+                          int64_t q_out_stride, void *stream) {
+    clear_err();
+    if (check_batch(batch) != QLIN_OK) return last_status();
+    if (!cache) return fail(QLIN_ERR_INVALID, "NULL cache");
+    if (check_heads(q_heads, cache->heads, head_dim) != QLIN_OK) return last_status();
+    if (check_cache(cache) != QLIN_OK) return last_status();
+    if (rotary_dim < 0 || rotary_dim > kHeadDim || rotary_dim % 16)
+        return fail(QLIN_ERR_INVALID, "rotary_dim must be a multiple of 16 in [0, 128]");
+    if (!(eps >= 0.0f) || std::isinf(eps)) return fail(QLIN_ERR_INVALID, "eps must be >= 0");
+    if (batch->rows == 0) return QLIN_OK;
+    if (check_batch_arrays(batch) != QLIN_OK) return last_status();
+    const int64_t wq = q_heads * kHeadDim, wk = cache->heads * kHeadDim, M = batch->rows;
+    if (check_rows(q, q_stride, wq, "q") != QLIN_OK || check_rows(k, k_stride, wk, "k") != QLIN_OK ||
+        check_rows(v, v_stride, wk, "v") != QLIN_OK || check_rows(q_out, q_out_stride, wq, "q_out") != QLIN_OK)
+        return last_status();
+    if (rotary_dim && !inv_freq) return fail(QLIN_ERR_INVALID, "NULL inv_freq");
+    if (!aligned(q_norm, 8) || !aligned(k_norm, 8) || !aligned(inv_freq, 8))
+        return fail(QLIN_ERR_ALIGN, "norm weights and inv_freq must be 8-byte aligned");
+    const Range rq = rows_range(q, M, q_stride, wq), rk = rows_range(k, M, k_stride, wk), rv = rows_range(v, M, v_stride, wk);
+    const Range ro = rows_range(q_out, M, q_out_stride, wq), ck = cache_range(cache->k, cache), cv = cache_range(cache->v, cache);
+    if ((overlap(ro, rq) && !(q_out == q && q_out_stride == q_stride)) || overlap(ro, ck) || overlap(ro, cv))
+        return fail(QLIN_ERR_INVALID, "q_out overlaps q (without being it) or the cache");
+    // in place, q_out lies in the rows of a fused projection: k and v between its rows are no overlap
+    if (q_out != q && (overlap(ro, rk) || overlap(ro, rv))) return fail(QLIN_ERR_INVALID, "q_out overlaps k or v");
+    for (const Range &r : {rq, rk, rv})
+        if (overlap(r, ck) || overlap(r, cv)) return fail(QLIN_ERR_INVALID, "q, k or v overlaps the cache");
+
+    AppendArgs a;
+    a.b = batch_args(batch, cache);
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.q_norm = q_norm;
+    a.k_norm = k_norm;
+    a.inv_freq = inv_freq;
+    a.q_out = q_out;
+    a.kc = cache->k;
+    a.vc = cache->v;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_out_stride = q_out_stride;
+    a.eps = eps;
+    a.Hq = (int)q_heads;
+    a.Hkv = (int)cache->heads;
+    a.half = (int)rotary_dim / 2;
+    a.interleaved = interleaved != 0;
+    const hipError_t e = launch_append(a, (hipStream_t)stream);
+    return e == hipSuccess ? QLIN_OK : hip_fail(e, "append launch");
+}
+
+int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t splits,
+                     int64_t *splits_out, int64_t *workspace_bytes, char *buf, int64_t buflen) {
+    clear_err();
+    if (check_batch(batch) != QLIN_OK || check_heads(q_heads, kv_heads, head_dim) != QLIN_OK) return last_status();
+    if (splits < 0 || splits > kMaxSplits) return fail(QLIN_ERR_INVALID, "splits must be in [0, 256]");
+    if (splits_out) *splits_out = 1;
+    if (workspace_bytes) *workspace_bytes = 0;
+    if (buf && buflen > 0) snprintf(buf, (size_t)buflen, "kernel=k_causal_row splits=1 combine=0");
+    return QLIN_OK;
+}
+
+int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, int64_t q_heads, int64_t head_dim,
+                          float scale, int64_t splits, const uint16_t *q, int64_t q_stride, uint16_t *out,
+                          int64_t out_stride, void *workspace, int64_t workspace_bytes, void *stream) {
+    clear_err();
+    if (check_batch(batch) != QLIN_OK) return last_status();
+    if (!cache) return fail(QLIN_ERR_INVALID, "NULL cache");
+    if (check_heads(q_heads, cache->heads, head_dim) != QLIN_OK) return last_status();
+    if (check_cache(cache) != QLIN_OK) return last_status();
+    if (splits < 0 || splits > kMaxSplits) return fail(QLIN_ERR_INVALID, "splits must be in [0, 256]");
+    if (!(scale >= 0.0f) || std::isinf(scale)) return fail(QLIN_ERR_INVALID, "scale must be positive and finite (or 0)");
+    if (workspace_bytes < 0) return fail(QLIN_ERR_INVALID, "workspace_bytes must be >= 0");
+    if (batch->rows == 0) return QLIN_OK;
+    if (check_batch_arrays(batch) != QLIN_OK) return last_status();
+    const int64_t w = q_heads * kHeadDim, M = batch->rows;
+    if (check_rows(q, q_stride, w, "q") != QLIN_OK || check_rows(out, out_stride, w, "out") != QLIN_OK) return last_status();
+    if (!aligned(workspace, 16)) return fail(QLIN_ERR_ALIGN, "workspace must be 16-byte aligned");
+    const Range rq = rows_range(q, M, q_stride, w), ro = rows_range(out, M, out_stride, w);
+    if (overlap(ro, rq) || overlap(ro, cache_range(cache->k, cache)) || overlap(ro, cache_range(cache->v, cache)))
+        return fail(QLIN_ERR_INVALID, "out overlaps q or the cache");
+
+    CausalArgs a;
+    a.b = batch_args(batch, cache);
+    a.q = q;
+    a.k = cache->k;
+    a.v = cache->v;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.Hq = (int)q_heads;
+    a.Hkv = (int)cache->heads;
+    a.G = (int)(q_heads / cache->heads);
+    a.c = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)kHeadDim)));
+    const hipError_t e = launch_causal(a, (hipStream_t)stream);
+    return e == hipSuccess ? QLIN_OK : hip_fail(e, "causal attention launch");
+}
+
+int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *workspace_bytes) {
+    clear_err();
+    if (n_seq < 0 || n_draft < 0 || vocab < 1) return fail(QLIN_ERR_INVALID, "n_seq and n_draft must be >= 0, vocab positive");
+    if (n_seq > kMaxSeq || n_draft > kMaxDraft || vocab > kMaxVocab)
+        return fail(QLIN_ERR_UNSUPPORTED, "at most 65536 sequences, 64 drafted tokens and 2^24 tokens of vocabulary");
+    if (workspace_bytes) *workspace_bytes = 0;
+    return QLIN_OK;
+}
+
+int qlin_verify_draft(int64_t n_seq, int64_t n_draft, int64_t vocab, const uint16_t *target, int64_t target_stride,
+                      const uint16_t *draft, int64_t draft_stride, const int32_t *drafted, const int32_t *count,
+                      const float *temperature, const float *uniform, int32_t *accepted, int32_t *tokens,
+                      void *workspace, int64_t workspace_bytes, void *stream) {
+    int64_t need = 0;
+    if (qlin_verify_plan(n_seq, n_draft, vocab, &need) != QLIN_OK) return last_status();
+    if (workspace_bytes < 0) return fail(QLIN_ERR_INVALID, "workspace_bytes must be >= 0");
+    if (n_seq == 0) return QLIN_OK;
+    if (!target || !uniform || !accepted || !tokens || (n_draft > 0 && !drafted))
+        return fail(QLIN_ERR_INVALID, "NULL target, drafted, uniform, accepted or tokens");
+    if (target_stride < vocab || target_stride > kMaxRowStride || (draft && (draft_stride < vocab || draft_stride > kMaxRowStride)))
+        return fail(QLIN_ERR_INVALID, "row strides must be at least vocab");
+    if (!aligned(target, 16) || !aligned(draft, 16) || !aligned(workspace, 16))
+        return fail(QLIN_ERR_ALIGN, "target, draft and workspace must be 16-byte aligned");
+    for (const void *p : {(const void *)drafted, (const void *)count, (const void *)temperature, (const void *)uniform,
+                          (const void *)accepted, (const void *)tokens})
+        if (!aligned(p, 4)) return fail(QLIN_ERR_ALIGN, "int32 and float arrays must be 4-byte aligned");
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(QLIN_ERR_INVALID, "workspace of %lld bytes needed (%lld given)", (long long)need,
+                    (long long)(workspace ? workspace_bytes : 0));
+    const size_t per = (size_t)n_seq * 4;
+    const Range outs[2] = {{(uintptr_t)accepted, per}, {(uintptr_t)tokens, per * (size_t)(n_draft + 1)}};
+    const Range ins[] = {rows_range(target, n_seq * (n_draft + 1), target_stride, vocab),
+                         rows_range(draft, draft ? n_seq * n_draft : 0, draft_stride, vocab),
+                         {(uintptr_t)drafted, per * (size_t)n_draft},
+                         {(uintptr_t)count, count ? per : 0},
+                         {(uintptr_t)temperature, temperature ? per : 0},
+                         {(uintptr_t)uniform, per * (size_t)(n_draft + 1)},
+                         {(uintptr_t)workspace, (size_t)need}};
+    for (const Range &o : outs)
+        for (const Range &i : ins)
+            if (overlap(o, i)) return fail(QLIN_ERR_INVALID, "accepted or tokens overlaps an input or the workspace");
+    if (overlap(outs[0], outs[1])) return fail(QLIN_ERR_INVALID, "accepted overlaps tokens");
+
+    VerifyArgs a;
+    a.target = target;
+    a.draft = draft;
+    a.drafted = drafted;
+    a.count = count;
+    a.temperature = temperature;
+    a.uniform = uniform;
+    a.accepted = accepted;
+    a.tokens = tokens;
+    a.target_stride = target_stride;
+    a.draft_stride = draft_stride;
+    a.n = (int)n_draft;
+    a.V = (int)vocab;
+    const hipError_t e = launch_verify(a, (int)n_seq, (hipStream_t)stream);
+    return e == hipSuccess ? QLIN_OK : hip_fail(e, "verify launch");
+}
+
+}  // extern "C"

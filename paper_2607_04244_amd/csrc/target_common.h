@@ -1,0 +1,39 @@
+// Device-side helpers shared by the target's kernels (append.hip, causal.hip):
+// a sequence's rows and slots, with every bound clamped.  Header-only, inline.
+#pragma once
+
+#include "device_common.h"
+#include "target_internal.h"
+
+namespace qlin {
+
+// Sequence b: its rows [row0, row0 + n), of which the first `rows` are computed, its
+// cached tokens L and the slot of token 0.  Whatever the arrays hold, rows stay in
+// [0, a.rows), and L is 0 unless slots [slot0, slot0 + L) are inside the cache.
+struct Seq {
+    int row0, n, rows, p0, L;
+    int64_t slot0;
+};
+
+__device__ inline Seq load_seq(const BatchArgs &a, int b) {
+    Seq s;
+    s.row0 = min(max(a.new_start[b], 0), a.rows);
+    s.n = min(max(a.new_start[b + 1], s.row0), a.rows) - s.row0;
+    s.rows = min(s.n, a.max_new);
+    const int L = max(a.length[b], 0);
+    s.p0 = L - s.n;                         // position of its first new token
+    s.slot0 = a.cache_start ? a.cache_start[b] : (int64_t)b * a.seq_slots;
+    s.L = s.slot0 >= 0 && s.slot0 <= a.slots - L ? L : 0;
+    return s;
+}
+
+// The sequence that row m belongs to (n_seq: padding), by the whole wave: the
+// number of sequences that end at or before m.
+__device__ inline int find_seq(const BatchArgs &a, int m, int lane) {
+    int b = 0;
+    for (int i = 0; i < a.n_seq; i += 64)
+        b += __popcll(__ballot(i + lane < a.n_seq && a.new_start[min(i + lane, a.n_seq - 1) + 1] <= m));
+    return b;
+}
+
+}  // namespace qlin

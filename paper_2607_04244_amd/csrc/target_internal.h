@@ -1,0 +1,56 @@
+// Internal interface between the C-ABI host code of the target's operators
+// (target_abi.cpp) and their HIP kernels (append.hip, causal.hip, verify.hip).
+// Not installed; the public ABI is include/qlin_target.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace qlin {
+
+constexpr int kHeadDim = 128;
+
+// The batch and the cache as the kernels take them (include/qlin_target.h).
+struct BatchArgs {
+    const int32_t *new_start, *length;
+    const int64_t *cache_start;     // or null: b * seq_slots
+    int64_t slots, seq_slots;
+    int64_t tok, head;              // elements between slots, between heads
+    int n_seq, rows, max_new;
+};
+
+struct AppendArgs {
+    BatchArgs b;
+    const uint16_t *q, *k, *v;
+    const uint16_t *q_norm, *k_norm;
+    const double *inv_freq;
+    uint16_t *q_out, *kc, *vc;
+    int64_t q_stride, k_stride, v_stride, q_out_stride;
+    float eps;
+    int Hq, Hkv, half, interleaved;
+};
+
+struct CausalArgs {
+    BatchArgs b;
+    const uint16_t *q, *k, *v;
+    uint16_t *out;
+    int64_t q_stride, out_stride;
+    int Hq, Hkv, G;
+    float c;                        // scale log2(e): scores to base-2 exponents
+};
+
+struct VerifyArgs {
+    const uint16_t *target, *draft;
+    const int32_t *drafted, *count;
+    const float *temperature, *uniform;
+    int32_t *accepted, *tokens;
+    int64_t target_stride, draft_stride;
+    int n, V;
+};
+
+hipError_t launch_append(const AppendArgs &a, hipStream_t st);
+hipError_t launch_causal(const CausalArgs &a, hipStream_t st);
+hipError_t launch_verify(const VerifyArgs &a, int n_seq, hipStream_t st);
+
+}  // namespace qlin
