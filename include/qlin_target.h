@@ -62,8 +62,8 @@ typedef struct qlin_kv_cache {
     uint16_t *k, *v;             /* DEVICE, 16-byte aligned */
     int64_t heads;               /* key/value heads */
     int64_t slots;               /* slots that may be addressed: s < slots, 1 .. 2^40 */
-    int64_t token_stride;        /* elements, >= 128, a multiple of 8 */
-    int64_t head_stride;         /* elements, >= 128, a multiple of 8 */
+    int64_t token_stride;        /* elements, 128 .. 2^28, a multiple of 8 */
+    int64_t head_stride;         /* elements, 128 .. 2^40, a multiple of 8 */
     int64_t seq_slots;           /* slots between sequences where cache_start is NULL, 0 .. 2^40 */
 } qlin_kv_cache;
 

@@ -19,6 +19,7 @@ namespace {
 constexpr int64_t kMaxSeq = 65536, kMaxRows = (int64_t)1 << 22, kMaxLen = (int64_t)1 << 28, kMaxSlots = (int64_t)1 << 40;
 constexpr int64_t kMaxHeads = 4096, kMaxGroup = 64, kMaxSplits = 256, kMaxStride = (int64_t)1 << 40;
 constexpr int64_t kMaxDraft = 64, kMaxVocab = (int64_t)1 << 24;
+constexpr int64_t kMaxTokenStride = (int64_t)1 << 28;       // 32-bit byte offsets over four tokens
 constexpr int64_t kMaxRowStride = (int64_t)1 << 32;
 constexpr int64_t kMaxExtent = (int64_t)1 << 60;      // elements of one strided array
 
@@ -67,7 +68,7 @@ int check_cache(const qlin_kv_cache *c) {
     if (c->slots < 1 || c->seq_slots < 0 || c->token_stride < kHeadDim || c->head_stride < kHeadDim)
         return fail(QLIN_ERR_INVALID, "cache: slots must be positive, seq_slots >= 0, strides >= 128");
     if (c->token_stride % 8 || c->head_stride % 8) return fail(QLIN_ERR_ALIGN, "cache strides must be multiples of 8");
-    if (c->slots > kMaxSlots || c->seq_slots > kMaxSlots || c->token_stride > kMaxStride || c->head_stride > kMaxStride ||
+    if (c->slots > kMaxSlots || c->seq_slots > kMaxSlots || c->token_stride > kMaxTokenStride || c->head_stride > kMaxStride ||
         (double)c->slots * (double)c->token_stride + (double)c->heads * (double)c->head_stride > (double)kMaxExtent)
         return fail(QLIN_ERR_UNSUPPORTED, "cache too large");
     if (!c->k || !c->v) return fail(QLIN_ERR_INVALID, "NULL cache");
@@ -96,6 +97,35 @@ BatchArgs batch_args(const qlin_batch *b, const qlin_kv_cache *c) {
     a.rows = (int)b->rows;
     a.max_new = (int)b->max_new;
     return a;
+}
+
+// The kernel and split of one causal attention, from the host's bounds.
+struct CausalPlan { int rt = 0, tiles = 0, one_tile = 0, S = 1; int64_t ws_bytes = 0; };
+
+int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, CausalPlan *p) {
+    const int64_t G = Hq / Hkv, most = b->max_new * G;
+    p->rt = most <= 16 ? 1 : most <= 32 ? 2 : most <= 64 ? 4 : 0;
+    const int64_t R = causal_tile_rows(p->rt), per = (most + R - 1) / R;
+    p->one_tile = per <= 1;
+    const int64_t tiles = p->one_tile ? b->n_seq : std::min(b->n_seq * per, b->rows * G / R + b->n_seq);
+    int64_t S = splits;
+    if (S == 0) {
+        int dev = 0, cus = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+        if (e != hipSuccess) return hip_fail(e, "device query");
+        const int64_t blocks = tiles * Hkv, least = p->rt ? 128 : 256;     // keys of a range
+        const int64_t wanted = (p->rt ? cus : 2 * cus) / std::max<int64_t>(blocks, 1);
+        S = std::min<int64_t>({wanted, (b->max_len + least - 1) / least, kMaxSplits});
+    }
+    S = std::max<int64_t>(S, 1);
+    // work items of 256 threads in a 32-bit grid
+    if (tiles * Hkv * S >= (int64_t)1 << 24 || (S > 1 && b->rows * Hq >= (int64_t)1 << 24))
+        return fail(QLIN_ERR_UNSUPPORTED, "too many rows, heads and key ranges for one call");
+    p->tiles = (int)tiles;
+    p->S = (int)S;
+    p->ws_bytes = S > 1 ? b->rows * Hq * S * (kHeadDim + 2) * 4 : 0;
+    return QLIN_OK;
 }
 
 }  // namespace
@@ -162,9 +192,13 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
     clear_err();
     if (check_batch(batch) != QLIN_OK || check_heads(q_heads, kv_heads, head_dim) != QLIN_OK) return last_status();
     if (splits < 0 || splits > kMaxSplits) return fail(QLIN_ERR_INVALID, "splits must be in [0, 256]");
-    if (splits_out) *splits_out = 1;
-    if (workspace_bytes) *workspace_bytes = 0;
-    if (buf && buflen > 0) snprintf(buf, (size_t)buflen, "kernel=k_causal_row splits=1 combine=0");
+    CausalPlan p;
+    if (make_causal_plan(batch, q_heads, kv_heads, splits, &p) != QLIN_OK) return last_status();
+    if (splits_out) *splits_out = p.S;
+    if (workspace_bytes) *workspace_bytes = p.ws_bytes;
+    if (buf && buflen > 0)
+        snprintf(buf, (size_t)buflen, "kernel=%s splits=%d grid=%lld combine=%d", causal_kernel_name(p.rt), p.S,
+                 (long long)p.tiles * kv_heads * p.S, p.S > 1 ? 1 : 0);
     return QLIN_OK;
 }
 
@@ -187,6 +221,13 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     const Range rq = rows_range(q, M, q_stride, w), ro = rows_range(out, M, out_stride, w);
     if (overlap(ro, rq) || overlap(ro, cache_range(cache->k, cache)) || overlap(ro, cache_range(cache->v, cache)))
         return fail(QLIN_ERR_INVALID, "out overlaps q or the cache");
+    CausalPlan p;
+    if (make_causal_plan(batch, q_heads, cache->heads, splits, &p) != QLIN_OK) return last_status();
+    if (p.ws_bytes > 0 && (!workspace || workspace_bytes < p.ws_bytes))
+        return fail(QLIN_ERR_INVALID, "workspace of %lld bytes needed (%lld given)", (long long)p.ws_bytes,
+                    (long long)(workspace ? workspace_bytes : 0));
+    if (overlap(ro, Range{(uintptr_t)workspace, (size_t)p.ws_bytes})) return fail(QLIN_ERR_INVALID, "out overlaps the workspace");
+    if (batch->max_new == 0) return QLIN_OK;
 
     CausalArgs a;
     a.b = batch_args(batch, cache);
@@ -199,8 +240,13 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     a.Hq = (int)q_heads;
     a.Hkv = (int)cache->heads;
     a.G = (int)(q_heads / cache->heads);
+    a.ws_o = (float *)workspace;
+    a.ws_ml = a.ws_o + (size_t)batch->rows * q_heads * p.S * kHeadDim;
+    a.tiles = p.tiles;
+    a.one_tile = p.one_tile;
+    a.S = p.S;
     a.c = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)kHeadDim)));
-    const hipError_t e = launch_causal(a, (hipStream_t)stream);
+    const hipError_t e = launch_causal(a, p.rt, (hipStream_t)stream);
     return e == hipSuccess ? QLIN_OK : hip_fail(e, "causal attention launch");
 }
 

@@ -37,8 +37,15 @@ struct CausalArgs {
     uint16_t *out;
     int64_t q_stride, out_stride;
     int Hq, Hkv, G;
+    float *ws_o, *ws_ml;            // S > 1: [rows][Hq][S][128] sums, [rows][Hq][S] (maximum, sum of weights)
+    int tiles;                      // row tiles, at least those there are
+    int one_tile;                   // one tile a sequence: tile i is sequence i
+    int S;                          // key ranges
     float c;                        // scale log2(e): scores to base-2 exponents
 };
+
+// Rows (tokens x heads of a group) of a tile of k_causal_few<rt>, or of k_causal_prompt (rt = 0).
+constexpr int causal_tile_rows(int rt) { return rt ? 16 * rt : 128; }
 
 struct VerifyArgs {
     const uint16_t *target, *draft;
@@ -50,7 +57,8 @@ struct VerifyArgs {
 };
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st);
-hipError_t launch_causal(const CausalArgs &a, hipStream_t st);
+hipError_t launch_causal(const CausalArgs &a, int rt, hipStream_t st);
+const char *causal_kernel_name(int rt);
 hipError_t launch_verify(const VerifyArgs &a, int n_seq, hipStream_t st);
 
 }  // namespace qlin
