@@ -62,13 +62,21 @@ __device__ inline v4s_t lds_read_tr(const void *p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(const __attribute__((address_space(3))) void *)p);
 }
 
-// K and V in LDS: 16-byte unit c of key kk at kk * 16 + (c ^ (kk & 15)); reads of one
-// unit of 16 keys, and the transposing reads, meet different banks.
+// K and V in LDS: the 16 units (16 bytes) of a key's row in an order that changes from key
+// to key, so that what lanes read together meets different banks: for K, one unit of 16
+// keys; for V by transposing reads, two units of 8 keys (16-wide products) or four of 4 keys
+// (32-wide).  With K's order for V, 60 % of the prompt kernel's LDS cycles were conflicts.
 __device__ inline int key_unit(int kk, int c) { return kk * 16 + (c ^ (kk & 15)); }
+__device__ inline int few_value_unit(int kk, int c) { return kk * 16 + (c ^ (2 * (kk & 7))); }
+__device__ inline int value_unit(int kk, int c) { return kk * 16 + (c ^ (4 * (kk & 3))); }
 
-// As load_lds_x16 (device_common.h) from a scalar address plus a 32-bit offset in bytes.
-__device__ inline void load_lds_s16(const uint16_t *base, uint32_t off, const uint4 *lds_dst) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_addr(lds_dst)), "v"(off), "s"(base) : "memory", "m0");
+// As load_lds_x16 (device_common.h) from a scalar address plus a 32-bit offset in bytes, to an
+// LDS byte address.
+__device__ inline void load_lds_s16(const uint16_t *base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ inline void load_lds_v16(const uint16_t *src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds), "v"(src) : "memory", "m0");
 }
 __device__ inline void load_lds_s16_nt(const uint16_t *base, uint32_t off, const uint4 *lds_dst) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds_addr(lds_dst)), "v"(off), "s"(base) : "memory", "m0");
@@ -104,43 +112,34 @@ __device__ inline Tile find_tile(const CausalArgs &a, int idx, int R, int lane) 
     return Tile{-1, 0};
 }
 
-// Work item -> (key/value head, rest).  Workgroup b runs on XCD b % 8: with a multiple of 8
-// heads, all work on one head is on one XCD and shares the head's keys in its L2.
-__device__ inline void split_item(int blk, int Hkv, int &h, int &rest) {
-    if ((Hkv & 7) == 0) {
-        const int q = blk >> 3, n = Hkv >> 3;
-        rest = q / n;
-        h = (blk & 7) + 8 * (q - rest * n);
-    } else {
-        rest = blk / Hkv;
-        h = blk - rest * Hkv;
-    }
-}
-
 // A row tile's part of the work, the same in both kernels.
 struct Work {
     Seq s;
     int h, split;
     int r0, rows;               // packed rows [r0, r0 + rows) of the sequence
+    int i0, rem;                // r0 = i0 G + rem
     int hi;                     // keys [0, hi) that some row of the tile sees
     const uint16_t *k, *v;      // token 0 of head h
 };
+
+// x / G for the x < 64 + 128 that a tile's rows reach (exact for x G < 2^32)
+__device__ inline int token_of(const CausalArgs &a, int x) { return a.G == 1 ? x : (int)__umulhi((uint32_t)x, a.inv_g); }
 
 __device__ inline int64_t uniform(int64_t v) {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
     return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// Workgroup (x, y): key range y of item x = tile * heads + head.  Workgroups go to the 8 XCDs
+// in turn, x first: with a multiple of 8 heads all work on one head is on one XCD, and its
+// keys are shared in that XCD's L2.
 template <int R>
-__device__ inline bool find_work(const CausalArgs &a, int item, int lane, Work &w) {
-    int rest;
-    split_item(item, a.Hkv, w.h, rest);
-    const int idx = rest / a.S;
-    w.split = rest - idx * a.S;
+__device__ inline bool find_work(const CausalArgs &a, int lane, Work &w) {
+    const int idx = gn_chunk(blockIdx.x, a.Hkv, a.inv_heads, a.heads_shift);
+    w.h = blockIdx.x - idx * a.Hkv;
+    w.split = blockIdx.y;
     Tile t{idx, 0};
-    if (a.one_tile) {                                     // one tile a sequence
-        if (idx >= a.b.n_seq) return false;
-    } else {
+    if (!a.one_tile) {
         t = find_tile(a, a.tiles - 1 - idx, R, lane);     // late tiles, which see the most keys, first
         if (t.b < 0) return false;
     }
@@ -148,7 +147,9 @@ __device__ inline bool find_work(const CausalArgs &a, int item, int lane, Work &
     w.r0 = t.t * R;
     w.rows = min(R, w.s.rows * a.G - w.r0);
     if (w.rows <= 0) return false;
-    w.hi = w.s.L > 0 ? max(w.s.p0 + (w.r0 + w.rows - 1) / a.G + 1, 0) : 0;
+    w.i0 = w.r0 / a.G;
+    w.rem = w.r0 - w.i0 * a.G;
+    w.hi = w.s.L > 0 ? max(w.s.p0 + w.i0 + token_of(a, w.rem + w.rows - 1) + 1, 0) : 0;
     // the same in every lane: scalars
     w.s.slot0 = uniform(w.s.slot0);
     w.s.row0 = __builtin_amdgcn_readfirstlane(w.s.row0);
@@ -157,21 +158,26 @@ __device__ inline bool find_work(const CausalArgs &a, int item, int lane, Work &
     w.r0 = __builtin_amdgcn_readfirstlane(w.r0);
     w.rows = __builtin_amdgcn_readfirstlane(w.rows);
     w.hi = __builtin_amdgcn_readfirstlane(w.hi);
+    w.i0 = __builtin_amdgcn_readfirstlane(w.i0);
+    w.rem = __builtin_amdgcn_readfirstlane(w.rem);
     const int64_t at = w.s.slot0 * a.b.tok + (int64_t)w.h * a.b.head;
     w.k = a.k + at;
     w.v = a.v + at;
     return true;
 }
 
-// Element offset of packed row r's query (stride a.q_stride) or output.
-__device__ inline int64_t row_at(const CausalArgs &a, const Work &w, int r, int64_t stride) {
-    const int i = r / a.G;
-    return (int64_t)(w.s.row0 + i) * stride + (int64_t)(w.h * a.G + r - i * a.G) * kHeadDim;
+// Packed row x of the tile: its token in the sequence and its query head.
+struct RowOf { int i, hq; };
+__device__ inline RowOf row_of(const CausalArgs &a, const Work &w, int x) {
+    const int t = token_of(a, w.rem + x);
+    return RowOf{w.i0 + t, w.h * a.G + w.rem + x - t * a.G};
 }
-// Index of packed row r among all rows and heads (partial results).
-__device__ inline int64_t row_index(const CausalArgs &a, const Work &w, int r) {
-    const int i = r / a.G;
-    return (int64_t)(w.s.row0 + i) * a.Hq + w.h * a.G + (r - i * a.G);
+__device__ inline int64_t row_at(const Work &w, const RowOf &r, int64_t stride) {
+    return (int64_t)(w.s.row0 + r.i) * stride + r.hq * kHeadDim;
+}
+// Its place among the partial results.
+__device__ inline int64_t part_at(const CausalArgs &a, const Work &w, const RowOf &r) {
+    return ((int64_t)(w.s.row0 + r.i) * a.Hq + r.hq) * a.S + w.split;
 }
 
 // The values of keys [key, key + 4) and [key2, key2 + 4), without those behind `last`.
@@ -183,6 +189,10 @@ __device__ inline v8bf values_up_to(v4s_t lo, v4s_t hi, int key, int key2, int l
     }
     return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
+
+// A row's sums are rescaled only when its maximum has grown by more than a factor 2^kLazy of
+// the weights: up to there the weights just exceed 1, with the same relative rounding.
+constexpr float kLazy = 8.0f;
 
 // ---------------------------------------------------------------- few rows
 
@@ -197,33 +207,35 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int g = lane >> 4, r = lane & 15;
     Work w;
-    if (!find_work<R>(a, blockIdx.x, lane, w)) return;
+    if (!find_work<R>(a, lane, w)) return;
 
     // units of this key range, and of this wave: u0 + wave, u0 + wave + 4, ...
     const int units = (w.hi + kFewKeys - 1) / kFewKeys;
     const int per = max((units + a.S - 1) / a.S, kFewWaves);
     const int u0 = w.split * per, u1 = min(u0 + per, units);
 
-    // byte offsets of a lane in four keys, for each of the four swizzles
-    uint32_t off[4];
+    // byte offsets of a lane in four keys, for each order of their units
+    uint32_t koff[4], voff[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) off[j] = 2u * ((uint32_t)g * (uint32_t)a.b.tok + 8u * (r ^ (4 * j + g)));
+    for (int j = 0; j < 4; ++j) koff[j] = 2u * ((uint32_t)g * (uint32_t)a.b.tok + 8u * (r ^ (4 * j + g)));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) voff[j] = 2u * ((uint32_t)g * (uint32_t)a.b.tok + 8u * (r ^ (2 * (4 * j + g))));
     auto issue = [&](int u, int st) {
         if ((u + 1) * kFewKeys <= w.hi) {
             const int64_t at = (int64_t)u * kFewKeys * a.b.tok;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                load_lds_s16_nt(w.k + at + 4 * j * a.b.tok, off[j & 3], &ring[wave][st][0][j * 64]);
-                load_lds_s16_nt(w.v + at + 4 * j * a.b.tok, off[j & 3], &ring[wave][st][1][j * 64]);
+                load_lds_s16_nt(w.k + at + 4 * j * a.b.tok, koff[j & 3], &ring[wave][st][0][j * 64]);
+                load_lds_s16_nt(w.v + at + 4 * j * a.b.tok, voff[j & 1], &ring[wave][st][1][j * 64]);
             }
             return;
         }
 #pragma unroll 1
         for (int j = 0; j < 8; ++j) {                    // the last, partial unit: its last key again
-            const int x = j * 64 + lane, kk = x >> 4, c = (x & 15) ^ (kk & 15);
-            const int64_t off = (int64_t)min(u * kFewKeys + kk, w.hi - 1) * a.b.tok + 8 * c;
-            load_lds_x16_nt(w.k + off, &ring[wave][st][0][j * 64]);
-            load_lds_x16_nt(w.v + off, &ring[wave][st][1][j * 64]);
+            const int kk = 4 * j + g;
+            const int64_t at = (int64_t)min(u * kFewKeys + kk, w.hi - 1) * a.b.tok;
+            load_lds_x16_nt(w.k + at + 8 * (r ^ (kk & 15)), &ring[wave][st][0][j * 64]);
+            load_lds_x16_nt(w.v + at + 8 * (r ^ (2 * (kk & 7))), &ring[wave][st][1][j * 64]);
         }
     };
 
@@ -232,13 +244,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
     int last[RT];                                             // last key that the row sees
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-        const int rr = w.r0 + min(16 * t + r, w.rows - 1);
-        last[t] = w.s.p0 + rr / a.G;
-        const uint16_t *qp = a.q + row_at(a, w, rr, a.q_stride) + 8 * g;
+        const RowOf row = row_of(a, w, min(16 * t + r, w.rows - 1));
+        last[t] = w.s.p0 + row.i;
+        const uint16_t *qp = a.q + row_at(w, row, a.q_stride) + 8 * g;
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) qf[t][ks] = *(const v8bf *)(qp + 32 * ks);
     }
-    const int first_last = w.s.p0 + w.r0 / a.G;               // keys up to here are seen by every row
+    const int first_last = w.s.p0 + w.i0;                     // keys up to here are seen by every row
 
     float m[RT], l[RT];
     v4f o[RT][8];
@@ -274,28 +286,39 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
                         sc[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][ks], sc[t][kt], 0, 0, 0);
                 }
             }
-            v8bf pb[RT];
+            if (masked) {
 #pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                if (masked) {
+                for (int t = 0; t < RT; ++t)
 #pragma unroll
                     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
                             sc[t][kt][i] = key0 + 16 * kt + 4 * g + i <= last[t] ? sc[t][kt][i] : kNegInf;
-                }
-                float mt = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])),
-                                 fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
-                mt = pair32_max(pair16_max(mt));
-                const float mn = fmaxf(m[t], mt);
-                const float muc = (mn == kNegInf ? 0.0f : mn) * a.c;
-                if (__ballot(mn != m[t])) {
-                    const float alpha = exp2_hw(__builtin_fmaf(m[t], a.c, -muc));
+            }
+            float mt[RT];
+            bool grown = false;
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                mt[t] = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])),
+                              fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
+                mt[t] = pair32_max(pair16_max(mt[t]));
+                grown |= mt[t] * a.c > __builtin_fmaf(m[t], a.c, kLazy);
+            }
+            if (__ballot(grown)) {                               // all row tiles at once: one branch
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const float mn = fmaxf(m[t], mt[t]);
+                    const float alpha = exp2_hw((m[t] - (mn == kNegInf ? 0.0f : mn)) * a.c);
                     l[t] *= alpha;
 #pragma unroll
                     for (int dt = 0; dt < 8; ++dt) o[t][dt] *= alpha;
                     m[t] = mn;
                 }
+            }
+            v8bf pb[RT];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const float muc = (m[t] == kNegInf ? 0.0f : m[t]) * a.c;
                 uint32_t pw[4];
                 float ls = 0.0f;
 #pragma unroll
@@ -312,15 +335,14 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) {
                 const int c = 2 * dt + (q >> 1), off = 8 * (q & 1);
-                const v4s_t lo4 = lds_read_tr((const char *)&vb[key_unit(kr, c)] + off);
-                const v4s_t hi4 = lds_read_tr((const char *)&vb[key_unit(kr + 16, c)] + off);
+                const v4s_t lo4 = lds_read_tr((const char *)&vb[few_value_unit(kr, c)] + off);
+                const v4s_t hi4 = lds_read_tr((const char *)&vb[few_value_unit(kr + 16, c)] + off);
                 if (careful && masked) {
 #pragma unroll
                     for (int t = 0; t < RT; ++t) {
-                        const int i0 = (w.r0 + min(16 * t, w.rows - 1)) / a.G, i1 = (w.r0 + min(16 * t + 15, w.rows - 1)) / a.G;
+                        const int p0 = w.s.p0 + row_of(a, w, min(16 * t, w.rows - 1)).i, p1 = w.s.p0 + row_of(a, w, min(16 * t + 15, w.rows - 1)).i;
                         v4f sum = o[t][dt];
-                        for (int i = i0; i <= i1; ++i) {
-                            const int p = w.s.p0 + i;
+                        for (int p = p0; p <= p1; ++p) {
                             const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values_up_to(lo4, hi4, key0 + 4 * g, key0 + 16 + 4 * g, p),
                                                                                   pb[t], o[t][dt], 0, 0, 0);
                             sum = last[t] == p ? x : sum;
@@ -376,14 +398,15 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
             ls += e.y * f;
             acc += sums[((i * RT + t) * 8 + dt) * 64 + lane] * f;
         }
-        const int rr = w.r0 + row, d = 16 * dt + 4 * g;
+        const RowOf ro = row_of(a, w, row);
+        const int d = 16 * dt + 4 * g;
         if (a.S == 1) {
-            const bool none = w.s.L == 0 || w.s.p0 + rr / a.G < 0;
+            const bool none = w.s.L == 0 || w.s.p0 + ro.i < 0;
             uint2 y = {};
             if (!none) y = make_uint2(cvt_pk_bf16(acc[0] / ls, acc[1] / ls), cvt_pk_bf16(acc[2] / ls, acc[3] / ls));
-            *(uint2 *)(a.out + row_at(a, w, rr, a.out_stride) + d) = y;
+            *(uint2 *)(a.out + row_at(w, ro, a.out_stride) + d) = y;
         } else {
-            const int64_t at = row_index(a, w, rr) * a.S + w.split;
+            const int64_t at = part_at(a, w, ro);
             *(v4f *)(a.ws_o + at * kHeadDim + d) = acc;
             if (dt == 0 && g == 0) *(float2 *)(a.ws_ml + 2 * at) = make_float2(M, ls);
         }
@@ -392,158 +415,256 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
 
 // ---------------------------------------------------------------- many rows
 
-constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves, kPromptKeys = 64, kPromptStages = 2;
-constexpr int kPromptUnits = kPromptKeys * kHeadDim / 8;      // 16-byte units of a K or V tile (1024)
-constexpr float kLazy = 8.0f;                                 // see below
+// Steps of 32 keys in a pipeline over three steps: while the softmax of step u runs on the
+// vector unit, the matrix cores take the scores of step u + 1 and the weighted sums of step
+// u - 1.  K and V each have a ring of four steps in LDS, filled by direct-to-LDS loads two
+// steps ahead; one barrier for two steps.
+constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves, kStepKeys = 32, kStepSlots = 4;
+constexpr int kStepUnits = kStepKeys * kHeadDim / 8;          // 16-byte units of a step's K or V (512)
 
 __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalArgs a) {
-    __shared__ __attribute__((aligned(16))) uint4 ring[kPromptStages][2][kPromptUnits];
+    __shared__ __attribute__((aligned(16))) uint4 kring[kStepSlots][kStepUnits], vring[kStepSlots][kStepUnits];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int hi = lane >> 5, r = lane & 31;
     Work w;
-    if (!find_work<kPromptRows>(a, blockIdx.x, lane, w)) return;
+    if (!find_work<kPromptRows>(a, lane, w)) return;
 
-    const int tiles = (w.hi + kPromptKeys - 1) / kPromptKeys;
-    const int per = (tiles + a.S - 1) / a.S;
-    const int t0 = w.split * per, t1 = min(t0 + per, tiles);
+    const int all = (w.hi + kStepKeys - 1) / kStepKeys;
+    const int per = (all + a.S - 1) / a.S;
+    const int u0 = w.split * per, n = max(min(u0 + per, all) - u0, 0);      // steps [u0, u0 + n)
+    const uint16_t *kp = w.k + (int64_t)u0 * kStepKeys * a.b.tok, *vp = w.v + (int64_t)u0 * kStepKeys * a.b.tok;
+    const int first_key = u0 * kStepKeys;
 
-    const uint32_t off = 2u * ((uint32_t)(lane >> 4) * (uint32_t)a.b.tok + 8u * ((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)));
-    auto issue = [&](int t) {
-        const int st = t & 1;
-        if ((t + 1) * kPromptKeys <= w.hi) {
-            const int64_t at = ((int64_t)t * kPromptKeys + 4 * wave) * a.b.tok;
-#pragma unroll
-            for (int j = 0; j < kPromptUnits / (kPromptWaves * 64); ++j) {
-                load_lds_s16(w.k + at + 16 * j * a.b.tok, off, &ring[st][0][(j * kPromptWaves + wave) * 64]);
-                load_lds_s16(w.v + at + 16 * j * a.b.tok, off, &ring[st][1][(j * kPromptWaves + wave) * 64]);
-            }
-            return;
-        }
+    // wave w loads keys 4 (w + 4 j) .. + 3 of a step, j = 0, 1, into slot u mod 4
+    const int lk = 4 * wave + (lane >> 4);
+    const uint32_t koff = 2u * ((uint32_t)(lane >> 4) * (uint32_t)a.b.tok + 8u * ((lane & 15) ^ lk));
+    const uint32_t voff = 2u * ((uint32_t)(lane >> 4) * (uint32_t)a.b.tok + 8u * ((lane & 15) ^ (4 * (lane >> 4))));
+    const uint32_t klds = lds_addr(kring) + wave * 1024, vlds = lds_addr(vring) + wave * 1024;
+    const int full = (w.hi - first_key) / kStepKeys;              // steps without keys past the last
+    const int64_t half = 16 * a.b.tok, whole = 32 * a.b.tok;
+    const uint16_t *kn = kp + 4 * wave * a.b.tok, *vn = vp + 4 * wave * a.b.tok;   // next steps to load
+    auto load = [&](const uint16_t *&next, const uint16_t *src, uint32_t lds, int u, uint32_t off, int swz) {
+        if (u < full) {
+            load_lds_s16(next, off, lds);
+            load_lds_s16(next + half, off, lds + 4096);
+        } else {                                                  // the last, partial step: its last key again
 #pragma unroll 1
-        for (int j = 0; j < kPromptUnits / (kPromptWaves * 64); ++j) {
-            const int x = (j * kPromptWaves + wave) * 64 + lane, kk = x >> 4, c = (x & 15) ^ (kk & 15);
-            const int64_t off = (int64_t)min(t * kPromptKeys + kk, w.hi - 1) * a.b.tok + 8 * c;
-            load_lds_x16(w.k + off, &ring[st][0][(j * kPromptWaves + wave) * 64]);
-            load_lds_x16(w.v + off, &ring[st][1][(j * kPromptWaves + wave) * 64]);
+            for (int j = 0; j < 2; ++j) {
+                const int key = min(u * kStepKeys + lk + 16 * j, w.hi - 1 - first_key);
+                load_lds_v16(src + (int64_t)key * a.b.tok + 8 * ((lane & 15) ^ swz), lds + 4096 * j);
+            }
         }
+        next += whole;
     };
+    auto load_k = [&](int u) { load(kn, kp, klds + (u & (kStepSlots - 1)) * 8192, u, koff, lk); };
+    auto load_v = [&](int u) { load(vn, vp, vlds + (u & (kStepSlots - 1)) * 8192, u, voff, 4 * (lane >> 4)); };
 
-    const int rw0 = min(32 * wave, w.rows - 1), rw1 = min(32 * wave + 31, w.rows - 1);
-    const int rr = w.r0 + min(32 * wave + r, w.rows - 1);
-    const int last = w.s.p0 + rr / a.G;                                   // last key this row sees
-    const int wave_first = w.s.p0 + (w.r0 + rw0) / a.G, wave_last = w.s.p0 + (w.r0 + rw1) / a.G;
-    const bool live = 32 * wave < w.rows;                                 // this wave has rows
+    const RowOf row = row_of(a, w, min(32 * wave + r, w.rows - 1));
+    const int last = w.s.p0 + row.i;                                       // last key this row sees
+    const int wave_first = __builtin_amdgcn_readfirstlane(w.s.p0 + row_of(a, w, min(32 * wave, w.rows - 1)).i);
+    const int wave_last = __builtin_amdgcn_readfirstlane(w.s.p0 + row_of(a, w, min(32 * wave + 31, w.rows - 1)).i);
     v8bf qf[8];
     {
-        const uint16_t *qp = a.q + row_at(a, w, rr, a.q_stride) + 8 * hi;
+        const uint16_t *qp = a.q + row_at(w, row, a.q_stride) + 8 * hi;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const v8bf *)(qp + 16 * ks);
     }
 
-    float m, l;
+    // operands from LDS: row r of the scores' A operand; of V, what the transposing read needs.
+    // Their places in a slot, so that a slot and a key only add a constant.
+    uint32_t kat[8], vat[4];
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) kat[ks] = 16u * key_unit(r, 2 * ks + hi);
+    {
+        const int vq = lane & 3, vk = 4 * hi + ((lane >> 2) & 3), vc = 2 * ((lane >> 4) & 1) + (vq >> 1);
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) vat[dt] = 16u * value_unit(vk, 4 * dt + vc) + 8 * (vq & 1);
+    }
+    auto k_frag = [&](int slot, int ks) { return *(const v8bf *)((const char *)kring + kat[ks] + slot * 8192); };
+    auto v_half = [&](int slot, int key, int dt) { return lds_read_tr((const char *)vring + vat[dt] + slot * 8192 + key * 256); };
+    auto v_frag = [&](int slot, int h, int dt) {
+        return __builtin_bit_cast(v8bf, __builtin_shufflevector(v_half(slot, 16 * h, dt), v_half(slot, 16 * h + 8, dt), 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto zero = [](v16f &x) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+    };
+    auto mask = [&](v16f &s, int key0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = key0 + 8 * (i >> 2) + 4 * hi + (i & 3) <= last ? s[i] : kNegInf;
+    };
+    auto row_max = [&](const v16f &s) {
+        float x = kNegInf;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x = fmaxf(x, s[i]);
+        return pair32_max(x);
+    };
+    auto operand = [](const uint32_t *p) { return __builtin_bit_cast(v8bf, v4u{p[0], p[1], p[2], p[3]}); };
+
+    float m = kNegInf, l = 0.0f;
     v16f o[4];
-    auto run = [&](auto mode) {                                  // whether the sums came out finite
-        constexpr bool careful = decltype(mode)::value;
-        m = kNegInf;
-        l = 0.0f;
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
+    for (int dt = 0; dt < 4; ++dt) zero(o[dt]);
+
+    if (n > 0) {
+        load_k(0);
+        if (n > 1) load_k(1);
+        if (n > 2) load_k(2);
+        load_v(0);
+        v16f s0, s1;
+        uint32_t p0[8], p1[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
-        if (t0 < t1) issue(t0);
-        for (int t = t0; t < t1; ++t) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            lds_barrier();                    // tile t is in LDS, and every wave is done with tile t - 1
-            if (t + 1 < t1) issue(t + 1);
-            const int key0 = t * kPromptKeys;
-            if (!live || key0 > wave_last) continue;
-            const bool masked = key0 + kPromptKeys - 1 > wave_first;
-            const uint4 *kb = ring[t & 1][0], *vb = ring[t & 1][1];
-            v16f sc[2];
+        for (int i = 0; i < 8; ++i) p1[i] = 0;                       // there is no step -1: zeros, also in its slot
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
+        for (int i = 0; i < kStepUnits; i += kPromptWaves * 64) vring[3][i + threadIdx.x] = uint4{};
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        zero(s0);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sc[kt][i] = 0.0f;
+        for (int ks = 0; ks < 8; ++ks) s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(0, ks), qf[ks], s0, 0, 0, 0);
+
+        // step u (u mod 4 = SLOT): softmax of s into p; scores of u + 1 into sn; sums of u - 1 with pp
+        auto step = [&](auto slot, int u, v16f &s, v16f &sn, uint32_t *p, const uint32_t *pp) {
+            constexpr int SLOT = decltype(slot)::value, KS = (SLOT + 1) & 3, VS = (SLOT + 3) & 3;
+            v8bf kf[4], vf[4];
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    const v8bf kf = *(const v8bf *)&kb[key_unit(32 * kt + r, 2 * ks + hi)];
-                    sc[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], sc[kt], 0, 0, 0);
-                }
+            for (int i = 0; i < 4; ++i) kf[i] = k_frag(KS, i);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vf[i] = v_frag(VS, 0, i);
+            const int key0 = first_key + u * kStepKeys;
+            if (key0 + kStepKeys - 1 > wave_first) mask(s, key0);
+            const float mt = row_max(s);
+            const bool grown = __ballot(mt * a.c > __builtin_fmaf(m, a.c, kLazy)) != 0;
+            const float mn = grown ? fmaxf(m, mt) : m;
+            const float mu = mn == kNegInf ? 0.0f : mn, muc = mu * a.c;
+            float ls = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i == 0) zero(sn);
+                sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i & 3], qf[i], sn, 0, 0, 0);
+                if (i < 4) kf[i] = k_frag(KS, i + 4);
+                o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i & 3], operand(pp + 4 * (i >> 2)), o[i & 3], 0, 0, 0);
+                if (i < 4) vf[i] = v_frag(VS, 1, i);
+                const float e0 = exp2_hw(__builtin_fmaf(s[2 * i], a.c, -muc)), e1 = exp2_hw(__builtin_fmaf(s[2 * i + 1], a.c, -muc));
+                p[i] = cvt_pk_bf16(e0, e1);
+                ls = dot2(p[i], kBf16OnePair, ls);
             }
-            if (masked) {
+            // the weights here, between the products, not behind the branch below
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+            for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(p[i]));
+            asm volatile("" : "+v"(ls));
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        sc[kt][i] = key0 + 32 * kt + 8 * (i >> 2) + 4 * hi + (i & 3) <= last ? sc[kt][i] : kNegInf;
+            for (int i = 0; i < 4; ++i) {                                // two products, six vector instructions, three LDS reads
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             }
-            float mt = kNegInf;
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[kt][i]);
-            mt = pair32_max(mt);
-            // The sums are rescaled only when a maximum has grown by more than 2^kLazy: up to
-            // there the weights just exceed 1, with the same relative rounding.
-            if (__ballot(mt * a.c > __builtin_fmaf(m, a.c, kLazy))) {
-                const float mn = fmaxf(m, mt);
-                const float alpha = exp2_hw((m - (mn == kNegInf ? 0.0f : mn)) * a.c);
+            for (int i = 0; i < 8; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+            }
+            if (grown) {                                             // the sums so far, up to step u - 1
+                const float alpha = exp2_hw((m - mu) * a.c);
+                m = mn;
                 l *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
-                m = mn;
             }
-            const float muc = (m == kNegInf ? 0.0f : m) * a.c;
-            uint32_t pw[2][8];
-            float ls = 0.0f;
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float e0 = exp2_hw(__builtin_fmaf(sc[kt][2 * i], a.c, -muc));
-                    const float e1 = exp2_hw(__builtin_fmaf(sc[kt][2 * i + 1], a.c, -muc));
-                    pw[kt][i] = cvt_pk_bf16(e0, e1);
-                    ls = dot2(pw[kt][i], kBf16OnePair, ls);
-                }
             l += ls;
-            const int q = lane & 3, kr = 4 * hi + ((lane >> 2) & 3), c0 = 2 * ((lane >> 4) & 1) + (q >> 1), off = 8 * (q & 1);
+        };
+        // Before steps u and u + 1 (u even): what they read, K of u + 1 and u + 2 and V of u - 1 and
+        // u, was loaded during the two steps before; what is loaded now takes the places of K of
+        // u - 1 and u and V of u - 3 and u - 2, which every wave is done with.
+        auto advance = [&](int u) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            lds_barrier();
+            if (u + 3 < n) load_k(u + 3);
+            if (u + 1 < n) load_v(u + 1);
+            if (u + 4 < n) load_k(u + 4);
+            if (u + 2 < n) load_v(u + 2);
+        };
+        for (int u = 0; u < n; u += 4) {
+            advance(u);
+            step(std::integral_constant<int, 0>{}, u, s0, s1, p0, p1);
+            if (u + 1 >= n) break;
+            step(std::integral_constant<int, 1>{}, u + 1, s1, s0, p1, p0);
+            if (u + 2 >= n) break;
+            advance(u + 2);
+            step(std::integral_constant<int, 2>{}, u + 2, s0, s1, p0, p1);
+            if (u + 3 >= n) break;
+            step(std::integral_constant<int, 3>{}, u + 3, s1, s0, p1, p0);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const uint32_t *ps = &pw[s >> 1][4 * (s & 1)];
-                const v8bf pb = __builtin_bit_cast(v8bf, v4u{ps[0], ps[1], ps[2], ps[3]});
+        for (int i = 0; i < 8; ++i)
+            o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag((n - 1) & 3, i >> 2, i & 3), operand((n & 1 ? p0 : p1) + 4 * (i >> 2)),
+                                                               o[i & 3], 0, 0, 0);
+    }
+    float bad = 0.0f;                                                // NaN if any sum is not finite
 #pragma unroll
-                for (int dt = 0; dt < 4; ++dt) {
-                    const v4s_t lo4 = lds_read_tr((const char *)&vb[key_unit(16 * s + kr, 4 * dt + c0)] + off);
-                    const v4s_t hi4 = lds_read_tr((const char *)&vb[key_unit(16 * s + 8 + kr, 4 * dt + c0)] + off);
-                    if (careful && masked) {
-                        v16f sum = o[dt];
-                        for (int p = wave_first; p <= wave_last; ++p) {
-                            const v16f x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                values_up_to(lo4, hi4, key0 + 16 * s + 4 * hi, key0 + 16 * s + 8 + 4 * hi, p), pb, o[dt], 0, 0, 0);
+    for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) sum[i] = last == p ? x[i] : sum[i];
-                        }
-                        o[dt] = sum;
-                    } else {
-                        const v8bf vf = __builtin_bit_cast(v8bf, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb, o[dt], 0, 0, 0);
-                    }
+        for (int i = 0; i < 16; ++i) bad = __builtin_fmaf(o[dt][i], 0.0f, bad);
+    if (__syncthreads_or(bad != 0.0f)) {
+        // careful: once more, step by step, every row with the values of its own keys only
+        m = kNegInf;
+        l = 0.0f;
+        kn = kp + 4 * wave * a.b.tok;
+        vn = vp + 4 * wave * a.b.tok;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) zero(o[dt]);
+#pragma unroll 1
+        for (int u = 0; u < n; ++u) {
+            lds_barrier();
+            load_k(u);                                               // into slot u mod 4
+            load_v(u);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            lds_barrier();
+            const int slot = u & (kStepSlots - 1), key0 = first_key + u * kStepKeys;
+            v16f s;
+            zero(s);
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(slot, ks), qf[ks], s, 0, 0, 0);
+            mask(s, key0);
+            const float mn = fmaxf(m, row_max(s)), mu = mn == kNegInf ? 0.0f : mn;
+            const float alpha = exp2_hw((m - mu) * a.c), muc = mu * a.c;
+            m = mn;
+            l *= alpha;
+            uint32_t p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = cvt_pk_bf16(exp2_hw(__builtin_fmaf(s[2 * i], a.c, -muc)), exp2_hw(__builtin_fmaf(s[2 * i + 1], a.c, -muc)));
+                l = dot2(p[i], kBf16OnePair, l);
+            }
+            const int t0 = min(wave_first, key0 + kStepKeys - 1), t1 = min(wave_last, key0 + kStepKeys - 1);   // later tokens see all
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) {
+                const v16f before = o[dt] * alpha;
+                o[dt] = before;
+#pragma unroll 1
+                for (int t = t0; t <= t1; ++t) {
+                    v16f x = before;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            values_up_to(v_half(slot, 16 * h, dt), v_half(slot, 16 * h + 8, dt), key0 + 16 * h + 4 * hi, key0 + 16 * h + 8 + 4 * hi, t),
+                            operand(p + 4 * h), x, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[dt][i] = min(last, key0 + kStepKeys - 1) == t ? x[i] : o[dt][i];
                 }
             }
         }
-        float bad = 0.0f;                                        // NaN if any sum is not finite
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) bad = __builtin_fmaf(o[dt][i], 0.0f, bad);
-        return !__syncthreads_or(bad != 0.0f);                   // also: every wave is done with the ring
-    };
-    if (!run(std::false_type{})) run(std::true_type{});
+    }
     l = pair32_sum(l);
     if (32 * wave + r >= w.rows) return;
     if (a.S == 1) {
         const bool none = w.s.L == 0 || last < 0;
-        uint16_t *op = a.out + row_at(a, w, rr, a.out_stride);
+        uint16_t *op = a.out + row_at(w, row, a.out_stride);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -554,7 +675,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
                 *(uint2 *)(op + 32 * dt + 8 * i + 4 * hi) = y;
             }
     } else {
-        const int64_t at = row_index(a, w, rr) * a.S + w.split;
+        const int64_t at = part_at(a, w, row);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -577,19 +698,19 @@ __global__ __launch_bounds__(256) void k_causal_combine(CausalArgs a) {
     static_assert(P >= 2, "the two groups of a wave share a row");
     const int grp = threadIdx.x >> 5, l = threadIdx.x & 31, lane = threadIdx.x & 63;
     const int part = grp % P;
-    int h, rest;                                      // the XCD that wrote the head's partials
-    split_item(blockIdx.x, a.Hkv, h, rest);
-    const int64_t x = (int64_t)rest * (8 / P) + grp / P;            // (row, head of the group)
-    const int64_t mrow = x / a.G;
-    const int b = find_seq(a.b, (int)min(mrow, (int64_t)a.b.rows), lane);      // one row a wave
+    const int rest = gn_chunk(blockIdx.x, a.Hkv, a.inv_heads, a.heads_shift);
+    const int h = blockIdx.x - rest * a.Hkv;                  // on the XCD that wrote the head's partials
+    const int x = rest * (8 / P) + grp / P;                   // (row, head of the group)
+    const int mrow = x / a.G;
+    const int b = find_seq(a.b, min(mrow, a.b.rows), lane);   // one row a wave
     bool on = mrow < a.b.rows && b < a.b.n_seq;
     Seq s = {};
     if (on) {
         s = load_seq(a.b, b);
         on = mrow >= s.row0 && mrow < s.row0 + s.rows;
     }
-    const int hq = h * a.G + (int)(x - mrow * a.G);
-    const int64_t at = (mrow * a.Hq + hq) * a.S;
+    const int hq = h * a.G + x - mrow * a.G;
+    const int64_t at = ((int64_t)mrow * a.Hq + hq) * a.S;
     float m = kNegInf, ls = 0.0f;
     float4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
     auto fold = [&](float m2, float l2, const float4 &v) {
@@ -625,7 +746,7 @@ __global__ __launch_bounds__(256) void k_causal_combine(CausalArgs a) {
     const bool none = s.L == 0 || s.p0 + (mrow - s.row0) < 0;
     uint2 y = {};
     if (!none) y = make_uint2(cvt_pk_bf16(acc.x / ls, acc.y / ls), cvt_pk_bf16(acc.z / ls, acc.w / ls));
-    *(uint2 *)(a.out + mrow * a.out_stride + (int64_t)hq * kHeadDim + 4 * l) = y;
+    *(uint2 *)(a.out + (int64_t)mrow * a.out_stride + (int64_t)hq * kHeadDim + 4 * l) = y;
 }
 
 }  // namespace
@@ -635,7 +756,7 @@ const char *causal_kernel_name(int rt) {
 }
 
 hipError_t launch_causal(const CausalArgs &a, int rt, hipStream_t st) {
-    const dim3 grid((unsigned)((int64_t)a.tiles * a.Hkv * a.S));
+    const dim3 grid((unsigned)(a.tiles * a.Hkv), (unsigned)a.S);
     if (rt == 1) hipLaunchKernelGGL(k_causal_few<1>, grid, dim3(kFewWaves * 64), 0, st, a);
     else if (rt == 2) hipLaunchKernelGGL(k_causal_few<2>, grid, dim3(kFewWaves * 64), 0, st, a);
     else if (rt == 4) hipLaunchKernelGGL(k_causal_few<4>, grid, dim3(kFewWaves * 64), 0, st, a);

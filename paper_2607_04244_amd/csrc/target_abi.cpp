@@ -245,6 +245,8 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     a.tiles = p.tiles;
     a.one_tile = p.one_tile;
     a.S = p.S;
+    gn_reciprocal(a.Hkv, &a.inv_heads, &a.heads_shift);
+    a.inv_g = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
     a.c = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)kHeadDim)));
     const hipError_t e = launch_causal(a, p.rt, (hipStream_t)stream);
     return e == hipSuccess ? QLIN_OK : hip_fail(e, "causal attention launch");

@@ -41,6 +41,8 @@ struct CausalArgs {
     int tiles;                      // row tiles, at least those there are
     int one_tile;                   // one tile a sequence: tile i is sequence i
     int S;                          // key ranges
+    uint32_t inv_heads, inv_g;      // x / Hkv by gn_chunk; ceil(2^32 / G) (0: G = 1)
+    int heads_shift;
     float c;                        // scale log2(e): scores to base-2 exponents
 };
 
