@@ -179,7 +179,7 @@ int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *wor
  *   workspace   DEVICE scratch of at least qlin_verify_plan's bytes, 16-byte
  *               aligned, no initialisation
  * 0 <= n_draft <= 64 (0: plain sampling; drafted may then be NULL), 1 <= vocab <=
- * 2^24, n_seq <= 65536 (0 is a no-op).  Outputs must not overlap inputs or each other.
+ * 2^24, n_seq <= 65535 (0 is a no-op).  Outputs must not overlap inputs or each other.
  * Errors: INVALID, UNSUPPORTED, ALIGN, HIP.
  */
 int qlin_verify_draft(int64_t n_seq, int64_t n_draft, int64_t vocab, const uint16_t *target, int64_t target_stride,

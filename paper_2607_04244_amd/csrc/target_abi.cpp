@@ -18,7 +18,7 @@ namespace {
 
 constexpr int64_t kMaxSeq = 65536, kMaxRows = (int64_t)1 << 22, kMaxLen = (int64_t)1 << 28, kMaxSlots = (int64_t)1 << 40;
 constexpr int64_t kMaxHeads = 4096, kMaxGroup = 64, kMaxSplits = 256, kMaxStride = (int64_t)1 << 40;
-constexpr int64_t kMaxDraft = 64, kMaxVocab = (int64_t)1 << 24;
+constexpr int64_t kMaxDraft = kVerifyMaxDraft, kMaxVocab = (int64_t)1 << 24, kMaxVerifySeq = 65535;   // sequences: a grid's y
 constexpr int64_t kMaxTokenStride = (int64_t)1 << 28;       // 32-bit byte offsets over four tokens
 constexpr int64_t kMaxRowStride = (int64_t)1 << 32;
 constexpr int64_t kMaxExtent = (int64_t)1 << 60;      // elements of one strided array
@@ -126,6 +126,19 @@ int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t split
     p->S = (int)S;
     p->ws_bytes = S > 1 ? b->rows * Hq * S * (kHeadDim + 2) * 4 : 0;
     return QLIN_OK;
+}
+
+// Workspace of the verification: the rows' statistics, then the chunks' sums, then the decisions.
+struct VerifyLayout { int64_t chunks, rows, sums, decisions, bytes; };
+
+VerifyLayout verify_layout(int64_t n_seq, int64_t n_draft, int64_t vocab) {
+    VerifyLayout l;
+    l.chunks = (vocab + 7 + kVerifyChunk - 1) / kVerifyChunk;
+    l.rows = 2 * n_draft + 1;
+    l.sums = n_seq * l.rows * l.chunks * (int64_t)sizeof(VerifyStat);
+    l.decisions = l.sums + (n_seq * l.chunks * 8 + 15) / 16 * 16;
+    l.bytes = l.decisions + n_seq * (int64_t)sizeof(VerifyDecision);
+    return l;
 }
 
 }  // namespace
@@ -255,9 +268,9 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
 int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *workspace_bytes) {
     clear_err();
     if (n_seq < 0 || n_draft < 0 || vocab < 1) return fail(QLIN_ERR_INVALID, "n_seq and n_draft must be >= 0, vocab positive");
-    if (n_seq > kMaxSeq || n_draft > kMaxDraft || vocab > kMaxVocab)
-        return fail(QLIN_ERR_UNSUPPORTED, "at most 65536 sequences, 64 drafted tokens and 2^24 tokens of vocabulary");
-    if (workspace_bytes) *workspace_bytes = 0;
+    if (n_seq > kMaxVerifySeq || n_draft > kMaxDraft || vocab > kMaxVocab)
+        return fail(QLIN_ERR_UNSUPPORTED, "at most 65535 sequences, 64 drafted tokens and 2^24 tokens of vocabulary");
+    if (workspace_bytes) *workspace_bytes = verify_layout(n_seq, n_draft, vocab).bytes;
     return QLIN_OK;
 }
 
@@ -308,6 +321,12 @@ int qlin_verify_draft(int64_t n_seq, int64_t n_draft, int64_t vocab, const uint1
     a.draft_stride = draft_stride;
     a.n = (int)n_draft;
     a.V = (int)vocab;
+    const VerifyLayout l = verify_layout(n_seq, n_draft, vocab);
+    a.chunks = (int)l.chunks;
+    a.all_rows = (int)(draft ? l.rows : n_draft + 1);
+    a.stats = (VerifyStat *)workspace;
+    a.sums = (double *)((char *)workspace + l.sums);
+    a.decisions = (VerifyDecision *)((char *)workspace + l.decisions);
     const hipError_t e = launch_verify(a, (int)n_seq, (hipStream_t)stream);
     return e == hipSuccess ? QLIN_OK : hip_fail(e, "verify launch");
 }

@@ -49,6 +49,12 @@ struct CausalArgs {
 // Rows (tokens x heads of a group) of a tile of k_causal_few<rt>, or of k_causal_prompt (rt = 0).
 constexpr int causal_tile_rows(int rt) { return rt ? 16 * rt : 128; }
 
+// Verification.  A row of logits is cut into chunks of kVerifyChunk from the 16-byte boundary at
+// or before it (up to 7 logits earlier).
+constexpr int kVerifyChunk = 8192, kVerifyMaxDraft = 64;
+struct VerifyStat { float m; int at; double z; };      // maximum, its lowest index (greedy), sum of the weights
+struct VerifyDecision { int accepted, rejected; VerifyStat p, q; };   // and the statistics of the row that decides
+
 struct VerifyArgs {
     const uint16_t *target, *draft;
     const int32_t *drafted, *count;
@@ -56,6 +62,10 @@ struct VerifyArgs {
     int32_t *accepted, *tokens;
     int64_t target_stride, draft_stride;
     int n, V;
+    int chunks, all_rows;           // chunks of a row; rows of a sequence (targets, then drafts)
+    VerifyStat *stats;              // [sequence][all_rows][chunks]
+    double *sums;                   // [sequence][chunks]
+    VerifyDecision *decisions;      // [sequence]
 };
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st);

@@ -125,7 +125,7 @@ def verify(**kw):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(n_seq=-1), INVALID), (dict(n_seq=65537), UNSUPPORTED), (dict(n=-1), INVALID), (dict(n=65), UNSUPPORTED),
+    (dict(n_seq=-1), INVALID), (dict(n_seq=65536), UNSUPPORTED), (dict(n=-1), INVALID), (dict(n=65), UNSUPPORTED),
     (dict(V=0), INVALID), (dict(V=(1 << 24) + 1), UNSUPPORTED), (dict(t=None), INVALID), (dict(u=None), INVALID),
     (dict(a=None), INVALID), (dict(tok=None), INVALID), (dict(x=None), INVALID), (dict(ts=999), INVALID),
     (dict(ds=999), INVALID), (dict(ts=1 << 33), INVALID), (dict(t=A + 2), ALIGN), (dict(d=A + STEP + 8), ALIGN),
