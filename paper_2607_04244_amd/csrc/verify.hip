@@ -25,35 +25,76 @@ constexpr float kNegInf = -__builtin_huge_valf(), kPosInf = __builtin_huge_valf(
 constexpr int kStatsThreads = 256, kStatsVecs = kVerifyChunk / (8 * kStatsThreads);
 constexpr int kPickThreads = kVerifyChunk / 8, kPickWaves = kPickThreads / 64;
 
-// 2^t, t >= -1100, relative error 4.7e-11: (2^f - 1) / f on [-1/2, 1/2] as the polynomial of
-// degree 6 whose largest weighted error is smallest; 2^0 is 1 exactly.
-__device__ inline double pow2(double t) {
-    const double n = rint(t), f = t - n;
-    double p = 1.5196156371520414e-05;
-    p = __builtin_fma(p, f, 0.00015466756333052078);
-    p = __builtin_fma(p, f, 0.0013333935056283428);
-    p = __builtin_fma(p, f, 0.009618038132000921);
-    p = __builtin_fma(p, f, 0.05550410365990573);
-    p = __builtin_fma(p, f, 0.2402265106656167);
-    p = __builtin_fma(p, f, 0.6931471807045319);
-    p = __builtin_fma(p, f, 1.0);
-    return __builtin_amdgcn_ldexp(p, (int)n);
-}
+// 2^t, relative error 4.7e-11: (2^f - 1) / f on [-1/2, 1/2] as the polynomial of degree 6 whose
+// largest weighted error is smallest; 2^0 is 1 exactly.  The coefficients are opaque scalars:
+// of constants the compiler makes copies into the accumulator, two moves a product.
+struct Pow2 {
+    double c[6];
+    __device__ inline Pow2() : c{0.6931471807045319, 0.2402265106656167, 0.05550410365990573, 0.009618038132000921,
+                                 0.0013333935056283428, 0.00015466756333052078} {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) asm("" : "+s"(c[i]));
+    }
+    __device__ inline double fraction(double f) const {
+        double p = __builtin_fma(f, 1.5196156371520414e-05, c[5]);
+#pragma unroll
+        for (int i = 4; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
+        return __builtin_fma(p, f, 1.0);
+    }
+    // t >= -1100; 0 below the smallest number
+    __device__ inline double operator()(double t) const {
+        const double n = rint(t);
+        return __builtin_amdgcn_ldexp(fraction(t - n), (int)n);
+    }
+    // -1000 <= t < 1000: rounding by the sum with 1.5 2^52, whose low word is the integer, and the
+    // exponent by an integer sum (5 instructions of the full rate for 4 with a conversion)
+    __device__ inline double within(double t) const {
+        constexpr double kRound = 6755399441055744.0;
+        const double n = t + kRound;
+        const uint64_t p = __builtin_bit_cast(uint64_t, fraction(t - (n - kRound)));
+        const uint32_t hi = (uint32_t)(p >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, n) << 20);
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)p);
+    }
+};
 
 // Weights of a row: 2^(k x - k m), k = log2(e) / T, m its maximum.  -infinity and NaN give 0
-// (2^-1100 is below the smallest number), an infinite maximum 1 to its equals alone.
+// (2^-1100 is below the smallest number); where m is infinite, its equals have weight 1 and
+// all others none.
 struct Scale {
     double k, km;
-    float m;
-    __device__ inline Scale(double k_, float m_) : k(k_), km(k_ * (double)m_), m(m_) {}
+    bool inf;
+    Pow2 pow2;
+    __device__ inline Scale(double k_, float m) : k(k_), km(k_ * (double)m), inf(m == kPosInf) {}
     __device__ inline double operator()(float x) const {
-        if (m == kPosInf) return x == kPosInf ? 1.0 : 0.0;
-        return pow2(fmax(__builtin_fma((double)x, k, -km), -1100.0));
+        return inf ? (x == kPosInf ? 1.0 : 0.0) : pow2(fmax(__builtin_fma((double)x, k, -km), -1100.0));
+    }
+    // of eight logits: one branch
+    __device__ inline void weights(const float x[8], double w[8]) const {
+        if (inf) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = x[e] == kPosInf ? 1.0 : 0.0;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = pow2(fmax(__builtin_fma((double)x[e], k, -km), -1100.0));
+        }
+    }
+    // their sum, where weights below 2^-1000 may count as that: next to the maximum's 1 they are
+    // no part of a 64-bit sum
+    __device__ inline double sum(const float x[8]) const {
+        double s[2] = {0.0, 0.0};
+        if (inf) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[0] += x[e] == kPosInf ? 1.0 : 0.0;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e & 1] += pow2.within(fmax(__builtin_fma((double)x[e], k, -km), -1000.0));
+        }
+        return s[0] + s[1];
     }
 };
 // The factor from weights relative to m to weights relative to the larger M.
 __device__ inline double rescale(double k, float m, float M) {
-    return m == M ? 1.0 : m == kNegInf || M == kPosInf ? 0.0 : pow2(fmax(((double)m - (double)M) * k, -1100.0));
+    return m == M ? 1.0 : m == kNegInf || M == kPosInf ? 0.0 : Pow2()(fmax(((double)m - (double)M) * k, -1100.0));
 }
 
 __device__ inline double wave_sum(double v) {
@@ -80,9 +121,9 @@ __device__ inline Request load_request(const VerifyArgs &a, int b) {
 // A row of logits in vectors of 8: its first logit is element `off` of the first vector, which
 // is 16-byte aligned.
 struct Row {
-    const uint16_t *base;   // of the first vector
     int off;
-    __device__ inline Row(const uint16_t *p) : base((const uint16_t *)((uintptr_t)p & ~(uintptr_t)15)), off((int)((uintptr_t)p & 15) / 2) {}
+    const uint16_t *base;   // of the first vector
+    __device__ inline Row(const uint16_t *p) : off((int)((uintptr_t)p & 15) / 2), base(p - off) {}
 };
 // Logits 8 v - off .. + 7 of a row, -infinity outside it.  A vector that ends past the row is
 // read logit by logit: the row may be the last of its memory.  (One that starts before it
@@ -114,6 +155,7 @@ __device__ inline const uint16_t *draft_row(const VerifyArgs &a, int b, int i) {
 // maximum and the weights.
 __global__ __launch_bounds__(kStatsThreads) void k_verify_stats(VerifyArgs a) {
     __shared__ VerifyStat part[kStatsThreads / 64];
+    __shared__ float wave_m[kStatsThreads / 64];
     const int b = blockIdx.y, which = blockIdx.x / a.chunks, c = blockIdx.x - which * a.chunks;
     const bool is_draft = which > a.n;
     const int i = is_draft ? which - a.n - 1 : which;
@@ -132,37 +174,35 @@ __global__ __launch_bounds__(kStatsThreads) void k_verify_stats(VerifyArgs a) {
         for (int e = 0; e < 8; ++e) m = fmaxf(m, x[k][e]);           // ignores NaN
 #pragma unroll
     for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    // the chunk's maximum, so that all its weights are relative to one
+    if (lane == 0) wave_m[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kStatsThreads / 64; ++k) m = fmaxf(m, wave_m[k]);
     VerifyStat st{m, 0x7FFFFFFF, 0.0};
     if (rq.greedy) {
-        int at = 0x7FFFFFFF;
 #pragma unroll
         for (int k = kStatsVecs - 1; k >= 0; --k)
 #pragma unroll
             for (int e = 7; e >= 0; --e)
-                if (x[k][e] == m) at = 8 * (v0 + k * kStatsThreads) - row.off + e;
+                if (x[k][e] == m) st.at = 8 * (v0 + k * kStatsThreads) - row.off + e;
 #pragma unroll
-        for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o));
-        st.at = at;
+        for (int o = 32; o; o >>= 1) st.at = min(st.at, __shfl_xor(st.at, o));
     } else if (m != kNegInf) {
         const Scale w(rq.k, m);
         double s = 0.0;
 #pragma unroll
-        for (int k = 0; k < kStatsVecs; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s += w(x[k][e]);
+        for (int k = 0; k < kStatsVecs; ++k) s += w.sum(x[k]);
         st.z = wave_sum(s);
     }
     if (lane == 0) part[wave] = st;
     __syncthreads();
     if (threadIdx.x == 0) {
-        float M = kNegInf;
-        for (int k = 0; k < kStatsThreads / 64; ++k) M = fmaxf(M, part[k].m);
-        VerifyStat all{M, 0x7FFFFFFF, 0.0};
-        for (int k = 0; k < kStatsThreads / 64; ++k) {
-            if (part[k].m == M) all.at = min(all.at, part[k].at);
-            all.z += part[k].z * rescale(rq.k, part[k].m, M);
+        for (int k = 1; k < kStatsThreads / 64; ++k) {
+            st.at = min(st.at, part[k].at);
+            st.z += part[k].z;
         }
-        a.stats[((int64_t)b * a.all_rows + which) * a.chunks + c] = all;
+        a.stats[((int64_t)b * a.all_rows + which) * a.chunks + c] = st;
     }
 }
 
@@ -205,8 +245,9 @@ struct Choice {
         load_logits(row, v, V, l);
         const Scale p(k, mp);
         const double inv_p = 1.0 / zp;
+        p.weights(l, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = p(l[e]) * inv_p;
+        for (int e = 0; e < 8; ++e) w[e] *= inv_p;
         if (!rest) return;
         const int j0 = 8 * v - row.off;
         if (q) {
@@ -220,8 +261,10 @@ struct Choice {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) d[e] = j0 + e >= 0 && j0 + e < V ? __uint_as_float((uint32_t)q[j0 + e] << 16) : kNegInf;
             }
+            double we[8];
+            s.weights(d, we);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = fmax(w[e] - s(d[e]) * inv_q, 0.0);
+            for (int e = 0; e < 8; ++e) w[e] = fmax(w[e] - we[e] * inv_q, 0.0);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -289,110 +332,100 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_weigh(VerifyArgs a) {
     }
 }
 
-// Sum over the threads before this one, and over all, in a fixed order.
-__device__ inline double before_of(double own, double *buf, double *total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double s = own;
+// Inclusive sum over the lanes.
+__device__ inline double lanes_upto(double v, int lane) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const double v = __shfl_up(s, o);
-        s += lane >= o ? v : 0.0;
+        const double u = __shfl_up(v, o);
+        v += lane >= o ? u : 0.0;
     }
-    __syncthreads();
-    if (lane == 63) buf[wave] = s;
-    __syncthreads();
-    double t = 0.0, at = 0.0;
-    for (int i = 0; i < kPickWaves; ++i) {
-        if (i == wave) at = t;
-        t += buf[i];
-    }
-    *total = t;
-    return at + (s - own);
+    return v;
 }
+__device__ inline double from_lane(double v, int l) { return __shfl(v, l); }
 
+// One workgroup a sequence.  Its chunk is found by every wave for itself, 64 chunks at a time;
+// the token by the running sum of its 8192, eight a thread.
 __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
-    __shared__ double buf[kPickWaves], base;
-    __shared__ int first, last;
-    const int b = blockIdx.x, tid = threadIdx.x;
+    __shared__ double part[kPickWaves];
+    __shared__ int chosen, last_of[kPickWaves];
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Request rq = load_request(a, b);
     const VerifyDecision d = a.decisions[b];
-    int next = -1;
-    if (rq.greedy) {
-        next = d.p.m != kNegInf ? d.p.at : -1;
-    } else if (d.p.z > 0.0) {
-        // a chunk's sum: what was weighed, or if nothing is left of the difference, the target's
-        const double *sums = a.sums + (int64_t)b * a.chunks;
-        const VerifyStat *stats = a.stats + ((int64_t)b * a.all_rows + d.accepted) * a.chunks;
-        const int per = (a.chunks + kPickThreads - 1) / kPickThreads, c0 = min(tid * per, a.chunks), c1 = min(c0 + per, a.chunks);
-        bool rest = d.rejected;
-        auto mass = [&](int c) { return rest ? sums[c] : stats[c].z * rescale(rq.k, stats[c].m, d.p.m); };
-        double own = 0.0, total, before;
-        for (int c = c0; c < c1; ++c) own += mass(c);
-        before = before_of(own, buf, &total);
-        if (rest && !(total > 0.0)) {                       // the same in every thread
-            rest = false;
-            own = 0.0;
-            for (int c = c0; c < c1; ++c) own += mass(c);
-            before = before_of(own, buf, &total);
-        }
-        const double r = (double)a.uniform[b * (a.n + 1) + a.n] * total;
-        if (tid == 0) {
-            first = 0x7FFFFFFF;
-            last = -1;
-        }
-        __syncthreads();
-        double run = before;
-        int mine = -1;
-        double mine_base = 0.0;
-        for (int c = c0; c < c1; ++c) {
-            const double s = mass(c);
-            if (s > 0.0) {
-                atomicMax(&last, c);
-                if (mine < 0 && run + s > r) {
-                    mine = c;
-                    mine_base = run;
-                    atomicMin(&first, c);
-                }
-            }
-            run += s;
-        }
-        __syncthreads();
-        const int chunk = first != 0x7FFFFFFF ? first : last;
-        const bool past = first == 0x7FFFFFFF;              // rounding left none: the last token of all
-        if (!past && mine == chunk) base = mine_base;
-        __syncthreads();
-        const double at = past ? 0.0 : base;
-        if (tid == 0) {
-            first = 0x7FFFFFFF;
-            last = -1;
-        }
-        double w[8];
-        const Choice ch = choice_of(a, b, d, rq.k);
-        const int v = chunk * (kVerifyChunk / 8) + tid;
-        ch.weights(v, a.V, rest, w);
-        own = 0.0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) own += w[e];
-        run = before_of(own, buf, &total);
-        // a chunk's mass from the statistics is relative to the row's maximum, weights to its sum
-        const double need = rest ? r - at : (r - at) / d.p.z;
-        int hit = 0x7FFFFFFF, end = -1;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            run += w[e];
-            const int j = 8 * v - ch.row.off + e;
-            if (w[e] > 0.0) {
-                end = j;
-                if (hit == 0x7FFFFFFF && !past && run > need) hit = j;
-            }
-        }
-        if (hit != 0x7FFFFFFF) atomicMin(&first, hit);
-        if (end >= 0) atomicMax(&last, end);
-        __syncthreads();
-        next = first != 0x7FFFFFFF ? first : last;
-    }
     if (tid == 0) a.accepted[b] = d.accepted;
-    if (tid <= a.n) a.tokens[b * (a.n + 1) + tid] = tid < d.accepted ? a.drafted[b * a.n + tid] : tid == d.accepted ? next : -1;
+    if (tid <= a.n && tid != d.accepted) a.tokens[b * (a.n + 1) + tid] = tid < d.accepted ? a.drafted[b * a.n + tid] : -1;
+    int *out = a.tokens + b * (a.n + 1) + d.accepted;
+    if (rq.greedy || !(d.p.z > 0.0)) {
+        if (tid == 0) *out = rq.greedy && d.p.m != kNegInf ? d.p.at : -1;
+        return;
+    }
+    // a chunk's mass: what was weighed, or, if nothing is left of the difference, the target's
+    const double *sums = a.sums + (int64_t)b * a.chunks;
+    const VerifyStat *stats = a.stats + ((int64_t)b * a.all_rows + d.accepted) * a.chunks;
+    bool rest = d.rejected;
+    auto mass = [&](int c) { return c >= a.chunks ? 0.0 : rest ? sums[c] : stats[c].z * rescale(rq.k, stats[c].m, d.p.m); };
+    auto total_mass = [&]() {
+        double t = 0.0;
+        for (int c = 0; c < a.chunks; c += 64) t += from_lane(lanes_upto(mass(c + lane), lane), 63);
+        return t;
+    };
+    double total = total_mass();
+    if (rest && !(total > 0.0)) {
+        rest = false;
+        total = total_mass();
+    }
+    const double r = (double)a.uniform[b * (a.n + 1) + a.n] * total;
+    int chunk = -1, any = 0;                                // the first chunk past r; the last with any mass
+    double at = 0.0, run = 0.0;
+    for (int c = 0; c < a.chunks && chunk < 0; c += 64) {
+        const double own = mass(c + lane), upto = run + lanes_upto(own, lane);
+        const uint64_t over = __ballot(own > 0.0 && upto > r), some = __ballot(own > 0.0);
+        if (some) any = c + 63 - __builtin_clzll(some);
+        if (over) {
+            const int l = __builtin_ctzll(over);
+            chunk = c + l;
+            at = from_lane(upto, l) - from_lane(own, l);
+        }
+        run = from_lane(upto, 63);
+    }
+    const bool past = chunk < 0;                            // rounding left none: the last token of all
+    if (past) chunk = any;
+    double w[8], own = 0.0;
+    const Choice ch = choice_of(a, b, d, rq.k);
+    const int v = chunk * (kVerifyChunk / 8) + tid, j0 = 8 * v - ch.row.off;
+    ch.weights(v, a.V, rest, w);
+    int end = -1;                                           // this thread's last token of any weight
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        own += w[e];
+        if (w[e] > 0.0) end = j0 + e;
+    }
+    const double upto = lanes_upto(own, lane);
+    int wave_end = end;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) wave_end = max(wave_end, __shfl_xor(wave_end, o));
+    if (lane == 63) part[wave] = upto;
+    if (lane == 0) last_of[wave] = wave_end;
+    if (tid == 0) chosen = 0x7FFFFFFF;
+    __syncthreads();
+    // a chunk's mass from the statistics is relative to the row's maximum, weights to its sum
+    const double need = rest ? r - at : (r - at) / d.p.z;
+    double before = 0.0;
+    for (int i = 0; i < wave; ++i) before += part[i];
+    double sum = before + (upto - own);
+    int hit = 0x7FFFFFFF;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        sum += w[e];
+        if (hit == 0x7FFFFFFF && w[e] > 0.0 && !past && sum > need) hit = j0 + e;
+    }
+    if (hit != 0x7FFFFFFF) atomicMin(&chosen, hit);
+    __syncthreads();
+    if (tid == 0) {
+        int next = chosen;
+        if (next == 0x7FFFFFFF)
+            for (int i = 0; i < kPickWaves; ++i) next = last_of[i] >= 0 ? last_of[i] : next;
+        *out = next;
+    }
 }
 
 }  // namespace
