@@ -84,32 +84,60 @@ __device__ inline void load_lds_s16_nt(const uint16_t *base, uint32_t off, const
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// The row tile (of R packed rows) that work item idx is, among all sequences' tiles in
-// order: its sequence (-1: past the last) and its number in it.  By the whole wave: tiles
-// of 64 sequences at a time are summed up.
-struct Tile { int b, t; };
-__device__ inline Tile find_tile(const CausalArgs &a, int idx, int R, int lane) {
+// The row tile (of R packed rows) that work item idx is, among all sequences' tiles: its
+// sequence and its number in it; false past the last.  The tiles that see the most keys come
+// first, in kClasses classes of equal steps of keys up to max_len (a tile with the longest
+// walk that starts late ends late: packed prompts of 1 to 2048 tokens 125 us in the order of
+// the rows).  By the whole wave: a class's tiles of 64 sequences at a time are summed up.
+constexpr int kClasses = 8;
+
+// Inclusive sum over the lanes by DPP: within rows of 16, then across them.
+__device__ inline int lanes_upto(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // lane 15 to the next row: rows 1, 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);     // lane 31 to rows 2, 3
+    return v;
+}
+__device__ inline int64_t lane_value(int64_t v, int l) {
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, l), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), l);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+__device__ inline bool find_tile(const CausalArgs &a, int idx, int R, int lane, Seq &s, int &tile) {
     for (int i = 0; i < a.b.n_seq; i += 64) {
-        int own = 0;
-        if (i + lane < a.b.n_seq) {
-            const int r0 = min(max(a.b.new_start[i + lane], 0), a.b.rows);
-            const int n = min(max(a.b.new_start[i + lane + 1], r0), a.b.rows) - r0;
-            own = (min(n, a.b.max_new) * a.G + R - 1) / R;
+        Seq own{};
+        int tiles = 0;
+        if (i + lane < a.b.n_seq) {                      // the sequences' data, a lane each
+            own = load_seq(a.b, i + lane);
+            tiles = (own.rows * a.G + R - 1) / R;
         }
-        int sum = own;                                   // inclusive sum over the lanes
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(sum, o);
-            sum += lane >= o ? v : 0;
+        // tiles whose first token is at class c's lower bound or later, and not in class c + 1
+        int upper = tiles;
+        const float per_token = (float)a.G / (float)R, step = (float)a.max_len / kClasses;
+        for (int c = kClasses - 1; c >= 0; --c) {
+            const float at = ((float)c * step - (float)own.p0) * per_token;
+            const int lower = c == 0 ? 0 : min(max((int)fminf(at, 1e9f), 0), upper);
+            const int sum = lanes_upto(upper - lower), total = __builtin_amdgcn_readlane(sum, 63);
+            if (idx < total) {
+                const int l = __popcll(__ballot(sum <= idx));
+                // the class's last tile of the sequence first
+                tile = __builtin_amdgcn_readlane(upper, l) - 1 - (idx - __builtin_amdgcn_readlane(sum - (upper - lower), l));
+                s.row0 = __builtin_amdgcn_readlane(own.row0, l);
+                s.n = __builtin_amdgcn_readlane(own.n, l);
+                s.rows = __builtin_amdgcn_readlane(own.rows, l);
+                s.p0 = __builtin_amdgcn_readlane(own.p0, l);
+                s.L = __builtin_amdgcn_readlane(own.L, l);
+                s.slot0 = lane_value(own.slot0, l);
+                return true;
+            }
+            idx -= total;
+            upper = lower;
         }
-        const int total = __shfl(sum, 63);
-        if (idx < total) {
-            const int at = __popcll(__ballot(sum <= idx));
-            return Tile{i + at, idx - (__shfl(sum, at) - __shfl(own, at))};
-        }
-        idx -= total;
     }
-    return Tile{-1, 0};
+    return false;
 }
 
 // A row tile's part of the work, the same in both kernels.
@@ -135,16 +163,19 @@ __device__ inline int64_t uniform(int64_t v) {
 // keys are shared in that XCD's L2.
 template <int R>
 __device__ inline bool find_work(const CausalArgs &a, int lane, Work &w) {
-    const int idx = gn_chunk(blockIdx.x, a.Hkv, a.inv_heads, a.heads_shift);
-    w.h = blockIdx.x - idx * a.Hkv;
+    const int item = gn_chunk(blockIdx.x, a.Hkv, a.inv_heads, a.heads_shift);
+    w.h = blockIdx.x - item * a.Hkv;
     w.split = blockIdx.y;
-    Tile t{idx, 0};
-    if (!a.one_tile) {
-        t = find_tile(a, a.tiles - 1 - idx, R, lane);     // late tiles, which see the most keys, first
-        if (t.b < 0) return false;
+    int tile = 0;
+    if (a.one_tile) {
+        if (item >= a.b.n_seq) return false;
+        w.s = load_seq(a.b, item);
+    } else {
+        // where all workgroups run at once, two a compute unit, a long one goes with a short one
+        const int half = (a.tiles + 1) / 2, idx = a.pairs && item >= half ? a.tiles - 1 - (item - half) : item;
+        if (!find_tile(a, idx, R, lane, w.s, tile)) return false;
     }
-    w.s = load_seq(a.b, t.b);
-    w.r0 = t.t * R;
+    w.r0 = tile * R;
     w.rows = min(R, w.s.rows * a.G - w.r0);
     if (w.rows <= 0) return false;
     w.i0 = w.r0 / a.G;
@@ -402,8 +433,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
         const int d = 16 * dt + 4 * g;
         if (a.S == 1) {
             const bool none = w.s.L == 0 || w.s.p0 + ro.i < 0;
+            const float inv = 1.0f / ls;
             uint2 y = {};
-            if (!none) y = make_uint2(cvt_pk_bf16(acc[0] / ls, acc[1] / ls), cvt_pk_bf16(acc[2] / ls, acc[3] / ls));
+            if (!none) y = make_uint2(cvt_pk_bf16(acc[0] * inv, acc[1] * inv), cvt_pk_bf16(acc[2] * inv, acc[3] * inv));
             *(uint2 *)(a.out + row_at(w, ro, a.out_stride) + d) = y;
         } else {
             const int64_t at = part_at(a, w, ro);
@@ -664,14 +696,15 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
     if (32 * wave + r >= w.rows) return;
     if (a.S == 1) {
         const bool none = w.s.L == 0 || last < 0;
+        const float inv = 1.0f / l;
         uint16_t *op = a.out + row_at(w, row, a.out_stride);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {                        // dimensions 32 dt + 8 i + 4 hi .. + 3
                 uint2 y = {};
-                if (!none) y = make_uint2(cvt_pk_bf16(o[dt][4 * i] / l, o[dt][4 * i + 1] / l),
-                                          cvt_pk_bf16(o[dt][4 * i + 2] / l, o[dt][4 * i + 3] / l));
+                if (!none) y = make_uint2(cvt_pk_bf16(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv),
+                                          cvt_pk_bf16(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv));
                 *(uint2 *)(op + 32 * dt + 8 * i + 4 * hi) = y;
             }
     } else {
@@ -744,8 +777,9 @@ __global__ __launch_bounds__(256) void k_causal_combine(CausalArgs a) {
 #pragma unroll
     for (int i = 1; i < P; ++i) fold(gml[grp + i].x, gml[grp + i].y, go[grp + i][l]);
     const bool none = s.L == 0 || s.p0 + (mrow - s.row0) < 0;
+    const float inv = 1.0f / ls;
     uint2 y = {};
-    if (!none) y = make_uint2(cvt_pk_bf16(acc.x / ls, acc.y / ls), cvt_pk_bf16(acc.z / ls, acc.w / ls));
+    if (!none) y = make_uint2(cvt_pk_bf16(acc.x * inv, acc.y * inv), cvt_pk_bf16(acc.z * inv, acc.w * inv));
     *(uint2 *)(a.out + (int64_t)mrow * a.out_stride + (int64_t)hq * kHeadDim + 4 * l) = y;
 }
 

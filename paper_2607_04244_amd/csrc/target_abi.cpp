@@ -100,7 +100,7 @@ BatchArgs batch_args(const qlin_batch *b, const qlin_kv_cache *c) {
 }
 
 // The kernel and split of one causal attention, from the host's bounds.
-struct CausalPlan { int rt = 0, tiles = 0, one_tile = 0, S = 1; int64_t ws_bytes = 0; };
+struct CausalPlan { int rt = 0, tiles = 0, one_tile = 0, pairs = 0, S = 1; int64_t ws_bytes = 0; };
 
 int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, CausalPlan *p) {
     const int64_t G = Hq / Hkv, most = b->max_new * G;
@@ -109,8 +109,9 @@ int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t split
     p->one_tile = per <= 1;
     const int64_t tiles = p->one_tile ? b->n_seq : std::min(b->n_seq * per, b->rows * G / R + b->n_seq);
     int64_t S = splits;
+    int cus = 256;                   // with forced ranges the plan is arithmetic
     if (S == 0) {
-        int dev = 0, cus = 0;
+        int dev = 0;
         hipError_t e = hipGetDevice(&dev);
         if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
         if (e != hipSuccess) return hip_fail(e, "device query");
@@ -124,6 +125,7 @@ int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t split
         return fail(QLIN_ERR_UNSUPPORTED, "too many rows, heads and key ranges for one call");
     p->tiles = (int)tiles;
     p->S = (int)S;
+    p->pairs = tiles * Hkv * S <= 2 * cus;
     p->ws_bytes = S > 1 ? b->rows * Hq * S * (kHeadDim + 2) * 4 : 0;
     return QLIN_OK;
 }
@@ -257,7 +259,9 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     a.ws_ml = a.ws_o + (size_t)batch->rows * q_heads * p.S * kHeadDim;
     a.tiles = p.tiles;
     a.one_tile = p.one_tile;
+    a.pairs = p.pairs;
     a.S = p.S;
+    a.max_len = (int)batch->max_len;
     gn_reciprocal(a.Hkv, &a.inv_heads, &a.heads_shift);
     a.inv_g = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
     a.c = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)kHeadDim)));

@@ -40,7 +40,9 @@ struct CausalArgs {
     float *ws_o, *ws_ml;            // S > 1: [rows][Hq][S][128] sums, [rows][Hq][S] (maximum, sum of weights)
     int tiles;                      // row tiles, at least those there are
     int one_tile;                   // one tile a sequence: tile i is sequence i
+    int pairs;                      // at most two workgroups a compute unit
     int S;                          // key ranges
+    int max_len;                    // bound of the sequences' lengths (orders the tiles)
     uint32_t inv_heads, inv_g;      // x / Hkv by gn_chunk; ceil(2^32 / G) (0: G = 1)
     int heads_shift;
     float c;                        // scale log2(e): scores to base-2 exponents

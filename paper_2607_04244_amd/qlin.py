@@ -367,76 +367,83 @@ def _check_out(out, shape, device):
         raise ValueError(f"out must be a contiguous bf16 tensor of shape {tuple(shape)} on {device}")
 
 
-def _need(name, t, dtype, device, shape=None, rank=None):
-    """Raise unless t is a tensor of this type, device and shape (None entries: any size)."""
-    import torch
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be a {dtype} tensor on {device}")
-    if rank is not None and t.dim() != rank:
-        raise ValueError(f"{name} must have rank {rank}")
-    if shape is not None and (t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape))):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+_torch = None
 
 
-def _current(name, t):
-    """The device of a tensor, which has to be the current one (the stream's)."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be a tensor on the current CUDA device")
-    return t.device
+def _device():
+    """The current device's index (and torch loaded, for callers that hold CUDA tensors)."""
+    global _torch, _raw_stream, _current_device
+    if _current_device is None:
+        import torch
+        _torch, _current_device, _raw_stream = torch, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    elif _torch is None:
+        import torch
+        _torch = torch
+    return _current_device()
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _address(name, t, dtype, dev):
+    """The address of a tensor, which has to be of this type on the current device (its
+    stream's).  The checks of a call cost about as much as its launch: one pass, no
+    torch.device objects."""
+    if not isinstance(t, _torch.Tensor) or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be a {dtype} tensor on the current CUDA device")
+    return t.data_ptr()
 
 
-def _kv_cache(k_cache, v_cache, device, cache_start):
+def _vector(name, t, dtype, dev, n):
+    """The address of a contiguous tensor of n values; None stays None."""
+    if t is None:
+        return None
+    p = _address(name, t, dtype, dev)
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, of shape ({n},)")
+    return p
+
+
+def _kv_cache(k_cache, v_cache, dev):
     """KVCache of [sequences, heads, capacity, 128] or packed [tokens, heads, 128] tensors."""
-    import torch
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _need(name, t, torch.bfloat16, device)
-    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+    k = _address("k_cache", k_cache, _torch.bfloat16, dev)
+    v = _address("v_cache", v_cache, _torch.bfloat16, dev)
+    shape, stride = k_cache.shape, k_cache.stride()
+    if v_cache.shape != shape or v_cache.stride() != stride:
         raise ValueError("k_cache and v_cache must have the same shape and strides")
-    if k_cache.dim() not in (3, 4) or k_cache.shape[-1] != 128 or k_cache.stride(-1) != 1 or k_cache.numel() == 0:
+    rank = len(shape)
+    if rank not in (3, 4) or shape[-1] != 128 or stride[-1] != 1 or k_cache.numel() == 0:
         raise ValueError("the cache must be [sequences, heads, capacity, 128] or [tokens, heads, 128], rows contiguous")
-    if k_cache.dim() == 3:
-        slots, heads, _ = k_cache.shape
-        token, head, _ = k_cache.stride()
-        return KVCache(k_cache.data_ptr(), v_cache.data_ptr(), heads, slots, token, head, 0)
-    n, heads, capacity, _ = k_cache.shape
-    seq, head, token, _ = k_cache.stride()
+    if rank == 3:
+        return KVCache(k, v, shape[1], shape[0], stride[0], stride[1], 0)
+    n, heads, capacity, _ = shape
+    seq, head, token, _ = stride
     if n == 1:
         seq = 0
     if token <= 0 or seq % token:
         raise ValueError("the cache's sequences must lie whole tokens apart")
-    seq_slots = seq // token
-    return KVCache(k_cache.data_ptr(), v_cache.data_ptr(), heads, (n - 1) * seq_slots + capacity, token, head, seq_slots)
+    seq //= token
+    return KVCache(k, v, heads, (n - 1) * seq + capacity, token, head, seq)
 
 
-def _batch(device, rows, new_start, length, max_new, max_len, cache_start, k_cache):
-    import torch
-    _need("length", length, torch.int32, device, rank=1)
+def _batch(dev, rows, new_start, length, max_new, max_len, cache_start, k_cache):
+    i32 = _torch.int32
+    lengths = _address("length", length, i32, dev)
+    if length.dim() != 1 or not length.is_contiguous():
+        raise ValueError("length must be contiguous, of rank 1")
     n = length.shape[0]
-    _need("new_start", new_start, torch.int32, device, (n + 1,))
-    if cache_start is not None:
-        _need("cache_start", cache_start, torch.int64, device, (n,))
-    for name, t in (("length", length), ("new_start", new_start), ("cache_start", cache_start)):
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-    if cache_start is None and n > 1 and (k_cache.dim() == 3 or k_cache.shape[0] < n):
+    starts = _vector("new_start", new_start, i32, dev, n + 1)
+    slots = _vector("cache_start", cache_start, _torch.int64, dev, n)
+    if slots is None and n > 1 and (k_cache.dim() == 3 or k_cache.shape[0] < n):
         raise ValueError("several sequences need cache_start or a cache of as many sequences")
     if max_len is None:
-        max_len = k_cache.shape[2] if k_cache.dim() == 4 else k_cache.shape[0]
-    return Batch(n, rows, rows if max_new is None else min(max_new, rows), max_len, new_start.data_ptr(),
-                 length.data_ptr(), _ptr(cache_start))
+        max_len = k_cache.shape[-2] if k_cache.dim() == 4 else k_cache.shape[0]
+    return Batch(n, rows, rows if max_new is None or max_new > rows else max_new, max_len, starts, lengths, slots)
 
 
-def _check_out_rows(name, t, shape, device):
-    """An output [rows, heads, 128] whose rows may be apart."""
-    import torch
-    _need(name, t, torch.bfloat16, device, shape)
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != 128):
+def _row_stride(name, t, heads):
+    """Elements between the rows of [rows, heads, 128], heads contiguous."""
+    row, head, one = t.stride()
+    if one != 1 or (heads > 1 and head != 128):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return row if t.shape[0] > 1 else heads * 128
 
 
 def norm_rope_append(q, k, v, k_cache, v_cache, new_start, length, max_new=None, max_len=None, cache_start=None,
@@ -452,34 +459,39 @@ def norm_rope_append(q, k, v, k_cache, v_cache, new_start, length, max_new=None,
     or None; inv_freq: float64 [rotary_dim / 2] or None.  Returns ``out`` [rows,
     q heads, 128]; rows of no sequence are left as they are.
     """
-    import torch
-    device = _current("q", q)
+    dev = _device()
+    bf16 = _torch.bfloat16
+    cache = _kv_cache(k_cache, v_cache, dev)
+    at, strides, widths = [], [], []
     for name, t in (("q", q), ("k", k), ("v", v)):
-        _need(name, t, torch.bfloat16, device, rank=2)
-        if t.shape[1] == 0 or t.shape[1] % 128 or t.stride(1) != 1 or t.shape[0] != q.shape[0]:
+        at.append(_address(name, t, bf16, dev))
+        if t.dim() != 2:
+            raise ValueError(f"{name} must have rank 2")
+        (rows, width), (row, one) = t.shape, t.stride()
+        if width == 0 or width % 128 or one != 1 or (widths and rows != q.shape[0]):
             raise ValueError(f"{name} must be [rows, heads * 128] with contiguous rows")
-    cache = _kv_cache(k_cache, v_cache, device, cache_start)
-    rows, Hq = q.shape[0], q.shape[1] // 128
-    if k.shape[1] != cache.heads * 128 or v.shape[1] != cache.heads * 128:
+        strides.append(row if rows > 1 else width)
+        widths.append(width)
+    Hq = widths[0] // 128
+    if widths[1] != cache.heads * 128 or widths[2] != widths[1]:
         raise ValueError(f"k and v must have the cache's {cache.heads} heads")
-    batch = _batch(device, rows, new_start, length, max_new, max_len, cache_start, k_cache)
-    for name, t in (("q_norm", q_norm), ("k_norm", k_norm)):
-        if t is not None:
-            _need(name, t, torch.bfloat16, device, (128,))
+    batch = _batch(dev, rows, new_start, length, max_new, max_len, cache_start, k_cache)
+    rotary, freq = 0, None
     if inv_freq is not None:
-        _need("inv_freq", inv_freq, torch.float64, device, rank=1)
-    for name, t in (("q_norm", q_norm), ("k_norm", k_norm), ("inv_freq", inv_freq)):
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
+        half = inv_freq.numel()
+        rotary, freq = 2 * half, _vector("inv_freq", inv_freq, _torch.float64, dev, half)
     if out is None:
-        out = torch.empty((rows, Hq, 128), dtype=torch.bfloat16, device=device)
+        out = _torch.empty((rows, Hq, 128), dtype=bf16, device=q.device)
+        out_at, out_stride = out.data_ptr(), widths[0]
     else:
-        _check_out_rows("out", out, (rows, Hq, 128), device)
-    stride = [t.stride(0) if rows > 1 else t.shape[1] for t in (q, k, v)]
-    _check(qlin_norm_rope_append(batch, cache, Hq, 128, q.data_ptr(), stride[0], k.data_ptr(), stride[1], v.data_ptr(),
-                                 stride[2], _ptr(q_norm), _ptr(k_norm), eps, _ptr(inv_freq),
-                                 0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved), out.data_ptr(),
-                                 out.stride(0) if rows > 1 else Hq * 128, _stream()))
+        out_at = _address("out", out, bf16, dev)
+        if out.shape != (rows, Hq, 128):
+            raise ValueError(f"out must have shape {(rows, Hq, 128)}")
+        out_stride = _row_stride("out", out, Hq)
+    _check(lib().qlin_norm_rope_append(batch, cache, Hq, 128, at[0], strides[0], at[1], strides[1], at[2], strides[2],
+                                       _vector("q_norm", q_norm, bf16, dev, 128),
+                                       _vector("k_norm", k_norm, bf16, dev, 128), eps, freq, rotary,
+                                       1 if interleaved else 0, out_at, out_stride, _raw_stream(dev)))
     return out
 
 
@@ -494,27 +506,52 @@ def causal_attention(q, k_cache, v_cache, new_start, length, max_new=None, max_l
     given.  Returns ``out`` [rows, q heads, 128]; rows of no sequence are left as
     they are.
     """
-    import torch
-    device = _current("q", q)
-    _need("q", q, torch.bfloat16, device, rank=3)
-    rows, Hq, D = q.shape
-    _check_out_rows("q", q, (rows, Hq, D), device)
-    cache = _kv_cache(k_cache, v_cache, device, cache_start)
-    batch = _batch(device, rows, new_start, length, max_new, max_len, cache_start, k_cache)
+    dev = _device()
+    bf16 = _torch.bfloat16
+    q_at = _address("q", q, bf16, dev)
+    if q.dim() != 3:
+        raise ValueError("q must have rank 3")
+    rows, Hq, D = shape = q.shape
+    q_stride = _row_stride("q", q, Hq)
+    cache = _kv_cache(k_cache, v_cache, dev)
+    batch = _batch(dev, rows, new_start, length, max_new, max_len, cache_start, k_cache)
     if workspace is None:
-        _, nbytes, _ = qlin_causal_plan(batch, Hq, cache.heads, D, splits)
-        if nbytes:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    elif workspace.device != device or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+        need = ctypes.c_int64()
+        _check(lib().qlin_causal_plan(batch, Hq, cache.heads, D, splits, None, ctypes.byref(need), None, 0))
+        if need.value:
+            workspace = _torch.empty(need.value, dtype=_torch.uint8, device=q.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
     if out is None:
-        out = torch.empty((rows, Hq, D), dtype=torch.bfloat16, device=device)
+        out = _torch.empty(shape, dtype=bf16, device=q.device)
+        out_at, out_stride = out.data_ptr(), Hq * D
     else:
-        _check_out_rows("out", out, (rows, Hq, D), device)
-    _check(qlin_causal_attention(batch, cache, Hq, D, scale, splits, q.data_ptr(), q.stride(0) if rows > 1 else Hq * D,
-                                 out.data_ptr(), out.stride(0) if rows > 1 else Hq * D, _ptr(workspace),
-                                 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+        out_at = _address("out", out, bf16, dev)
+        if out.shape != shape:
+            raise ValueError(f"out must have shape {tuple(shape)}")
+        out_stride = _row_stride("out", out, Hq)
+    _check(lib().qlin_causal_attention(batch, cache, Hq, D, scale, splits, q_at, q_stride, out_at, out_stride,
+                                       *_scratch(workspace), _raw_stream(dev)))
     return out
+
+
+def _scratch(workspace):
+    """(address, bytes) of a workspace or None."""
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def _logit_rows(name, t, n, rows, vocab):
+    """Elements between the rows of [n, rows, vocab] logits, all rows at one distance."""
+    if t.shape != (n, rows, vocab):
+        raise ValueError(f"{name} must have shape {(n, rows, vocab)}")
+    seq, row, one = t.stride()
+    if rows == 1:
+        row = seq
+    if n * rows <= 1:
+        return vocab
+    if (one != 1 and vocab > 1) or (n > 1 and seq != rows * row):
+        raise ValueError(f"{name} must have contiguous rows at one distance")
+    return row
 
 
 def verify_draft(target, drafted, uniform, draft=None, n_draft=None, temperature=None, accepted=None, tokens=None,
@@ -528,46 +565,40 @@ def verify_draft(target, drafted, uniform, draft=None, n_draft=None, temperature
     tokens of each sequence, or None; temperature: float32 [n], or None (1).  Returns
     (accepted int32 [n], tokens int32 [n, drafts + 1], -1 behind the last).
     """
-    import torch
-    device = _current("target", target)
-    _need("target", target, torch.bfloat16, device, rank=3)
+    dev = _device()
+    bf16, i32, f32 = _torch.bfloat16, _torch.int32, _torch.float32
+    target_at = _address("target", target, bf16, dev)
+    if target.dim() != 3 or target.shape[1] == 0:
+        raise ValueError("target must be [n, drafts + 1, vocab]")
     n, rows, vocab = target.shape
-    _need("drafted", drafted, torch.int32, device, (n, rows - 1))
-    _need("uniform", uniform, torch.float32, device, (n, rows))
+    target_stride = _logit_rows("target", target, n, rows, vocab)
+    draft_at, draft_stride = None, vocab
     if draft is not None:
-        _need("draft", draft, torch.bfloat16, device, (n, rows - 1, vocab))
-        draft = draft if rows > 1 else None                 # no drafted tokens, no rows
-    if n_draft is not None:
-        _need("n_draft", n_draft, torch.int32, device, (n,))
-    if temperature is not None:
-        _need("temperature", temperature, torch.float32, device, (n,))
-    strides = []
-    for name, t in (("target", target), ("draft", draft)):
-        if t is None or t.shape[0] * t.shape[1] <= 1:
-            row = vocab
-        else:
-            row = t.stride(1) if t.shape[1] > 1 else t.stride(0)
-        if t is not None and (t.stride(2) != 1 or (t.shape[0] > 1 and t.stride(0) != t.shape[1] * row)):
-            raise ValueError(f"{name} must have contiguous rows at one distance")
-        strides.append(row)
+        draft_at = _address("draft", draft, bf16, dev)
+        draft_stride = _logit_rows("draft", draft, n, rows - 1, vocab)
+        if rows == 1:                                       # no drafted tokens, no rows
+            draft_at = None
     if accepted is None:
-        accepted = torch.empty(n, dtype=torch.int32, device=device)
+        accepted = _torch.empty(n, dtype=i32, device=target.device)
     if tokens is None:
-        tokens = torch.empty((n, rows), dtype=torch.int32, device=device)
-    _need("accepted", accepted, torch.int32, device, (n,))
-    _need("tokens", tokens, torch.int32, device, (n, rows))
-    for name, t in (("drafted", drafted), ("uniform", uniform), ("n_draft", n_draft), ("temperature", temperature),
-                    ("accepted", accepted), ("tokens", tokens), ("workspace", workspace)):
-        if t is not None and (t.device != device or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous tensor on {device}")
+        tokens = _torch.empty((n, rows), dtype=i32, device=target.device)
+    at = []
+    for name, t, dtype, cols in (("drafted", drafted, i32, rows - 1), ("uniform", uniform, f32, rows), ("tokens", tokens, i32, rows)):
+        at.append(_address(name, t, dtype, dev))
+        if t.shape != (n, cols) or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous, of shape {(n, cols)}")
     if workspace is None:
-        nbytes = qlin_verify_plan(n, rows - 1, vocab)
-        if nbytes:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    _check(qlin_verify_draft(n, rows - 1, vocab, target.data_ptr(), strides[0], _ptr(draft), strides[1],
-                             drafted.data_ptr(), _ptr(n_draft), _ptr(temperature), uniform.data_ptr(),
-                             accepted.data_ptr(), tokens.data_ptr(), _ptr(workspace),
-                             0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+        need = ctypes.c_int64()
+        _check(lib().qlin_verify_plan(n, rows - 1, vocab, ctypes.byref(need)))
+        if need.value:
+            workspace = _torch.empty(need.value, dtype=_torch.uint8, device=target.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
+    _check(lib().qlin_verify_draft(n, rows - 1, vocab, target_at, target_stride, draft_at, draft_stride, at[0],
+                                   _vector("n_draft", n_draft, i32, dev, n),
+                                   _vector("temperature", temperature, f32, dev, n), at[1],
+                                   _vector("accepted", accepted, i32, dev, n), at[2], *_scratch(workspace),
+                                   _raw_stream(dev)))
     return accepted, tokens
 
 
