@@ -14,7 +14,7 @@
 //       units in flight, no barrier until the waves' sums are merged.
 //   k_causal_prompt    128 rows, 32 a wave, 64-key tiles shared by four waves: bound by
 //       the matrix cores and the softmax between them.
-//   k_causal_combine   joins key ranges, in order.
+//   k_causal_join      joins key ranges, in order.
 //
 // Softmax statistics are fp32.  Weights are rounded to bf16 once (the operand) and the
 // sum adds the rounded weights.
@@ -158,14 +158,14 @@ __device__ inline int64_t uniform(int64_t v) {
     return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// Workgroup (x, y): key range y of item x = tile * heads + head.  Workgroups go to the 8 XCDs
+// Workgroup (x, y): key range y of item x = tile number * heads + head.  Workgroups go to the 8 XCDs
 // in turn, x first: with a multiple of 8 heads all work on one head is on one XCD, and its
 // keys are shared in that XCD's L2.
 template <int R>
-__device__ inline bool find_work(const CausalArgs &a, int lane, Work &w) {
+__device__ inline bool find_work(const CausalArgs &a, int lane, int split, Work &w) {
     const int item = gn_chunk(blockIdx.x, a.Hkv, a.inv_heads, a.heads_shift);
     w.h = blockIdx.x - item * a.Hkv;
-    w.split = blockIdx.y;
+    w.split = split;
     int tile = 0;
     if (a.one_tile) {
         if (item >= a.b.n_seq) return false;
@@ -206,9 +206,24 @@ __device__ inline RowOf row_of(const CausalArgs &a, const Work &w, int x) {
 __device__ inline int64_t row_at(const Work &w, const RowOf &r, int64_t stride) {
     return (int64_t)(w.s.row0 + r.i) * stride + r.hq * kHeadDim;
 }
-// Its place among the partial results.
-__device__ inline int64_t part_at(const CausalArgs &a, const Work &w, const RowOf &r) {
-    return ((int64_t)(w.s.row0 + r.i) * a.Hq + r.hq) * a.S + w.split;
+// The steps [first, end) of a key range, of `all` steps in ranges of at least `least`: as few
+// ranges as hold them (used), the last ones of a.S empty.
+struct Range { int first, end, used; };
+__device__ inline Range range_of(const CausalArgs &a, int all, int least, int split) {
+    const int per = max((all + a.S - 1) / a.S, least);
+    return Range{split * per, min((split + 1) * per, all), (all + per - 1) / per};
+}
+
+// Partial results: for each item and range the tile's sums as the matrix cores leave them, in
+// units of 64 lanes x 4 values (1 KiB, one store of a wave), and (maximum, sum of weights) of
+// its rows.
+template <int R>
+__device__ inline float *unit_at(const CausalArgs &a, int split, int unit) {
+    return a.ws_o + (((int64_t)blockIdx.x * a.S + split) * (R / 2) + unit) * 256;
+}
+template <int R>
+__device__ inline float2 *row_ml(const CausalArgs &a, int split, int row) {
+    return (float2 *)a.ws_ml + ((int64_t)blockIdx.x * a.S + split) * R + row;
 }
 
 // The values of keys [key, key + 4) and [key2, key2 + 4), without those behind `last`.
@@ -238,12 +253,12 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int g = lane >> 4, r = lane & 15;
     Work w;
-    if (!find_work<R>(a, lane, w)) return;
+    if (!find_work<R>(a, lane, blockIdx.y, w)) return;
 
     // units of this key range, and of this wave: u0 + wave, u0 + wave + 4, ...
-    const int units = (w.hi + kFewKeys - 1) / kFewKeys;
-    const int per = max((units + a.S - 1) / a.S, kFewWaves);
-    const int u0 = w.split * per, u1 = min(u0 + per, units);
+    const Range range = range_of(a, (w.hi + kFewKeys - 1) / kFewKeys, kFewWaves, w.split);
+    if (a.S > 1 && w.split >= range.used) return;
+    const int u0 = range.first, u1 = range.end;
 
     // byte offsets of a lane in four keys, for each order of their units
     uint32_t koff[4], voff[2];
@@ -438,9 +453,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
             if (!none) y = make_uint2(cvt_pk_bf16(acc[0] * inv, acc[1] * inv), cvt_pk_bf16(acc[2] * inv, acc[3] * inv));
             *(uint2 *)(a.out + row_at(w, ro, a.out_stride) + d) = y;
         } else {
-            const int64_t at = part_at(a, w, ro);
-            *(v4f *)(a.ws_o + at * kHeadDim + d) = acc;
-            if (dt == 0 && g == 0) *(float2 *)(a.ws_ml + 2 * at) = make_float2(M, ls);
+            *(v4f *)(unit_at<R>(a, w.split, x) + 4 * lane) = acc;
+            if (dt == 0 && g == 0) *row_ml<R>(a, w.split, row) = make_float2(M, ls);
         }
     }
 }
@@ -452,6 +466,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
 // u - 1.  K and V each have a ring of four steps in LDS, filled by direct-to-LDS loads two
 // steps ahead; one barrier for two steps.
 constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves, kStepKeys = 32, kStepSlots = 4;
+constexpr int kPromptSteps = 8;                               // least steps of a key range
 constexpr int kStepUnits = kStepKeys * kHeadDim / 8;          // 16-byte units of a step's K or V (512)
 
 __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalArgs a) {
@@ -459,11 +474,11 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int hi = lane >> 5, r = lane & 31;
     Work w;
-    if (!find_work<kPromptRows>(a, lane, w)) return;
+    if (!find_work<kPromptRows>(a, lane, blockIdx.y, w)) return;
 
-    const int all = (w.hi + kStepKeys - 1) / kStepKeys;
-    const int per = (all + a.S - 1) / a.S;
-    const int u0 = w.split * per, n = max(min(u0 + per, all) - u0, 0);      // steps [u0, u0 + n)
+    const Range range = range_of(a, (w.hi + kStepKeys - 1) / kStepKeys, kPromptSteps, w.split);
+    if (a.S > 1 && w.split >= range.used) return;
+    const int u0 = range.first, n = range.end - u0;               // steps [u0, u0 + n)
     const uint16_t *kp = w.k + (int64_t)u0 * kStepKeys * a.b.tok, *vp = w.v + (int64_t)u0 * kStepKeys * a.b.tok;
     const int first_key = u0 * kStepKeys;
 
@@ -708,79 +723,93 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
                 *(uint2 *)(op + 32 * dt + 8 * i + 4 * hi) = y;
             }
     } else {
-        const int64_t at = part_at(a, w, row);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                *(v4f *)(a.ws_o + at * kHeadDim + 32 * dt + 8 * i + 4 * hi) =
+                *(v4f *)(unit_at<kPromptRows>(a, w.split, (4 * wave + dt) * 4 + i) + 4 * lane) =
                     v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-        if (hi == 0) *(float2 *)(a.ws_ml + 2 * at) = make_float2(m, l);
+        if (hi == 0) *row_ml<kPromptRows>(a, w.split, 32 * wave + r) = make_float2(m, l);
     }
 }
 
 // ---------------------------------------------------------------- joining key ranges
 
-// Eight groups of 32 lanes, four dimensions a lane; P groups share a row, each every P-th
-// range, and are merged through LDS in group order.
-template <int P>
-__global__ __launch_bounds__(256) void k_causal_combine(CausalArgs a) {
-    constexpr int kBatch = 4;
-    __shared__ float2 gml[8];
-    __shared__ float4 go[8][32];
-    static_assert(P >= 2, "the two groups of a wave share a row");
-    const int grp = threadIdx.x >> 5, l = threadIdx.x & 31, lane = threadIdx.x & 63;
-    const int part = grp % P;
-    const int rest = gn_chunk(blockIdx.x, a.Hkv, a.inv_heads, a.heads_shift);
-    const int h = blockIdx.x - rest * a.Hkv;                  // on the XCD that wrote the head's partials
-    const int x = rest * (8 / P) + grp / P;                   // (row, head of the group)
-    const int mrow = x / a.G;
-    const int b = find_seq(a.b, min(mrow, a.b.rows), lane);   // one row a wave
-    bool on = mrow < a.b.rows && b < a.b.n_seq;
-    Seq s = {};
-    if (on) {
-        s = load_seq(a.b, b);
-        on = mrow >= s.row0 && mrow < s.row0 + s.rows;
+// A wave takes one unit of an item (or every P-th range of it, P waves together, merged through
+// LDS in wave order), a lane 4 dimensions of a row.  Bound by the partial results' bytes, or
+// with few rows by one trip to memory for the lengths and one for all ranges.
+constexpr int kJoinBatch = 8;      // ranges requested together
+
+template <int RT, int P>
+__global__ __launch_bounds__(256) void k_causal_join(CausalArgs a) {
+    constexpr int R = causal_tile_rows(RT);
+    __shared__ float2 gml[4][64];
+    __shared__ v4f go[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = wave % P;
+    const int unit = (blockIdx.y * 4 + wave) / P;
+    Work w;
+    if (!find_work<R>(a, lane, 0, w)) return;
+    int row, d;                                                    // of this lane
+    if (RT) {
+        row = 16 * (unit >> 3) + (lane & 15);
+        d = 16 * (unit & 7) + 4 * (lane >> 4);
+    } else {
+        row = 32 * (unit >> 4) + (lane & 31);
+        d = 8 * (unit & 15) + 4 * (lane >> 5);
     }
-    const int hq = h * a.G + x - mrow * a.G;
-    const int64_t at = ((int64_t)mrow * a.Hq + hq) * a.S;
+    const int keys = RT ? kFewKeys : kStepKeys;
+    const int used = w.hi > 0 ? range_of(a, (w.hi + keys - 1) / keys, RT ? kFewWaves : kPromptSteps, 0).used : 0;
+    const bool on = row < w.rows;
     float m = kNegInf, ls = 0.0f;
-    float4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto fold = [&](float m2, float l2, const float4 &v) {
-        const float M = fmaxf(m, m2), mu = M == kNegInf ? 0.0f : M;
-        const float f1 = exp2_hw((m - mu) * a.c), f2 = exp2_hw((m2 - mu) * a.c);
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto fold = [&](const float2 &e, const v4f &v) {
+        const float M = fmaxf(m, e.x), mu = M == kNegInf ? 0.0f : M;
+        const float f1 = exp2_hw((m - mu) * a.c), f2 = exp2_hw((e.x - mu) * a.c);
         m = M;
-        ls = ls * f1 + l2 * f2;
-        acc.x = acc.x * f1 + v.x * f2;
-        acc.y = acc.y * f1 + v.y * f2;
-        acc.z = acc.z * f1 + v.z * f2;
-        acc.w = acc.w * f1 + v.w * f2;
+        ls = ls * f1 + e.y * f2;
+        acc = acc * f1 + v * f2;
     };
     if (on) {
-        for (int s0 = part; s0 < a.S; s0 += P * kBatch) {
-            float2 e[kBatch];
-            float4 v[kBatch];
+        for (int s0 = part; s0 < used; s0 += P * kJoinBatch) {
+            float2 e[kJoinBatch];
+            v4f v[kJoinBatch];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const int si = s0 + P * i;
-                e[i] = si < a.S ? *(const float2 *)(a.ws_ml + 2 * (at + si)) : make_float2(kNegInf, 0.0f);
-                v[i] = si < a.S ? *(const float4 *)(a.ws_o + (at + si) * kHeadDim + 4 * l) : float4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int i = 0; i < kJoinBatch; ++i) {
+                const int s = s0 + P * i;
+                e[i] = make_float2(kNegInf, 0.0f);
+                v[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                if (s < used) {
+                    e[i] = *row_ml<R>(a, s, row);
+                    v[i] = *(const v4f *)(unit_at<R>(a, s, unit) + 4 * lane);
+                }
             }
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) fold(e[i].x, e[i].y, v[i]);
+            for (int i = 0; i < kJoinBatch; ++i)
+                if (s0 + P * i < used) fold(e[i], v[i]);
         }
     }
-    if (l == 0) gml[grp] = make_float2(m, ls);
-    go[grp][l] = acc;
-    __syncthreads();
-    if (part != 0 || !on) return;
+    if (P > 1) {
+        gml[wave][lane] = make_float2(m, ls);
+        go[wave][lane] = acc;
+        __syncthreads();
+        if (part != 0) return;
 #pragma unroll
-    for (int i = 1; i < P; ++i) fold(gml[grp + i].x, gml[grp + i].y, go[grp + i][l]);
-    const bool none = s.L == 0 || s.p0 + (mrow - s.row0) < 0;
+        for (int i = 1; i < P; ++i) fold(gml[wave + i][lane], go[wave + i][lane]);
+    }
+    if (!on) return;
+    const RowOf ro = row_of(a, w, row);
+    const bool none = w.s.L == 0 || w.s.p0 + ro.i < 0;
     const float inv = 1.0f / ls;
     uint2 y = {};
-    if (!none) y = make_uint2(cvt_pk_bf16(acc.x * inv, acc.y * inv), cvt_pk_bf16(acc.z * inv, acc.w * inv));
-    *(uint2 *)(a.out + (int64_t)mrow * a.out_stride + (int64_t)hq * kHeadDim + 4 * l) = y;
+    if (!none) y = make_uint2(cvt_pk_bf16(acc[0] * inv, acc[1] * inv), cvt_pk_bf16(acc[2] * inv, acc[3] * inv));
+    *(uint2 *)(a.out + row_at(w, ro, a.out_stride) + d) = y;
+}
+
+template <int RT>
+void launch_join(const CausalArgs &a, hipStream_t st) {
+    constexpr int units = causal_tile_rows(RT) / 2;                // of an item
+    if (a.S > 4) hipLaunchKernelGGL((k_causal_join<RT, 4>), dim3((unsigned)(a.tiles * a.Hkv), units), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_causal_join<RT, 1>), dim3((unsigned)(a.tiles * a.Hkv), units / 4), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -797,12 +826,10 @@ hipError_t launch_causal(const CausalArgs &a, int rt, hipStream_t st) {
     else hipLaunchKernelGGL(k_causal_prompt, grid, dim3(kPromptWaves * 64), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;
-    const int64_t pairs = (int64_t)a.b.rows * a.G;                 // (row, head of a group)
-    const int P = a.S >= 5 ? 8 : a.S >= 3 ? 4 : 2;
-    const dim3 cgrid((unsigned)((pairs * P + 7) / 8 * a.Hkv));
-    if (P == 8) hipLaunchKernelGGL(k_causal_combine<8>, cgrid, dim3(256), 0, st, a);
-    else if (P == 4) hipLaunchKernelGGL(k_causal_combine<4>, cgrid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(k_causal_combine<2>, cgrid, dim3(256), 0, st, a);
+    if (rt == 1) launch_join<1>(a, st);
+    else if (rt == 2) launch_join<2>(a, st);
+    else if (rt == 4) launch_join<4>(a, st);
+    else launch_join<0>(a, st);
     return hipGetLastError();
 }
 

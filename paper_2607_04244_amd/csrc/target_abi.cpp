@@ -120,13 +120,13 @@ int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t split
         S = std::min<int64_t>({wanted, (b->max_len + least - 1) / least, kMaxSplits});
     }
     S = std::max<int64_t>(S, 1);
-    // work items of 256 threads in a 32-bit grid
-    if (tiles * Hkv * S >= (int64_t)1 << 24 || (S > 1 && b->rows * Hq >= (int64_t)1 << 24))
+    // work items of 256 threads in a 32-bit grid, also those that join the ranges
+    if (tiles * Hkv * std::max(S, S > 1 ? R / 2 : 0) >= (int64_t)1 << 24)
         return fail(QLIN_ERR_UNSUPPORTED, "too many rows, heads and key ranges for one call");
     p->tiles = (int)tiles;
     p->S = (int)S;
     p->pairs = tiles * Hkv * S <= 2 * cus;
-    p->ws_bytes = S > 1 ? b->rows * Hq * S * (kHeadDim + 2) * 4 : 0;
+    p->ws_bytes = S > 1 ? tiles * Hkv * S * R * (kHeadDim + 2) * 4 : 0;
     return QLIN_OK;
 }
 
@@ -256,7 +256,7 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     a.Hkv = (int)cache->heads;
     a.G = (int)(q_heads / cache->heads);
     a.ws_o = (float *)workspace;
-    a.ws_ml = a.ws_o + (size_t)batch->rows * q_heads * p.S * kHeadDim;
+    a.ws_ml = a.ws_o + (size_t)p.tiles * a.Hkv * p.S * causal_tile_rows(p.rt) * kHeadDim;
     a.tiles = p.tiles;
     a.one_tile = p.one_tile;
     a.pairs = p.pairs;

@@ -37,7 +37,7 @@ struct CausalArgs {
     uint16_t *out;
     int64_t q_stride, out_stride;
     int Hq, Hkv, G;
-    float *ws_o, *ws_ml;            // S > 1: [rows][Hq][S][128] sums, [rows][Hq][S] (maximum, sum of weights)
+    float *ws_o, *ws_ml;            // S > 1: sums and (maximum, sum of weights) of each item, range and row
     int tiles;                      // row tiles, at least those there are
     int one_tile;                   // one tile a sequence: tile i is sequence i
     int pairs;                      // at most two workgroups a compute unit

@@ -157,7 +157,7 @@ def test_verify_workspace_is_checked():
 def test_attention_workspace_is_checked():
     """Forced key ranges need no device: the plan is arithmetic."""
     splits, need, text = qlin.qlin_causal_plan(batch(), 32, 8, 128, 3)
-    assert (splits, need) == (3, 40 * 32 * 3 * 130 * 4) and "k_causal_few<4>" in text and "combine=1" in text
+    assert (splits, need) == (3, 3 * 8 * 64 * 3 * 130 * 4) and "k_causal_few<4>" in text and "combine=1" in text
     assert attend(splits=3, wb=need - 16) == INVALID and attend(splits=3, ws=None, wb=0) == INVALID
     assert "workspace" in qlin.last_error()
     assert attend(splits=3, out=A + 7 * STEP + 64) == INVALID
