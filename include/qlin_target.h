@@ -109,7 +109,7 @@ int qlin_norm_rope_append(const qlin_batch *batch, const qlin_kv_cache *cache, i
  *   splits           0 = the planner's choice, else the number of key ranges
  *                    (at most 256)
  * Outputs (each may be NULL): *splits_out, *workspace_bytes (0 when one range
- * suffices), and text such as "kernel=k_causal_few<1> splits=32 grid=256 combine=1"
+ * suffices), and text such as "kernel=k_causal_few splits=32 grid=256 combine=1"
  * in buf (at most buflen bytes).
  * Errors: INVALID, UNSUPPORTED, HIP (device query).
  */

@@ -9,9 +9,10 @@
 // the weights are already the B operand of O^T += V^T P^T, whose A operand the
 // transposing LDS read takes from V as it lies in the cache.
 //
-//   k_causal_few<RT>   up to 16 RT rows (RT = 1, 2, 4: one token, draft blocks): bound by
-//       the cache's bytes.  Four waves, each with units of 32 keys and LDS of its own, two
-//       units in flight, no barrier until the waves' sums are merged.
+//   k_causal_few       up to 16 rows (single tokens): bound by the cache's bytes.  Four waves,
+//       each with units of 32 keys and LDS of its own, two units in flight, no barrier until
+//       the waves' sums are merged.
+//   k_causal_mid<NR>   up to 32 NR rows (draft blocks): the cache's bytes, then the products.
 //   k_causal_prompt    128 rows, 32 a wave, 64-key tiles shared by four waves: bound by
 //       the matrix cores and the softmax between them.
 //   k_causal_join      joins key ranges, in order.
@@ -78,8 +79,8 @@ __device__ inline void load_lds_s16(const uint16_t *base, uint32_t off, uint32_t
 __device__ inline void load_lds_v16(const uint16_t *src, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds), "v"(src) : "memory", "m0");
 }
-__device__ inline void load_lds_s16_nt(const uint16_t *base, uint32_t off, const uint4 *lds_dst) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds_addr(lds_dst)), "v"(off), "s"(base) : "memory", "m0");
+__device__ inline void load_lds_s16_nt(const uint16_t *base, uint32_t off, uint32_t lds) {      // for data a call reads once
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -206,11 +207,11 @@ __device__ inline RowOf row_of(const CausalArgs &a, const Work &w, int x) {
 __device__ inline int64_t row_at(const Work &w, const RowOf &r, int64_t stride) {
     return (int64_t)(w.s.row0 + r.i) * stride + r.hq * kHeadDim;
 }
-// The steps [first, end) of a key range, of `all` steps in ranges of at least `least`: as few
+// The steps [first, end) of a key range, of `all` steps in ranges of at least a.least: as few
 // ranges as hold them (used), the last ones of a.S empty.
 struct Range { int first, end, used; };
-__device__ inline Range range_of(const CausalArgs &a, int all, int least, int split) {
-    const int per = max((all + a.S - 1) / a.S, least);
+__device__ inline Range range_of(const CausalArgs &a, int all, int split) {
+    const int per = max((all + a.S - 1) / a.S, a.least);
     return Range{split * per, min((split + 1) * per, all), (all + per - 1) / per};
 }
 
@@ -240,14 +241,43 @@ __device__ inline v8bf values_up_to(v4s_t lo, v4s_t hi, int key, int key2, int l
 // the weights: up to there the weights just exceed 1, with the same relative rounding.
 constexpr float kLazy = 8.0f;
 
+// The sums of W waves, each relative to its own maximum, as one: returns (maximum, sum of
+// weights) and the values in acc.
+template <int W>
+__device__ inline float2 merged(const float2 *ml, int ml_stride, const v4f *sums, int stride, float c, v4f &acc) {
+    float M = kNegInf;
+#pragma unroll
+    for (int i = 0; i < W; ++i) M = fmaxf(M, ml[i * ml_stride].x);
+    const float mu = M == kNegInf ? 0.0f : M;
+    float l = 0.0f;
+    acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const float2 e = ml[i * ml_stride];
+        const float f = exp2_hw((e.x - mu) * c);
+        l += e.y * f;
+        acc += sums[i * stride] * f;
+    }
+    return make_float2(M, l);
+}
+
+// Four dimensions of an output row from their sums and the sum of weights.
+__device__ inline void store_out(const CausalArgs &a, const Work &w, const RowOf &row, int d, const v4f &acc, float l) {
+    uint2 y = {};
+    if (w.s.L > 0 && w.s.p0 + row.i >= 0) {
+        const float inv = 1.0f / l;
+        y = make_uint2(cvt_pk_bf16(acc[0] * inv, acc[1] * inv), cvt_pk_bf16(acc[2] * inv, acc[3] * inv));
+    }
+    *(uint2 *)(a.out + row_at(w, row, a.out_stride) + d) = y;
+}
+
 // ---------------------------------------------------------------- few rows
 
-constexpr int kFewWaves = 4, kFewKeys = 32, kFewStages = 2;
+constexpr int kFewRows = 16, kFewWaves = 4, kFewKeys = 32, kFewStages = 2;
 constexpr int kFewUnits = kFewKeys * kHeadDim / 8;        // 16-byte units of one unit's K or V (512)
 
-template <int RT>
 __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) {
-    constexpr int R = 16 * RT;
+    constexpr int R = kFewRows;
     __shared__ __attribute__((aligned(16))) uint4 ring[kFewWaves][kFewStages][2][kFewUnits];   // then the waves' sums
     __shared__ float2 ml[kFewWaves][R];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -256,7 +286,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
     if (!find_work<R>(a, lane, blockIdx.y, w)) return;
 
     // units of this key range, and of this wave: u0 + wave, u0 + wave + 4, ...
-    const Range range = range_of(a, (w.hi + kFewKeys - 1) / kFewKeys, kFewWaves, w.split);
+    const Range range = range_of(a, (w.hi + kFewKeys - 1) / kFewKeys, w.split);
     if (a.S > 1 && w.split >= range.used) return;
     const int u0 = range.first, u1 = range.end;
 
@@ -266,13 +296,15 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
     for (int j = 0; j < 4; ++j) koff[j] = 2u * ((uint32_t)g * (uint32_t)a.b.tok + 8u * (r ^ (4 * j + g)));
 #pragma unroll
     for (int j = 0; j < 2; ++j) voff[j] = 2u * ((uint32_t)g * (uint32_t)a.b.tok + 8u * (r ^ (2 * (4 * j + g))));
+    const uint32_t lds = lds_addr(ring[wave]);
     auto issue = [&](int u, int st) {
+        const uint32_t to = lds + st * (2 * kFewUnits * 16);
         if ((u + 1) * kFewKeys <= w.hi) {
             const int64_t at = (int64_t)u * kFewKeys * a.b.tok;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                load_lds_s16_nt(w.k + at + 4 * j * a.b.tok, koff[j & 3], &ring[wave][st][0][j * 64]);
-                load_lds_s16_nt(w.v + at + 4 * j * a.b.tok, voff[j & 1], &ring[wave][st][1][j * 64]);
+                load_lds_s16_nt(w.k + at + 4 * j * a.b.tok, koff[j & 3], to + j * 1024);
+                load_lds_s16_nt(w.v + at + 4 * j * a.b.tok, voff[j & 1], to + kFewUnits * 16 + j * 1024);
             }
             return;
         }
@@ -280,35 +312,30 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
         for (int j = 0; j < 8; ++j) {                    // the last, partial unit: its last key again
             const int kk = 4 * j + g;
             const int64_t at = (int64_t)min(u * kFewKeys + kk, w.hi - 1) * a.b.tok;
-            load_lds_x16_nt(w.k + at + 8 * (r ^ (kk & 15)), &ring[wave][st][0][j * 64]);
-            load_lds_x16_nt(w.v + at + 8 * (r ^ (2 * (kk & 7))), &ring[wave][st][1][j * 64]);
+            load_lds_v16(w.k + at + 8 * (r ^ (kk & 15)), to + j * 1024);
+            load_lds_v16(w.v + at + 8 * (r ^ (2 * (kk & 7))), to + kFewUnits * 16 + j * 1024);
         }
     };
 
-    // queries: B operand, row r of row tile t
-    v8bf qf[RT][4];
-    int last[RT];                                             // last key that the row sees
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const RowOf row = row_of(a, w, min(16 * t + r, w.rows - 1));
-        last[t] = w.s.p0 + row.i;
+    // queries: B operand, row r
+    const RowOf row = row_of(a, w, min(r, w.rows - 1));
+    const int last = w.s.p0 + row.i;                          // last key that the row sees
+    v8bf qf[4];
+    {
         const uint16_t *qp = a.q + row_at(w, row, a.q_stride) + 8 * g;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) qf[t][ks] = *(const v8bf *)(qp + 32 * ks);
+        for (int ks = 0; ks < 4; ++ks) qf[ks] = *(const v8bf *)(qp + 32 * ks);
     }
     const int first_last = w.s.p0 + w.i0;                     // keys up to here are seen by every row
 
-    float m[RT], l[RT];
-    v4f o[RT][8];
+    float m, l;
+    v4f o[8];
     auto run = [&](auto mode) {                               // whether the sums came out finite
         constexpr bool careful = decltype(mode)::value;
+        m = kNegInf;
+        l = 0.0f;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            m[t] = kNegInf;
-            l[t] = 0.0f;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) o[t][dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        }
+        for (int dt = 0; dt < 8; ++dt) o[dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         int st = 0;
         if (u0 + wave < u1) issue(u0 + wave, 0);
         if (u0 + wave + kFewWaves < u1) issue(u0 + wave + kFewWaves, 1);
@@ -319,64 +346,41 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
             const uint4 *kb = ring[wave][st][0], *vb = ring[wave][st][1];
             const int key0 = u * kFewKeys;
             const bool masked = key0 + kFewKeys - 1 > first_last;
-            v4f sc[RT][2];
+            v4f sc[2];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) {
+                sc[kt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int t = 0; t < RT; ++t) sc[t][kt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks) {
-                    const v8bf kf = *(const v8bf *)&kb[key_unit(16 * kt + r, 4 * ks + g)];
-#pragma unroll
-                    for (int t = 0; t < RT; ++t)
-                        sc[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][ks], sc[t][kt], 0, 0, 0);
-                }
+                for (int ks = 0; ks < 4; ++ks)
+                    sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const v8bf *)&kb[key_unit(16 * kt + r, 4 * ks + g)], qf[ks], sc[kt], 0, 0, 0);
             }
             if (masked) {
 #pragma unroll
-                for (int t = 0; t < RT; ++t)
+                for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            sc[t][kt][i] = key0 + 16 * kt + 4 * g + i <= last[t] ? sc[t][kt][i] : kNegInf;
+                    for (int i = 0; i < 4; ++i) sc[kt][i] = key0 + 16 * kt + 4 * g + i <= last ? sc[kt][i] : kNegInf;
             }
-            float mt[RT];
-            bool grown = false;
+            float mt = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                             fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+            mt = pair32_max(pair16_max(mt));
+            if (__ballot(mt * a.c > __builtin_fmaf(m, a.c, kLazy))) {
+                const float mn = fmaxf(m, mt);
+                const float alpha = exp2_hw((m - (mn == kNegInf ? 0.0f : mn)) * a.c);
+                l *= alpha;
 #pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                mt[t] = fmaxf(fmaxf(fmaxf(sc[t][0][0], sc[t][0][1]), fmaxf(sc[t][0][2], sc[t][0][3])),
-                              fmaxf(fmaxf(sc[t][1][0], sc[t][1][1]), fmaxf(sc[t][1][2], sc[t][1][3])));
-                mt[t] = pair32_max(pair16_max(mt[t]));
-                grown |= mt[t] * a.c > __builtin_fmaf(m[t], a.c, kLazy);
+                for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
+                m = mn;
             }
-            if (__ballot(grown)) {                               // all row tiles at once: one branch
+            const float muc = (m == kNegInf ? 0.0f : m) * a.c;
+            uint32_t pw[4];
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const float mn = fmaxf(m[t], mt[t]);
-                    const float alpha = exp2_hw((m[t] - (mn == kNegInf ? 0.0f : mn)) * a.c);
-                    l[t] *= alpha;
-#pragma unroll
-                    for (int dt = 0; dt < 8; ++dt) o[t][dt] *= alpha;
-                    m[t] = mn;
-                }
+            for (int i = 0; i < 4; ++i) {
+                const float e0 = exp2_hw(__builtin_fmaf(sc[i >> 1][2 * (i & 1)], a.c, -muc));
+                const float e1 = exp2_hw(__builtin_fmaf(sc[i >> 1][2 * (i & 1) + 1], a.c, -muc));
+                pw[i] = cvt_pk_bf16(e0, e1);
+                l = dot2(pw[i], kBf16OnePair, l);
             }
-            v8bf pb[RT];
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                const float muc = (m[t] == kNegInf ? 0.0f : m[t]) * a.c;
-                uint32_t pw[4];
-                float ls = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e0 = exp2_hw(__builtin_fmaf(sc[t][i >> 1][2 * (i & 1)], a.c, -muc));
-                    const float e1 = exp2_hw(__builtin_fmaf(sc[t][i >> 1][2 * (i & 1) + 1], a.c, -muc));
-                    pw[i] = cvt_pk_bf16(e0, e1);
-                    ls = dot2(pw[i], kBf16OnePair, ls);
-                }
-                l[t] += ls;
-                pb[t] = __builtin_bit_cast(v8bf, v4u{pw[0], pw[1], pw[2], pw[3]});
-            }
+            const v8bf pb = __builtin_bit_cast(v8bf, v4u{pw[0], pw[1], pw[2], pw[3]});
             const int q = r & 3, kr = 4 * g + (r >> 2);        // keys of elements 0..3; + 16 for 4..7
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) {
@@ -384,21 +388,17 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
                 const v4s_t lo4 = lds_read_tr((const char *)&vb[few_value_unit(kr, c)] + off);
                 const v4s_t hi4 = lds_read_tr((const char *)&vb[few_value_unit(kr + 16, c)] + off);
                 if (careful && masked) {
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        const int p0 = w.s.p0 + row_of(a, w, min(16 * t, w.rows - 1)).i, p1 = w.s.p0 + row_of(a, w, min(16 * t + 15, w.rows - 1)).i;
-                        v4f sum = o[t][dt];
-                        for (int p = p0; p <= p1; ++p) {
-                            const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values_up_to(lo4, hi4, key0 + 4 * g, key0 + 16 + 4 * g, p),
-                                                                                  pb[t], o[t][dt], 0, 0, 0);
-                            sum = last[t] == p ? x : sum;
-                        }
-                        o[t][dt] = sum;
+                    const int p1 = w.s.p0 + row_of(a, w, w.rows - 1).i;
+                    v4f sum = o[dt];
+                    for (int p = first_last; p <= p1; ++p) {
+                        const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values_up_to(lo4, hi4, key0 + 4 * g, key0 + 16 + 4 * g, p),
+                                                                              pb, o[dt], 0, 0, 0);
+                        sum = last == p ? x : sum;
                     }
+                    o[dt] = sum;
                 } else {
-                    const v8bf vf = __builtin_bit_cast(v8bf, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) o[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[t], o[t][dt], 0, 0, 0);
+                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(v8bf, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7)), pb, o[dt], 0, 0, 0);
                 }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this slot has been read
@@ -406,55 +406,203 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
         }
         float bad = 0.0f;                                        // NaN if any sum is not finite
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
+        for (int dt = 0; dt < 8; ++dt)
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) bad = __builtin_fmaf(o[t][dt][i], 0.0f, bad);
+            for (int i = 0; i < 4; ++i) bad = __builtin_fmaf(o[dt][i], 0.0f, bad);
         return !__ballot(bad != 0.0f);
     };
     if (!run(std::false_type{})) run(std::true_type{});
-#pragma unroll
-    for (int t = 0; t < RT; ++t) l[t] = pair32_sum(pair16_sum(l[t]));
+    l = pair32_sum(pair16_sum(l));
 
     // the waves' sums through LDS, in the matrix cores' order
     __syncthreads();
     v4f *sums = (v4f *)&ring[0][0][0][0];
-    static_assert(sizeof(ring) >= sizeof(v4f) * kFewWaves * RT * 8 * 64, "the sums fit the ring");
+    static_assert(sizeof(ring) >= sizeof(v4f) * kFewWaves * 8 * 64, "the sums fit the ring");
+    if (g == 0) ml[wave][r] = make_float2(m, l);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        if (g == 0) ml[wave][16 * t + r] = make_float2(m[t], l[t]);
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) sums[((wave * RT + t) * 8 + dt) * 64 + lane] = o[t][dt];
-    }
+    for (int dt = 0; dt < 8; ++dt) sums[(wave * 8 + dt) * 64 + lane] = o[dt];
     __syncthreads();
-    for (int x = wave; x < RT * 8; x += kFewWaves) {
-        const int t = x >> 3, dt = x & 7, row = 16 * t + r;
-        if (row >= w.rows) continue;
-        float M = kNegInf;
+    if (r >= w.rows) return;
 #pragma unroll
-        for (int i = 0; i < kFewWaves; ++i) M = fmaxf(M, ml[i][row].x);
-        const float mu = M == kNegInf ? 0.0f : M;
-        float ls = 0.0f;
-        v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < kFewWaves; ++i) {
-            const float2 e = ml[i][row];
-            const float f = exp2_hw((e.x - mu) * a.c);
-            ls += e.y * f;
-            acc += sums[((i * RT + t) * 8 + dt) * 64 + lane] * f;
-        }
-        const RowOf ro = row_of(a, w, row);
+    for (int dt = wave; dt < 8; dt += kFewWaves) {
+        v4f acc;
+        const float2 e = merged<kFewWaves>(&ml[0][r], R, sums + dt * 64 + lane, 8 * 64, a.c, acc);
         const int d = 16 * dt + 4 * g;
         if (a.S == 1) {
-            const bool none = w.s.L == 0 || w.s.p0 + ro.i < 0;
-            const float inv = 1.0f / ls;
-            uint2 y = {};
-            if (!none) y = make_uint2(cvt_pk_bf16(acc[0] * inv, acc[1] * inv), cvt_pk_bf16(acc[2] * inv, acc[3] * inv));
-            *(uint2 *)(a.out + row_at(w, ro, a.out_stride) + d) = y;
+            store_out(a, w, row, d, acc, e.y);
         } else {
-            *(v4f *)(unit_at<R>(a, w.split, x) + 4 * lane) = acc;
-            if (dt == 0 && g == 0) *row_ml<R>(a, w.split, row) = make_float2(M, ls);
+            *(v4f *)(unit_at<R>(a, w.split, dt) + 4 * lane) = acc;
+            if (dt == 0 && g == 0) *row_ml<R>(a, w.split, r) = e;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- draft blocks
+
+// 32 NR rows, NR = 1, 2: four waves for each 32 rows, a quarter of a step's 128 keys each, so
+// that a key range of 256 keys (a 16-token block over 8192 keys on all compute units) is two
+// steps, requested at once.  With 16-row tiles, all of them in each of four waves, the same
+// range took 15.0 us of 17.0; its products wait for one another.
+constexpr int kMidKeys = 128, kMidUnits = kMidKeys * kHeadDim / 8;
+
+template <int NR>
+__global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
+    constexpr int W = 4 * NR, R = 32 * NR;
+    __shared__ __attribute__((aligned(16))) uint4 ring[2][2][kMidUnits];      // [stage][K, V], then the waves' sums
+    __shared__ float2 ml[W][32];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int hi = lane >> 5, r = lane & 31, rt = wave >> 2, ku = wave & 3;
+    Work w;
+    if (!find_work<R>(a, lane, blockIdx.y, w)) return;
+    const Range range = range_of(a, (w.hi + kMidKeys - 1) / kMidKeys, w.split);
+    if (a.S > 1 && w.split >= range.used) return;
+
+    // a wave loads 4 keys at a time, W waves 4 W of a step
+    const uint32_t koff = 2u * ((uint32_t)(lane >> 4) * (uint32_t)a.b.tok + 8u * ((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)));
+    const uint32_t voff = 2u * ((uint32_t)(lane >> 4) * (uint32_t)a.b.tok + 8u * ((lane & 15) ^ (4 * (lane >> 4))));
+    const uint32_t lds = lds_addr(ring) + wave * 1024;
+    auto issue = [&](int t) {
+        const uint32_t to = lds + (t & 1) * (2 * kMidUnits * 16);
+        const int64_t at = ((int64_t)t * kMidKeys + 4 * wave) * a.b.tok;
+        if ((t + 1) * kMidKeys <= w.hi) {
+#pragma unroll
+            for (int j = 0; j < kMidKeys / (4 * W); ++j) {
+                load_lds_s16_nt(w.k + at + 4 * W * j * a.b.tok, koff, to + j * W * 1024);
+                load_lds_s16_nt(w.v + at + 4 * W * j * a.b.tok, voff, to + kMidUnits * 16 + j * W * 1024);
+            }
+            return;
+        }
+#pragma unroll 1
+        for (int j = 0; j < kMidKeys / (4 * W); ++j) {                // the last, partial step: its last key again
+            const int kk = 4 * (j * W + wave) + (lane >> 4);
+            const int64_t key = (int64_t)min(t * kMidKeys + kk, w.hi - 1) * a.b.tok;
+            load_lds_v16(w.k + key + 8 * ((lane & 15) ^ (kk & 15)), to + j * W * 1024);
+            load_lds_v16(w.v + key + 8 * ((lane & 15) ^ (4 * (kk & 3))), to + kMidUnits * 16 + j * W * 1024);
+        }
+    };
+
+    const RowOf row = row_of(a, w, min(32 * rt + r, w.rows - 1));
+    const int last = w.s.p0 + row.i;                                       // last key this row sees
+    const int tile_first = __builtin_amdgcn_readfirstlane(w.s.p0 + row_of(a, w, min(32 * rt, w.rows - 1)).i);
+    const int tile_last = __builtin_amdgcn_readfirstlane(w.s.p0 + row_of(a, w, min(32 * rt + 31, w.rows - 1)).i);
+    v8bf qf[8];
+    {
+        const uint16_t *qp = a.q + row_at(w, row, a.q_stride) + 8 * hi;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const v8bf *)(qp + 16 * ks);
+    }
+    const int vk = 4 * hi + ((lane >> 2) & 3), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+
+    float m, l;
+    v16f o[4];
+    auto run = [&](auto mode) {                                  // whether the sums came out finite
+        constexpr bool careful = decltype(mode)::value;
+        m = kNegInf;
+        l = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+        if (range.first < range.end) issue(range.first);
+        if (range.first + 1 < range.end) issue(range.first + 1);
+        for (int t = range.first; t < range.end; ++t) {
+            // this step's loads have landed; the next step's may be in flight
+            if (t + 1 < range.end) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * kMidKeys / (4 * W)) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            lds_barrier();
+            const int key0 = t * kMidKeys + 32 * ku;             // this wave's 32 keys
+            if (key0 < w.hi && 32 * rt < w.rows) {
+                const char *kb = (const char *)ring[t & 1][0] + ku * 8192, *vb = (const char *)ring[t & 1][1] + ku * 8192;
+                v16f s;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const v8bf *)(kb + 16 * key_unit(r, 2 * ks + hi)), qf[ks], s, 0, 0, 0);
+                const bool masked = key0 + 31 > tile_first;
+                if (masked) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = key0 + 8 * (i >> 2) + 4 * hi + (i & 3) <= last ? s[i] : kNegInf;
+                }
+                float mt = kNegInf;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[i]);
+                mt = pair32_max(mt);
+                if (__ballot(mt * a.c > __builtin_fmaf(m, a.c, kLazy))) {
+                    const float mn = fmaxf(m, mt);
+                    const float alpha = exp2_hw((m - (mn == kNegInf ? 0.0f : mn)) * a.c);
+                    l *= alpha;
+#pragma unroll
+                    for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
+                    m = mn;
+                }
+                const float muc = (m == kNegInf ? 0.0f : m) * a.c;
+                uint32_t p[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = cvt_pk_bf16(exp2_hw(__builtin_fmaf(s[2 * i], a.c, -muc)), exp2_hw(__builtin_fmaf(s[2 * i + 1], a.c, -muc)));
+                    l = dot2(p[i], kBf16OnePair, l);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int h = i >> 2, dt = i & 3;
+                    const char *vp = vb + 16 * value_unit(16 * h + vk, 4 * dt + vc) + 8 * (lane & 1);
+                    const v4s_t lo4 = lds_read_tr(vp), hi4 = lds_read_tr(vp + 8 * 256);
+                    const v8bf pb = __builtin_bit_cast(v8bf, v4u{p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]});
+                    if (careful && masked) {
+                        v16f sum = o[dt];
+#pragma unroll 1
+                        for (int x = tile_first; x <= tile_last; ++x) {
+                            const v16f y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                values_up_to(lo4, hi4, key0 + 16 * h + 4 * hi, key0 + 16 * h + 8 + 4 * hi, x), pb, o[dt], 0, 0, 0);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) sum[j] = last == x ? y[j] : sum[j];
+                        }
+                        o[dt] = sum;
+                    } else {
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            __builtin_bit_cast(v8bf, __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7)), pb, o[dt], 0, 0, 0);
+                    }
+                }
+            }
+            if (t + 2 < range.end) {
+                lds_barrier();                                   // every wave is done with this stage
+                issue(t + 2);
+            }
+        }
+        float bad = 0.0f;                                        // NaN if any sum is not finite
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) bad = __builtin_fmaf(o[dt][i], 0.0f, bad);
+        return !__syncthreads_or(bad != 0.0f);                   // also: every wave is done with the ring
+    };
+    if (!run(std::false_type{})) {
+        run(std::true_type{});
+    }
+    l = pair32_sum(l);
+
+    // the four waves' sums of each 32 rows through LDS, in the matrix cores' order
+    v4f *sums = (v4f *)&ring[0][0][0];
+    static_assert(sizeof(ring) >= sizeof(v4f) * W * 16 * 64, "the sums fit the ring");
+    if (hi == 0) ml[wave][r] = make_float2(m, l);
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sums[(wave * 16 + dt * 4 + i) * 64 + lane] = v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+    __syncthreads();
+    if (32 * rt + r >= w.rows) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int x = 4 * ku + j;                                // unit of this row tile: dimensions 8 x + 4 hi .. + 3
+        v4f acc;
+        const float2 e = merged<4>(&ml[4 * rt][r], 32, sums + (rt * 64 + x) * 64 + lane, 16 * 64, a.c, acc);
+        if (a.S == 1) {
+            store_out(a, w, row, 8 * x + 4 * hi, acc, e.y);
+        } else {
+            *(v4f *)(unit_at<R>(a, w.split, rt * 16 + x) + 4 * lane) = acc;
+            if (x == 0 && hi == 0) *row_ml<R>(a, w.split, 32 * rt + r) = e;
         }
     }
 }
@@ -466,7 +614,6 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
 // u - 1.  K and V each have a ring of four steps in LDS, filled by direct-to-LDS loads two
 // steps ahead; one barrier for two steps.
 constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves, kStepKeys = 32, kStepSlots = 4;
-constexpr int kPromptSteps = 8;                               // least steps of a key range
 constexpr int kStepUnits = kStepKeys * kHeadDim / 8;          // 16-byte units of a step's K or V (512)
 
 __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalArgs a) {
@@ -476,7 +623,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
     Work w;
     if (!find_work<kPromptRows>(a, lane, blockIdx.y, w)) return;
 
-    const Range range = range_of(a, (w.hi + kStepKeys - 1) / kStepKeys, kPromptSteps, w.split);
+    const Range range = range_of(a, (w.hi + kStepKeys - 1) / kStepKeys, w.split);
     if (a.S > 1 && w.split >= range.used) return;
     const int u0 = range.first, n = range.end - u0;               // steps [u0, u0 + n)
     const uint16_t *kp = w.k + (int64_t)u0 * kStepKeys * a.b.tok, *vp = w.v + (int64_t)u0 * kStepKeys * a.b.tok;
@@ -710,18 +857,11 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
     l = pair32_sum(l);
     if (32 * wave + r >= w.rows) return;
     if (a.S == 1) {
-        const bool none = w.s.L == 0 || last < 0;
-        const float inv = 1.0f / l;
-        uint16_t *op = a.out + row_at(w, row, a.out_stride);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                        // dimensions 32 dt + 8 i + 4 hi .. + 3
-                uint2 y = {};
-                if (!none) y = make_uint2(cvt_pk_bf16(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv),
-                                          cvt_pk_bf16(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv));
-                *(uint2 *)(op + 32 * dt + 8 * i + 4 * hi) = y;
-            }
+            for (int i = 0; i < 4; ++i)                          // dimensions 32 dt + 8 i + 4 hi .. + 3
+                store_out(a, w, row, 32 * dt + 8 * i + 4 * hi, v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]}, l);
     } else {
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
@@ -750,15 +890,15 @@ __global__ __launch_bounds__(256) void k_causal_join(CausalArgs a) {
     Work w;
     if (!find_work<R>(a, lane, 0, w)) return;
     int row, d;                                                    // of this lane
-    if (RT) {
+    if (RT == 1) {
         row = 16 * (unit >> 3) + (lane & 15);
         d = 16 * (unit & 7) + 4 * (lane >> 4);
     } else {
         row = 32 * (unit >> 4) + (lane & 31);
         d = 8 * (unit & 15) + 4 * (lane >> 5);
     }
-    const int keys = RT ? kFewKeys : kStepKeys;
-    const int used = w.hi > 0 ? range_of(a, (w.hi + keys - 1) / keys, RT ? kFewWaves : kPromptSteps, 0).used : 0;
+    const int keys = RT == 0 ? kStepKeys : RT == 1 ? kFewKeys : kMidKeys;
+    const int used = w.hi > 0 ? range_of(a, (w.hi + keys - 1) / keys, 0).used : 0;
     const bool on = row < w.rows;
     float m = kNegInf, ls = 0.0f;
     v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -797,12 +937,7 @@ __global__ __launch_bounds__(256) void k_causal_join(CausalArgs a) {
         for (int i = 1; i < P; ++i) fold(gml[wave + i][lane], go[wave + i][lane]);
     }
     if (!on) return;
-    const RowOf ro = row_of(a, w, row);
-    const bool none = w.s.L == 0 || w.s.p0 + ro.i < 0;
-    const float inv = 1.0f / ls;
-    uint2 y = {};
-    if (!none) y = make_uint2(cvt_pk_bf16(acc[0] * inv, acc[1] * inv), cvt_pk_bf16(acc[2] * inv, acc[3] * inv));
-    *(uint2 *)(a.out + row_at(w, ro, a.out_stride) + d) = y;
+    store_out(a, w, row_of(a, w, row), d, acc, ls);
 }
 
 template <int RT>
@@ -815,14 +950,14 @@ void launch_join(const CausalArgs &a, hipStream_t st) {
 }  // namespace
 
 const char *causal_kernel_name(int rt) {
-    return rt == 1 ? "k_causal_few<1>" : rt == 2 ? "k_causal_few<2>" : rt == 4 ? "k_causal_few<4>" : "k_causal_prompt";
+    return rt == 1 ? "k_causal_few" : rt == 2 ? "k_causal_mid<1>" : rt == 4 ? "k_causal_mid<2>" : "k_causal_prompt";
 }
 
 hipError_t launch_causal(const CausalArgs &a, int rt, hipStream_t st) {
     const dim3 grid((unsigned)(a.tiles * a.Hkv), (unsigned)a.S);
-    if (rt == 1) hipLaunchKernelGGL(k_causal_few<1>, grid, dim3(kFewWaves * 64), 0, st, a);
-    else if (rt == 2) hipLaunchKernelGGL(k_causal_few<2>, grid, dim3(kFewWaves * 64), 0, st, a);
-    else if (rt == 4) hipLaunchKernelGGL(k_causal_few<4>, grid, dim3(kFewWaves * 64), 0, st, a);
+    if (rt == 1) hipLaunchKernelGGL(k_causal_few, grid, dim3(kFewWaves * 64), 0, st, a);
+    else if (rt == 2) hipLaunchKernelGGL(k_causal_mid<1>, grid, dim3(256), 0, st, a);
+    else if (rt == 4) hipLaunchKernelGGL(k_causal_mid<2>, grid, dim3(512), 0, st, a);
     else hipLaunchKernelGGL(k_causal_prompt, grid, dim3(kPromptWaves * 64), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;

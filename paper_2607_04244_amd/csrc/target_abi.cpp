@@ -100,7 +100,23 @@ BatchArgs batch_args(const qlin_batch *b, const qlin_kv_cache *c) {
 }
 
 // The kernel and split of one causal attention, from the host's bounds.
-struct CausalPlan { int rt = 0, tiles = 0, one_tile = 0, pairs = 0, S = 1; int64_t ws_bytes = 0; };
+struct CausalPlan { int rt = 0, tiles = 0, one_tile = 0, pairs = 0, S = 1, least = 1; int64_t ws_bytes = 0; };
+
+// Estimated microseconds of a call whose `blocks` (tile, head) items walk L keys in S ranges.
+// Fitted to graph replays of 32 / 8 heads: a workgroup has 4 us without keys; alone on its
+// compute unit it takes a key (of 4 rows or of 128) in 0.018 us (prompt), one of two in 0.033,
+// and 0.026 us where every compute unit reads the cache (few rows).  More workgroups than run
+// at once keep the units busy up to a part of the last one's time: a half for few rows, whose
+// sequences come in any order (64 sequences of 130 to 8190 keys: 1 range 187 us, 2 179, 4 177,
+// 6 188), less for prompts, whose longest tiles come first.  Measured for 500 tokens behind
+// 7400 keys, 128 items: 1 range 144 us, 2 85, 3 85, 4 80, 6 94; for one token over 8191 keys, 8
+// items: 16 ranges 11.9, 32 10.2, 64 over 13.
+double causal_cost(int rt, double blocks, double L, double S, double cus) {
+    const double W = blocks * S, slots = rt ? cus : 2 * cus;
+    const double key = rt ? 0.026 : W <= cus ? 0.018 : 0.033, one = L / S * key + 4.0;
+    const double join = S > 1 ? 3.0 + W * causal_tile_rows(rt) * (kHeadDim + 2) * 4 / 8e6 : 0.0;
+    return join + (W <= slots ? one : W * one / slots + (rt ? 0.5 : 0.1) * one);
+}
 
 int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, CausalPlan *p) {
     const int64_t G = Hq / Hkv, most = b->max_new * G;
@@ -108,24 +124,35 @@ int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t split
     const int64_t R = causal_tile_rows(p->rt), per = (most + R - 1) / R;
     p->one_tile = per <= 1;
     const int64_t tiles = p->one_tile ? b->n_seq : std::min(b->n_seq * per, b->rows * G / R + b->n_seq);
-    int64_t S = splits;
-    int cus = 256;                   // with forced ranges the plan is arithmetic
-    if (S == 0) {
+    const int64_t blocks = std::max<int64_t>(tiles * Hkv, 1);
+    const int64_t least = p->rt ? 128 : 256;     // keys of a range: a step of each wave, eight of a prompt
+    int64_t S = std::max<int64_t>(splits, 1);
+    int cus = 256;                               // with forced ranges the plan is arithmetic
+    if (splits == 0) {
         int dev = 0;
         hipError_t e = hipGetDevice(&dev);
         if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
         if (e != hipSuccess) return hip_fail(e, "device query");
-        const int64_t blocks = tiles * Hkv, least = p->rt ? 128 : 256;     // keys of a range
-        const int64_t wanted = (p->rt ? cus : 2 * cus) / std::max<int64_t>(blocks, 1);
-        S = std::min<int64_t>({wanted, (b->max_len + least - 1) / least, kMaxSplits});
+        const int64_t most_S = std::min<int64_t>((b->max_len + least - 1) / least, kMaxSplits);
+        double best = causal_cost(p->rt, (double)blocks, (double)b->max_len, 1, cus);
+        for (const int64_t s : {(int64_t)2, (int64_t)3, (int64_t)4, (int64_t)6, (int64_t)8, cus / blocks, 2 * cus / blocks}) {
+            if (s < 2 || s > most_S) continue;
+            const double t = causal_cost(p->rt, (double)blocks, (double)b->max_len, (double)s, cus);
+            if (t < best) {
+                best = t;
+                S = s;
+            }
+        }
     }
-    S = std::max<int64_t>(S, 1);
-    // work items of 256 threads in a 32-bit grid, also those that join the ranges
-    if (tiles * Hkv * std::max(S, S > 1 ? R / 2 : 0) >= (int64_t)1 << 24)
+    // work items of up to 512 threads in a 32-bit grid, also those that join the ranges
+    if (tiles * Hkv * std::max(S, S > 1 ? R / 2 : 0) >= (int64_t)1 << 23)
         return fail(QLIN_ERR_UNSUPPORTED, "too many rows, heads and key ranges for one call");
     p->tiles = (int)tiles;
     p->S = (int)S;
-    p->pairs = tiles * Hkv * S <= 2 * cus;
+    p->pairs = blocks * S <= 2 * cus;
+    // ranges that only balance sequences of different lengths leave the short ones whole
+    const int64_t keys = splits == 0 && blocks * S > (p->rt ? cus : 2 * cus) ? 4 * 128 : least;
+    p->least = (int)(keys / (p->rt == 0 ? 32 : p->rt == 1 ? 32 : 128));
     p->ws_bytes = S > 1 ? tiles * Hkv * S * R * (kHeadDim + 2) * 4 : 0;
     return QLIN_OK;
 }
@@ -260,6 +287,7 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     a.tiles = p.tiles;
     a.one_tile = p.one_tile;
     a.pairs = p.pairs;
+    a.least = p.least;
     a.S = p.S;
     a.max_len = (int)batch->max_len;
     gn_reciprocal(a.Hkv, &a.inv_heads, &a.heads_shift);

@@ -41,14 +41,15 @@ struct CausalArgs {
     int tiles;                      // row tiles, at least those there are
     int one_tile;                   // one tile a sequence: tile i is sequence i
     int pairs;                      // at most two workgroups a compute unit
-    int S;                          // key ranges
+    int S, least;                   // key ranges; least steps of one
     int max_len;                    // bound of the sequences' lengths (orders the tiles)
     uint32_t inv_heads, inv_g;      // x / Hkv by gn_chunk; ceil(2^32 / G) (0: G = 1)
     int heads_shift;
     float c;                        // scale log2(e): scores to base-2 exponents
 };
 
-// Rows (tokens x heads of a group) of a tile of k_causal_few<rt>, or of k_causal_prompt (rt = 0).
+// Rows (tokens x heads of a group) of a tile of k_causal_few (rt = 1), of k_causal_mid (2, 4) or
+// of k_causal_prompt (0).
 constexpr int causal_tile_rows(int rt) { return rt ? 16 * rt : 128; }
 
 // Verification.  A row of logits is cut into chunks of kVerifyChunk from the 16-byte boundary at

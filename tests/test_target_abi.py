@@ -157,12 +157,12 @@ def test_verify_workspace_is_checked():
 def test_attention_workspace_is_checked():
     """Forced key ranges need no device: the plan is arithmetic."""
     splits, need, text = qlin.qlin_causal_plan(batch(), 32, 8, 128, 3)
-    assert (splits, need) == (3, 3 * 8 * 64 * 3 * 130 * 4) and "k_causal_few<4>" in text and "combine=1" in text
+    assert (splits, need) == (3, 3 * 8 * 64 * 3 * 130 * 4) and "k_causal_mid<2>" in text and "combine=1" in text
     assert attend(splits=3, wb=need - 16) == INVALID and attend(splits=3, ws=None, wb=0) == INVALID
     assert "workspace" in qlin.last_error()
     assert attend(splits=3, out=A + 7 * STEP + 64) == INVALID
-    assert "k_causal_few<1>" in qlin.qlin_causal_plan(batch(max_new=1), 128, 8, 128, 1)[2]
-    assert "k_causal_few<2>" in qlin.qlin_causal_plan(batch(max_new=16), 16, 8, 128, 1)[2]
+    assert "k_causal_few " in qlin.qlin_causal_plan(batch(max_new=1), 128, 8, 128, 1)[2]
+    assert "k_causal_mid<1>" in qlin.qlin_causal_plan(batch(max_new=16), 16, 8, 128, 1)[2]
     assert "k_causal_prompt" in qlin.qlin_causal_plan(batch(max_new=17), 32, 8, 128, 1)[2]
     assert qlin.qlin_causal_plan(batch(max_new=0), 32, 8, 128, 1)[0] == 1
     with pytest.raises(qlin.QlinError) as e:
