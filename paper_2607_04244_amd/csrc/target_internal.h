@@ -56,7 +56,8 @@ constexpr int causal_tile_rows(int rt) { return rt ? 16 * rt : 128; }
 // or before it (up to 7 logits earlier).
 constexpr int kVerifyChunk = 8192, kVerifyMaxDraft = 64;
 struct VerifyStat { float m; int at; double z; };      // maximum, its lowest index (greedy), sum of the weights
-struct VerifyDecision { int accepted, rejected; VerifyStat p, q; };   // and the statistics of the row that decides
+// done: known from the rows looked at; p and q are then the statistics of the row that decides
+struct VerifyDecision { int accepted, rejected, done; VerifyStat p, q; };
 
 struct VerifyArgs {
     const uint16_t *target, *draft;
@@ -68,12 +69,14 @@ struct VerifyArgs {
     int chunks, all_rows;           // chunks of a row; rows of a sequence (targets, then drafts)
     VerifyStat *stats;              // [sequence][all_rows][chunks]
     double *sums;                   // [sequence][chunks]
-    VerifyDecision *decisions;      // [sequence]
+    VerifyDecision *decisions, *final_decisions;   // [sequence] from the first rows (if first_rows), from all
+    int first_rows;                 // rows whose statistics come first, 0: all together
+    int row0, row1;                 // rows of this launch of k_verify_stats
 };
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st);
 hipError_t launch_causal(const CausalArgs &a, int rt, hipStream_t st);
 const char *causal_kernel_name(int rt);
-hipError_t launch_verify(const VerifyArgs &a, int n_seq, hipStream_t st);
+hipError_t launch_verify(VerifyArgs a, int n_seq, hipStream_t st);
 
 }  // namespace qlin

@@ -1,13 +1,15 @@
 // The decision on drafted tokens (qlin_verify_draft in include/qlin_target.h).
 //
-// Three kernels, bound by the bytes of the logits and the 64-bit exponentials of all of them:
+// Bound by the bytes of the logits and the 64-bit exponentials of all of them:
 //   k_verify_stats   (row, chunk of 8192 tokens): maximum, its lowest index, and the sum of
-//       the weights e^((x - maximum) / T), for every row that a decision can need.
-//   k_verify_weigh   (sequence, chunk): the accepted prefix from the rows' statistics, and, if a
-//       token was refused, the chunk's sum of max(P - Q, 0).
+//       the weights e^((x - maximum) / T).
+//   k_verify_decide  (sequence): whether the first rows already refuse a token.  Large calls
+//       only: the statistics of the other rows are then taken where they can still matter.
+//   k_verify_weigh   (sequence, chunk), with draft logits: the accepted prefix from the rows'
+//       statistics, and, if a token was refused, the chunk's sum of max(P - Q, 0).
 //   k_verify_pick    (sequence): the chunk, then the token, that the running sum passes the
-//       uniform number in.
-// Each later kernel reads one or two rows a sequence.
+//       uniform number in.  Without draft logits the chunks' sums follow from the statistics,
+//       and the accepted prefix is found here.
 //
 // Weights and sums are 64-bit: a running sum over a vocabulary of 10^5 has a boundary every
 // 10^-5 of it or closer, and 32-bit weights (off by up to 6e-8 each) would put a few of a
@@ -23,7 +25,7 @@ namespace {
 
 constexpr float kNegInf = -__builtin_huge_valf(), kPosInf = __builtin_huge_valf();
 constexpr int kStatsThreads = 256, kStatsVecs = kVerifyChunk / (8 * kStatsThreads);
-constexpr int kPickThreads = kVerifyChunk / 8, kPickWaves = kPickThreads / 64;
+constexpr int kPickThreads = kVerifyChunk / 8, kPickWaves = kPickThreads / 64, kWeighThreads = 512;
 
 // 2^t, relative error 4.7e-11: (2^f - 1) / f on [-1/2, 1/2] as the polynomial of degree 6 whose
 // largest weighted error is smallest; 2^0 is 1 exactly.  The coefficients are opaque scalars:
@@ -97,10 +99,53 @@ __device__ inline double rescale(double k, float m, float M) {
     return m == M ? 1.0 : m == kNegInf || M == kPosInf ? 0.0 : Pow2()(fmax(((double)m - (double)M) * k, -1100.0));
 }
 
-__device__ inline double wave_sum(double v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+// Sums, maxima and minima over the lanes by DPP: within rows of 16 (row_shr 1, 2, 4, 8), then
+// lane 15 of a row to the next and lane 31 to the upper half; lane 63 has them all.  Lanes
+// without a partner keep `old`.  (Shuffles go through LDS: 12 of them in a row, for a 64-bit
+// sum, cost a microsecond.)
+template <int CTRL, int ROWS>
+__device__ inline int dpp(int old, int v) { return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xF, false); }
+template <int CTRL, int ROWS>
+__device__ inline double dpp(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = dpp<CTRL, ROWS>(0, (int)(uint32_t)u), hi = dpp<CTRL, ROWS>(0, (int)(uint32_t)(u >> 32));
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Inclusive sum over the lanes.
+__device__ inline double lanes_upto(double v) {
+    v += dpp<0x111, 0xF>(v);
+    v += dpp<0x112, 0xF>(v);
+    v += dpp<0x114, 0xF>(v);
+    v += dpp<0x118, 0xF>(v);
+    v += dpp<0x142, 0xA>(v);
+    v += dpp<0x143, 0xC>(v);
     return v;
+}
+__device__ inline double from_lane(double v, int l) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)u, l), hi = __builtin_amdgcn_readlane((uint32_t)(u >> 32), l);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ inline double wave_sum(double v) { return from_lane(lanes_upto(v), 63); }
+template <int CTRL, int ROWS>
+__device__ inline float dpp_max(float v) { return fmaxf(v, __int_as_float(dpp<CTRL, ROWS>(__float_as_int(v), __float_as_int(v)))); }
+__device__ inline float wave_max(float v) {
+    v = dpp_max<0x111, 0xF>(v);
+    v = dpp_max<0x112, 0xF>(v);
+    v = dpp_max<0x114, 0xF>(v);
+    v = dpp_max<0x118, 0xF>(v);
+    v = dpp_max<0x142, 0xA>(v);
+    v = dpp_max<0x143, 0xC>(v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ inline int wave_min(int v) {
+    v = min(v, dpp<0x111, 0xF>(v, v));
+    v = min(v, dpp<0x112, 0xF>(v, v));
+    v = min(v, dpp<0x114, 0xF>(v, v));
+    v = min(v, dpp<0x118, 0xF>(v, v));
+    v = min(v, dpp<0x142, 0xA>(v, v));
+    v = min(v, dpp<0x143, 0xC>(v, v));
+    return __builtin_amdgcn_readlane(v, 63);
 }
 
 // What a sequence asks for.
@@ -147,7 +192,7 @@ __device__ inline void load_logits(const Row &r, int v, int V, float x[8]) {
     }
 }
 
-// The rows of sequence b: target rows 0 .. n, then draft rows 0 .. n - 1.
+// The rows of sequence b: target rows 0 .. n, then draft rows 0 .. n - 1 (`which` in this order).
 __device__ inline const uint16_t *target_row(const VerifyArgs &a, int b, int i) { return a.target + ((int64_t)b * (a.n + 1) + i) * a.target_stride; }
 __device__ inline const uint16_t *draft_row(const VerifyArgs &a, int b, int i) { return a.draft + ((int64_t)b * a.n + i) * a.draft_stride; }
 
@@ -156,11 +201,13 @@ __device__ inline const uint16_t *draft_row(const VerifyArgs &a, int b, int i) {
 __global__ __launch_bounds__(kStatsThreads) void k_verify_stats(VerifyArgs a) {
     __shared__ VerifyStat part[kStatsThreads / 64];
     __shared__ float wave_m[kStatsThreads / 64];
-    const int b = blockIdx.y, which = blockIdx.x / a.chunks, c = blockIdx.x - which * a.chunks;
-    const bool is_draft = which > a.n;
-    const int i = is_draft ? which - a.n - 1 : which;
+    // this launch's rows: targets [row0, row1), then drafts [row0, row1) that there are
+    const int b = blockIdx.y, x_row = blockIdx.x / a.chunks, c = blockIdx.x - x_row * a.chunks;
+    const bool is_draft = x_row >= a.row1 - a.row0;
+    const int i = a.row0 + (is_draft ? x_row - (a.row1 - a.row0) : x_row), which = is_draft ? a.n + 1 + i : i;
     const Request rq = load_request(a, b);
     if (is_draft ? i >= rq.count || rq.greedy : i > rq.count) return;
+    if (a.row0 > 0 && a.decisions[b].done) return;               // the first rows sufficed
     const Row row(is_draft ? draft_row(a, b, i) : target_row(a, b, i));
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float x[kStatsVecs][8];
@@ -172,8 +219,7 @@ __global__ __launch_bounds__(kStatsThreads) void k_verify_stats(VerifyArgs a) {
     for (int k = 0; k < kStatsVecs; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e) m = fmaxf(m, x[k][e]);           // ignores NaN
-#pragma unroll
-    for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    m = wave_max(m);
     // the chunk's maximum, so that all its weights are relative to one
     if (lane == 0) wave_m[wave] = m;
     __syncthreads();
@@ -186,8 +232,7 @@ __global__ __launch_bounds__(kStatsThreads) void k_verify_stats(VerifyArgs a) {
 #pragma unroll
             for (int e = 7; e >= 0; --e)
                 if (x[k][e] == m) st.at = 8 * (v0 + k * kStatsThreads) - row.off + e;
-#pragma unroll
-        for (int o = 32; o; o >>= 1) st.at = min(st.at, __shfl_xor(st.at, o));
+        st.at = wave_min(st.at);
     } else if (m != kNegInf) {
         const Scale w(rq.k, m);
         double s = 0.0;
@@ -217,19 +262,14 @@ __device__ inline VerifyStat row_stat(const VerifyArgs &a, int b, int which, dou
         st.at = e.m > st.m ? e.at : e.m == st.m ? min(st.at, e.at) : st.at;
         st.m = M;
     }
-    float M = st.m;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    st.z = wave_sum(st.z * rescale(k, st.m, M));
-    int at = st.m == M ? st.at : 0x7FFFFFFF;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o));
-    return VerifyStat{M, at, st.z};
+    const float M = wave_max(st.m);
+    const double z = wave_sum(st.z * rescale(k, st.m, M));
+    return VerifyStat{M, wave_min(st.m == M ? st.at : 0x7FFFFFFF), z};
 }
 
-// The probability of token x in a row with these statistics.
-__device__ inline double probability(const uint16_t *row, int x, const VerifyStat &st, double k) {
-    return st.z > 0.0 ? Scale(k, st.m)(__uint_as_float((uint32_t)row[x] << 16)) / st.z : 0.0;
+// The probability of a token with logit x in a row with these statistics.
+__device__ inline double probability(float x, const VerifyStat &st, double k) {
+    return st.z > 0.0 ? Scale(k, st.m)(x) / st.z : 0.0;
 }
 
 // The weights that the next token is drawn by, in 8 tokens of a chunk: those of the target's
@@ -279,78 +319,101 @@ __device__ inline Choice choice_of(const VerifyArgs &a, int b, const VerifyDecis
                   d.rejected && !a.draft ? a.drafted[b * a.n + d.accepted] : -1, k, d.p.z, d.q.z, d.p.m, d.q.m};
 }
 
-// One workgroup a (sequence, chunk).  Every workgroup of a sequence finds its decision by
-// itself, a wave a drafted token: cheaper than a kernel for it.
-__global__ __launch_bounds__(kPickThreads) void k_verify_weigh(VerifyArgs a) {
-    __shared__ VerifyStat ps[kVerifyMaxDraft + 1], qs[kVerifyMaxDraft + 1];
-    __shared__ int keeps[kVerifyMaxDraft + 1];
-    __shared__ double part[kPickWaves];
-    const int b = blockIdx.y, c = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Request rq = load_request(a, b);
+// The decision of a sequence from the statistics of its rows below `limit`, a wave a row: the
+// first refused token, or all accepted (done only if row `count` is below the limit too).
+struct Rows { VerifyStat p[kVerifyMaxDraft + 1], q[kVerifyMaxDraft + 1]; int keep[kVerifyMaxDraft + 1]; };
+__device__ inline VerifyDecision decide(const VerifyArgs &a, int b, const Request &rq, int limit, Rows &rows) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const bool draft = a.draft && !rq.greedy;
-    for (int i = wave; i <= rq.count; i += kPickWaves) {
+    for (int i = wave; i <= rq.count && i < limit; i += blockDim.x >> 6) {
+        // what the last step needs is requested with the statistics
+        const int x = i < rq.count ? a.drafted[b * a.n + i] : -1;
+        const bool in = x >= 0 && x < a.V;
+        const float u = a.uniform[b * (a.n + 1) + i];
+        const float xp = in ? __uint_as_float((uint32_t)target_row(a, b, i)[x] << 16) : kNegInf;
+        const float xq = in && draft ? __uint_as_float((uint32_t)draft_row(a, b, i)[x] << 16) : kNegInf;
         const VerifyStat p = row_stat(a, b, i, rq.k, lane);
         VerifyStat q{0.0f, 0, 0.0};
-        bool keep = false;
-        if (i < rq.count) {
-            const int x = a.drafted[b * a.n + i];
-            const bool in = x >= 0 && x < a.V;
-            double px = 0.0, qx = 1.0;
-            if (in) px = rq.greedy ? (p.m != kNegInf && x == p.at ? 1.0 : 0.0) : probability(target_row(a, b, i), x, p, rq.k);
-            if (draft) {
-                q = row_stat(a, b, a.n + 1 + i, rq.k, lane);
-                qx = in ? probability(draft_row(a, b, i), x, q, rq.k) : 0.0;
-            }
-            keep = (double)a.uniform[b * (a.n + 1) + i] * qx < px;
-        }
+        if (draft && i < rq.count) q = row_stat(a, b, a.n + 1 + i, rq.k, lane);
+        double px = 0.0, qx = 1.0;
+        if (in) px = rq.greedy ? (p.m != kNegInf && x == p.at ? 1.0 : 0.0) : probability(xp, p, rq.k);
+        if (draft) qx = in ? probability(xq, q, rq.k) : 0.0;
         if (lane == 0) {
-            ps[i] = p;
-            qs[i] = q;
-            keeps[i] = keep;
+            rows.p[i] = p;
+            rows.q[i] = q;
+            rows.keep[i] = (double)u * qx < px;
         }
     }
     __syncthreads();
+    const int end = min(rq.count, limit);
+    VerifyDecision d{};
+    const uint64_t refused = __ballot(lane < end && !rows.keep[min(lane, end)]);     // at most 64 drafted tokens
+    d.accepted = refused ? __builtin_ctzll(refused) : end;
+    d.rejected = d.accepted < end;
+    d.done = d.rejected || rq.count < limit;
+    if (d.done) {
+        d.p = rows.p[d.accepted];
+        d.q = rows.q[d.accepted];
+    }
+    return d;
+}
+
+__global__ __launch_bounds__(kPickThreads) void k_verify_decide(VerifyArgs a) {
+    __shared__ Rows rows;
+    const int b = blockIdx.x;
+    const VerifyDecision d = decide(a, b, load_request(a, b), a.first_rows, rows);
+    if (threadIdx.x == 0) a.decisions[b] = d;
+}
+
+// One workgroup a (sequence, chunk).  Every workgroup of a sequence finds its decision by
+// itself, where the first rows have not: cheaper than a kernel for it.
+__global__ __launch_bounds__(kWeighThreads) void k_verify_weigh(VerifyArgs a) {
+    __shared__ Rows rows;
+    __shared__ double part[kWeighThreads / 64];
+    const int b = blockIdx.y, c = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Request rq = load_request(a, b);
     VerifyDecision d;
-    d.accepted = 0;
-    while (d.accepted < rq.count && keeps[d.accepted]) ++d.accepted;
-    d.rejected = d.accepted < rq.count;
-    d.p = ps[d.accepted];
-    d.q = qs[d.accepted];
-    if (c == 0 && threadIdx.x == 0) a.decisions[b] = d;
+    if (a.first_rows && a.decisions[b].done) {
+        d = a.decisions[b];
+    } else {
+        d = decide(a, b, rq, a.n + 1, rows);
+        if (c == 0 && threadIdx.x == 0) a.final_decisions[b] = d;
+    }
     if (rq.greedy || !d.rejected || !(d.p.z > 0.0)) return;      // the rows' statistics suffice
     double w[8], s = 0.0;
-    choice_of(a, b, d, rq.k).weights(c * (kVerifyChunk / 8) + threadIdx.x, a.V, true, w);
+    const Choice ch = choice_of(a, b, d, rq.k);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s += w[e];
+    for (int k = 0; k < kVerifyChunk / 8 / kWeighThreads; ++k) {
+        ch.weights(c * (kVerifyChunk / 8) + k * kWeighThreads + threadIdx.x, a.V, true, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += w[e];
+    }
     s = wave_sum(s);
     if (lane == 0) part[wave] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
         double t = 0.0;
-        for (int i = 0; i < kPickWaves; ++i) t += part[i];
+        for (int i = 0; i < kWeighThreads / 64; ++i) t += part[i];
         a.sums[(int64_t)b * a.chunks + c] = t;
     }
 }
 
-// Inclusive sum over the lanes.
-__device__ inline double lanes_upto(double v, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double u = __shfl_up(v, o);
-        v += lane >= o ? u : 0.0;
-    }
-    return v;
-}
-__device__ inline double from_lane(double v, int l) { return __shfl(v, l); }
-
 // One workgroup a sequence.  Its chunk is found by every wave for itself, 64 chunks at a time;
 // the token by the running sum of its 8192, eight a thread.
 __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
+    __shared__ Rows rows;
     __shared__ double part[kPickWaves];
     __shared__ int chosen, last_of[kPickWaves];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Request rq = load_request(a, b);
-    const VerifyDecision d = a.decisions[b];
+    const float u = a.uniform[b * (a.n + 1) + a.n];
+    const bool weighed = a.draft;
+    const double *sums = a.sums + (int64_t)b * a.chunks;
+    const double early = weighed && lane < a.chunks ? sums[lane] : 0.0;      // with the decision, not after it
+    VerifyDecision d;
+    if (a.first_rows && a.decisions[b].done) d = a.decisions[b];
+    else if (a.draft) d = a.final_decisions[b];
+    else d = decide(a, b, rq, a.n + 1, rows);
     if (tid == 0) a.accepted[b] = d.accepted;
     if (tid <= a.n && tid != d.accepted) a.tokens[b * (a.n + 1) + tid] = tid < d.accepted ? a.drafted[b * a.n + tid] : -1;
     int *out = a.tokens + b * (a.n + 1) + d.accepted;
@@ -358,39 +421,58 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
         if (tid == 0) *out = rq.greedy && d.p.m != kNegInf ? d.p.at : -1;
         return;
     }
-    // a chunk's mass: what was weighed, or, if nothing is left of the difference, the target's
-    const double *sums = a.sums + (int64_t)b * a.chunks;
+    // A chunk's mass: what was weighed; or the target's from its statistics, relative to the row's
+    // maximum, less the drafted token's where it was refused (in the chunk's own scale that
+    // weight is a term of the sum, bit for bit); without any mass left, the target's alone.
     const VerifyStat *stats = a.stats + ((int64_t)b * a.all_rows + d.accepted) * a.chunks;
     bool rest = d.rejected;
-    auto mass = [&](int c) { return c >= a.chunks ? 0.0 : rest ? sums[c] : stats[c].z * rescale(rq.k, stats[c].m, d.p.m); };
-    auto total_mass = [&]() {
-        double t = 0.0;
-        for (int c = 0; c < a.chunks; c += 64) t += from_lane(lanes_upto(mass(c + lane), lane), 63);
-        return t;
-    };
-    double total = total_mass();
-    if (rest && !(total > 0.0)) {
-        rest = false;
-        total = total_mass();
+    const Choice ch = choice_of(a, b, d, rq.k);
+    float gone = kNegInf;
+    int gone_chunk = -1;
+    if (rest && !weighed && ch.x >= 0 && ch.x < a.V) {
+        gone = __uint_as_float((uint32_t)target_row(a, b, d.accepted)[ch.x] << 16);
+        gone_chunk = (ch.x + ch.row.off) / kVerifyChunk;
     }
-    const double r = (double)a.uniform[b * (a.n + 1) + a.n] * total;
-    int chunk = -1, any = 0;                                // the first chunk past r; the last with any mass
-    double at = 0.0, run = 0.0;
-    for (int c = 0; c < a.chunks && chunk < 0; c += 64) {
-        const double own = mass(c + lane), upto = run + lanes_upto(own, lane);
+    auto mass = [&](int c) {
+        if (c >= a.chunks) return 0.0;
+        if (rest && weighed) return c == lane ? early : sums[c];
+        const VerifyStat st = stats[c];
+        double z = st.z;
+        if (rest && c == gone_chunk && st.m != kNegInf) z = fmax(z - Scale(rq.k, st.m)(gone), 0.0);
+        return z * rescale(rq.k, st.m, d.p.m);
+    };
+    // the first chunk whose running sum passes r = u total, and the last with any mass
+    int chunk = -1, any = 0;
+    double at = 0.0, r = 0.0;
+    auto find = [&](int c, double own, double upto) {
         const uint64_t over = __ballot(own > 0.0 && upto > r), some = __ballot(own > 0.0);
         if (some) any = c + 63 - __builtin_clzll(some);
-        if (over) {
-            const int l = __builtin_ctzll(over);
-            chunk = c + l;
-            at = from_lane(upto, l) - from_lane(own, l);
+        if (!over) return;
+        const int l = __builtin_ctzll(over);
+        chunk = c + l;
+        at = from_lane(upto, l) - from_lane(own, l);
+    };
+    for (int again = 0; again < 2; ++again) {
+        double own = mass(lane), upto = lanes_upto(own), total = from_lane(upto, 63);
+        for (int c = 64; c < a.chunks; c += 64) total += wave_sum(mass(c + lane));
+        if (rest && !(total > 0.0)) {                        // nothing is left of the difference
+            rest = false;
+            continue;
         }
-        run = from_lane(upto, 63);
+        r = (double)u * total;
+        find(0, own, upto);
+        double run = from_lane(upto, 63);
+        for (int c = 64; c < a.chunks && chunk < 0; c += 64) {
+            own = mass(c + lane);
+            upto = run + lanes_upto(own);
+            find(c, own, upto);
+            run = from_lane(upto, 63);
+        }
+        break;
     }
     const bool past = chunk < 0;                            // rounding left none: the last token of all
     if (past) chunk = any;
     double w[8], own = 0.0;
-    const Choice ch = choice_of(a, b, d, rq.k);
     const int v = chunk * (kVerifyChunk / 8) + tid, j0 = 8 * v - ch.row.off;
     ch.weights(v, a.V, rest, w);
     int end = -1;                                           // this thread's last token of any weight
@@ -399,16 +481,13 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
         own += w[e];
         if (w[e] > 0.0) end = j0 + e;
     }
-    const double upto = lanes_upto(own, lane);
-    int wave_end = end;
-#pragma unroll
-    for (int o = 32; o; o >>= 1) wave_end = max(wave_end, __shfl_xor(wave_end, o));
+    const double upto = lanes_upto(own);
+    const int wave_end = -wave_min(-end);
     if (lane == 63) part[wave] = upto;
     if (lane == 0) last_of[wave] = wave_end;
     if (tid == 0) chosen = 0x7FFFFFFF;
     __syncthreads();
-    // a chunk's mass from the statistics is relative to the row's maximum, weights to its sum
-    const double need = rest ? r - at : (r - at) / d.p.z;
+    const double need = rest && weighed ? r - at : (r - at) / d.p.z;     // weights are relative to the sum
     double before = 0.0;
     for (int i = 0; i < wave; ++i) before += part[i];
     double sum = before + (upto - own);
@@ -430,13 +509,25 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
 
 }  // namespace
 
-hipError_t launch_verify(const VerifyArgs &a, int n_seq, hipStream_t st) {
-    hipLaunchKernelGGL(k_verify_stats, dim3((unsigned)(a.chunks * a.all_rows), (unsigned)n_seq), dim3(kStatsThreads), 0, st, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_verify_weigh, dim3((unsigned)a.chunks, (unsigned)n_seq), dim3(kPickThreads), 0, st, a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+hipError_t launch_verify(VerifyArgs a, int n_seq, hipStream_t st) {
+    auto stats = [&](int row0, int row1) {
+        a.row0 = row0;
+        a.row1 = row1;
+        const int rows = row1 - row0 + (a.draft ? (row1 < a.n ? row1 : a.n) - row0 : 0);
+        hipLaunchKernelGGL(k_verify_stats, dim3((unsigned)(a.chunks * rows), (unsigned)n_seq), dim3(kStatsThreads), 0, st, a);
+        return hipGetLastError();
+    };
+    hipError_t e;
+    if (a.first_rows) {
+        if ((e = stats(0, a.first_rows)) != hipSuccess) return e;
+        hipLaunchKernelGGL(k_verify_decide, dim3((unsigned)n_seq), dim3(kPickThreads), 0, st, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if ((e = stats(a.first_rows, a.n + 1)) != hipSuccess) return e;
+    if (a.draft) {
+        hipLaunchKernelGGL(k_verify_weigh, dim3((unsigned)a.chunks, (unsigned)n_seq), dim3(kWeighThreads), 0, st, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     hipLaunchKernelGGL(k_verify_pick, dim3((unsigned)n_seq), dim3(kPickThreads), 0, st, a);
     return hipGetLastError();
 }
