@@ -34,7 +34,10 @@ grid, GB/s) | swa1024 | swa2048 | attn-full | attn-short (the drafter's
 block attention: 32 query heads over 8 key/value heads of dimension 128, 16
 block queries, a T = 8192 cache with a symmetric window of 1024 or 2048
 tokens, full attention, and T = 700 inside the window; GB/s of the visible
-key/value span) | gemm128 | gemm512 | gemm2048 (diagnostic only: the
+key/value span) | target-step (the 36-layer pass at M=16 with everything the
+target runs between its linears: norms, rotation and cache append, causal
+attention over T = 8192, and the decision on 15 drafted tokens at the end, one
+graph) | target-ops (those operators one by one, GB/s or TFLOP/s) | gemm128 | gemm512 | gemm2048 (diagnostic only: the
 vendor bf16 GEMM on weights already dequantized to bf16, at the same
 per-layer shapes and M, summed to a 36-layer pass); ``--separate-qkv`` runs
 q, k and v as three launches;
@@ -551,6 +554,154 @@ def bench_attention(args, name):
     print(json.dumps(res), flush=True)
 
 
+# The target between its linears: 32 query and 8 key/value heads of dimension
+# 128, a 16-token draft block, a vocabulary of 151936 tokens.
+TARGET_T, TARGET_CAPACITY, TARGET_VOCAB, TARGET_BLOCK = 8192, 8448, 151936, 16
+
+
+def append_bytes(rows, Hq, Hkv):
+    """q, k, v read, q_out and the cache's k and v written."""
+    return 2 * 128 * rows * (2 * Hq + 4 * Hkv)
+
+
+def causal_work(new, length, Hq, Hkv):
+    """(bytes, flops) of one causal attention: keys and values once, q and out; products of
+    the visible pairs."""
+    keys = sum(t for n, t in zip(new, length) if n)
+    pairs = sum(n * t - n * (n - 1) // 2 for n, t in zip(new, length))
+    return 2 * 128 * (2 * Hkv * keys + 2 * Hq * sum(new)), 4 * 128 * Hq * pairs
+
+
+class TargetBatch:
+    """The device arrays of a batch and a cache for it (filled with N(0, 1))."""
+
+    def __init__(self, torch, new, length, capacity, Hq=32, Hkv=8):
+        i32 = dict(dtype=torch.int32, device="cuda")
+        g = torch.Generator(device="cuda").manual_seed(sum(new) + sum(length))
+        normal = lambda *shape: torch.randn(shape, device="cuda", generator=g).to(torch.bfloat16)
+        self.new, self.length, self.Hq, self.Hkv = new, length, Hq, Hkv
+        self.kwargs = dict(new_start=torch.tensor(np.concatenate([[0], np.cumsum(new)]), **i32),
+                           length=torch.tensor(length, **i32), max_new=max(new), max_len=max(length))
+        self.k_cache, self.v_cache = (normal(len(new), Hkv, capacity, 128) for _ in range(2))
+        self.rows = [normal(sum(new), h * 128) for h in (Hq, Hkv, Hkv)]
+        self.norm = (1 + 0.1 * torch.randn(128, device="cuda", generator=g)).to(torch.bfloat16)
+        self.freq = 1e6 ** (-torch.arange(64, dtype=torch.float64, device="cuda") / 64)
+        self.q = torch.empty((sum(new), Hq, 128), dtype=torch.bfloat16, device="cuda")
+        self.out = torch.empty_like(self.q)
+
+    def append(self, qlin, rows=None):
+        return qlin.norm_rope_append(*(rows or self.rows), self.k_cache, self.v_cache, q_norm=self.norm,
+                                     k_norm=self.norm, inv_freq=self.freq, out=self.q, **self.kwargs)
+
+    def attend(self, qlin, workspace=None):
+        return qlin.causal_attention(self.q, self.k_cache, self.v_cache, out=self.out, workspace=workspace,
+                                     **self.kwargs)
+
+    def plan(self, qlin):
+        b = qlin.Batch(len(self.new), sum(self.new), max(self.new), max(self.length), None, None, None)
+        return qlin.qlin_causal_plan(b, self.Hq, self.Hkv, 128)
+
+
+def verify_inputs(torch, n_seq, drafts, vocab, with_draft):
+    g = torch.Generator(device="cuda").manual_seed(vocab + n_seq)
+    target = (2.5 * torch.randn((n_seq, drafts + 1, vocab), device="cuda", generator=g)).to(torch.bfloat16)
+    near = (target[:, :drafts].float() + 0.4 * torch.randn((n_seq, drafts, vocab), device="cuda", generator=g)).to(torch.bfloat16)
+    return dict(target=target, drafted=near.float().argmax(2).to(torch.int32),
+                uniform=torch.rand((n_seq, drafts + 1), device="cuda", generator=g), draft=near if with_draft else None)
+
+
+def bench_target_ops(args):
+    """The target's operators one by one, replayed from a graph (inputs not rotated)."""
+    import torch
+
+    from paper_2607_04244_amd import qlin
+    torch.cuda.set_device(0)
+    stream = torch.cuda.Stream()
+    out = []
+
+    def report(name, call, nbytes, flops=0, plan=None):
+        calls = 4 if nbytes > 1e8 else 40                  # a replay has a fixed cost of its own
+        us, g = graph_time_us(torch, stream, [call] * calls, reps=max(2, min(20, args.steps // calls)))
+        del g
+        line = {"operator": name, "us_per_call": round(us, 2), "bytes_per_call": nbytes,
+                "GBps": round(nbytes / us / 1e3, 1), "pct_of_peak_hbm": round(nbytes / us / 10 / PEAK_HBM_GBS, 2)}
+        if flops:
+            line.update(TFLOPs=round(flops / us / 1e6, 1), mfma_util_pct=round(flops / us / 1e4 / PEAK_BF16_TFLOPS, 2))
+        if plan:
+            line["plan"] = plan
+        out.append(line)
+
+    for name, new, length, cap in (("one token, T=8192", [1], [TARGET_T], TARGET_CAPACITY),
+                                   ("16-token block, T=8192", [TARGET_BLOCK], [TARGET_T], TARGET_CAPACITY),
+                                   ("64 single tokens, T=4096", [1] * 64, [4096] * 64, 4096),
+                                   ("prompt of 8192", [8192], [8192], 8192)):
+        b = TargetBatch(torch, new, length, cap)
+        report("append, " + name, lambda: b.append(qlin), append_bytes(sum(new), 32, 8))
+        nbytes, flops = causal_work(new, length, 32, 8)
+        _, need, plan = b.plan(qlin)
+        ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+        report("causal attention, " + name, lambda: b.attend(qlin, ws), nbytes, flops, plan)
+        del b, ws
+        torch.cuda.empty_cache()
+    for name, n, with_draft in (("one block of 15 tokens", 1, False), ("32 blocks with draft logits", 32, True)):
+        v = verify_inputs(torch, n, TARGET_BLOCK - 1, TARGET_VOCAB, with_draft)
+        rows = n * (TARGET_BLOCK + (TARGET_BLOCK - 1 if with_draft else 0))
+        ws = torch.empty(qlin.qlin_verify_plan(n, TARGET_BLOCK - 1, TARGET_VOCAB), dtype=torch.uint8, device="cuda")
+        report("verification, " + name, lambda: qlin.verify_draft(**v, workspace=ws), 2 * TARGET_VOCAB * rows)
+    print(json.dumps({"workload": "the target's operators between its linears (32 query and 8 key/value heads of 128)",
+                      "operators": out}), flush=True)
+
+
+def bench_target_step(args):
+    """One verification step of the target at M = 16 as one graph: per layer q|k|v (one
+    launch), norms, rotation and append, causal attention over T = 8192 cached tokens (a
+    cache of its own a layer), o on the attention's output, gate|up and down on fixed
+    activations; then the decision on 15 drafted tokens (fixed logits)."""
+    import torch
+
+    from paper_2607_04244_amd import qlin
+    from synth import gen
+    torch.cuda.set_device(0)
+    M, drafts = TARGET_BLOCK, TARGET_BLOCK - 1
+    rng = np.random.default_rng(8)
+    dev = lambda K: torch.from_numpy(gen.draw_activations(rng, M, K, 1.0, 0.0).view(np.int16)).view(torch.bfloat16).cuda()
+    xs = {K: dev(K) for K in (2560, 9728)}
+    calls, keep, total, attention = [], [], 0, 0
+    for layer in range(gen.N_LAYERS):
+        ws = [gen.model_linear(layer, p) for p in range(len(gen.LAYER_SHAPES))]
+        lins = [qlin.QLinear(w["packed"], w["scales"], w["zeros"]) for w in ws]
+        ys = [torch.empty((M, l.N), dtype=torch.bfloat16, device="cuda") for l in lins]
+        b = TargetBatch(torch, [M], [TARGET_T], TARGET_CAPACITY)
+        keep.append((lins, ys, b))
+        total += sum(algorithmic_bytes(M, l.K, l.N) for l in lins)
+        attention += append_bytes(M, 32, 8) + causal_work([M], [TARGET_T], 32, 8)[0]
+    scratch = torch.empty(max(keep[0][2].plan(qlin)[1], 16), dtype=torch.uint8, device="cuda")
+    need = max(qlin.group_plan(g, M)[0] for lins, _, _ in keep for g in (lins[:3], [lins[3]], [lins[4]], [lins[5]]))
+    wsb = qlin.new_workspace(need) if need else None
+    v = verify_inputs(torch, 1, drafts, TARGET_VOCAB, False)
+    vws = torch.empty(qlin.qlin_verify_plan(1, drafts, TARGET_VOCAB), dtype=torch.uint8, device="cuda")
+
+    def layer_call(lins, ys, b):
+        qlin.forward_group(lins[:3], xs[2560], ys[:3], workspace=wsb)
+        b.append(qlin, ys[:3])
+        b.attend(qlin, scratch)
+        qlin.forward_group([lins[3]], b.out.view(M, -1), [ys[3]], workspace=wsb)
+        qlin.forward_group([lins[4]], xs[2560], [ys[4]], workspace=wsb)
+        qlin.forward_group([lins[5]], xs[9728], [ys[5]], workspace=wsb)
+
+    stream = torch.cuda.Stream()
+    calls = [(lambda k=k: layer_call(*k)) for k in keep] + [lambda: qlin.verify_draft(**v, workspace=vws)]
+    us, g = graph_time_us(torch, stream, calls, reps=max(5, min(50, args.steps // 144)))
+    us_step = us * len(calls)
+    del g
+    total += attention + 2 * TARGET_VOCAB * (drafts + 1)
+    print(json.dumps({"workload": f"target verification step, 36 layers, M={M}, T={TARGET_T}: linears, append, causal "
+                                  f"attention, decision on {drafts} tokens (one graph)",
+                      "us_per_step": round(us_step, 2), "us_per_layer": round(us_step / gen.N_LAYERS, 3),
+                      "bytes_per_step": total, "GBps": round(total / us_step / 1e3, 1),
+                      "pct_of_peak_hbm": round(total / us_step / 10 / PEAK_HBM_GBS, 2)}), flush=True)
+
+
 def linear_rate(case, steps, warmup, path=0, split=0):
     """Time `steps` forwards of one linear (HIP-graph replays over R handles
     with their own weight copies, > 1 GiB together, so the weights come from
@@ -672,6 +823,10 @@ def main():
         return bench_quantize(args)
     if args.workload in ATTN_WORKLOADS:
         return bench_attention(args, args.workload)
+    if args.workload == "target-ops":
+        return bench_target_ops(args)
+    if args.workload == "target-step":
+        return bench_target_step(args)
 
     import torch
 

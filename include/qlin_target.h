@@ -88,7 +88,7 @@ typedef struct qlin_kv_cache {
  *               rotary_dim is 0)
  *   rotary_dim  a multiple of 16, 0 .. 128
  *   q_out       DEVICE bf16 [rows][q_heads][128], rows q_out_stride elements
- *               apart; q itself (same stride), or memory apart from every input
+ *               apart; q itself (same stride), or elements apart from every input
  *               and the cache
  * All pointers 16-byte aligned (norm weights and inv_freq: 8).  k and v must not
  * overlap the cache.  Two new tokens must not share a slot (sequences sharing
@@ -127,12 +127,14 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
  * once (the matrix cores' operand) and the sum adds the rounded weights.
  *
  *   q, out      DEVICE bf16 rows of q_heads x 128, q_stride / out_stride elements
- *               apart (multiples of 8), 16-byte aligned; out must not overlap q,
- *               the cache or the workspace
+ *               apart (multiples of 8), 16-byte aligned; out must not share elements
+ *               with q nor overlap the cache or the workspace
  *   q_heads     a multiple of cache->heads, at most 64 times it, at most 4096
  *   scale       > 0 and finite, or 0 for 1 / sqrt(128)
  *   workspace   DEVICE scratch of the bytes qlin_causal_plan reports for the same
  *               arguments (NULL when 0), 16-byte aligned, no initialisation
+ * max_new chooses the kernel: a batch of single tokens is read at the cache's rate only
+ * if max_new says 1, so single tokens and long chunks are better two calls.
  * For fixed splits the same inputs give the same bits.  Calls sharing a workspace
  * must be ordered on one stream.
  * Errors: INVALID (NULL, sizes, overlap, workspace too small), UNSUPPORTED
@@ -180,6 +182,7 @@ int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *wor
  *               aligned, no initialisation
  * 0 <= n_draft <= 64 (0: plain sampling; drafted may then be NULL), 1 <= vocab <=
  * 2^24, n_seq <= 65535 (0 is a no-op).  Outputs must not overlap inputs or each other.
+ * Calls sharing a workspace must be ordered on one stream.
  * Errors: INVALID, UNSUPPORTED, ALIGN, HIP.
  */
 int qlin_verify_draft(int64_t n_seq, int64_t n_draft, int64_t vocab, const uint16_t *target, int64_t target_stride,

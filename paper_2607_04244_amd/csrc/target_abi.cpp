@@ -33,6 +33,15 @@ Range rows_range(const void *p, int64_t rows, int64_t stride, int64_t width) {
     return Range{(uintptr_t)p, rows > 0 ? (size_t)((rows - 1) * stride + width) * 2 : 0};
 }
 
+// Whether two arrays of rows share an element.  Slices of the rows of one array do not, though
+// their ranges overlap.
+bool rows_meet(const void *p, int64_t stride, int64_t width, const void *q, int64_t q_stride, int64_t q_width, int64_t rows) {
+    if (!overlap(rows_range(p, rows, stride, width), rows_range(q, rows, q_stride, q_width))) return false;
+    if (stride != q_stride) return true;
+    const int64_t d = ((int64_t)((uintptr_t)q - (uintptr_t)p) / 2 % stride + stride) % stride;   // 16-byte aligned both
+    return d < width || d + q_width > stride;
+}
+
 Range cache_range(const void *p, const qlin_kv_cache *c) {
     return Range{(uintptr_t)p, (size_t)((c->slots - 1) * c->token_stride + (c->heads - 1) * c->head_stride + kHeadDim) * 2};
 }
@@ -199,10 +208,11 @@ int qlin_norm_rope_append(const qlin_batch *batch, const qlin_kv_cache *cache, i
         return fail(QLIN_ERR_ALIGN, "norm weights and inv_freq must be 8-byte aligned");
     const Range rq = rows_range(q, M, q_stride, wq), rk = rows_range(k, M, k_stride, wk), rv = rows_range(v, M, v_stride, wk);
     const Range ro = rows_range(q_out, M, q_out_stride, wq), ck = cache_range(cache->k, cache), cv = cache_range(cache->v, cache);
-    if ((overlap(ro, rq) && !(q_out == q && q_out_stride == q_stride)) || overlap(ro, ck) || overlap(ro, cv))
-        return fail(QLIN_ERR_INVALID, "q_out overlaps q (without being it) or the cache");
-    // in place, q_out lies in the rows of a fused projection: k and v between its rows are no overlap
-    if (q_out != q && (overlap(ro, rk) || overlap(ro, rv))) return fail(QLIN_ERR_INVALID, "q_out overlaps k or v");
+    if (!(q_out == q && q_out_stride == q_stride) && rows_meet(q, q_stride, wq, q_out, q_out_stride, wq, M))
+        return fail(QLIN_ERR_INVALID, "q_out overlaps q without being it");
+    if (rows_meet(k, k_stride, wk, q_out, q_out_stride, wq, M) || rows_meet(v, v_stride, wk, q_out, q_out_stride, wq, M))
+        return fail(QLIN_ERR_INVALID, "q_out overlaps k or v");
+    if (overlap(ro, ck) || overlap(ro, cv)) return fail(QLIN_ERR_INVALID, "q_out overlaps the cache");
     for (const Range &r : {rq, rk, rv})
         if (overlap(r, ck) || overlap(r, cv)) return fail(QLIN_ERR_INVALID, "q, k or v overlaps the cache");
 
@@ -261,8 +271,8 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     const int64_t w = q_heads * kHeadDim, M = batch->rows;
     if (check_rows(q, q_stride, w, "q") != QLIN_OK || check_rows(out, out_stride, w, "out") != QLIN_OK) return last_status();
     if (!aligned(workspace, 16)) return fail(QLIN_ERR_ALIGN, "workspace must be 16-byte aligned");
-    const Range rq = rows_range(q, M, q_stride, w), ro = rows_range(out, M, out_stride, w);
-    if (overlap(ro, rq) || overlap(ro, cache_range(cache->k, cache)) || overlap(ro, cache_range(cache->v, cache)))
+    const Range ro = rows_range(out, M, out_stride, w);
+    if (rows_meet(q, q_stride, w, out, out_stride, w, M) || overlap(ro, cache_range(cache->k, cache)) || overlap(ro, cache_range(cache->v, cache)))
         return fail(QLIN_ERR_INVALID, "out overlaps q or the cache");
     CausalPlan p;
     if (make_causal_plan(batch, q_heads, cache->heads, splits, &p) != QLIN_OK) return last_status();

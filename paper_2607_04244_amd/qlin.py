@@ -501,7 +501,9 @@ def causal_attention(q, k_cache, v_cache, new_start, length, max_new=None, max_l
     include/qlin_target.h).
 
     q: CUDA bf16 [rows, q heads, 128], rows may be apart; cache and batch as for
-    ``norm_rope_append``.  max_new and max_len size the work split.  ``workspace``
+    ``norm_rope_append``.  max_new (default: the rows) and max_len (default: the
+    cache's capacity) choose the kernel and its split: give 1 for single tokens, and
+    chunks of prompts a call of their own.  ``workspace``
     (a CUDA tensor of at least the planned bytes) is allocated when needed and not
     given.  Returns ``out`` [rows, q heads, 128]; rows of no sequence are left as
     they are.
@@ -523,7 +525,8 @@ def causal_attention(q, k_cache, v_cache, new_start, length, max_new=None, max_l
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
     if out is None:
-        out = _torch.empty(shape, dtype=bf16, device=q.device)
+        # of a contiguous tensor, empty_like costs half of empty
+        out = _torch.empty_like(q) if q.is_contiguous() else _torch.empty(shape, dtype=bf16, device=q.device)
         out_at, out_stride = out.data_ptr(), Hq * D
     else:
         out_at = _address("out", out, bf16, dev)

@@ -503,7 +503,92 @@ def test_verify_ties_take_the_lowest_index():
     assert check_verify(target, None, [[5], [2999]], [[0.5, 0.5], [0.5, 0.5]], T=[0.0, 0.0]) == [1, 0]
 
 
+def test_verify_large_calls_look_at_the_first_rows_first():
+    """Above 2^26 logits a third of the rows is looked at first: sequences that end there and
+    behind it, counts on both sides, greedy ones, and a drafter whose tokens are all kept."""
+    n, drafts, V = 16, 15, 151936
+    g = torch.Generator(device="cuda").manual_seed(1)
+    target = (2.0 * torch.randn((n, drafts + 1, V), device="cuda", generator=g)).to(torch.bfloat16)
+    draft = (target[:, :drafts].float() + 0.3 * torch.randn((n, drafts, V), device="cuda", generator=g)).to(torch.bfloat16)
+    draft[5], draft[9] = target[5, :drafts], target[9, :drafts]
+    drafted = (draft.float() - torch.empty_like(draft, dtype=torch.float32).exponential_(generator=g).log()).argmax(2)
+    T = [1.0, 0.0, 0.9, 1.3, 0.0, 1.0, 1.0, 0.8, 1.0, 1.0, 1.0, 0.7, 1.0, 1.0, 0.0, 1.0]
+    drafted[1] = target[1, :drafts].argmax(1)
+    drafted = drafted.tolist()
+    u = np.random.default_rng(2).random((n, drafts + 1)).astype(np.float32).tolist()
+    count = [15] * 10 + [4, 5, 6, 0, 15, 5]
+    assert n * (2 * drafts + 1) * V >= 1 << 26
+    acc = check_verify(target, draft, drafted, u, T=T, count=count)
+    assert max(acc) == 15 and min(acc) < 5
+    target2 = torch.cat([target, target])                               # without draft logits: 2^26 again
+    best = target2[:, :drafts].argmax(2)
+    best[::2, 3:] = 7
+    assert 2 * n * (drafts + 1) * V >= 1 << 26
+    acc = check_verify(target2, None, best.tolist(), u + u, T=[0.0] * n + [0.2] * n, count=count + count)
+    assert max(acc) >= 5
+
+
 # ---------------------------------------------------------------- together
+
+
+def test_two_streams_at_once():
+    """The operators on two streams at the same time, each with scratch of its own."""
+    new, length = [16, 3], [3000, 700]
+    c = Cache("heads", length, 2, 1)
+    q = [rand(i, (19, 8, HEAD), 2.0).cuda() for i in (2, 3)]
+    v = [verify_case(4, 7, 50257, s) for s in (1, 2)]
+    v = [(t.cuda(), i32(x), torch.tensor(u, device="cuda"), d.cuda()) for t, d, x, u in v]
+    b = dict(new_start=i32(starts(new)), max_new=16, **c.kwargs())
+    alone = [(qlin.causal_attention(q[i], *c.dev, **b).clone(), *[t.clone() for t in qlin.verify_draft(*v[i][:3], draft=v[i][3])]) for i in (0, 1)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in (0, 1)], [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append((qlin.causal_attention(q[i], *c.dev, **b), *qlin.verify_draft(*v[i][:3], draft=v[i][3])))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for out, acc, tok in got[i]:
+            assert torch.equal(out.view(torch.int16), alone[i][0].view(torch.int16))
+            assert torch.equal(acc, alone[i][1]) and torch.equal(tok, alone[i][2])
+
+
+def test_a_layer_between_quantized_linears():
+    """q|k|v of a quantized layer in one launch, norms, rotation and append of their outputs,
+    attention, and the o projection on its output: each stage against the oracle on what the
+    stage before it left on the device."""
+    from oracle import qlin_ref
+    from synth import gen
+    Hq, Hkv, K, M, L = 8, 2, 512, 16, 140
+    ws = [gen.random_case(60 + i, M, K, n * HEAD) for i, n in enumerate((Hq, Hkv, Hkv))]
+    o = gen.random_case(70, M, Hq * HEAD, K)
+    lins = [qlin.QLinear(w["packed"], w["scales"], w["zeros"]) for w in ws + [o]]
+    bits = lambda t: t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+    x = torch.from_numpy(ws[0]["x"].view(np.int16)).view(torch.bfloat16).cuda()
+    c = Cache("heads", [L], Hkv, 3)
+    w = (1 + rand(1, (HEAD,), 0.1))
+    freq = 1e6 ** (-torch.arange(64, dtype=torch.float64) / 64)
+    batch = dict(new_start=i32([0, M]), max_new=M, **c.kwargs())
+    need = max(qlin.group_plan(lins[:3], M)[0], qlin.group_plan(lins[3:], M)[0])
+    wsb = qlin.new_workspace(need)
+    q, k, v = qlin.forward_group(lins[:3], x, workspace=wsb)
+    kc, vc = c.dev
+    qr = qlin.norm_rope_append(q, k, v, kc, vc, q_norm=w.cuda(), k_norm=w.cuda(), inv_freq=freq.cuda(), **batch)
+    att = qlin.causal_attention(qr, kc, vc, **batch)
+    y = qlin.forward_group(lins[3:], att.view(M, Hq * HEAD), workspace=wsb)[0]
+    torch.cuda.synchronize()
+    for got, e in zip((q, k, v), ws):
+        assert qlin_ref.compare(bits(got), qlin_ref.forward(ws[0]["x"], e["packed"], e["scales"], e["zeros"]))["ok"]
+    for i in range(M):
+        for got, src, heads in ((f64(qr[i]), q, Hq), (f64(kc[0, :, L - M + i]), k, Hkv)):
+            want = ref.rotate(ref.norm(f64(src[i]).reshape(heads, HEAD), f64(w), 1e-6), L - M + i, freq.numpy(), False)
+            assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -17)      # values of size 4 and below
+    assert torch.equal(vc[0, :, L - M:L].transpose(0, 1).reshape(M, -1).view(torch.int16), v.view(torch.int16))
+    want, A = ref.causal_attention(f64(qr), f64(kc[0, :, :L].transpose(0, 1)), f64(vc[0, :, :L].transpose(0, 1)), HEAD ** -0.5)
+    assert np.all(np.abs(f64(att) - want) <= 2.0 ** -7 * (A + np.abs(want)))
+    assert qlin_ref.compare(bits(y), qlin_ref.forward(bits(att.view(M, -1)), o["packed"], o["scales"], o["zeros"]))["ok"]
+    for l in lins:
+        l.close()
 
 
 def test_prompt_then_blocks_then_tokens_through_one_cache():

@@ -88,6 +88,10 @@ COMMON = [(dict(D=64), UNSUPPORTED), (dict(D=0), UNSUPPORTED), (dict(Hq=0), INVA
     (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID), (dict(out=A + 4 * STEP), INVALID),
     (dict(out=A + 5 * STEP + 32), INVALID), (dict(k=A + STEP), INVALID), (dict(v=A + 2 * STEP + 2048), INVALID),
     (dict(q=A + 2 * STEP), INVALID), (dict(out=A + 3 * STEP, os=4104), INVALID),
+    # rows of 6144: q, k, v side by side; q_out on them must be q itself or columns of no input
+    (dict(qs=6144, ks=6144, vs=6144, os=6144, k=A + 3 * STEP + 8192, v=A + 3 * STEP + 10240, out=A + 3 * STEP + 2048), INVALID),
+    (dict(qs=6144, ks=6144, vs=6144, os=6144, k=A + 3 * STEP + 8000, v=A + 3 * STEP + 10240, out=A + 3 * STEP), INVALID),
+    (dict(qs=8192, ks=8192, vs=8192, os=8192, k=A + 3 * STEP + 8192, v=A + 3 * STEP + 10240, out=A + 3 * STEP + 10240), INVALID),
 ])
 def test_append_refuses(kw, code):
     assert append(**kw) == code and qlin.qlin_last_status() == code
