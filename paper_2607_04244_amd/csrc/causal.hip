@@ -102,11 +102,6 @@ __device__ inline int lanes_upto(int v) {
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);     // lane 31 to rows 2, 3
     return v;
 }
-__device__ inline int64_t lane_value(int64_t v, int l) {
-    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, l), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), l);
-    return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
 __device__ inline bool find_tile(const CausalArgs &a, int idx, int R, int lane, Seq &s, int &tile) {
     for (int i = 0; i < a.b.n_seq; i += 64) {
         Seq own{};
@@ -126,12 +121,7 @@ __device__ inline bool find_tile(const CausalArgs &a, int idx, int R, int lane, 
                 const int l = __popcll(__ballot(sum <= idx));
                 // the class's last tile of the sequence first
                 tile = __builtin_amdgcn_readlane(upper, l) - 1 - (idx - __builtin_amdgcn_readlane(sum - (upper - lower), l));
-                s.row0 = __builtin_amdgcn_readlane(own.row0, l);
-                s.n = __builtin_amdgcn_readlane(own.n, l);
-                s.rows = __builtin_amdgcn_readlane(own.rows, l);
-                s.p0 = __builtin_amdgcn_readlane(own.p0, l);
-                s.L = __builtin_amdgcn_readlane(own.L, l);
-                s.slot0 = lane_value(own.slot0, l);
+                s = lane_value(own, l);
                 return true;
             }
             idx -= total;

@@ -27,6 +27,17 @@ __device__ inline Seq load_seq(const BatchArgs &a, int b) {
     return s;
 }
 
+// Value of lane l, the same in every lane.
+__device__ inline int lane_value(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ inline int64_t lane_value(int64_t v, int l) {
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)v, l), hi = __builtin_amdgcn_readlane((uint32_t)(v >> 32), l);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ inline Seq lane_value(const Seq &s, int l) {
+    return Seq{lane_value(s.row0, l), lane_value(s.n, l), lane_value(s.rows, l), lane_value(s.p0, l), lane_value(s.L, l),
+               lane_value(s.slot0, l)};
+}
+
 // The sequence that row m belongs to (n_seq: padding), by the whole wave: the
 // number of sequences that end at or before m.
 __device__ inline int find_seq(const BatchArgs &a, int m, int lane) {

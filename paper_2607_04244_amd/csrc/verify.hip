@@ -251,11 +251,14 @@ __global__ __launch_bounds__(kStatsThreads) void k_verify_stats(VerifyArgs a) {
     }
 }
 
-// A row's statistics from its chunks', by a wave.
-__device__ inline VerifyStat row_stat(const VerifyArgs &a, int b, int which, double k, int lane) {
-    const VerifyStat *p = a.stats + ((int64_t)b * a.all_rows + which) * a.chunks;
-    VerifyStat st{kNegInf, 0x7FFFFFFF, 0.0};
-    for (int c = lane; c < a.chunks; c += 64) {
+// A row's statistics from its chunks', by a wave; `own` is its lane's chunk, loaded before.
+__device__ inline const VerifyStat *row_stats(const VerifyArgs &a, int b, int which) {
+    return a.stats + ((int64_t)b * a.all_rows + which) * a.chunks;
+}
+__device__ inline VerifyStat row_stat(const VerifyArgs &a, int b, int which, const VerifyStat &own, double k, int lane) {
+    const VerifyStat *p = row_stats(a, b, which);
+    VerifyStat st = own;
+    for (int c = lane + 64; c < a.chunks; c += 64) {
         const VerifyStat e = p[c];
         const float M = fmaxf(st.m, e.m);
         st.z = st.z * rescale(k, st.m, M) + e.z * rescale(k, e.m, M);
@@ -322,19 +325,25 @@ __device__ inline Choice choice_of(const VerifyArgs &a, int b, const VerifyDecis
 // The decision of a sequence from the statistics of its rows below `limit`, a wave a row: the
 // first refused token, or all accepted (done only if row `count` is below the limit too).
 struct Rows { VerifyStat p[kVerifyMaxDraft + 1], q[kVerifyMaxDraft + 1]; int keep[kVerifyMaxDraft + 1]; };
-__device__ inline VerifyDecision decide(const VerifyArgs &a, int b, const Request &rq, int limit, Rows &rows) {
+__device__ inline VerifyDecision decide(const VerifyArgs &a, int b, int limit, Rows &rows, Request &rq) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const bool draft = a.draft && !rq.greedy;
-    for (int i = wave; i <= rq.count && i < limit; i += blockDim.x >> 6) {
-        // what the last step needs is requested with the statistics
-        const int x = i < rq.count ? a.drafted[b * a.n + i] : -1;
-        const bool in = x >= 0 && x < a.V;
+    const VerifyStat none{kNegInf, 0x7FFFFFFF, 0.0};
+    for (int i = wave; i <= a.n && i < limit; i += blockDim.x >> 6) {
+        // everything but the drafted token's logits in one trip to memory, also for rows that turn
+        // out to be behind the last (their statistics are not used)
+        const VerifyStat own_p = lane < a.chunks ? row_stats(a, b, i)[lane] : none;
+        const VerifyStat own_q = a.draft && i < a.n && lane < a.chunks ? row_stats(a, b, a.n + 1 + i)[lane] : none;
+        const int x = i < a.n ? a.drafted[b * a.n + i] : -1;
         const float u = a.uniform[b * (a.n + 1) + i];
+        const bool in = x >= 0 && x < a.V;
         const float xp = in ? __uint_as_float((uint32_t)target_row(a, b, i)[x] << 16) : kNegInf;
-        const float xq = in && draft ? __uint_as_float((uint32_t)draft_row(a, b, i)[x] << 16) : kNegInf;
-        const VerifyStat p = row_stat(a, b, i, rq.k, lane);
+        const float xq = in && a.draft ? __uint_as_float((uint32_t)draft_row(a, b, i)[x] << 16) : kNegInf;
+        rq = load_request(a, b);
+        if (i > rq.count) break;
+        const bool draft = a.draft && !rq.greedy;
+        const VerifyStat p = row_stat(a, b, i, own_p, rq.k, lane);
         VerifyStat q{0.0f, 0, 0.0};
-        if (draft && i < rq.count) q = row_stat(a, b, a.n + 1 + i, rq.k, lane);
+        if (draft && i < rq.count) q = row_stat(a, b, a.n + 1 + i, own_q, rq.k, lane);
         double px = 0.0, qx = 1.0;
         if (in) px = rq.greedy ? (p.m != kNegInf && x == p.at ? 1.0 : 0.0) : probability(xp, p, rq.k);
         if (draft) qx = in ? probability(xq, q, rq.k) : 0.0;
@@ -344,6 +353,7 @@ __device__ inline VerifyDecision decide(const VerifyArgs &a, int b, const Reques
             rows.keep[i] = (double)u * qx < px;
         }
     }
+    rq = load_request(a, b);                    // waves without a row too
     __syncthreads();
     const int end = min(rq.count, limit);
     VerifyDecision d{};
@@ -361,7 +371,8 @@ __device__ inline VerifyDecision decide(const VerifyArgs &a, int b, const Reques
 __global__ __launch_bounds__(kPickThreads) void k_verify_decide(VerifyArgs a) {
     __shared__ Rows rows;
     const int b = blockIdx.x;
-    const VerifyDecision d = decide(a, b, load_request(a, b), a.first_rows, rows);
+    Request rq;
+    const VerifyDecision d = decide(a, b, a.first_rows, rows, rq);
     if (threadIdx.x == 0) a.decisions[b] = d;
 }
 
@@ -371,12 +382,13 @@ __global__ __launch_bounds__(kWeighThreads) void k_verify_weigh(VerifyArgs a) {
     __shared__ Rows rows;
     __shared__ double part[kWeighThreads / 64];
     const int b = blockIdx.y, c = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Request rq = load_request(a, b);
+    Request rq;
     VerifyDecision d;
     if (a.first_rows && a.decisions[b].done) {
         d = a.decisions[b];
+        rq = load_request(a, b);
     } else {
-        d = decide(a, b, rq, a.n + 1, rows);
+        d = decide(a, b, a.n + 1, rows, rq);
         if (c == 0 && threadIdx.x == 0) a.final_decisions[b] = d;
     }
     if (rq.greedy || !d.rejected || !(d.p.z > 0.0)) return;      // the rows' statistics suffice
@@ -404,16 +416,17 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
     __shared__ Rows rows;
     __shared__ double part[kPickWaves];
     __shared__ int chosen, last_of[kPickWaves];
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const Request rq = load_request(a, b);
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    Request rq;
     const float u = a.uniform[b * (a.n + 1) + a.n];
     const bool weighed = a.draft;
     const double *sums = a.sums + (int64_t)b * a.chunks;
     const double early = weighed && lane < a.chunks ? sums[lane] : 0.0;      // with the decision, not after it
     VerifyDecision d;
+    if (a.draft || a.first_rows) rq = load_request(a, b);
     if (a.first_rows && a.decisions[b].done) d = a.decisions[b];
     else if (a.draft) d = a.final_decisions[b];
-    else d = decide(a, b, rq, a.n + 1, rows);
+    else d = decide(a, b, a.n + 1, rows, rq);
     if (tid == 0) a.accepted[b] = d.accepted;
     if (tid <= a.n && tid != d.accepted) a.tokens[b * (a.n + 1) + tid] = tid < d.accepted ? a.drafted[b * a.n + tid] : -1;
     int *out = a.tokens + b * (a.n + 1) + d.accepted;
@@ -424,7 +437,7 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
     // A chunk's mass: what was weighed; or the target's from its statistics, relative to the row's
     // maximum, less the drafted token's where it was refused (in the chunk's own scale that
     // weight is a term of the sum, bit for bit); without any mass left, the target's alone.
-    const VerifyStat *stats = a.stats + ((int64_t)b * a.all_rows + d.accepted) * a.chunks;
+    const VerifyStat *stats = row_stats(a, b, d.accepted);
     bool rest = d.rejected;
     const Choice ch = choice_of(a, b, d, rq.k);
     float gone = kNegInf;
@@ -488,9 +501,8 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
     if (tid == 0) chosen = 0x7FFFFFFF;
     __syncthreads();
     const double need = rest && weighed ? r - at : (r - at) / d.p.z;     // weights are relative to the sum
-    double before = 0.0;
-    for (int i = 0; i < wave; ++i) before += part[i];
-    double sum = before + (upto - own);
+    const double waves = lanes_upto(lane < kPickWaves ? part[lane] : 0.0);
+    double sum = (wave ? from_lane(waves, wave - 1) : 0.0) + (upto - own);
     int hit = 0x7FFFFFFF;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
