@@ -509,7 +509,8 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
         sum += w[e];
         if (hit == 0x7FFFFFFF && w[e] > 0.0 && !past && sum > need) hit = j0 + e;
     }
-    if (hit != 0x7FFFFFFF) atomicMin(&chosen, hit);
+    const uint64_t hits = __ballot(hit != 0x7FFFFFFF);      // the lowest lane's token is the wave's first
+    if (hits && lane == __builtin_ctzll(hits)) atomicMin(&chosen, hit);
     __syncthreads();
     if (tid == 0) {
         int next = chosen;
