@@ -103,6 +103,11 @@ __device__ inline int lanes_upto(int v) {
     return v;
 }
 __device__ inline bool find_tile(const CausalArgs &a, int idx, int R, int lane, Seq &s, int &tile) {
+    if (a.b.n_seq == 1) {                                // no order to find out
+        s = load_seq(a.b, 0);
+        tile = (s.rows * a.G + R - 1) / R - 1 - idx;
+        return tile >= 0;
+    }
     for (int i = 0; i < a.b.n_seq; i += 64) {
         Seq own{};
         int tiles = 0;
