@@ -6,9 +6,11 @@
 // many of their q, k and v heads at a time as it has groups.  The R x half angles of
 // its tokens are computed once, by its first threads, into LDS: p * inv_freq in turns
 // is reduced in 64 bits, where 2^28 positions leave 30 bits of a turn, and only the
-// rest of at most half a turn goes through 32-bit sine and cosine.  R = 4 tokens a workgroup
-// from 1024 rows on (2 and 8: 54.8 and 51.2 us against 49.8 of 4, 8192 tokens without the
-// hint below), one below: a single token takes 3.5 us, of which a launch is 1.6.
+// rest of at most half a turn goes through 32-bit sine and cosine.  One token a workgroup for
+// few tokens (a single one takes 3.5 us, of which a launch is 1.6), four for many: 512 rows
+// of 32 / 8 heads 7.2 against 7.7 us, 768 rows 10.2 against 8.3, 2048 rows 21.3 against 13.3
+// (in the last-level cache 5.7 / 7.6, 7.8 / 7.8, 16.6 / 11.1).  Two and eight tokens: 54.8
+// and 51.2 us against 49.8 of four (8192 tokens, without the hint below).
 #include "target_common.h"
 
 #include <type_traits>
@@ -19,6 +21,7 @@ namespace {
 
 constexpr int kGroupLanes = 16;          // lanes of a head row
 constexpr int kAppendThreads = 1024;
+constexpr int kManyRows = 640;           // R = 4 from here on
 
 // Sum over the 16 lanes of a DPP row, in every lane.
 __device__ inline float row_sum(float v) {
@@ -156,7 +159,7 @@ hipError_t launch_append(const AppendArgs &a, hipStream_t st) {
     const int heads = a.Hq + 2 * a.Hkv;
     const int threads = heads * kGroupLanes > kAppendThreads ? kAppendThreads : (heads * kGroupLanes + 63) / 64 * 64;
     if (a.b.rows == 0) return hipSuccess;
-    if (a.b.rows < 1024) hipLaunchKernelGGL(k_norm_rope_append<1>, dim3(a.b.rows), dim3(threads), 0, st, a);
+    if (a.b.rows < kManyRows) hipLaunchKernelGGL(k_norm_rope_append<1>, dim3(a.b.rows), dim3(threads), 0, st, a);
     else hipLaunchKernelGGL(k_norm_rope_append<4>, dim3((a.b.rows + 3) / 4), dim3(threads), 0, st, a);
     return hipGetLastError();
 }

@@ -11,11 +11,17 @@
 //
 //   k_causal_few       up to 16 rows (single tokens): bound by the cache's bytes.  Four waves,
 //       each with units of 32 keys and LDS of its own, two units in flight, no barrier until
-//       the waves' sums are merged.
+//       the waves' sums are merged.  64 tokens of 32 / 8 heads over 4096 keys each: 174 to
+//       180 us, 6.0 to 6.2 TB/s; one token over 8192 keys 7.1 us and 2.9 for the join.
 //   k_causal_mid<NR>   up to 32 NR rows (draft blocks): the cache's bytes, then the products.
-//   k_causal_prompt    128 rows, 32 a wave, 64-key tiles shared by four waves: bound by
-//       the matrix cores and the softmax between them.
-//   k_causal_join      joins key ranges, in order.
+//       16 tokens over 8192 keys: 12.4 us, of which the keys take 5.4 at that rate.
+//   k_causal_prompt    128 rows, 32 a wave, 32 keys a step for four waves: bound by the matrix
+//       cores and the softmax between them.  8192 tokens: 511 to 545 us on different boxes,
+//       1010 to 1075 TFLOP/s, where the library's large bf16 product reaches 1194.
+//   k_causal_join      joins key ranges, in order: bound by the partial results' bytes.
+// Which kernel goes by the rows of the longest sequence (max_new G): a tile with room for more
+// rows than there are costs the few their bandwidth (one token over 8191 keys through 128-row
+// tiles walks 0.6 us a step of 32 keys), a smaller one reads the keys again for each tile.
 //
 // Softmax statistics are fp32.  Weights are rounded to bf16 once (the operand) and the
 // sum adds the rounded weights.
@@ -89,7 +95,8 @@ __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // sequence and its number in it; false past the last.  The tiles that see the most keys come
 // first, in kClasses classes of equal steps of keys up to max_len (a tile with the longest
 // walk that starts late ends late: packed prompts of 1 to 2048 tokens 125 us in the order of
-// the rows).  By the whole wave: a class's tiles of 64 sequences at a time are summed up.
+// the rows, 113 in this one).  By the whole wave: a class's tiles of 64 sequences at a time are
+// summed up.
 constexpr int kClasses = 8;
 
 // Inclusive sum over the lanes by DPP: within rows of 16, then across them.
@@ -436,8 +443,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
 
 // 32 NR rows, NR = 1, 2: four waves for each 32 rows, a quarter of a step's 128 keys each, so
 // that a key range of 256 keys (a 16-token block over 8192 keys on all compute units) is two
-// steps, requested at once.  With 16-row tiles, all of them in each of four waves, the same
-// range took 15.0 us of 17.0; its products wait for one another.
+// steps, requested at once.  With four 16-row tiles in each of four waves the same kernel took
+// 15.0 us (12.4 here): its products waited for one another, with one wave a SIMD.
 constexpr int kMidKeys = 128, kMidUnits = kMidKeys * kHeadDim / 8;
 
 template <int NR>
@@ -607,7 +614,16 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 // Steps of 32 keys in a pipeline over three steps: while the softmax of step u runs on the
 // vector unit, the matrix cores take the scores of step u + 1 and the weighted sums of step
 // u - 1.  K and V each have a ring of four steps in LDS, filled by direct-to-LDS loads two
-// steps ahead; one barrier for two steps.
+// steps ahead; one barrier for two steps.  Two workgroups a compute unit (64 KiB of LDS and
+// 218 registers each).
+//
+// A step has 16 products of 32 cycles and about 80 vector instructions of 5 cycles, which fit
+// between the products (a product with 4 fma and 1 exp: 33.4 cycles at two waves a SIMD).
+// Measured over 8192 tokens: matrix cores busy 52 % of the cycles, vector unit 38 %, LDS 25 %
+// without conflicts, at 1.8 to 1.9 GHz: the clock of dense products, not the nominal 2.4.
+// One step after the other, a barrier each: 567 us; as here 539, and 521 with the searches and
+// divisions before the first step shortened.  Other orders of products, vector instructions
+// and LDS reads, and raised wave priorities, were equal or slower.
 constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves, kStepKeys = 32, kStepSlots = 4;
 constexpr int kStepUnits = kStepKeys * kHeadDim / 8;          // 16-byte units of a step's K or V (512)
 
