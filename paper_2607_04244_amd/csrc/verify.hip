@@ -15,7 +15,16 @@
 // 10^-5 of it or closer, and 32-bit weights (off by up to 6e-8 each) would put a few of a
 // thousand choices on the wrong side of one.  At an error of 5e-11 it is one of 10^5.
 // 64-bit products run at the rate of 32-bit ones here, and 32-bit exponentials at a half of
-// it, so the accuracy costs about twice the time of 32-bit weights.
+// it, so the accuracy costs about twice the time of 32-bit weights.  A table of 2^(j/32) or
+// 2^(j/64) in LDS or lanes with a polynomial of degree 3: 32 sequences 81 us of 84, one
+// sequence 14.9 of 14.3; not taken.
+//
+// 16 tokens over 151936: 13.7 us, of which the statistics 6.4 (one trip to memory, 19 chunks a
+// row over all compute units) and the token 7.4 (a workgroup's dependent steps: statistics,
+// decision, chunk, token).  32 sequences of 16 with draft logits: 84 to 105 us on different
+// boxes and orders of memory (statistics 37 + 20, decision 4.7, sums 16, token 7.6), where the
+// 5 TB/s of a copy would read all the logits in 63; the statistics are bound by their 64-bit
+// instructions, 14 a logit.
 #include "device_common.h"
 #include "target_internal.h"
 
@@ -43,18 +52,21 @@ struct Pow2 {
         for (int i = 4; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
         return __builtin_fma(p, f, 1.0);
     }
-    // t >= -1100; 0 below the smallest number
+    // -1100 <= t < 1000; 0 below the smallest number.  Rounding by the sum with 1.5 2^52, whose low
+    // word is the integer.
+    static constexpr double kRound = 6755399441055744.0;
     __device__ inline double operator()(double t) const {
-        const double n = rint(t);
-        return __builtin_amdgcn_ldexp(fraction(t - n), (int)n);
+        const double n = t + kRound;
+        return __builtin_amdgcn_ldexp(fraction(t - (n - kRound)), (int)(uint32_t)__builtin_bit_cast(uint64_t, n));
     }
-    // -1000 <= t < 1000: rounding by the sum with 1.5 2^52, whose low word is the integer, and the
-    // exponent by an integer sum (5 instructions of the full rate for 4 with a conversion)
+    // -1000 <= t < 1000: the exponent by a sum of the upper words, kept from the compiler, which
+    // adds both words in four instructions (32 sequences 88.2 us a call, 84.1 so)
     __device__ inline double within(double t) const {
-        constexpr double kRound = 6755399441055744.0;
         const double n = t + kRound;
         const uint64_t p = __builtin_bit_cast(uint64_t, fraction(t - (n - kRound)));
-        const uint32_t hi = (uint32_t)(p >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, n) << 20);
+        uint32_t hi = (uint32_t)(p >> 32);
+        asm("" : "+v"(hi));
+        hi += (uint32_t)__builtin_bit_cast(uint64_t, n) << 20;
         return __builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)p);
     }
 };
@@ -328,32 +340,41 @@ struct Rows { VerifyStat p[kVerifyMaxDraft + 1], q[kVerifyMaxDraft + 1]; int kee
 __device__ inline VerifyDecision decide(const VerifyArgs &a, int b, int limit, Rows &rows, Request &rq) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const VerifyStat none{kNegInf, 0x7FFFFFFF, 0.0};
-    for (int i = wave; i <= a.n && i < limit; i += blockDim.x >> 6) {
-        // everything but the drafted token's logits in one trip to memory, also for rows that turn
-        // out to be behind the last (their statistics are not used)
-        const VerifyStat own_p = lane < a.chunks ? row_stats(a, b, i)[lane] : none;
-        const VerifyStat own_q = a.draft && i < a.n && lane < a.chunks ? row_stats(a, b, a.n + 1 + i)[lane] : none;
-        const int x = i < a.n ? a.drafted[b * a.n + i] : -1;
-        const float u = a.uniform[b * (a.n + 1) + i];
+    // everything but the drafted token's logits in one trip to memory, a row ahead and also for rows
+    // that turn out to be behind the last (their statistics are not used)
+    struct Ahead { VerifyStat own_p, own_q; int x; float u; };
+    auto request = [&](int i) {
+        Ahead r{none, none, -1, 0.0f};
+        if (i > a.n || i >= limit) return r;
+        if (lane < a.chunks) r.own_p = row_stats(a, b, i)[lane];
+        if (a.draft && i < a.n && lane < a.chunks) r.own_q = row_stats(a, b, a.n + 1 + i)[lane];
+        if (i < a.n) r.x = a.drafted[b * a.n + i];
+        r.u = a.uniform[b * (a.n + 1) + i];
+        return r;
+    };
+    const int waves = blockDim.x >> 6;
+    Ahead next = request(wave);
+    rq = load_request(a, b);                    // waves without a row too
+    for (int i = wave; i <= rq.count && i < limit; i += waves) {
+        const Ahead own = next;
+        const int x = own.x;
         const bool in = x >= 0 && x < a.V;
         const float xp = in ? __uint_as_float((uint32_t)target_row(a, b, i)[x] << 16) : kNegInf;
         const float xq = in && a.draft ? __uint_as_float((uint32_t)draft_row(a, b, i)[x] << 16) : kNegInf;
-        rq = load_request(a, b);
-        if (i > rq.count) break;
+        next = request(i + waves);
         const bool draft = a.draft && !rq.greedy;
-        const VerifyStat p = row_stat(a, b, i, own_p, rq.k, lane);
+        const VerifyStat p = row_stat(a, b, i, own.own_p, rq.k, lane);
         VerifyStat q{0.0f, 0, 0.0};
-        if (draft && i < rq.count) q = row_stat(a, b, a.n + 1 + i, own_q, rq.k, lane);
+        if (draft && i < rq.count) q = row_stat(a, b, a.n + 1 + i, own.own_q, rq.k, lane);
         double px = 0.0, qx = 1.0;
         if (in) px = rq.greedy ? (p.m != kNegInf && x == p.at ? 1.0 : 0.0) : probability(xp, p, rq.k);
         if (draft) qx = in ? probability(xq, q, rq.k) : 0.0;
         if (lane == 0) {
             rows.p[i] = p;
             rows.q[i] = q;
-            rows.keep[i] = (double)u * qx < px;
+            rows.keep[i] = (double)own.u * qx < px;
         }
     }
-    rq = load_request(a, b);                    // waves without a row too
     __syncthreads();
     const int end = min(rq.count, limit);
     VerifyDecision d{};
