@@ -148,6 +148,14 @@ def test_append_many_rows():
     check_append([700, 1, 0, 522], [700, 900, 5, 600], "packed", Hq=3, Hkv=1, pad=4, seed=9)
 
 
+@pytest.mark.parametrize("rows,kw", [(639, dict(fused=True)), (640, dict(fused=True, in_place=True)), (641, dict(pad=6, interleaved=True, rot=48)),
+                                     (643, dict(rot=0, max_new=300))])
+def test_append_around_the_change_of_form(rows, kw):
+    """Either side of the rows from which a workgroup takes several tokens; sequences that meet
+    inside a workgroup, one of them ahead of its first position."""
+    check_append([rows - 333, 1, 0, 2, 330], [rows, 1, 0, 1, 331], "packed", Hq=3, Hkv=1, seed=rows, **kw)
+
+
 def test_append_far_positions_keep_their_angles():
     """Position 2^24 + 5: the first frequency turns 2.7 million times."""
     n = (1 << 24) + 6
@@ -551,6 +559,44 @@ def test_two_streams_at_once():
         for out, acc, tok in got[i]:
             assert torch.equal(out.view(torch.int16), alone[i][0].view(torch.int16))
             assert torch.equal(acc, alone[i][1]) and torch.equal(tok, alone[i][2])
+
+
+def test_graphs_that_share_a_workspace():
+    """Two captured graphs over one workspace, replayed in turn on one stream between eager calls:
+    attention split over keys, single tokens and blocks, and the decision with draft logits."""
+    c = Cache("heads", [4000, 3100], 2, 1)
+    logits, draft, tokens, u = verify_case(3, 7, 50257, 5)
+    v = (logits.cuda(), i32(tokens), torch.tensor(u, device="cuda"))
+    draft = draft.cuda()
+    cases = []
+    for seed, new in enumerate(([1, 1], [16, 9])):
+        b = dict(new_start=i32(starts(new)), max_new=max(new), **c.kwargs())
+        cases.append((rand(seed, (sum(new), 8, HEAD), 2.0).cuda(), b))
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+
+    def step(i):
+        q, b = cases[i]
+        return (qlin.causal_attention(q, *c.dev, workspace=ws, **b), *qlin.verify_draft(*v, draft=draft if i else None, workspace=ws))
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        want = [step(i) for i in (0, 1)]
+        s.synchronize()
+        graphs, got = [], []
+        for i in (0, 1):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[i], stream=s):
+                got.append(step(i))
+        for k in range(4):
+            for i in (k & 1, 1, 0):
+                for t in got[i]:
+                    t.zero_()
+                graphs[i].replay()
+                step(1 - i)
+                s.synchronize()
+                for x, y in zip(got[i], want[i]):
+                    assert torch.equal(x, y)
 
 
 def test_a_layer_between_quantized_linears():
