@@ -864,16 +864,32 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
                 }
             }
         }
+        lds_barrier();                                               // the rings are free
     }
     l = pair32_sum(l);
-    if (32 * wave + r >= w.rows) return;
     if (a.S == 1) {
+        // through LDS of the wave's own (the keys' ring, which nothing reads any more), so that 16
+        // lanes store a row (packed prompts 114.4 us with 8 bytes of 32 rows a store, 110.8 so): unit
+        // 4 dt + i has dimensions 32 dt + 8 i .. + 7, 4 of them a lane
+        char *const rows = (char *)kring + wave * 8192;
+        const bool sees = w.s.L > 0 && last >= 0;
+        const float inv = 1.0f / l;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)                          // dimensions 32 dt + 8 i + 4 hi .. + 3
-                store_out(a, w, row, 32 * dt + 8 * i + 4 * hi, v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]}, l);
-    } else {
+            for (int i = 0; i < 4; ++i) {
+                const uint2 y = make_uint2(cvt_pk_bf16(o[dt][4 * i] * inv, o[dt][4 * i + 1] * inv),
+                                           cvt_pk_bf16(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv));
+                *(uint2 *)(rows + 16 * key_unit(r, 4 * dt + i) + 8 * hi) = sees ? y : uint2{};
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int x = 4 * j + (lane >> 4), c = lane & 15;
+            if (32 * wave + x >= w.rows) break;
+            *(uint4 *)(a.out + row_at(w, row_of(a, w, 32 * wave + x), a.out_stride) + 8 * c) = *(const uint4 *)(rows + 16 * key_unit(x, c));
+        }
+    } else if (32 * wave + r < w.rows) {
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
