@@ -15,7 +15,7 @@
 //       180 us, 6.0 to 6.2 TB/s; one token over 8192 keys 7.1 us and 2.9 for the join.
 //   k_causal_mid<NR>   up to 32 NR rows (draft blocks): the cache's bytes, then the products.
 //       16 tokens over 8192 keys: 12.4 us, of which the keys take 5.4 at that rate.
-//   k_causal_prompt    128 rows, 32 a wave, 32 keys a step for four waves: bound by the matrix
+//   k_causal_prompt<H> 128 rows, 32 a wave, 32 keys a step for four waves: bound by the matrix
 //       cores and the softmax between them.  8192 tokens: 511 to 545 us on different boxes,
 //       1010 to 1075 TFLOP/s, where the library's large bf16 product reaches 1194.
 //   k_causal_join      joins key ranges, in order: bound by the partial results' bytes.
@@ -240,7 +240,9 @@ __device__ inline v8bf values_up_to(v4s_t lo, v4s_t hi, int key, int key2, int l
 }
 
 // A row's sums are rescaled only when its maximum has grown by more than a factor 2^kLazy of
-// the weights: up to there the weights just exceed 1, with the same relative rounding.
+// the weights: up to there the weights just exceed 1, with the same relative rounding.  Each row
+// goes by its own maximum, and a careful pass by the same steps, so that not a bit of a row
+// depends on what lies behind its token.
 constexpr float kLazy = 8.0f;
 
 // The sums of W waves, each relative to its own maximum, as one: returns (maximum, sum of
@@ -365,8 +367,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
             float mt = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
                              fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
             mt = pair32_max(pair16_max(mt));
-            if (__ballot(mt * a.c > __builtin_fmaf(m, a.c, kLazy))) {
-                const float mn = fmaxf(m, mt);
+            const bool own = mt * a.c > __builtin_fmaf(m, a.c, kLazy);
+            if (__ballot(own)) {
+                const float mn = own ? mt : m;
                 const float alpha = exp2_hw((m - (mn == kNegInf ? 0.0f : mn)) * a.c);
                 l *= alpha;
 #pragma unroll
@@ -530,8 +533,9 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[i]);
                 mt = pair32_max(mt);
-                if (__ballot(mt * a.c > __builtin_fmaf(m, a.c, kLazy))) {
-                    const float mn = fmaxf(m, mt);
+                const bool own = mt * a.c > __builtin_fmaf(m, a.c, kLazy);
+                if (__ballot(own)) {
+                    const float mn = own ? mt : m;
                     const float alpha = exp2_hw((m - (mn == kNegInf ? 0.0f : mn)) * a.c);
                     l *= alpha;
 #pragma unroll
@@ -615,7 +619,9 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 // vector unit, the matrix cores take the scores of step u + 1 and the weighted sums of step
 // u - 1.  K and V each have a ring of four steps in LDS, filled by direct-to-LDS loads two
 // steps ahead; one barrier for two steps.  Two workgroups a compute unit (64 KiB of LDS and
-// 218 registers each).
+// 218 registers each), or, HALVES = 2, one of eight waves, four for each half of the keys, whose
+// sums meet in LDS: where there is work for one workgroup a unit but not for two, that saves a
+// split and its join (a prompt of 1185 tokens 35.0 us in two ranges, 26.8 so).
 //
 // A step has 16 products of 32 cycles and about 80 vector instructions of 5 cycles, which fit
 // between the products (a product with 4 fma and 1 exp: 33.4 cycles at two waves a SIMD).
@@ -627,16 +633,22 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves, kStepKeys = 32, kStepSlots = 4;
 constexpr int kStepUnits = kStepKeys * kHeadDim / 8;          // 16-byte units of a step's K or V (512)
 
-__global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalArgs a) {
-    __shared__ __attribute__((aligned(16))) uint4 kring[kStepSlots][kStepUnits], vring[kStepSlots][kStepUnits];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+template <int HALVES>
+__global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_causal_prompt(CausalArgs a) {
+    __shared__ __attribute__((aligned(16))) uint4 rings[HALVES][2][kStepSlots][kStepUnits];    // K, V
+    __shared__ float2 second[HALVES == 2 ? kPromptRows : 1];       // (maximum, sum of weights) of the second half
+    const int wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % kPromptWaves), lane = threadIdx.x & 63;
+    const int part = HALVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (kPromptWaves * 64));
     const int hi = lane >> 5, r = lane & 31;
+    uint4 (*const kring)[kStepUnits] = rings[part][0], (*const vring)[kStepUnits] = rings[part][1];
     Work w;
     if (!find_work<kPromptRows>(a, lane, blockIdx.y, w)) return;
 
     const Range range = range_of(a, (w.hi + kStepKeys - 1) / kStepKeys, w.split);
     if (a.S > 1 && w.split >= range.used) return;
-    const int u0 = range.first, n = range.end - u0;               // steps [u0, u0 + n)
+    // steps [u0, u0 + n); an odd number of steps leaves the second half one without keys
+    const int n = HALVES == 1 ? range.end - range.first : (range.end - range.first + 1) / 2, u0 = range.first + part * n;
+    const int most = range.end * kStepKeys - 1;                   // the range's last key
     const uint16_t *kp = w.k + (int64_t)u0 * kStepKeys * a.b.tok, *vp = w.v + (int64_t)u0 * kStepKeys * a.b.tok;
     const int first_key = u0 * kStepKeys;
 
@@ -665,9 +677,9 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
     auto load_v = [&](int u) { load(vn, vp, vlds + (u & (kStepSlots - 1)) * 8192, u, voff, 4 * (lane >> 4)); };
 
     const RowOf row = row_of(a, w, min(32 * wave + r, w.rows - 1));
-    const int last = w.s.p0 + row.i;                                       // last key this row sees
-    const int wave_first = __builtin_amdgcn_readfirstlane(w.s.p0 + row_of(a, w, min(32 * wave, w.rows - 1)).i);
-    const int wave_last = __builtin_amdgcn_readfirstlane(w.s.p0 + row_of(a, w, min(32 * wave + 31, w.rows - 1)).i);
+    const int last = min(w.s.p0 + row.i, most);                            // last key this row sees
+    const int wave_first = __builtin_amdgcn_readfirstlane(min(w.s.p0 + row_of(a, w, min(32 * wave, w.rows - 1)).i, most));
+    const int wave_last = __builtin_amdgcn_readfirstlane(min(w.s.p0 + row_of(a, w, min(32 * wave + 31, w.rows - 1)).i, most));
     v8bf qf[8];
     {
         const uint16_t *qp = a.q + row_at(w, row, a.q_stride) + 8 * hi;
@@ -721,7 +733,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
 #pragma unroll
         for (int i = 0; i < 8; ++i) p1[i] = 0;                       // there is no step -1: zeros, also in its slot
 #pragma unroll
-        for (int i = 0; i < kStepUnits; i += kPromptWaves * 64) vring[3][i + threadIdx.x] = uint4{};
+        for (int i = 0; i < kStepUnits; i += kPromptWaves * 64) vring[3][i + threadIdx.x % (kPromptWaves * 64)] = uint4{};
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
         zero(s0);
@@ -739,8 +751,8 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
             const int key0 = first_key + u * kStepKeys;
             if (key0 + kStepKeys - 1 > wave_first) mask(s, key0);
             const float mt = row_max(s);
-            const bool grown = __ballot(mt * a.c > __builtin_fmaf(m, a.c, kLazy)) != 0;
-            const float mn = grown ? fmaxf(m, mt) : m;
+            const bool own = mt * a.c > __builtin_fmaf(m, a.c, kLazy), grown = __ballot(own) != 0;
+            const float mn = own ? mt : m;
             const float mu = mn == kNegInf ? 0.0f : mn, muc = mu * a.c;
             float ls = 0.0f;
 #pragma unroll
@@ -836,21 +848,28 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(slot, ks), qf[ks], s, 0, 0, 0);
             mask(s, key0);
-            const float mn = fmaxf(m, row_max(s)), mu = mn == kNegInf ? 0.0f : mn;
-            const float alpha = exp2_hw((m - mu) * a.c), muc = mu * a.c;
-            m = mn;
-            l *= alpha;
+            const float mt = row_max(s);
+            const bool own = mt * a.c > __builtin_fmaf(m, a.c, kLazy);
+            const float mn = own ? mt : m, mu = mn == kNegInf ? 0.0f : mn, muc = mu * a.c;
+            if (__ballot(own)) {
+                const float alpha = exp2_hw((m - mu) * a.c);
+                m = mn;
+                l *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
+            }
+            float ls = 0.0f;
             uint32_t p[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 p[i] = cvt_pk_bf16(exp2_hw(__builtin_fmaf(s[2 * i], a.c, -muc)), exp2_hw(__builtin_fmaf(s[2 * i + 1], a.c, -muc)));
-                l = dot2(p[i], kBf16OnePair, l);
+                ls = dot2(p[i], kBf16OnePair, ls);
             }
+            l += ls;
             const int t0 = min(wave_first, key0 + kStepKeys - 1), t1 = min(wave_last, key0 + kStepKeys - 1);   // later tokens see all
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
-                const v16f before = o[dt] * alpha;
-                o[dt] = before;
+                const v16f before = o[dt];
 #pragma unroll 1
                 for (int t = t0; t <= t1; ++t) {
                     v16f x = before;
@@ -867,6 +886,33 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void k_causal_prompt(CausalAr
         lds_barrier();                                               // the rings are free
     }
     l = pair32_sum(l);
+    if constexpr (HALVES == 2) {
+        // the second half's sums through its rings, which nothing reads any more
+        v4f *const sums = (v4f *)rings[1];
+        if (part == 1) {
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sums[((4 * wave + dt) * 4 + i) * 64 + lane] = v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+            if (hi == 0) second[32 * wave + r] = make_float2(m, l);
+        }
+        lds_barrier();
+        if (part == 1) return;
+        const float2 e = second[32 * wave + r];
+        const float M = fmaxf(m, e.x), mu = M == kNegInf ? 0.0f : M;
+        const float f1 = exp2_hw((m - mu) * a.c), f2 = exp2_hw((e.x - mu) * a.c);
+        m = M;
+        l = l * f1 + e.y * f2;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const v4f x = sums[((4 * wave + dt) * 4 + i) * 64 + lane];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[dt][4 * i + k] = o[dt][4 * i + k] * f1 + x[k] * f2;
+            }
+    }
     if (a.S == 1) {
         // through LDS of the wave's own (the keys' ring, which nothing reads any more), so that 16
         // lanes store a row (packed prompts 114.4 us with 8 bytes of 32 rows a store, 110.8 so): unit
@@ -976,16 +1022,17 @@ void launch_join(const CausalArgs &a, hipStream_t st) {
 
 }  // namespace
 
-const char *causal_kernel_name(int rt) {
-    return rt == 1 ? "k_causal_few" : rt == 2 ? "k_causal_mid<1>" : rt == 4 ? "k_causal_mid<2>" : "k_causal_prompt";
+const char *causal_kernel_name(int rt, int halves) {
+    return rt == 1 ? "k_causal_few" : rt == 2 ? "k_causal_mid<1>" : rt == 4 ? "k_causal_mid<2>" : halves == 2 ? "k_causal_prompt<2>" : "k_causal_prompt<1>";
 }
 
-hipError_t launch_causal(const CausalArgs &a, int rt, hipStream_t st) {
+hipError_t launch_causal(const CausalArgs &a, int rt, int halves, hipStream_t st) {
     const dim3 grid((unsigned)(a.tiles * a.Hkv), (unsigned)a.S);
     if (rt == 1) hipLaunchKernelGGL(k_causal_few, grid, dim3(kFewWaves * 64), 0, st, a);
     else if (rt == 2) hipLaunchKernelGGL(k_causal_mid<1>, grid, dim3(256), 0, st, a);
     else if (rt == 4) hipLaunchKernelGGL(k_causal_mid<2>, grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL(k_causal_prompt, grid, dim3(kPromptWaves * 64), 0, st, a);
+    else if (halves == 2) hipLaunchKernelGGL(k_causal_prompt<2>, grid, dim3(2 * kPromptWaves * 64), 0, st, a);
+    else hipLaunchKernelGGL(k_causal_prompt<1>, grid, dim3(kPromptWaves * 64), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;
     if (rt == 1) launch_join<1>(a, st);

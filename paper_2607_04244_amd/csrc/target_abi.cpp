@@ -110,22 +110,32 @@ BatchArgs batch_args(const qlin_batch *b, const qlin_kv_cache *c) {
 }
 
 // The kernel and split of one causal attention, from the host's bounds.
-struct CausalPlan { int rt = 0, tiles = 0, one_tile = 0, pairs = 0, S = 1, least = 1; int64_t ws_bytes = 0; };
+struct CausalPlan { int rt = 0, halves = 1, tiles = 0, one_tile = 0, pairs = 0, S = 1, least = 1; int64_t ws_bytes = 0; };
 
-// Estimated microseconds of a call whose `blocks` (tile, head) items walk L keys in S ranges.
-// Fitted to graph replays of 32 / 8 heads: a workgroup has 4 us without keys; alone on its
-// compute unit it takes a key (of 4 rows or of 128) in 0.018 us (prompt), one of two in 0.033,
-// and 0.026 us where every compute unit reads the cache (few rows).  More workgroups than run
-// at once keep the units busy up to a part of the last one's time: a half for few rows, whose
-// sequences come in any order (64 sequences of 130 to 8190 keys: 1 range 187 us, 2 179, 4 177,
-// 6 188), less for prompts, whose longest tiles come first.  Measured for 500 tokens behind
-// 7400 keys, 128 items: 1 range 144 us, 2 85, 3 85, 4 80, 6 94; for one token over 8191 keys, 8
-// items: 16 ranges 11.9, 32 10.2, 64 over 13.
-double causal_cost(int rt, double blocks, double L, double S, double cus) {
-    const double W = blocks * S, slots = rt ? cus : 2 * cus;
-    const double key = rt ? 0.026 : W <= cus ? 0.018 : 0.033, one = L / S * key + 4.0;
+// Estimated microseconds of a call whose `blocks` (tile, head) items walk L keys in S ranges, in
+// k_causal_prompt by workgroups of one or two `halves`.  Fitted to graph replays of 32 / 8 heads.
+// A workgroup has some time without keys and then takes a key (of 4 rows or of 128) in, for few
+// rows, 0.026 us (every compute unit reads the cache); for prompts, alone on its compute unit,
+// 0.017 us as one half and 0.0125 as two, and 0.004 more where all units work (their clock
+// falls); of two on a unit 0.033.  More workgroups than run at once keep the units busy up to a
+// part of the last one's time: a half for few rows, whose sequences come in any order, less for
+// prompts, whose longest tiles come first, and least where two share a unit (the last ones have
+// it alone).  Where one sequence may be much longer than the others (`ragged`) two halves of all
+// its keys end late.
+//
+// Measured (halves/ranges: us).  64 sequences of 130 to 8190 keys, few rows: 1 range 187, 2 179,
+// 4 177, 6 188; one token over 8191 keys: 16 ranges 11.9, 32 10.2, 64 over 13.  500 tokens behind
+// 7400, 128 items: 1/1 154, 1/2 91, 1/3 86, 1/4 79, 1/6 92, 2/1 111, 2/2 79, 2/4 85; 200 behind
+// 1800, 56 items: 1/2 27.9, 1/4 20.9, 2/2 26.4, 2/4 22.1; prompts of 512: 1/1 16.1, 2/1 16.7; 1185:
+// 1/2 35.0, 2/1 26.8; 1500: 1/1 39.7, 1/2 44.2, 2/1 33.9; 4000: 1/1 136, 2/1 151; 56 new tokens of
+// 7940 and 1649 of 2412: 1/3 76, 2/1 118.  Over 360 random batches the choice of halves takes the
+// 71 calls that it makes faster to 0.88 of their time; 14 are slower, the worst 1.16.
+double causal_cost(int rt, int halves, double ragged, double blocks, double L, double S, double cus) {
+    const double W = blocks * S, slots = rt || halves == 2 ? cus : 2 * cus, busy = std::min(W / cus, 1.0);
+    const double key = rt ? 0.026 : halves == 2 ? 0.0125 + 0.0043 * busy : W <= cus ? 0.017 + 0.004 * busy : 0.033;
+    const double one = L / S * key + (rt ? 4.0 : halves == 2 ? 8.3 : W <= cus ? 5.4 : 8.0);
     const double join = S > 1 ? 3.0 + W * causal_tile_rows(rt) * (kHeadDim + 2) * 4 / 8e6 : 0.0;
-    return join + (W <= slots ? one : W * one / slots + (rt ? 0.5 : 0.1) * one);
+    return join + (halves == 2 ? ragged * one : 0.0) + (W <= slots ? one : W * one / slots + (rt ? 0.5 : 0.1 * halves) * one);
 }
 
 int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, CausalPlan *p) {
@@ -143,25 +153,35 @@ int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t split
         hipError_t e = hipGetDevice(&dev);
         if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
         if (e != hipSuccess) return hip_fail(e, "device query");
-        const int64_t most_S = std::min<int64_t>((b->max_len + least - 1) / least, kMaxSplits);
-        double best = causal_cost(p->rt, (double)blocks, (double)b->max_len, 1, cus);
-        for (const int64_t s : {(int64_t)2, (int64_t)3, (int64_t)4, (int64_t)6, (int64_t)8, cus / blocks, 2 * cus / blocks}) {
-            if (s < 2 || s > most_S) continue;
-            const double t = causal_cost(p->rt, (double)blocks, (double)b->max_len, (double)s, cus);
-            if (t < best) {
-                best = t;
-                S = s;
-            }
-        }
+    }
+    // of several sequences behind cached tokens, maybe a few only have the most keys
+    const double ragged = b->n_seq > 1 && b->max_len > b->max_new ? 0.07 * (double)(b->max_len - b->max_new) / (double)b->max_len : 0.0;
+    auto cost = [&](int halves, int64_t s) {
+        return causal_cost(p->rt, halves, ragged, (double)blocks, (double)b->max_len, (double)s, cus);
+    };
+    double best = cost(1, S);
+    for (int halves = 1; halves <= (p->rt ? 1 : 2); ++halves) {
+        auto consider = [&](int64_t ranges) {
+            const double t = cost(halves, ranges);
+            if (t >= best) return;
+            best = t;
+            S = ranges;
+            p->halves = halves;
+        };
+        const int64_t most_S = std::min<int64_t>((b->max_len + halves * least - 1) / (halves * least), kMaxSplits);
+        if (splits) consider(splits);
+        else
+            for (const int64_t s : {(int64_t)1, (int64_t)2, (int64_t)3, (int64_t)4, (int64_t)6, (int64_t)8, cus / blocks, 2 * cus / blocks})
+                if (s >= 1 && s <= most_S) consider(s);
     }
     // work items of up to 512 threads in a 32-bit grid, also those that join the ranges
     if (tiles * Hkv * std::max(S, S > 1 ? R / 2 : 0) >= (int64_t)1 << 23)
         return fail(QLIN_ERR_UNSUPPORTED, "too many rows, heads and key ranges for one call");
     p->tiles = (int)tiles;
     p->S = (int)S;
-    p->pairs = blocks * S <= 2 * cus;
+    p->pairs = p->halves == 1 && blocks * S <= 2 * cus;
     // ranges that only balance sequences of different lengths leave the short ones whole
-    const int64_t keys = splits == 0 && blocks * S > (p->rt ? cus : 2 * cus) ? 4 * 128 : least;
+    const int64_t keys = splits == 0 && p->halves == 1 && blocks * S > (p->rt ? cus : 2 * cus) ? 4 * 128 : p->halves * least;
     p->least = (int)(keys / (p->rt == 0 ? 32 : p->rt == 1 ? 32 : 128));
     p->ws_bytes = S > 1 ? tiles * Hkv * S * R * (kHeadDim + 2) * 4 : 0;
     return QLIN_OK;
@@ -250,7 +270,7 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
     if (splits_out) *splits_out = p.S;
     if (workspace_bytes) *workspace_bytes = p.ws_bytes;
     if (buf && buflen > 0)
-        snprintf(buf, (size_t)buflen, "kernel=%s splits=%d grid=%lld combine=%d", causal_kernel_name(p.rt), p.S,
+        snprintf(buf, (size_t)buflen, "kernel=%s splits=%d grid=%lld combine=%d", causal_kernel_name(p.rt, p.halves), p.S,
                  (long long)p.tiles * kv_heads * p.S, p.S > 1 ? 1 : 0);
     return QLIN_OK;
 }
@@ -304,7 +324,7 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     gn_reciprocal(a.Hkv, &a.inv_heads, &a.heads_shift);
     a.inv_g = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
     a.c = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)kHeadDim)));
-    const hipError_t e = launch_causal(a, p.rt, (hipStream_t)stream);
+    const hipError_t e = launch_causal(a, p.rt, p.halves, (hipStream_t)stream);
     return e == hipSuccess ? QLIN_OK : hip_fail(e, "causal attention launch");
 }
 

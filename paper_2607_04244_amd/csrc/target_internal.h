@@ -75,8 +75,8 @@ struct VerifyArgs {
 };
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st);
-hipError_t launch_causal(const CausalArgs &a, int rt, hipStream_t st);
-const char *causal_kernel_name(int rt);
+hipError_t launch_causal(const CausalArgs &a, int rt, int halves, hipStream_t st);
+const char *causal_kernel_name(int rt, int halves);
 hipError_t launch_verify(VerifyArgs a, int n_seq, hipStream_t st);
 
 }  // namespace qlin

@@ -243,6 +243,17 @@ def test_attention_head_groups(Hq, Hkv, new, length):
     check_attention(new, length, Hq=Hq, Hkv=Hkv, seed=Hq)
 
 
+@pytest.mark.parametrize("splits", [1, 2, 5])
+@pytest.mark.parametrize("new,length", [([33], [33]), ([40, 200, 1, 64], [40, 995, 1, 64]), ([130, 17], [1100, 16]), ([20, 0, 34], [352, 0, 65]),
+                                        ([300], [300]), ([25], [2000])])
+def test_attention_prompts_in_two_halves(splits, new, length):
+    """A large bound of the lengths takes the form whose workgroups walk two halves of a range:
+    one step of keys and none, odd numbers of steps, a last step that is no whole one."""
+    b = qlin.Batch(len(new), sum(new), max(new), 1 << 20, None, None, None)
+    assert "k_causal_prompt<2>" in qlin.qlin_causal_plan(b, 8, 2, HEAD, splits)[2]
+    check_attention(new, length, Hq=8, Hkv=2, splits=splits, max_len=1 << 20, pad=3, seed=7)
+
+
 @pytest.mark.parametrize("splits", [1, 2, 3, 7, 64, 256])
 @pytest.mark.parametrize("new,length", [([1, 1, 1], [1000, 3, 64]), ([16, 5], [500, 5]), ([150], [600])])
 def test_attention_forced_splits(splits, new, length):
@@ -318,6 +329,41 @@ def test_attention_keys_and_values_behind_a_token_have_no_influence(new, length,
         keep = slice(m, m + max(n - 2, 0))
         assert torch.equal(first[keep].view(torch.int16), second[keep].view(torch.int16)), (b, n)
         m += n
+
+
+@pytest.mark.parametrize("new,length,splits,max_len", [([130], [130], 1, 1 << 20), ([130, 20], [611, 33], 2, 1 << 20), ([64], [32 * 5 + 64], 1, 1 << 20),
+                                                       ([60], [700], 1, None), ([61], [900], 2, None), ([3], [900], 1, None), ([4, 4], [600, 33], 2, None),
+                                                       ([7], [1000], 1, None), ([16, 9], [1100, 70], 1, None)])
+def test_attention_of_long_walks_without_influence_from_behind(new, length, splits, max_len):
+    """As above over many steps of every kernel, the first ones in the form of two halves, where
+    the keys and values behind a token lie in its tile; and one-hot values that count the keys of
+    each row."""
+    Hq, Hkv = 8, 2
+    c = Cache("heads", length, Hkv, 5)
+    c.host[1].zero_()
+    for j in range(c.host[1].shape[2]):
+        c.host[1][:, :, j, j % HEAD] = 1.0
+    c.dev[1].copy_(c.host[1])
+    q = torch.zeros((sum(new), Hq, HEAD), dtype=torch.bfloat16)
+    form = dict(splits=splits, max_len=max_len)
+    out = f64(check_attention(new, length, Hq=Hq, Hkv=Hkv, cache=c, q=q, **form))
+    for m, (b, p) in enumerate(ref.positions(new, length)):
+        count = np.array([len(range(d, p + 1, HEAD)) for d in range(HEAD)])
+        assert np.all(np.abs(out[m] - count / (p + 1)) <= 2.0 ** -8 * count / (p + 1)), (m, p)
+        assert np.all(out[m][:, count == 0] == 0)
+    q = rand(6, (sum(new), Hq, HEAD), 2.0)
+    first = check_attention(new, length, Hq=Hq, Hkv=Hkv, cache=c, q=q, **form).clone()
+    for bad in (float("inf"), float("nan"), -3e38, 40.0):
+        for b, L in enumerate(length):
+            for t in c.dev:
+                t[b, :, L - 2:] = bad
+        second = torch.zeros_like(first)
+        qlin.causal_attention(q.cuda(), *c.dev, i32(starts(new)), max_new=max(new), out=second, **form, **c.kwargs())
+        torch.cuda.synchronize()
+        m = 0
+        for b, n in enumerate(new):
+            assert torch.equal(first[m:m + n - 2].view(torch.int16), second[m:m + n - 2].view(torch.int16)), (b, bad)
+            m += n
 
 
 def test_attention_infinite_values_reach_those_that_see_them():
