@@ -132,7 +132,8 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
  *   q_heads     a multiple of cache->heads, at most 64 times it, at most 4096
  *   scale       > 0 and finite, or 0 for 1 / sqrt(128)
  *   workspace   DEVICE scratch of the bytes qlin_causal_plan reports for the same
- *               arguments (NULL when 0), 16-byte aligned, no initialisation
+ *               arguments (NULL when 0), 16-byte aligned, no initialisation, apart from
+ *               q, out and the cache
  * max_new chooses the kernel: a batch of single tokens is read at the cache's rate only
  * if max_new says 1, so single tokens and long chunks are better two calls.
  * For fixed splits the same inputs give the same bits.  Calls sharing a workspace
@@ -181,7 +182,8 @@ int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *wor
  *   workspace   DEVICE scratch of at least qlin_verify_plan's bytes, 16-byte
  *               aligned, no initialisation
  * 0 <= n_draft <= 64 (0: plain sampling; drafted may then be NULL), 1 <= vocab <=
- * 2^24, n_seq <= 65535 (0 is a no-op).  Outputs must not overlap inputs or each other.
+ * 2^24, n_seq <= 65535 (0 is a no-op).  Outputs and the workspace must not overlap
+ * inputs or each other.
  * Calls sharing a workspace must be ordered on one stream.
  * Errors: INVALID, UNSUPPORTED, ALIGN, HIP.
  */

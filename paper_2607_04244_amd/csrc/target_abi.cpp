@@ -299,7 +299,9 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     if (p.ws_bytes > 0 && (!workspace || workspace_bytes < p.ws_bytes))
         return fail(QLIN_ERR_INVALID, "workspace of %lld bytes needed (%lld given)", (long long)p.ws_bytes,
                     (long long)(workspace ? workspace_bytes : 0));
-    if (overlap(ro, Range{(uintptr_t)workspace, (size_t)p.ws_bytes})) return fail(QLIN_ERR_INVALID, "out overlaps the workspace");
+    const Range ws{(uintptr_t)workspace, (size_t)p.ws_bytes};
+    for (const Range &r : {ro, rows_range(q, M, q_stride, w), cache_range(cache->k, cache), cache_range(cache->v, cache)})
+        if (overlap(r, ws)) return fail(QLIN_ERR_INVALID, "the workspace overlaps q, out or the cache");
     if (batch->max_new == 0) return QLIN_OK;
 
     CausalArgs a;
@@ -364,11 +366,15 @@ int qlin_verify_draft(int64_t n_seq, int64_t n_draft, int64_t vocab, const uint1
                          {(uintptr_t)drafted, per * (size_t)n_draft},
                          {(uintptr_t)count, count ? per : 0},
                          {(uintptr_t)temperature, temperature ? per : 0},
-                         {(uintptr_t)uniform, per * (size_t)(n_draft + 1)},
-                         {(uintptr_t)workspace, (size_t)need}};
+                         {(uintptr_t)uniform, per * (size_t)(n_draft + 1)}};
+    const Range ws{(uintptr_t)workspace, (size_t)need};
+    for (const Range &i : ins) {
+        for (const Range &o : outs)
+            if (overlap(o, i)) return fail(QLIN_ERR_INVALID, "accepted or tokens overlaps an input");
+        if (overlap(i, ws)) return fail(QLIN_ERR_INVALID, "the workspace overlaps an input");
+    }
     for (const Range &o : outs)
-        for (const Range &i : ins)
-            if (overlap(o, i)) return fail(QLIN_ERR_INVALID, "accepted or tokens overlaps an input or the workspace");
+        if (overlap(o, ws)) return fail(QLIN_ERR_INVALID, "the workspace overlaps accepted or tokens");
     if (overlap(outs[0], outs[1])) return fail(QLIN_ERR_INVALID, "accepted overlaps tokens");
 
     VerifyArgs a;

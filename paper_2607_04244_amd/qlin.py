@@ -386,9 +386,12 @@ def _address(name, t, dtype, dev):
     """The address of a tensor, which has to be of this type on the current device (its
     stream's).  The checks of a call cost about as much as its launch: one pass, no
     torch.device objects."""
-    if not isinstance(t, _torch.Tensor) or t.dtype is not dtype or t.get_device() != dev:
-        raise ValueError(f"{name} must be a {dtype} tensor on the current CUDA device")
-    return t.data_ptr()
+    try:
+        if t.dtype is dtype and t.get_device() == dev:
+            return t.data_ptr()
+    except AttributeError:                                  # no tensor
+        pass
+    raise ValueError(f"{name} must be a {dtype} tensor on the current CUDA device")
 
 
 def _vector(name, t, dtype, dev, n):
@@ -409,7 +412,7 @@ def _kv_cache(k_cache, v_cache, dev):
     if v_cache.shape != shape or v_cache.stride() != stride:
         raise ValueError("k_cache and v_cache must have the same shape and strides")
     rank = len(shape)
-    if rank not in (3, 4) or shape[-1] != 128 or stride[-1] != 1 or k_cache.numel() == 0:
+    if rank not in (3, 4) or shape[-1] != 128 or stride[-1] != 1 or 0 in shape:
         raise ValueError("the cache must be [sequences, heads, capacity, 128] or [tokens, heads, 128], rows contiguous")
     if rank == 3:
         return KVCache(k, v, shape[1], shape[0], stride[0], stride[1], 0)
@@ -465,9 +468,10 @@ def norm_rope_append(q, k, v, k_cache, v_cache, new_start, length, max_new=None,
     at, strides, widths = [], [], []
     for name, t in (("q", q), ("k", k), ("v", v)):
         at.append(_address(name, t, bf16, dev))
-        if t.dim() != 2:
+        shape = t.shape
+        if len(shape) != 2:
             raise ValueError(f"{name} must have rank 2")
-        (rows, width), (row, one) = t.shape, t.stride()
+        (rows, width), (row, one) = shape, t.stride()
         if width == 0 or width % 128 or one != 1 or (widths and rows != q.shape[0]):
             raise ValueError(f"{name} must be [rows, heads * 128] with contiguous rows")
         strides.append(row if rows > 1 else width)

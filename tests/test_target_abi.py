@@ -172,3 +172,19 @@ def test_attention_workspace_is_checked():
     with pytest.raises(qlin.QlinError) as e:
         qlin.qlin_causal_plan(batch(rows=1 << 22, max_new=1 << 22), 4096, 64, 128, 2)
     assert e.value.code == UNSUPPORTED
+
+
+def test_a_workspace_on_an_input_is_refused():
+    assert attend(splits=3, ws=A + 3 * STEP, wb=1 << 31) == INVALID and "workspace" in qlin.last_error()     # q
+    assert attend(splits=3, ws=A + STEP + 256, wb=1 << 31) == INVALID and "workspace" in qlin.last_error()   # k of the cache
+    assert attend(splits=3, ws=A + 2 * STEP, wb=1 << 31) == INVALID and "workspace" in qlin.last_error()     # v
+    for i in (0, 1, 2, 3, 4, 5, 6, 7):                                   # target, draft, drafted, ..., accepted, tokens
+        assert verify(ws=A + i * STEP) == INVALID and "workspace" in qlin.last_error()
+
+
+def test_prompts_in_two_halves_are_planned():
+    """Forced ranges of long walks over few items; short ones, and many items, in one half."""
+    plan = lambda n, L, S: qlin.qlin_causal_plan(batch(rows=n, max_new=n, max_len=L), 32, 8, 128, S)[2]
+    assert "k_causal_prompt<2> splits=1" in plan(500, 8000, 1) and "k_causal_prompt<2> splits=2" in plan(500, 8000, 2)
+    assert "k_causal_prompt<1>" in plan(500, 500, 1) and "k_causal_prompt<1>" in plan(500, 2000, 4)
+    assert "k_causal_prompt<1>" in plan(8192, 8192, 1)
