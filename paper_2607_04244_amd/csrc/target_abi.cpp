@@ -21,7 +21,7 @@ constexpr int64_t kMaxHeads = 4096, kMaxGroup = 64, kMaxSplits = 256, kMaxStride
 constexpr int64_t kMaxDraft = kVerifyMaxDraft, kMaxVocab = (int64_t)1 << 24, kMaxVerifySeq = 65535;   // sequences: a grid's y
 constexpr int64_t kMaxTokenStride = (int64_t)1 << 28;       // 32-bit byte offsets over four tokens
 constexpr int64_t kMaxRowStride = (int64_t)1 << 32;
-constexpr int64_t kVerifyTwoParts = (int64_t)1 << 26;           // logits of a call: see qlin_verify_draft
+constexpr int64_t kVerifyTwoParts = (int64_t)1 << 26, kVerifyMany = (int64_t)1 << 25;     // logits of a call: see qlin_verify_draft
 constexpr int64_t kMaxExtent = (int64_t)1 << 60;      // elements of one strided array
 
 // An address range, in bytes.
@@ -399,10 +399,10 @@ int qlin_verify_draft(int64_t n_seq, int64_t n_draft, int64_t vocab, const uint1
     a.final_decisions = a.decisions + n_seq;
     // Large calls look at a third of the rows first: a sequence that refuses a token there, as
     // most do at 3 of 4 tokens kept, needs no more.
-    const bool large = n_seq * (n_draft + 1 + (draft ? n_draft : 0)) * vocab >= kVerifyTwoParts;
-    a.first_rows = large && n_draft >= 3 ? (int)(n_draft + 1) / 3 : 0;
+    const int64_t logits = n_seq * (n_draft + 1 + (draft ? n_draft : 0)) * vocab;
+    a.first_rows = logits >= kVerifyTwoParts && n_draft >= 3 ? (int)(n_draft + 1) / 3 : 0;
     a.row0 = a.row1 = 0;
-    const hipError_t e = launch_verify(a, (int)n_seq, (hipStream_t)stream);
+    const hipError_t e = launch_verify(a, (int)n_seq, logits >= kVerifyMany, (hipStream_t)stream);
     return e == hipSuccess ? QLIN_OK : hip_fail(e, "verify launch");
 }
 

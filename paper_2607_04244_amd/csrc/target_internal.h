@@ -54,7 +54,7 @@ constexpr int causal_tile_rows(int rt) { return rt ? 16 * rt : 128; }
 
 // Verification.  A row of logits is cut into chunks of kVerifyChunk from the 16-byte boundary at
 // or before it (up to 7 logits earlier).
-constexpr int kVerifyChunk = 8192, kVerifyMaxDraft = 64;
+constexpr int kVerifyChunk = 4096, kVerifyMaxDraft = 64;
 struct VerifyStat { float m; int at; double z; };      // maximum, its lowest index (greedy), sum of the weights
 // done: known from the rows looked at; p and q are then the statistics of the row that decides
 struct VerifyDecision { int accepted, rejected, done; VerifyStat p, q; };
@@ -77,6 +77,6 @@ struct VerifyArgs {
 hipError_t launch_append(const AppendArgs &a, hipStream_t st);
 hipError_t launch_causal(const CausalArgs &a, int rt, int halves, hipStream_t st);
 const char *causal_kernel_name(int rt, int halves);
-hipError_t launch_verify(VerifyArgs a, int n_seq, hipStream_t st);
+hipError_t launch_verify(VerifyArgs a, int n_seq, bool many, hipStream_t st);
 
 }  // namespace qlin

@@ -1,11 +1,11 @@
 // The decision on drafted tokens (qlin_verify_draft in include/qlin_target.h).
 //
 // Bound by the bytes of the logits and the 64-bit exponentials of all of them:
-//   k_verify_stats   (row, chunk of 8192 tokens): maximum, its lowest index, and the sum of
+//   k_verify_stats   (row, chunk of 4096 tokens): maximum, its lowest index, and the sum of
 //       the weights e^((x - maximum) / T).
 //   k_verify_decide  (sequence): whether the first rows already refuse a token.  Large calls
 //       only: the statistics of the other rows are then taken where they can still matter.
-//   k_verify_weigh   (sequence, chunk), with draft logits: the accepted prefix from the rows'
+//   k_verify_weigh   (sequence, chunks), with draft logits: the accepted prefix from the rows'
 //       statistics, and, if a token was refused, the chunk's sum of max(P - Q, 0).
 //   k_verify_pick    (sequence): the chunk, then the token, that the running sum passes the
 //       uniform number in.  Without draft logits the chunks' sums follow from the statistics,
@@ -33,8 +33,9 @@ namespace qlin {
 namespace {
 
 constexpr float kNegInf = -__builtin_huge_valf(), kPosInf = __builtin_huge_valf();
-constexpr int kStatsThreads = 256, kStatsVecs = kVerifyChunk / (8 * kStatsThreads);
-constexpr int kPickThreads = kVerifyChunk / 8, kPickWaves = kPickThreads / 64, kWeighThreads = 512;
+constexpr int kChunkVecs = kVerifyChunk / 8;             // vectors of 8 logits
+constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kWeighThreads = kChunkVecs;
+static_assert(kChunkVecs <= kPickThreads, "a chunk's vectors");
 
 // 2^t, relative error 4.7e-11: (2^f - 1) / f on [-1/2, 1/2] as the polynomial of degree 6 whose
 // largest weighted error is smallest; 2^0 is 1 exactly.  The coefficients are opaque scalars:
@@ -208,9 +209,11 @@ __device__ inline void load_logits(const Row &r, int v, int V, float x[8]) {
 __device__ inline const uint16_t *target_row(const VerifyArgs &a, int b, int i) { return a.target + ((int64_t)b * (a.n + 1) + i) * a.target_stride; }
 __device__ inline const uint16_t *draft_row(const VerifyArgs &a, int b, int i) { return a.draft + ((int64_t)b * a.n + i) * a.draft_stride; }
 
-// One workgroup a (row, chunk); each thread holds its 32 logits in registers between the
-// maximum and the weights.
-__global__ __launch_bounds__(kStatsThreads) void k_verify_stats(VerifyArgs a) {
+// One workgroup of T threads a (row, chunk); each thread holds its logits in registers between
+// the maximum and the weights.
+template <int T>
+__global__ __launch_bounds__(T) void k_verify_stats(VerifyArgs a) {
+    constexpr int kStatsThreads = T, kStatsVecs = kChunkVecs / T;
     __shared__ VerifyStat part[kStatsThreads / 64];
     __shared__ float wave_m[kStatsThreads / 64];
     // this launch's rows: targets [row0, row1), then drafts [row0, row1) that there are
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(kStatsThreads) void k_verify_stats(VerifyArgs a) {
     const Row row(is_draft ? draft_row(a, b, i) : target_row(a, b, i));
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float x[kStatsVecs][8];
-    const int v0 = c * (kVerifyChunk / 8) + threadIdx.x;
+    const int v0 = c * kChunkVecs + threadIdx.x;
 #pragma unroll
     for (int k = 0; k < kStatsVecs; ++k) load_logits(row, v0 + k * kStatsThreads, a.V, x[k]);
     float m = kNegInf;
@@ -397,12 +400,13 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_decide(VerifyArgs a) {
     if (threadIdx.x == 0) a.decisions[b] = d;
 }
 
-// One workgroup a (sequence, chunk).  Every workgroup of a sequence finds its decision by
+// One workgroup a (sequence, C chunks).  Every workgroup of a sequence finds its decision by
 // itself, where the first rows have not: cheaper than a kernel for it.
+template <int C>
 __global__ __launch_bounds__(kWeighThreads) void k_verify_weigh(VerifyArgs a) {
     __shared__ Rows rows;
-    __shared__ double part[kWeighThreads / 64];
-    const int b = blockIdx.y, c = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ double part[C][kWeighThreads / 64];
+    const int b = blockIdx.y, c = blockIdx.x * C, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     Request rq;
     VerifyDecision d;
     if (a.first_rows && a.decisions[b].done) {
@@ -413,26 +417,26 @@ __global__ __launch_bounds__(kWeighThreads) void k_verify_weigh(VerifyArgs a) {
         if (c == 0 && threadIdx.x == 0) a.final_decisions[b] = d;
     }
     if (rq.greedy || !d.rejected || !(d.p.z > 0.0)) return;      // the rows' statistics suffice
-    double w[8], s = 0.0;
     const Choice ch = choice_of(a, b, d, rq.k);
 #pragma unroll
-    for (int k = 0; k < kVerifyChunk / 8 / kWeighThreads; ++k) {
-        ch.weights(c * (kVerifyChunk / 8) + k * kWeighThreads + threadIdx.x, a.V, true, w);
+    for (int k = 0; k < C; ++k) {
+        double w[8], s = 0.0;
+        ch.weights((c + k) * kChunkVecs + threadIdx.x, a.V, true, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += w[e];
+        s = wave_sum(s);
+        if (lane == 0) part[k][wave] = s;
     }
-    s = wave_sum(s);
-    if (lane == 0) part[wave] = s;
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (threadIdx.x < C && c + threadIdx.x < a.chunks) {
         double t = 0.0;
-        for (int i = 0; i < kWeighThreads / 64; ++i) t += part[i];
-        a.sums[(int64_t)b * a.chunks + c] = t;
+        for (int i = 0; i < kWeighThreads / 64; ++i) t += part[threadIdx.x][i];
+        a.sums[(int64_t)b * a.chunks + c + threadIdx.x] = t;
     }
 }
 
 // One workgroup a sequence.  Its chunk is found by every wave for itself, 64 chunks at a time;
-// the token by the running sum of its 8192, eight a thread.
+// the token by the running sum of its 4096, eight a thread of half the waves.
 __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
     __shared__ Rows rows;
     __shared__ double part[kPickWaves];
@@ -506,9 +510,9 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
     }
     const bool past = chunk < 0;                            // rounding left none: the last token of all
     if (past) chunk = any;
-    double w[8], own = 0.0;
-    const int v = chunk * (kVerifyChunk / 8) + tid, j0 = 8 * v - ch.row.off;
-    ch.weights(v, a.V, rest, w);
+    double w[8] = {}, own = 0.0;
+    const int v = chunk * kChunkVecs + tid, j0 = 8 * v - ch.row.off;
+    if (tid < kChunkVecs) ch.weights(v, a.V, rest, w);
     int end = -1;                                           // this thread's last token of any weight
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -543,12 +547,18 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
 
 }  // namespace
 
-hipError_t launch_verify(VerifyArgs a, int n_seq, hipStream_t st) {
+// Few logits go to many small workgroups, many to larger ones, by the call's logits (small / large
+// form, graph replays): 2.4 million 12.3 / 13.4 us, with draft logits 3.9 million 18.2 / 20.5, 9.4
+// 24.1 / 26.0, 26.7 37.5 / 40.2, 37.7 48.0 / 45.8, 65.9 70.3 / 65.1.  Chunks of 8192 and 2048 tokens
+// took 14.0 and 13.6 us for the first, 22.2 and 17.6 for the second.
+hipError_t launch_verify(VerifyArgs a, int n_seq, bool many, hipStream_t st) {
     auto stats = [&](int row0, int row1) {
         a.row0 = row0;
         a.row1 = row1;
         const int rows = row1 - row0 + (a.draft ? (row1 < a.n ? row1 : a.n) - row0 : 0);
-        hipLaunchKernelGGL(k_verify_stats, dim3((unsigned)(a.chunks * rows), (unsigned)n_seq), dim3(kStatsThreads), 0, st, a);
+        const dim3 grid((unsigned)(a.chunks * rows), (unsigned)n_seq);
+        if (many) hipLaunchKernelGGL(k_verify_stats<128>, grid, dim3(128), 0, st, a);
+        else hipLaunchKernelGGL(k_verify_stats<256>, grid, dim3(256), 0, st, a);
         return hipGetLastError();
     };
     hipError_t e;
@@ -559,7 +569,8 @@ hipError_t launch_verify(VerifyArgs a, int n_seq, hipStream_t st) {
     }
     if ((e = stats(a.first_rows, a.n + 1)) != hipSuccess) return e;
     if (a.draft) {
-        hipLaunchKernelGGL(k_verify_weigh, dim3((unsigned)a.chunks, (unsigned)n_seq), dim3(kWeighThreads), 0, st, a);
+        if (many) hipLaunchKernelGGL(k_verify_weigh<2>, dim3((unsigned)(a.chunks + 1) / 2, (unsigned)n_seq), dim3(kWeighThreads), 0, st, a);
+        else hipLaunchKernelGGL(k_verify_weigh<1>, dim3((unsigned)a.chunks, (unsigned)n_seq), dim3(kWeighThreads), 0, st, a);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     hipLaunchKernelGGL(k_verify_pick, dim3((unsigned)n_seq), dim3(kPickThreads), 0, st, a);
