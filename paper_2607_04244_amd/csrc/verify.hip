@@ -16,15 +16,17 @@
 // thousand choices on the wrong side of one.  At an error of 5e-11 it is one of 10^5.
 // 64-bit products run at the rate of 32-bit ones here, and 32-bit exponentials at a half of
 // it, so the accuracy costs about twice the time of 32-bit weights.  A table of 2^(j/32) or
-// 2^(j/64) in LDS or lanes with a polynomial of degree 3: 32 sequences 81 us of 84, one
-// sequence 14.9 of 14.3; not taken.
+// 2^(j/64) in LDS or lanes with a polynomial of degree 3 took 32 sequences from 84 to 81 us and
+// one from 14.3 to 14.9; not taken.
 //
-// 16 tokens over 151936: 13.7 us, of which the statistics 6.4 (one trip to memory, 19 chunks a
-// row over all compute units) and the token 7.4 (a workgroup's dependent steps: statistics,
-// decision, chunk, token).  32 sequences of 16 with draft logits: 84 to 105 us on different
-// boxes and orders of memory (statistics 37 + 20, decision 4.7, sums 16, token 7.6), where the
-// 5 TB/s of a copy would read all the logits in 63; the statistics are bound by their 64-bit
-// instructions, 14 a logit.
+// 16 tokens over 151936: 12.4 us, of which the statistics 5.5 (one trip to memory, 38 chunks a
+// row over all compute units) and the token 6.8, a workgroup's dependent steps: decision 3.2,
+// chunk 1.2, its logits 1, token 1.  Handing the decision what it reads again later, or the
+// drafted tokens' logits with the statistics, took trips away but no time: it is the latency of
+// the instructions.  32 sequences of 16 with draft logits: 85 to 99 us on different boxes and
+// orders of memory (statistics 38 + 20, decision 4.7, sums 16, token 6.4), where the 5 TB/s of a
+// copy would read all the logits in 63; the statistics are bound by their 64-bit instructions,
+// 14 a logit.
 #include "device_common.h"
 #include "target_internal.h"
 
