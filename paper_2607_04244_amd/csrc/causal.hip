@@ -239,6 +239,19 @@ __device__ inline v8bf values_up_to(v4s_t lo, v4s_t hi, int key, int key2, int l
     return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Whether a lane's sums are all finite: 0 x is 0 only then.  Four chains: one of 64 products in a
+// row takes as long as a dozen matrix products.
+template <int N, typename V>
+__device__ inline bool all_finite(const V (&o)[N]) {
+    constexpr int E = sizeof(V) / sizeof(float);
+    float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int dt = 0; dt < N; ++dt)
+#pragma unroll
+        for (int i = 0; i < E; ++i) z[i & 3] = __builtin_fmaf(o[dt][i], 0.0f, z[i & 3]);
+    return (z[0] + z[1]) + (z[2] + z[3]) == 0.0f;
+}
+
 // A row's sums are rescaled only when its maximum has grown by more than a factor 2^kLazy of
 // the weights: up to there the weights just exceed 1, with the same relative rounding.  Each row
 // goes by its own maximum, and a careful pass by the same steps, so that not a bit of a row
@@ -409,12 +422,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this slot has been read
             if (u + 2 * kFewWaves < u1) issue(u + 2 * kFewWaves, st);
         }
-        float bad = 0.0f;                                        // NaN if any sum is not finite
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) bad = __builtin_fmaf(o[dt][i], 0.0f, bad);
-        return !__ballot(bad != 0.0f);
+        return !__ballot(!all_finite(o));
     };
     if (!run(std::false_type{})) run(std::true_type{});
     l = pair32_sum(pair16_sum(l));
@@ -455,6 +463,7 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
     constexpr int W = 4 * NR, R = 32 * NR;
     __shared__ __attribute__((aligned(16))) uint4 ring[2][2][kMidUnits];      // [stage][K, V], then the waves' sums
     __shared__ float2 ml[W][32];
+    __shared__ int not_finite[W];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int hi = lane >> 5, r = lane & 31, rt = wave >> 2, ku = wave & 3;
     Work w;
@@ -500,6 +509,8 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 
     float m, l;
     v16f o[4];
+    v4f *const sums = (v4f *)&ring[0][0][0];
+    static_assert(sizeof(ring) >= sizeof(v4f) * W * 16 * 64, "the sums fit the ring");
     auto run = [&](auto mode) {                                  // whether the sums came out finite
         constexpr bool careful = decltype(mode)::value;
         m = kNegInf;
@@ -576,28 +587,24 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
                 issue(t + 2);
             }
         }
-        float bad = 0.0f;                                        // NaN if any sum is not finite
+        lds_barrier();                                           // every wave is done with the ring
+        // the four waves' sums of each 32 rows through LDS, in the matrix cores' order
+        l = pair32_sum(l);
+        if (hi == 0) ml[wave][r] = make_float2(m, l);
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) bad = __builtin_fmaf(o[dt][i], 0.0f, bad);
-        return !__syncthreads_or(bad != 0.0f);                   // also: every wave is done with the ring
+            for (int i = 0; i < 4; ++i)
+                sums[(wave * 16 + dt * 4 + i) * 64 + lane] = v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+        const uint64_t bad = __ballot(!all_finite(o));
+        if (lane == 0) not_finite[wave] = bad != 0;
+        lds_barrier();
+        int any = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) any |= not_finite[i];
+        return any == 0;
     };
-    if (!run(std::false_type{})) {
-        run(std::true_type{});
-    }
-    l = pair32_sum(l);
-
-    // the four waves' sums of each 32 rows through LDS, in the matrix cores' order
-    v4f *sums = (v4f *)&ring[0][0][0];
-    static_assert(sizeof(ring) >= sizeof(v4f) * W * 16 * 64, "the sums fit the ring");
-    if (hi == 0) ml[wave][r] = make_float2(m, l);
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            sums[(wave * 16 + dt * 4 + i) * 64 + lane] = v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-    __syncthreads();
+    if (!run(std::false_type{})) run(std::true_type{});
     if (32 * rt + r >= w.rows) return;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -636,6 +643,7 @@ constexpr int kStepUnits = kStepKeys * kHeadDim / 8;          // 16-byte units o
 template <int HALVES>
 __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_causal_prompt(CausalArgs a) {
     __shared__ __attribute__((aligned(16))) uint4 rings[HALVES][2][kStepSlots][kStepUnits];    // K, V
+    __shared__ int not_finite[HALVES * kPromptWaves];
     __shared__ float2 second[HALVES == 2 ? kPromptRows : 1];       // (maximum, sum of weights) of the second half
     const int wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % kPromptWaves), lane = threadIdx.x & 63;
     const int part = HALVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (kPromptWaves * 64));
@@ -822,12 +830,13 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
             o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag((n - 1) & 3, i >> 2, i & 3), operand((n & 1 ? p0 : p1) + 4 * (i >> 2)),
                                                                o[i & 3], 0, 0, 0);
     }
-    float bad = 0.0f;                                                // NaN if any sum is not finite
+    const uint64_t bad = __ballot(!all_finite(o));
+    if (lane == 0) not_finite[part * kPromptWaves + wave] = bad != 0;
+    lds_barrier();
+    int any = 0;
 #pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) bad = __builtin_fmaf(o[dt][i], 0.0f, bad);
-    if (__syncthreads_or(bad != 0.0f)) {
+    for (int i = 0; i < HALVES * kPromptWaves; ++i) any |= not_finite[i];
+    if (any) {
         // careful: once more, step by step, every row with the values of its own keys only
         m = kNegInf;
         l = 0.0f;
