@@ -6,8 +6,10 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
+#include <cstring>
 
 #include "qlin_internal.h"
 #include "target_internal.h"
@@ -138,7 +140,12 @@ double causal_cost(int rt, int halves, double ragged, double blocks, double L, d
     return join + (halves == 2 ? ragged * one : 0.0) + (W <= slots ? one : W * one / slots + (rt ? 0.5 : 0.1 * halves) * one);
 }
 
-int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, CausalPlan *p) {
+// What a plan depends on; compared bit by bit.
+struct CausalKey { int64_t n_seq, rows, max_new, max_len, Hq, Hkv, splits, cus; };
+
+int make_causal_plan(const CausalKey &k, CausalPlan *p) {
+    const CausalKey *const b = &k;
+    const int64_t Hq = k.Hq, Hkv = k.Hkv, splits = k.splits, cus = k.cus;
     const int64_t G = Hq / Hkv, most = b->max_new * G;
     p->rt = most <= 16 ? 1 : most <= 32 ? 2 : most <= 64 ? 4 : 0;
     const int64_t R = causal_tile_rows(p->rt), per = (most + R - 1) / R;
@@ -147,17 +154,10 @@ int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t split
     const int64_t blocks = std::max<int64_t>(tiles * Hkv, 1);
     const int64_t least = p->rt ? 128 : 256;     // keys of a range: a step of each wave, eight of a prompt
     int64_t S = std::max<int64_t>(splits, 1);
-    int cus = 256;                               // with forced ranges the plan is arithmetic
-    if (splits == 0) {
-        int dev = 0;
-        hipError_t e = hipGetDevice(&dev);
-        if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
-        if (e != hipSuccess) return hip_fail(e, "device query");
-    }
     // of several sequences behind cached tokens, maybe a few only have the most keys
     const double ragged = b->n_seq > 1 && b->max_len > b->max_new ? 0.07 * (double)(b->max_len - b->max_new) / (double)b->max_len : 0.0;
     auto cost = [&](int halves, int64_t s) {
-        return causal_cost(p->rt, halves, ragged, (double)blocks, (double)b->max_len, (double)s, cus);
+        return causal_cost(p->rt, halves, ragged, (double)blocks, (double)b->max_len, (double)s, (double)cus);
     };
     double best = cost(1, S);
     for (int halves = 1; halves <= (p->rt ? 1 : 2); ++halves) {
@@ -184,6 +184,42 @@ int make_causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t split
     const int64_t keys = splits == 0 && p->halves == 1 && blocks * S > (p->rt ? cus : 2 * cus) ? 4 * 128 : p->halves * least;
     p->least = (int)(keys / (p->rt == 0 ? 32 : p->rt == 1 ? 32 : 128));
     p->ws_bytes = S > 1 ? tiles * Hkv * S * R * (kHeadDim + 2) * 4 : 0;
+    return QLIN_OK;
+}
+
+// Compute units of the current device.
+int compute_units(int64_t *cus) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices];
+    int dev = 0, n = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess && dev >= 0 && dev < kDevices) n = known[dev].load(std::memory_order_relaxed);
+    if (e == hipSuccess && n == 0) {
+        e = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev);
+        if (e == hipSuccess && dev >= 0 && dev < kDevices) known[dev].store(n, std::memory_order_relaxed);
+    }
+    if (e != hipSuccess) return hip_fail(e, "device query");
+    *cus = n;
+    return QLIN_OK;
+}
+
+// The plan of a call.  Each thread remembers 64, directly mapped: the layers of a model ask for
+// the same one, and weighing the choices takes longer than all the checks.
+int causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, CausalPlan *p) {
+    CausalKey k{b->n_seq, b->rows, b->max_new, b->max_len, Hq, Hkv, splits, 256};   // forced ranges: arithmetic
+    if (splits == 0 && compute_units(&k.cus) != QLIN_OK) return last_status();
+    struct Entry { CausalKey key; CausalPlan plan; bool used; };
+    static thread_local Entry memory[64];
+    uint64_t words[sizeof k / 8], h = 0;
+    memcpy(words, &k, sizeof k);
+    for (const uint64_t w : words) h = (h ^ w) * 0x9E3779B97F4A7C15ull;
+    Entry &e = memory[h >> 58];
+    if (!e.used || memcmp(&e.key, &k, sizeof k)) {
+        CausalPlan made;
+        if (make_causal_plan(k, &made) != QLIN_OK) return last_status();
+        e = Entry{k, made, true};
+    }
+    *p = e.plan;
     return QLIN_OK;
 }
 
@@ -266,7 +302,7 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
     if (check_batch(batch) != QLIN_OK || check_heads(q_heads, kv_heads, head_dim) != QLIN_OK) return last_status();
     if (splits < 0 || splits > kMaxSplits) return fail(QLIN_ERR_INVALID, "splits must be in [0, 256]");
     CausalPlan p;
-    if (make_causal_plan(batch, q_heads, kv_heads, splits, &p) != QLIN_OK) return last_status();
+    if (causal_plan(batch, q_heads, kv_heads, splits, &p) != QLIN_OK) return last_status();
     if (splits_out) *splits_out = p.S;
     if (workspace_bytes) *workspace_bytes = p.ws_bytes;
     if (buf && buflen > 0)
@@ -295,7 +331,7 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     if (rows_meet(q, q_stride, w, out, out_stride, w, M) || overlap(ro, cache_range(cache->k, cache)) || overlap(ro, cache_range(cache->v, cache)))
         return fail(QLIN_ERR_INVALID, "out overlaps q or the cache");
     CausalPlan p;
-    if (make_causal_plan(batch, q_heads, cache->heads, splits, &p) != QLIN_OK) return last_status();
+    if (causal_plan(batch, q_heads, cache->heads, splits, &p) != QLIN_OK) return last_status();
     if (p.ws_bytes > 0 && (!workspace || workspace_bytes < p.ws_bytes))
         return fail(QLIN_ERR_INVALID, "workspace of %lld bytes needed (%lld given)", (long long)p.ws_bytes,
                     (long long)(workspace ? workspace_bytes : 0));

@@ -399,8 +399,8 @@ def _vector(name, t, dtype, dev, n):
     if t is None:
         return None
     p = _address(name, t, dtype, dev)
-    if t.shape != (n,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous, of shape ({n},)")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, of {n} values")
     return p
 
 
@@ -429,9 +429,9 @@ def _kv_cache(k_cache, v_cache, dev):
 def _batch(dev, rows, new_start, length, max_new, max_len, cache_start, k_cache):
     i32 = _torch.int32
     lengths = _address("length", length, i32, dev)
-    if length.dim() != 1 or not length.is_contiguous():
-        raise ValueError("length must be contiguous, of rank 1")
-    n = length.shape[0]
+    n = length.numel()
+    if not length.is_contiguous():
+        raise ValueError("length must be contiguous")
     starts = _vector("new_start", new_start, i32, dev, n + 1)
     slots = _vector("cache_start", cache_start, _torch.int64, dev, n)
     if slots is None and n > 1 and (k_cache.dim() == 3 or k_cache.shape[0] < n):
@@ -522,10 +522,14 @@ def causal_attention(q, k_cache, v_cache, new_start, length, max_new=None, max_l
     cache = _kv_cache(k_cache, v_cache, dev)
     batch = _batch(dev, rows, new_start, length, max_new, max_len, cache_start, k_cache)
     if workspace is None:
-        need = ctypes.c_int64()
-        _check(lib().qlin_causal_plan(batch, Hq, cache.heads, D, splits, None, ctypes.byref(need), None, 0))
-        if need.value:
-            workspace = _torch.empty(need.value, dtype=_torch.uint8, device=q.device)
+        size = batch.n_seq, rows, batch.max_new, batch.max_len, Hq, cache.heads, D, splits, dev
+        need = _scratch_bytes.get(size)
+        if need is None:
+            need = ctypes.c_int64()
+            _check(lib().qlin_causal_plan(batch, Hq, cache.heads, D, splits, None, ctypes.byref(need), None, 0))
+            need = _remember(size, need.value)
+        if need:
+            workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
     if out is None:
@@ -540,6 +544,16 @@ def causal_attention(q, k_cache, v_cache, new_start, length, max_new=None, max_l
     _check(lib().qlin_causal_attention(batch, cache, Hq, D, scale, splits, q_at, q_stride, out_at, out_stride,
                                        *_scratch(workspace), _raw_stream(dev)))
     return out
+
+
+_scratch_bytes = {}                 # of a call's sizes
+
+
+def _remember(size, need):
+    if len(_scratch_bytes) >= 1024:
+        _scratch_bytes.clear()
+    _scratch_bytes[size] = need
+    return need
 
 
 def _scratch(workspace):
@@ -595,10 +609,12 @@ def verify_draft(target, drafted, uniform, draft=None, n_draft=None, temperature
         if t.shape != (n, cols) or not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous, of shape {(n, cols)}")
     if workspace is None:
-        need = ctypes.c_int64()
-        _check(lib().qlin_verify_plan(n, rows - 1, vocab, ctypes.byref(need)))
-        if need.value:
-            workspace = _torch.empty(need.value, dtype=_torch.uint8, device=target.device)
+        size = n, rows, vocab
+        need = _scratch_bytes.get(size)
+        if need is None:
+            need = _remember(size, qlin_verify_plan(n, rows - 1, vocab))
+        if need:
+            workspace = _torch.empty(need, dtype=_torch.uint8, device=target.device)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
     _check(lib().qlin_verify_draft(n, rows - 1, vocab, target_at, target_stride, draft_at, draft_stride, at[0],

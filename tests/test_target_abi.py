@@ -188,3 +188,20 @@ def test_prompts_in_two_halves_are_planned():
     assert "k_causal_prompt<2> splits=1" in plan(500, 8000, 1) and "k_causal_prompt<2> splits=2" in plan(500, 8000, 2)
     assert "k_causal_prompt<1>" in plan(500, 500, 1) and "k_causal_prompt<1>" in plan(500, 2000, 4)
     assert "k_causal_prompt<1>" in plan(8192, 8192, 1)
+
+
+def test_remembered_plans_are_the_plans():
+    """More calls than a thread remembers, in two orders and in two threads."""
+    import threading
+    asks = [(n, rows, L, Hq, S) for n in (1, 3, 40) for rows in (40, 700, 4000) for L in (500, 9000) for Hq in (8, 32) for S in (1, 2, 9)]
+    ask = lambda n, rows, L, Hq, S: qlin.qlin_causal_plan(batch(n_seq=n, rows=rows, max_new=rows // n, max_len=L), Hq, 8, 128, S)
+    assert len(asks) > 64
+    first = [ask(*a) for a in asks]
+    assert len(set(first)) > 40
+    assert [ask(*a) for a in asks] == first and [ask(*a) for a in asks[::-1]] == first[::-1]
+    other = []
+    t = threading.Thread(target=lambda: other.extend(ask(*a) for a in asks for _ in (0, 1)))
+    t.start()
+    t.join()
+    assert other[::2] == first and other[1::2] == first
+    assert [p[0] for p in first] == [a[4] for a in asks]
