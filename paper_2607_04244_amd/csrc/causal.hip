@@ -83,13 +83,13 @@ __device__ inline int value_unit(int kk, int c) { return kk * 16 + (c ^ (4 * (kk
 // As load_lds_x16 (device_common.h) from a scalar address plus a 32-bit offset in bytes, to an
 // LDS byte address.
 __device__ inline void load_lds_s16(const uint16_t *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ inline void load_lds_v16(const uint16_t *src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds), "v"(src) : "memory", "m0");
 }
 __device__ inline void load_lds_s16_nt(const uint16_t *base, uint32_t off, uint32_t lds) {      // for data a call reads once
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }

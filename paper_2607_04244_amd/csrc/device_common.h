@@ -310,25 +310,26 @@ __device__ inline void valu_dequant(uint32_t P, const ValuDeq &d, const ExtractC
 // load before each later LDS read.  The caller waits for it explicitly
 // (s_waitcnt vmcnt) before the barrier that publishes the data; loads the
 // compiler does track and issues later are younger, so its own waits stay
-// sufficient.  These statements set m0 themselves and list it as clobbered;
+// sufficient.  A load to LDS needs one wait state after a scalar write of m0, which nobody
+// adds inside inline assembly: s_nop 0.  These statements set m0 themselves and list it as clobbered;
 // the compiler warns that it may not preserve a reserved register across
 // them, which matters only if it kept a value of its own in m0: the
 // generated code of every kernel here has no other m0 access.
 __device__ inline void load_lds_x16(const void *src, const uint4 *lds_dst) {
     const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)lds_dst);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(m0), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(m0), "v"(src) : "memory", "m0");
 }
 
 // The same with the non-temporal hint, for data a call reads once.
 __device__ inline void load_lds_x16_nt(const void *src, const uint4 *lds_dst) {
     const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)lds_dst);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "s"(m0), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "s"(m0), "v"(src) : "memory", "m0");
 }
 
 // The same with 4 bytes per lane: lane l's dword lands at lds_dst + 4 l.
 __device__ inline void load_lds_x4(const void *src, const void *lds_dst) {
     const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)lds_dst);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" :: "s"(m0), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(m0), "v"(src) : "memory", "m0");
 }
 
 // LDS byte address of p (wave-uniform), as a scalar.
@@ -341,11 +342,11 @@ __device__ inline uint32_t lds_addr(const void *p) {
 // Inline assembly for the same reason as load_lds_x16; lds and soff are
 // scalars, so a load whose per-lane offset is fixed costs no vector work.
 __device__ inline void load_lds_buf16(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                  :: "s"(lds), "v"(voff), "s"(r), "s"(soff) : "memory", "m0");
 }
 __device__ inline void load_lds_buf4(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
                  :: "s"(lds), "v"(voff), "s"(r), "s"(soff) : "memory", "m0");
 }
 
