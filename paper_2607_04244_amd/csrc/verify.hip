@@ -74,7 +74,16 @@ struct Pow2 {
     }
 };
 
-// Weights of a row: 2^(k x - k m), k = log2(e) / T, m its maximum.  -infinity and NaN give 0
+// log2(e) / T, in 45 bits (relative error 2^-45): its product with a bf16 number, of 8 bits, is
+// exact in 64, so that k x - k m is rounded once, as a difference, and is 0 for the maximum
+// however large |m| / T is.  (With k in 53 bits the rounding of k m stays in every exponent, and
+// from |m| / T = 10^19 it exceeds the range of the weights.)
+__device__ inline double exponent_scale(float T) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, 1.4426950408889634 / (double)T);
+    return __builtin_bit_cast(double, (u + 0x80) & ~(uint64_t)0xFF);
+}
+
+// Weights of a row: 2^(k x - k m), k = exponent_scale(T), m its maximum.  -infinity and NaN give 0
 // (2^-1100 is below the smallest number); where m is infinite, its equals have weight 1 and
 // all others none.
 struct Scale {
@@ -111,7 +120,7 @@ struct Scale {
 };
 // The factor from weights relative to m to weights relative to the larger M.
 __device__ inline double rescale(double k, float m, float M) {
-    return m == M ? 1.0 : m == kNegInf || M == kPosInf ? 0.0 : Pow2()(fmax(((double)m - (double)M) * k, -1100.0));
+    return m == M ? 1.0 : m == kNegInf || M == kPosInf ? 0.0 : Pow2()(fmax(__builtin_fma((double)m, k, -(k * (double)M)), -1100.0));
 }
 
 // Sums, maxima and minima over the lanes by DPP: within rows of 16 (row_shr 1, 2, 4, 8), then
@@ -167,14 +176,14 @@ __device__ inline int wave_min(int v) {
 struct Request {
     int count;
     bool greedy;
-    double k;               // log2(e) / T
+    double k;               // exponent_scale(T)
 };
 __device__ inline Request load_request(const VerifyArgs &a, int b) {
     Request r;
     r.count = a.count ? min(max(a.count[b], 0), a.n) : a.n;
     const float T = a.temperature ? a.temperature[b] : 1.0f;
     r.greedy = !(T > 0.0f);
-    r.k = r.greedy ? 1.0 : 1.4426950408889634 / (double)T;
+    r.k = r.greedy ? 1.0 : exponent_scale(T);
     return r;
 }
 

@@ -1,0 +1,52 @@
+"""GPU tests of qlin_verify_draft at the ends of its range, against the float64 oracle
+(whole numbers: equal)."""
+
+import pytest
+import torch
+
+from test_target import check_verify, verify_case
+
+pytestmark = pytest.mark.gpu
+
+MOST = float(torch.finfo(torch.bfloat16).max)
+
+
+def sampled(target, u, T):
+    """Plain sampling of every row: [n, 1, V], one uniform number and temperature each."""
+    n = target.shape[0]
+    return check_verify(target, None, [[]] * n, [[x] for x in u], T=T)
+
+
+# ---------------------------------------------------------------- large logits over a temperature
+
+
+@pytest.mark.parametrize("V", [4, 4099])
+@pytest.mark.parametrize("top", [17.25, -17.25, 1e-3, 1e20, -1e20, MOST, -MOST])
+def test_exponents_of_large_logits_over_small_temperatures(top, V):
+    """The largest logit has the weight 1 however large |logit| / T is, and its equals too."""
+    temperatures = [1e-45, 1e-38, 1e-30, 1e-20, 1e-10, 1e-6, 0.3, 0.5, 0.6, 0.7, 0.8, 1.0, 1.7, 1e20, float("inf")]
+    low = -2.0 if abs(top) < 1e10 else -MOST
+    values = [low, 0.25 * top if top > 0 else 2 * top if top > -1e30 else low, top, low]
+    t = torch.full((len(temperatures), 1, V), low, dtype=torch.bfloat16)
+    t[:, :, :4] = torch.tensor(values, dtype=torch.bfloat16)
+    for u in (0.0, 0.3, 0.99):
+        sampled(t, [u] * len(temperatures), temperatures)
+    t[:, :, V - 1] = t[:, :, 2]                                          # a tie, in another chunk if there are two
+    for u in (0.0, 0.3, 0.7, 0.99):
+        sampled(t, [u] * len(temperatures), temperatures)
+
+
+@pytest.mark.parametrize("with_draft", [True, False])
+@pytest.mark.parametrize("mask", [1e20, -1e20, MOST, -MOST])
+def test_decisions_with_forced_and_masked_logits(mask, with_draft):
+    """Logits forced up or masked by finite numbers, in the target, the draft or both."""
+    target, draft, drafted, u = verify_case(6, 3, 9001, 4, with_draft=with_draft)
+    force = torch.zeros(9001, dtype=torch.bool)
+    force[[5, 700, 8999] if mask > 0 else slice(0, 9001, 2)] = True
+    target[:3, :, force] = mask
+    if with_draft:
+        draft[1:4, :, force] = mask
+    for T in ([1.0] * 6, [0.5, 0.6, 0.7, 0.8, 0.9, 1.3], [1e-20, 1e-12, 1e-8, 1e-5, 1e-20, 0.0]):
+        check_verify(target, draft, drafted, u, T=T)
+    drafted = [[5, 700, 5]] * 6
+    check_verify(target, draft, drafted, u, T=[0.8, 1.0, 0.7, 0.6, 1e-15, 1e-30])
