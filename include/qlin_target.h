@@ -160,7 +160,8 @@ int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *wor
  *   P_i = softmax(target[b][i] / T),  i <= n;  T = temperature[b]
  *   Q_i = softmax(draft[b][i] / T),  i < n;  all mass on x_i if draft is NULL
  *   a = the first i with not u[b][i] Q_i(x_i) < P_i(x_i), or n
- *   W = max(P_a - Q_a, 0) (P_a itself where that is zero everywhere) if a < n, or P_n
+ *   W = max(P_a - Q_a, 0) (P_a itself where that is zero everywhere) if a < n, or P_n;
+ *       a difference below 2^-44 P_a is the rounding of 64-bit sums and counts as zero
  *   next = the lowest index whose running sum of W exceeds u[b][n_draft] sum(W)
  *          (the last index of positive W if rounding leaves none)
  * T = 0 (or below, or NaN) is the greedy limit: P_i is the lowest index of the

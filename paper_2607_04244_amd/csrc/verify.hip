@@ -40,7 +40,7 @@ constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kWeighThreads
 static_assert(kChunkVecs <= kPickThreads, "a chunk's vectors");
 
 // 2^t, relative error 4.7e-11: (2^f - 1) / f on [-1/2, 1/2] as the polynomial of degree 6 whose
-// largest weighted error is smallest; 2^0 is 1 exactly.  The coefficients are opaque scalars:
+// largest weighted error is smallest.  The coefficients are opaque scalars:
 // of constants the compiler makes copies into the accumulator, two moves a product.
 struct Pow2 {
     double c[6];
@@ -83,16 +83,18 @@ __device__ inline double exponent_scale(float T) {
     return __builtin_bit_cast(double, (u + 0x80) & ~(uint64_t)0xFF);
 }
 
-// Weights of a row: 2^(k x - k m), k = exponent_scale(T), m its maximum.  -infinity and NaN give 0
-// (2^-1100 is below the smallest number); where m is infinite, its equals have weight 1 and
-// all others none.
+// Weights of a row or chunk: 2^(k x - n), k = exponent_scale(T), n = ceil(k m), m its maximum.
+// With a whole n the weights of the same logit relative to two maxima differ by a power of two
+// exactly, so that sums over chunks cut differently, of two rows with the same logits, agree to
+// the rounding of the sums.  -infinity and NaN give 0 (2^-1100 is below the smallest number);
+// where m is infinite, its equals have weight 1 and all others none.
 struct Scale {
-    double k, km;
+    double k, n;
     bool inf;
     Pow2 pow2;
-    __device__ inline Scale(double k_, float m) : k(k_), km(k_ * (double)m), inf(m == kPosInf) {}
+    __device__ inline Scale(double k_, float m) : k(k_), n(ceil(k_ * (double)m)), inf(m == kPosInf) {}
     __device__ inline double operator()(float x) const {
-        return inf ? (x == kPosInf ? 1.0 : 0.0) : pow2(fmax(__builtin_fma((double)x, k, -km), -1100.0));
+        return inf ? (x == kPosInf ? 1.0 : 0.0) : pow2(fmax(__builtin_fma((double)x, k, -n), -1100.0));
     }
     // of eight logits: one branch
     __device__ inline void weights(const float x[8], double w[8]) const {
@@ -101,11 +103,11 @@ struct Scale {
             for (int e = 0; e < 8; ++e) w[e] = x[e] == kPosInf ? 1.0 : 0.0;
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = pow2(fmax(__builtin_fma((double)x[e], k, -km), -1100.0));
+            for (int e = 0; e < 8; ++e) w[e] = pow2(fmax(__builtin_fma((double)x[e], k, -n), -1100.0));
         }
     }
-    // their sum, where weights below 2^-1000 may count as that: next to the maximum's 1 they are
-    // no part of a 64-bit sum
+    // their sum, where weights below 2^-1000 may count as that: next to the maximum's, 1/2 to 1,
+    // they are no part of a 64-bit sum
     __device__ inline double sum(const float x[8]) const {
         double s[2] = {0.0, 0.0};
         if (inf) {
@@ -113,14 +115,14 @@ struct Scale {
             for (int e = 0; e < 8; ++e) s[0] += x[e] == kPosInf ? 1.0 : 0.0;
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e & 1] += pow2.within(fmax(__builtin_fma((double)x[e], k, -km), -1000.0));
+            for (int e = 0; e < 8; ++e) s[e & 1] += pow2.within(fmax(__builtin_fma((double)x[e], k, -n), -1000.0));
         }
         return s[0] + s[1];
     }
 };
-// The factor from weights relative to m to weights relative to the larger M.
+// The factor from weights relative to m to weights relative to the larger M: a power of two.
 __device__ inline double rescale(double k, float m, float M) {
-    return m == M ? 1.0 : m == kNegInf || M == kPosInf ? 0.0 : Pow2()(fmax(__builtin_fma((double)m, k, -(k * (double)M)), -1100.0));
+    return m == M ? 1.0 : m == kNegInf || M == kPosInf ? 0.0 : __builtin_amdgcn_ldexp(1.0, (int)fmax(ceil(k * (double)m) - ceil(k * (double)M), -1100.0));
 }
 
 // Sums, maxima and minima over the lanes by DPP: within rows of 16 (row_shr 1, 2, 4, 8), then
@@ -301,6 +303,12 @@ __device__ inline double probability(float x, const VerifyStat &st, double k) {
     return st.z > 0.0 ? Scale(k, st.m)(x) / st.z : 0.0;
 }
 
+// P and Q closer than this, relative to P, are equal: the weights of equal logits are equal, so P and
+// Q of equal rows differ by the rounding of two sums of up to 90 steps one after the other (9 in a
+// thread, 9 over a workgroup, 65 chunks in a lane, 6 over the lanes) and of two quotients, below
+// 190 2^-53.  Without it the next token would be drawn from that rounding.
+constexpr double kSame = 0x1p-44;
+
 // The weights that the next token is drawn by, in 8 tokens of a chunk: those of the target's
 // row, less the draft's (or the drafted token's) if `rest`.
 struct Choice {
@@ -333,7 +341,10 @@ struct Choice {
             double we[8];
             s.weights(d, we);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = fmax(w[e] - we[e] * inv_q, 0.0);
+            for (int e = 0; e < 8; ++e) {
+                const double d = __builtin_fma(-we[e], inv_q, w[e]);
+                w[e] = d > kSame * w[e] ? d : 0.0;
+            }
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)

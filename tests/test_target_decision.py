@@ -4,7 +4,7 @@
 import pytest
 import torch
 
-from test_target import check_verify, verify_case
+from test_target import check_verify, rand, verify_case
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,35 @@ def test_decisions_with_forced_and_masked_logits(mask, with_draft):
         check_verify(target, draft, drafted, u, T=T)
     drafted = [[5, 700, 5]] * 6
     check_verify(target, draft, drafted, u, T=[0.8, 1.0, 0.7, 0.6, 1e-15, 1e-30])
+
+
+# ---------------------------------------------------------------- equal rows
+
+
+@pytest.mark.parametrize("V,stride", [(64, None), (4097, None), (50257, None), (9000, 9001), (20011, 20013)])
+def test_equal_rows_leave_the_target_when_a_token_is_refused(V, stride):
+    """Where target and draft agree, a token of probability 0 is refused and nothing is left
+    of P - Q: the next token comes from P, at any distance of the rows from 16 bytes."""
+    n, drafts = 6, 3
+    target = rand(V, (n, drafts + 1, V), 2.0)
+    target[:, :, 7] = float("-inf")
+    draft = target[:, :drafts].clone()
+    drafted = [[-1, 2, 3], [7, 2, 3], [V, 1, 1], [2, -5, 1], [3, 4, 7], [1, 7, 7]]
+    T = [1.0, 0.7, 1.3, 1.0, 0.9, 2.0]
+    for u in (0.0, 0.1, 0.37, 0.5, 0.83, 0.999):
+        acc = check_verify(target, draft, drafted, [[0.5] * drafts + [u]] * n, T=T, stride=stride)
+        assert acc == [0, 0, 0, 1, 2, 1]
+
+
+def test_nearly_equal_rows_are_told_apart():
+    """One logit that differs by a step of bf16: the rest of P - Q is that token alone, or all
+    the others."""
+    V = 3000
+    target = rand(3, (2, 2, V), 1.0)
+    draft = target[:, :1].clone()
+    draft[0, 0, 1234] = 0.5
+    draft[1, 0, 1234] = 0.5
+    target[0, 0, 1234] = 0.50390625                                      # more probable: the only token of the rest
+    target[1, 0, 1234] = 0.498046875                                     # less: all others share the rest
+    for u in (0.0, 0.2, 0.6, 0.97):
+        check_verify(target, draft, [[-1], [-1]], [[0.5, u]] * 2)
