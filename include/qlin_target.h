@@ -163,7 +163,8 @@ int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *wor
  *   W = max(P_a - Q_a, 0) (P_a itself where that is zero everywhere) if a < n, or P_n;
  *       a difference below 2^-44 P_a is the rounding of 64-bit sums and counts as zero
  *   next = the lowest index whose running sum of W exceeds u[b][n_draft] sum(W)
- *          (the last index of positive W if rounding leaves none)
+ *          (the last index of positive W if rounding leaves none); tokens less likely
+ *          than 2^-900 times the row's likeliest may count as impossible
  * T = 0 (or below, or NaN) is the greedy limit: P_i is the lowest index of the
  * largest logit, Q_i all mass on x_i.  A logit of -infinity or NaN is a masked token
  * of probability 0.  A row without any token has P = 0 everywhere; next is then -1.

@@ -309,6 +309,12 @@ __device__ inline double probability(float x, const VerifyStat &st, double k) {
 // 190 2^-53.  Without it the next token would be drawn from that rounding.
 constexpr double kSame = 0x1p-44;
 
+// A chunk whose largest weight is below this, relative to the row's, holds no token to draw.  So a
+// chunk with any mass has a token whose probability is a number: without a refused token its
+// largest one, above 2^-901 2^-24; and what is left of a sum after a refused token's weight is
+// taken out, if anything is, was at least 2^-54 of it, over 4096 tokens.
+constexpr double kLeast = 0x1p-900;
+
 // The weights that the next token is drawn by, in 8 tokens of a chunk: those of the target's
 // row, less the draft's (or the drafted token's) if `rest`.
 struct Choice {
@@ -499,7 +505,8 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
         const VerifyStat st = stats[c];
         double z = st.z;
         if (rest && c == gone_chunk && st.m != kNegInf) z = fmax(z - Scale(rq.k, st.m)(gone), 0.0);
-        return z * rescale(rq.k, st.m, d.p.m);
+        const double f = rescale(rq.k, st.m, d.p.m);
+        return f < kLeast ? 0.0 : z * f;
     };
     // the first chunk whose running sum passes r = u total, and the last with any mass
     int chunk = -1, any = 0;
@@ -561,8 +568,10 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
     __syncthreads();
     if (tid == 0) {
         int next = chosen;
-        if (next == 0x7FFFFFFF)
+        if (next == 0x7FFFFFFF) {
+            next = -1;
             for (int i = 0; i < kPickWaves; ++i) next = last_of[i] >= 0 ? last_of[i] : next;
+        }
         *out = next;
     }
 }

@@ -1,6 +1,7 @@
 """GPU tests of qlin_verify_draft at the ends of its range, against the float64 oracle
 (whole numbers: equal)."""
 
+import numpy as np
 import pytest
 import torch
 
@@ -82,3 +83,67 @@ def test_nearly_equal_rows_are_told_apart():
     target[1, 0, 1234] = 0.498046875                                     # less: all others share the rest
     for u in (0.0, 0.2, 0.6, 0.97):
         check_verify(target, draft, [[-1], [-1]], [[0.5, u]] * 2)
+
+
+# ---------------------------------------------------------------- weights at the end of the range
+
+
+@pytest.mark.parametrize("low", [-600.0, -744.0, -740.0, -710.0, -1000.0, -1e4, -1e9])
+@pytest.mark.parametrize("V", [8192, 8189, 12288])
+def test_chunks_of_vanishing_weight_hold_no_token(low, V):
+    """u = 0 draws the first token of any weight: not one of a chunk whose weights are no
+    numbers any more, relative to the largest (e^-600 still is one)."""
+    t = torch.full((1, 2, V), low, dtype=torch.bfloat16)
+    t[:, :, 4096:] = 0.0
+    for u in (0.0, 1e-30, 0.5):
+        acc, tok = decide(t, None, [[-1]], [[0.5, u]])
+        assert acc == [0] and 0 <= tok[0][0] < V
+        if low > -650.0 and u == 0.0:
+            assert tok[0][0] == 0
+        elif low < -740.0 or u > 0.0:
+            assert tok[0][0] >= 4096 - (8 if u > 0.0 else 0)
+    if low < -740.0 or low > -650.0:
+        check_verify(t, None, [[-1]], [[0.5, 0.0]])
+        check_verify(t, None, [[-1]], [[0.5, 0.9]])
+
+
+def test_a_refused_token_that_had_almost_all_of_its_chunk():
+    """The refused token held all but 2^-50 of its chunk, which itself is e^-600 of the row."""
+    V = 8192
+    t = torch.full((1, 2, V), float("-inf"), dtype=torch.bfloat16)
+    t[:, :, 5] = -600.0
+    t[:, :, 9] = -636.0
+    t[:, :, 5000] = 0.0
+    check_verify(t, None, [[5]], [[0.5, 0.0]])
+    check_verify(t, None, [[5]], [[0.5, 0.5]])
+
+
+def decide(target, draft, drafted, u, T=None):
+    from paper_2607_04244_amd import qlin
+    n, r, _ = target.shape
+    f32 = lambda x: torch.tensor(x, dtype=torch.float32, device="cuda")
+    acc, tok = qlin.verify_draft(target.cuda(), torch.tensor(drafted, dtype=torch.int32, device="cuda").view(n, r - 1), f32(u).view(n, r),
+                                 draft=None if draft is None else draft.cuda(), temperature=None if T is None else f32(T))
+    torch.cuda.synchronize()
+    return acc.tolist(), tok.tolist()
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_every_token_is_one_of_the_vocabulary(seed):
+    """Rows of wild values: the next token always has a number of the vocabulary and a logit
+    that is not masked, and equals the oracle's where that is settled."""
+    rng = np.random.default_rng(seed)
+    V, n, drafts = int(rng.choice([3, 100, 4096, 4100, 13001])), 4, 2
+    pool = [0.0, 1.0, -1.0, 30.0, -700.0, -745.0, 1e3, -1e4, 1e20, -1e20, MOST, -MOST, float("-inf"), 1e-30]
+    pick = lambda *shape: torch.tensor(np.asarray(pool)[rng.integers(0, len(pool), shape) if seed % 2 else
+                                                        rng.choice(rng.integers(0, len(pool), 3), shape)]).to(torch.bfloat16)
+    target, draft = pick(n, drafts + 1, V), pick(n, drafts, V) if seed % 3 else None
+    target[:, :, int(rng.integers(V))] = 2.0
+    drafted = rng.integers(-1, V, (n, drafts)).tolist()
+    u = rng.choice([0.0, 1e-20, 0.25, 0.5, 0.99999], (n, drafts + 1)).tolist()
+    T = rng.choice([1e-30, 1e-3, 0.5, 1.0, 2.0, 1e10], n).tolist()
+    acc, tok = decide(target, draft, drafted, u, T)
+    for b in range(n):
+        assert 0 <= acc[b] <= drafts
+        nxt = tok[b][acc[b]]
+        assert 0 <= nxt < V and float(target[b, acc[b], nxt]) > float("-inf"), (b, acc[b], nxt)
