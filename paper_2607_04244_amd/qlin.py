@@ -568,11 +568,11 @@ def _logit_rows(name, t, n, rows, vocab):
     seq, row, one = t.stride()
     if rows == 1:
         row = seq
-    if n * rows <= 1:
+    if n * rows == 0:
         return vocab
     if (one != 1 and vocab > 1) or (n > 1 and seq != rows * row):
         raise ValueError(f"{name} must have contiguous rows at one distance")
-    return row
+    return row if n * rows > 1 else vocab
 
 
 def verify_draft(target, drafted, uniform, draft=None, n_draft=None, temperature=None, accepted=None, tokens=None,
