@@ -36,8 +36,8 @@ extern "C" {
  * sequence without new tokens is skipped.  Whatever the device arrays hold, no
  * call reads or writes outside the row arrays and the cache's slots: bounds are
  * clamped to [0, rows], new tokens past the first max_new of a sequence are left
- * out, and a sequence whose slots are not all inside the cache counts as one
- * without cached tokens.
+ * out, and a sequence whose slots are not all inside the cache, and inside its own
+ * room there (capacity below), counts as one without cached tokens.
  */
 typedef struct qlin_batch {
     int64_t n_seq;               /* sequences, 1 .. 65536 */
@@ -57,14 +57,19 @@ typedef struct qlin_batch {
  *                                      seq_slots heads * capacity
  *   [tokens][heads][128] (packed)      token_stride heads * 128, head_stride 128,
  *                                      cache_start given
+ * In the first, the slots past a sequence's capacity are other heads' or sequences':
+ * capacity tells where its room ends, and a longer sequence counts as one without cached
+ * tokens.  Rooms begin every seq_slots slots; with cache_start a sequence may begin inside
+ * one, and has the rest of it.
  */
 typedef struct qlin_kv_cache {
+    int64_t capacity;            /* slots of one sequence's room, 0 .. 2^40; 0: no bound but slots */
     uint16_t *k, *v;             /* DEVICE, 16-byte aligned */
     int64_t heads;               /* key/value heads */
     int64_t slots;               /* slots that may be addressed: s < slots, 1 .. 2^40 */
     int64_t token_stride;        /* elements, 128 .. 2^28, a multiple of 8 */
     int64_t head_stride;         /* elements, 128 .. 2^40, a multiple of 8 */
-    int64_t seq_slots;           /* slots between sequences where cache_start is NULL, 0 .. 2^40 */
+    int64_t seq_slots;           /* slots between sequences where cache_start is NULL, and between rooms, 0 .. 2^40 */
 } qlin_kv_cache;
 
 /*

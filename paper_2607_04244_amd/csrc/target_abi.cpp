@@ -77,10 +77,10 @@ int check_heads(int64_t q_heads, int64_t kv_heads, int64_t head_dim) {
 
 int check_cache(const qlin_kv_cache *c) {
     if (!c) return fail(QLIN_ERR_INVALID, "NULL cache");
-    if (c->slots < 1 || c->seq_slots < 0 || c->token_stride < kHeadDim || c->head_stride < kHeadDim)
-        return fail(QLIN_ERR_INVALID, "cache: slots must be positive, seq_slots >= 0, strides >= 128");
+    if (c->slots < 1 || c->seq_slots < 0 || c->capacity < 0 || c->token_stride < kHeadDim || c->head_stride < kHeadDim)
+        return fail(QLIN_ERR_INVALID, "cache: slots must be positive, seq_slots and capacity >= 0, strides >= 128");
     if (c->token_stride % 8 || c->head_stride % 8) return fail(QLIN_ERR_ALIGN, "cache strides must be multiples of 8");
-    if (c->slots > kMaxSlots || c->seq_slots > kMaxSlots || c->token_stride > kMaxTokenStride || c->head_stride > kMaxStride ||
+    if (c->slots > kMaxSlots || c->seq_slots > kMaxSlots || c->capacity > kMaxSlots || c->token_stride > kMaxTokenStride || c->head_stride > kMaxStride ||
         (double)c->slots * (double)c->token_stride + (double)c->heads * (double)c->head_stride > (double)kMaxExtent)
         return fail(QLIN_ERR_UNSUPPORTED, "cache too large");
     if (!c->k || !c->v) return fail(QLIN_ERR_INVALID, "NULL cache");
@@ -103,6 +103,7 @@ BatchArgs batch_args(const qlin_batch *b, const qlin_kv_cache *c) {
     a.cache_start = b->cache_start;
     a.slots = c->slots;
     a.seq_slots = c->seq_slots;
+    a.capacity = c->capacity;
     a.tok = c->token_stride;
     a.head = c->head_stride;
     a.n_seq = (int)b->n_seq;

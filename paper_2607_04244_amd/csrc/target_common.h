@@ -9,7 +9,8 @@ namespace qlin {
 
 // Sequence b: its rows [row0, row0 + n), of which the first `rows` are computed, its
 // cached tokens L and the slot of token 0.  Whatever the arrays hold, rows stay in
-// [0, a.rows), and L is 0 unless slots [slot0, slot0 + L) are inside the cache.
+// [0, a.rows), and L is 0 unless slots [slot0, slot0 + L) are inside the cache and, with a
+// capacity, inside one sequence's room.
 struct Seq {
     int row0, n, rows, p0, L;
     int64_t slot0;
@@ -23,7 +24,9 @@ __device__ inline Seq load_seq(const BatchArgs &a, int b) {
     const int L = max(a.length[b], 0);
     s.p0 = L - s.n;                         // position of its first new token
     s.slot0 = a.cache_start ? a.cache_start[b] : (int64_t)b * a.seq_slots;
-    s.L = s.slot0 >= 0 && s.slot0 <= a.slots - L ? L : 0;
+    int64_t room = a.capacity ? a.capacity : a.slots;
+    if (a.capacity && a.cache_start && a.seq_slots) room -= s.slot0 % a.seq_slots;
+    s.L = s.slot0 >= 0 && s.slot0 <= a.slots - L && L <= room ? L : 0;
     return s;
 }
 

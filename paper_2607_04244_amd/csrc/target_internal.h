@@ -15,7 +15,7 @@ constexpr int kHeadDim = 128;
 struct BatchArgs {
     const int32_t *new_start, *length;
     const int64_t *cache_start;     // or null: b * seq_slots
-    int64_t slots, seq_slots;
+    int64_t slots, seq_slots, capacity;
     int64_t tok, head;              // elements between slots, between heads
     int n_seq, rows, max_new;
 };

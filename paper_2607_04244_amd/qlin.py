@@ -8,6 +8,7 @@ module raises if the library has not been built - there is no fallback.
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -43,10 +44,21 @@ class Batch(ctypes.Structure):
                 ("cache_start", ctypes.c_void_p)]
 
 
-class KVCache(ctypes.Structure):
-    """struct qlin_kv_cache (include/qlin_target.h); strides in elements."""
+class _Room(ctypes.Structure):
+    _fields_ = [("capacity", ctypes.c_int64)]
+
+
+class KVCache(_Room):
+    """struct qlin_kv_cache (include/qlin_target.h); strides in elements.  Its first member,
+    capacity, is given by name, and is 0 (no bound) without."""
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("heads", ctypes.c_int64), ("slots", ctypes.c_int64),
                 ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("seq_slots", ctypes.c_int64)]
+
+    def __init__(self, *fields, capacity=0):
+        super().__init__(capacity, *fields)
+
+
+_cache_members = struct.Struct("=8q").pack
 
 
 class QlinError(RuntimeError):
@@ -423,7 +435,8 @@ def _kv_cache(k_cache, v_cache, dev):
     if token <= 0 or seq % token:
         raise ValueError("the cache's sequences must lie whole tokens apart")
     seq //= token
-    return KVCache(k, v, heads, (n - 1) * seq + capacity, token, head, seq)
+    # the members packed: a third of the constructor's time
+    return KVCache.from_buffer_copy(_cache_members(capacity, k, v, heads, (n - 1) * seq + capacity, token, head, seq))
 
 
 def _batch(dev, rows, new_start, length, max_new, max_len, cache_start, k_cache):
