@@ -261,6 +261,16 @@ __device__ inline bool all_finite(const V (&o)[N]) {
 // depends on what lies behind its token.
 constexpr float kLazy = 8.0f;
 
+// The weights' exponents s c - m c are fused products less a rounded m c: its rounding is in all of a
+// row's weights alike and cancels, while |m c| is at most kFar and it is at most 1.  Above, where it
+// could take all weights past their range, a careful pass takes (s - m) c, at the steps of the rows
+// where that is so; a row that ever is there sends its tile through one, whatever lies behind it.
+constexpr float kFar = 16777216.0f;
+
+__device__ inline float exponent(float s, float c, float mu, float muc, bool far) {
+    return far ? (s - mu) * c : __builtin_fmaf(s, c, -muc);
+}
+
 // The sums of W waves, each relative to its own maximum, as one: returns (maximum, sum of
 // weights) and the values in acc.
 template <int W>
@@ -354,6 +364,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
         constexpr bool careful = decltype(mode)::value;
         m = kNegInf;
         l = 0.0f;
+        uint64_t gone_far = 0;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) o[dt] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         int st = 0;
@@ -383,7 +394,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
             float mt = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
                              fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
             mt = pair32_max(pair16_max(mt));
-            const bool own = mt * a.c > __builtin_fmaf(m, a.c, kLazy);
+            const bool own = (mt - m) * a.c > kLazy;
             if (__ballot(own)) {
                 const float mn = own ? mt : m;
                 const float alpha = exp2_hw((m - (mn == kNegInf ? 0.0f : mn)) * a.c);
@@ -391,13 +402,15 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
                 m = mn;
+                gone_far |= __ballot(m != kNegInf && fabsf(m * a.c) > kFar);
             }
-            const float muc = (m == kNegInf ? 0.0f : m) * a.c;
+            const float mu = m == kNegInf ? 0.0f : m, muc = mu * a.c;
+            const bool far = careful && fabsf(muc) > kFar;
             uint32_t pw[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float e0 = exp2_hw(__builtin_fmaf(sc[i >> 1][2 * (i & 1)], a.c, -muc));
-                const float e1 = exp2_hw(__builtin_fmaf(sc[i >> 1][2 * (i & 1) + 1], a.c, -muc));
+                const float e0 = exp2_hw(exponent(sc[i >> 1][2 * (i & 1)], a.c, mu, muc, far));
+                const float e1 = exp2_hw(exponent(sc[i >> 1][2 * (i & 1) + 1], a.c, mu, muc, far));
                 pw[i] = cvt_pk_bf16(e0, e1);
                 l = dot2(pw[i], kBf16OnePair, l);
             }
@@ -425,7 +438,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this slot has been read
             if (u + 2 * kFewWaves < u1) issue(u + 2 * kFewWaves, st);
         }
-        return !__ballot(!all_finite(o));
+        return !__ballot(!all_finite(o)) && !gone_far;
     };
     if (!run(std::false_type{})) run(std::true_type{});
     l = pair32_sum(pair16_sum(l));
@@ -518,6 +531,7 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
         constexpr bool careful = decltype(mode)::value;
         m = kNegInf;
         l = 0.0f;
+        uint64_t gone_far = 0;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -547,7 +561,7 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[i]);
                 mt = pair32_max(mt);
-                const bool own = mt * a.c > __builtin_fmaf(m, a.c, kLazy);
+                const bool own = (mt - m) * a.c > kLazy;
                 if (__ballot(own)) {
                     const float mn = own ? mt : m;
                     const float alpha = exp2_hw((m - (mn == kNegInf ? 0.0f : mn)) * a.c);
@@ -555,12 +569,14 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 #pragma unroll
                     for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
                     m = mn;
+                    gone_far |= __ballot(m != kNegInf && fabsf(m * a.c) > kFar);
                 }
-                const float muc = (m == kNegInf ? 0.0f : m) * a.c;
+                const float mu = m == kNegInf ? 0.0f : m, muc = mu * a.c;
+                const bool far = careful && fabsf(muc) > kFar;
                 uint32_t p[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    p[i] = cvt_pk_bf16(exp2_hw(__builtin_fmaf(s[2 * i], a.c, -muc)), exp2_hw(__builtin_fmaf(s[2 * i + 1], a.c, -muc)));
+                    p[i] = cvt_pk_bf16(exp2_hw(exponent(s[2 * i], a.c, mu, muc, far)), exp2_hw(exponent(s[2 * i + 1], a.c, mu, muc, far)));
                     l = dot2(p[i], kBf16OnePair, l);
                 }
 #pragma unroll
@@ -599,7 +615,7 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 sums[(wave * 16 + dt * 4 + i) * 64 + lane] = v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-        const uint64_t bad = __ballot(!all_finite(o));
+        const uint64_t bad = __ballot(!all_finite(o)) | gone_far;
         if (lane == 0) not_finite[wave] = bad != 0;
         lds_barrier();
         int any = 0;
@@ -730,6 +746,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
     auto operand = [](const uint32_t *p) { return __builtin_bit_cast(v8bf, v4u{p[0], p[1], p[2], p[3]}); };
 
     float m = kNegInf, l = 0.0f;
+    uint64_t gone_far = 0;
     v16f o[4];
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt) zero(o[dt]);
@@ -762,7 +779,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
             const int key0 = first_key + u * kStepKeys;
             if (key0 + kStepKeys - 1 > wave_first) mask(s, key0);
             const float mt = row_max(s);
-            const bool own = mt * a.c > __builtin_fmaf(m, a.c, kLazy), grown = __ballot(own) != 0;
+            const bool own = (mt - m) * a.c > kLazy, grown = __ballot(own) != 0;
             const float mn = own ? mt : m;
             const float mu = mn == kNegInf ? 0.0f : mn, muc = mu * a.c;
             float ls = 0.0f;
@@ -801,6 +818,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
                 l *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
+                gone_far |= __ballot(fabsf(muc) > kFar);
             }
             l += ls;
         };
@@ -833,7 +851,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
             o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag((n - 1) & 3, i >> 2, i & 3), operand((n & 1 ? p0 : p1) + 4 * (i >> 2)),
                                                                o[i & 3], 0, 0, 0);
     }
-    const uint64_t bad = __ballot(!all_finite(o));
+    const uint64_t bad = __ballot(!all_finite(o)) | gone_far;
     if (lane == 0) not_finite[part * kPromptWaves + wave] = bad != 0;
     lds_barrier();
     int any = 0;
@@ -861,7 +879,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
             for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(slot, ks), qf[ks], s, 0, 0, 0);
             mask(s, key0);
             const float mt = row_max(s);
-            const bool own = mt * a.c > __builtin_fmaf(m, a.c, kLazy);
+            const bool own = (mt - m) * a.c > kLazy;
             const float mn = own ? mt : m, mu = mn == kNegInf ? 0.0f : mn, muc = mu * a.c;
             if (__ballot(own)) {
                 const float alpha = exp2_hw((m - mu) * a.c);
@@ -870,11 +888,12 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
             }
+            const bool far = fabsf(muc) > kFar;
             float ls = 0.0f;
             uint32_t p[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                p[i] = cvt_pk_bf16(exp2_hw(__builtin_fmaf(s[2 * i], a.c, -muc)), exp2_hw(__builtin_fmaf(s[2 * i + 1], a.c, -muc)));
+                p[i] = cvt_pk_bf16(exp2_hw(exponent(s[2 * i], a.c, mu, muc, far)), exp2_hw(exponent(s[2 * i + 1], a.c, mu, muc, far)));
                 ls = dot2(p[i], kBf16OnePair, ls);
             }
             l += ls;
