@@ -96,7 +96,7 @@ typedef struct qlin_kv_cache {
  *               apart; q itself (same stride), or elements apart from every input
  *               and the cache
  * All pointers 16-byte aligned (norm weights and inv_freq: 8).  k and v must not
- * overlap the cache.  Two new tokens must not share a slot (sequences sharing
+ * overlap the cache, and the batch's arrays neither q_out nor the cache.  Two new tokens must not share a slot (sequences sharing
  * slots: which of them is stored is not defined).
  * Errors: INVALID (NULL, sizes, strides, overlap, eps), UNSUPPORTED (head_dim !=
  * 128, limits), ALIGN, HIP.
@@ -133,12 +133,12 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
  *
  *   q, out      DEVICE bf16 rows of q_heads x 128, q_stride / out_stride elements
  *               apart (multiples of 8), 16-byte aligned; out must not share elements
- *               with q nor overlap the cache or the workspace
+ *               with q nor overlap the cache, the workspace or the batch's arrays
  *   q_heads     a multiple of cache->heads, at most 64 times it, at most 4096
  *   scale       > 0 and finite, or 0 for 1 / sqrt(128)
  *   workspace   DEVICE scratch of the bytes qlin_causal_plan reports for the same
  *               arguments (NULL when 0), 16-byte aligned, no initialisation, apart from
- *               q, out and the cache
+ *               q, out, the cache and the batch's arrays
  * max_new chooses the kernel: a batch of single tokens is read at the cache's rate only
  * if max_new says 1, so single tokens and long chunks are better two calls.
  * For fixed splits the same inputs give the same bits.  Calls sharing a workspace

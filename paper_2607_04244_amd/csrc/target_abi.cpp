@@ -88,6 +88,13 @@ int check_cache(const qlin_kv_cache *c) {
     return QLIN_OK;
 }
 
+// Whether the arrays that describe a batch share an element with a range.
+bool batch_meets(const qlin_batch *b, const Range &r) {
+    const size_t n = (size_t)b->n_seq;
+    return overlap(r, Range{(uintptr_t)b->new_start, (n + 1) * 4}) || overlap(r, Range{(uintptr_t)b->length, n * 4}) ||
+           overlap(r, Range{(uintptr_t)b->cache_start, b->cache_start ? n * 8 : 0});
+}
+
 // Row arrays of `width` elements: stride and alignment.
 int check_rows(const void *p, int64_t stride, int64_t width, const char *name) {
     if (!p) return fail(QLIN_ERR_INVALID, "NULL %s", name);
@@ -272,6 +279,13 @@ int qlin_norm_rope_append(const qlin_batch *batch, const qlin_kv_cache *cache, i
     if (overlap(ro, ck) || overlap(ro, cv)) return fail(QLIN_ERR_INVALID, "q_out overlaps the cache");
     for (const Range &r : {rq, rk, rv})
         if (overlap(r, ck) || overlap(r, cv)) return fail(QLIN_ERR_INVALID, "q, k or v overlaps the cache");
+    const Range small[] = {{(uintptr_t)q_norm, q_norm ? (size_t)kHeadDim * 2 : 0}, {(uintptr_t)k_norm, k_norm ? (size_t)kHeadDim * 2 : 0},
+                           {(uintptr_t)inv_freq, (size_t)rotary_dim / 2 * 8}};
+    for (const Range &w : {ro, ck, cv}) {
+        if (batch_meets(batch, w)) return fail(QLIN_ERR_INVALID, "q_out or the cache overlaps new_start, length or cache_start");
+        for (const Range &r : small)
+            if (overlap(w, r)) return fail(QLIN_ERR_INVALID, "q_out or the cache overlaps norm weights or inv_freq");
+    }
 
     AppendArgs a;
     a.b = batch_args(batch, cache);
@@ -331,6 +345,7 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     const Range ro = rows_range(out, M, out_stride, w);
     if (rows_meet(q, q_stride, w, out, out_stride, w, M) || overlap(ro, cache_range(cache->k, cache)) || overlap(ro, cache_range(cache->v, cache)))
         return fail(QLIN_ERR_INVALID, "out overlaps q or the cache");
+    if (batch_meets(batch, ro)) return fail(QLIN_ERR_INVALID, "out overlaps new_start, length or cache_start");
     CausalPlan p;
     if (causal_plan(batch, q_heads, cache->heads, splits, &p) != QLIN_OK) return last_status();
     if (p.ws_bytes > 0 && (!workspace || workspace_bytes < p.ws_bytes))
@@ -339,6 +354,7 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     const Range ws{(uintptr_t)workspace, (size_t)p.ws_bytes};
     for (const Range &r : {ro, rows_range(q, M, q_stride, w), cache_range(cache->k, cache), cache_range(cache->v, cache)})
         if (overlap(r, ws)) return fail(QLIN_ERR_INVALID, "the workspace overlaps q, out or the cache");
+    if (batch_meets(batch, ws)) return fail(QLIN_ERR_INVALID, "the workspace overlaps new_start, length or cache_start");
     if (batch->max_new == 0) return QLIN_OK;
 
     CausalArgs a;
