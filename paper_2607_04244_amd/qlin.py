@@ -385,12 +385,10 @@ _torch = None
 def _device():
     """The current device's index (and torch loaded, for callers that hold CUDA tensors)."""
     global _torch, _raw_stream, _current_device
-    if _current_device is None:
+    if _torch is None:
         import torch
-        _torch, _current_device, _raw_stream = torch, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-    elif _torch is None:
-        import torch
-        _torch = torch
+        _current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        _torch = torch                                      # last: what the test above goes by, in any thread
     return _current_device()
 
 
