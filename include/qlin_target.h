@@ -135,7 +135,7 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
  *               apart (multiples of 8), 16-byte aligned; out must not share elements
  *               with q nor overlap the cache, the workspace or the batch's arrays
  *   q_heads     a multiple of cache->heads, at most 64 times it, at most 4096
- *   scale       > 0 and finite, or 0 for 1 / sqrt(128)
+ *   scale       > 0, scale log2(e) a finite float, or 0 for 1 / sqrt(128)
  *   workspace   DEVICE scratch of the bytes qlin_causal_plan reports for the same
  *               arguments (NULL when 0), 16-byte aligned, no initialisation, apart from
  *               q, out, the cache and the batch's arrays

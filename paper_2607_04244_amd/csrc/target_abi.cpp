@@ -335,7 +335,9 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     if (check_heads(q_heads, cache->heads, head_dim) != QLIN_OK) return last_status();
     if (check_cache(cache) != QLIN_OK) return last_status();
     if (splits < 0 || splits > kMaxSplits) return fail(QLIN_ERR_INVALID, "splits must be in [0, 256]");
-    if (!(scale >= 0.0f) || std::isinf(scale)) return fail(QLIN_ERR_INVALID, "scale must be positive and finite (or 0)");
+    // scores to base-2 exponents
+    const float factor = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)kHeadDim)));
+    if (!(scale >= 0.0f) || std::isinf(factor)) return fail(QLIN_ERR_INVALID, "scale must be positive (or 0), scale log2(e) a finite float");
     if (workspace_bytes < 0) return fail(QLIN_ERR_INVALID, "workspace_bytes must be >= 0");
     if (batch->rows == 0) return QLIN_OK;
     if (check_batch_arrays(batch) != QLIN_OK) return last_status();
@@ -378,7 +380,7 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     a.max_len = (int)batch->max_len;
     gn_reciprocal(a.Hkv, &a.inv_heads, &a.heads_shift);
     a.inv_g = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
-    a.c = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)kHeadDim)));
+    a.c = factor;
     const hipError_t e = launch_causal(a, p.rt, p.halves, (hipStream_t)stream);
     return e == hipSuccess ? QLIN_OK : hip_fail(e, "causal attention launch");
 }
