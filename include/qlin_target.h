@@ -127,7 +127,8 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
  *   s_j = scale * q[m][h] . k[g][j],  j <= p       (fp32)
  *   out[m][h] = RNE_bf16( sum_j softmax_j(s) v[g][j] )
  * A token that sees no key (p < 0, or a sequence without cached tokens) gives
- * zeros.  Keys and values behind p, infinities and NaN among them, have no
+ * zeros; one whose visible scores are all -infinity gives NaN (its softmax is 0 / 0),
+ * as does one with a score of +infinity or NaN.  Keys and values behind p, infinities and NaN among them, have no
  * influence.  Softmax statistics and sums are fp32; each weight is rounded to bf16
  * once (the matrix cores' operand) and the sum adds the rounded weights.
  *

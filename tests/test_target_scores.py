@@ -70,3 +70,26 @@ def test_rows_beside_one_of_large_scores_keep_their_bits(form):
     keep[ends] = False
     assert torch.equal(first[keep.cuda()].view(torch.int16), second[keep.cuda()].view(torch.int16))
     assert torch.isfinite(second).all()
+
+
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_scores_of_minus_infinity_alone_give_nan(form):
+    """A row whose visible scores are all -infinity has no softmax (0 / 0): NaN; one finite score
+    among them has all the weight; a row without visible keys gives zeros."""
+    new, length, splits, max_len = FORMS[form]
+    c = Cache("heads", length, 2, 5)
+    c.host[0].zero_()
+    c.host[0][..., 7] = float("-inf")
+    c.host[0][:, 1, 1, 7] = 0.0                        # head 1: token 1 has score 0
+    c.dev[0].copy_(c.host[0])
+    q = torch.zeros((sum(new), 8, HEAD), dtype=torch.bfloat16)
+    q[..., 7] = 1.0
+    out = qlin.causal_attention(q.cuda(), *c.dev, i32(starts(new)), max_new=max(new), max_len=max_len, splits=splits, **c.kwargs())
+    torch.cuda.synchronize()
+    got = f64(out)
+    for m, (b, p) in enumerate(ref.positions(new, length)):
+        assert np.all(np.isnan(got[m, :4])) if p >= 0 else np.all(got[m] == 0)
+        if p >= 1:
+            assert np.array_equal(got[m, 4:], np.broadcast_to(f64(c.host[1][b, 1, 1]), (4, HEAD)))
+        elif p == 0:
+            assert np.all(np.isnan(got[m, 4:]))
