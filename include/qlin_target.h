@@ -78,7 +78,8 @@ typedef struct qlin_kv_cache {
  *   q_out[m][h] = rotate(p, norm(q[m][h], q_norm))     h < q_heads
  *   k cache slot of p, head h = rotate(p, norm(k[m][h], k_norm))
  *   v cache slot of p, head h = v[m][h]
- *   norm(x, w)[d] = x[d] / sqrt(mean(x^2) + eps) * w[d], or x where w is NULL
+ *   norm(x, w)[d] = x[d] / sqrt(mean(x^2) + eps) * w[d], or x where w is NULL; the
+ *     squares' sum is fp32: a row of values above 2^60 comes out as zeros
  *   rotate(p, x): with angle a_i = p * inv_freq[i], i < rotary_dim / 2, the pairs
  *     (x[i], x[i + rotary_dim / 2]), or (x[2 i], x[2 i + 1]) if interleaved, become
  *     (x cos a - y sin a, x sin a + y cos a); dimensions >= rotary_dim stay.
