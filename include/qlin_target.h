@@ -175,8 +175,9 @@ int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *wor
  * T = 0 (or below, or NaN) is the greedy limit: P_i is the lowest index of the
  * largest logit, Q_i all mass on x_i.  A logit of -infinity or NaN is a masked token
  * of probability 0.  A row without any token has P = 0 everywhere; next is then -1.
- * A drafted token outside [0, vocab) has probability 0.  Weights and sums are
- * 64-bit, in a fixed order: the same inputs give the same tokens.
+ * A drafted token outside [0, vocab) has probability 0.  Each weight e^(x / T) has a
+ * relative error of at most 7e-11, sums are 64-bit, in a fixed order: the same
+ * inputs give the same tokens.
  *
  *   target      DEVICE bf16 [n_seq][n_draft + 1][vocab], rows target_stride
  *               elements apart, 16-byte aligned

@@ -14,17 +14,21 @@
 //       the waves' sums are merged.  64 tokens of 32 / 8 heads over 4096 keys each: 174 to
 //       180 us, 6.0 to 6.2 TB/s; one token over 8192 keys 7.1 us and 2.9 for the join.
 //   k_causal_mid<NR>   up to 32 NR rows (draft blocks): the cache's bytes, then the products.
-//       16 tokens over 8192 keys: 12.4 us, of which the keys take 5.4 at that rate.
+//       16 tokens over 8192 keys: 12.2 to 12.5 us in a trace of kernels (10.8 by its own clock, from
+//       its first instruction to its last store), of which the keys take 5.4 at that rate; 3.9
+//       for the join, and 14.0 to 15.1 the call in a graph.
 //   k_causal_prompt<H> 128 rows, 32 a wave, 32 keys a step for four waves: bound by the matrix
-//       cores and the softmax between them.  8192 tokens: 511 to 545 us on different boxes,
-//       1010 to 1075 TFLOP/s, where the library's large bf16 product reaches 1194.
+//       cores and the softmax between them.  8192 tokens: 509 to 550 us on different cards,
+//       1000 to 1080 TFLOP/s, where the library's large bf16 product reaches 1194.
 //   k_causal_join      joins key ranges, in order: bound by the partial results' bytes.
 // The kernel goes by the rows of the longest sequence (max_new G): a larger tile leaves more of
 // the matrix cores' work unused, a smaller one reads the keys again for each tile.  Through few /
 // mid<1> / mid<2> / prompt, 32 / 8 heads, us with the join: one sequence of 8192 keys, 1 new token
-// 10.4 / 12.7 / 13.3 / 14.2, 4 tokens 11.5 / 12.2 / 12.6 / 14.0, 8 - / 13.1 / 13.3 / 14.6, 16
-// - / - / 15.1 / 16.1; 32 sequences of 4096, 1 token 83 / 84 / 81 / 95, 8 - / 87 / 83 / 96, 16
-// - / - / 89 / 98.
+// 10.4 / 12.8 / 13.2 / 14.2, 4 tokens 11.6 / 12.3 / 12.7 / 14.0, 8 - / 13.1 / 13.3 / 14.6, 16
+// - / - / 15.1 / 16.0; 32 sequences of 4096, 1 token 84 / 84 / 81 / 95, 8 - / 87 / 83 / 97, 16
+// - / - / 90 / 98.  Between mid<1> and mid<2> the rows alone do not decide: at 8 tokens mid<1> is
+// ahead where a workgroup walks up to 256 keys (1000 keys 9.0 / 9.7, 8 sequences of 1000 12.0 /
+// 12.7) and behind where it walks more (2 of 8192 18.6 / 17.5, 8 of 4096 29.6 / 27.1).
 //
 // Softmax statistics are fp32.  Weights are rounded to bf16 once (the operand) and the
 // sum adds the rounded weights.
@@ -146,7 +150,7 @@ __device__ inline bool find_tile(const CausalArgs &a, int idx, int R, int lane, 
     return false;
 }
 
-// A row tile's part of the work, the same in both kernels.
+// A row tile's part of the work, the same in every kernel.
 struct Work {
     Seq s;
     int h, split;
@@ -470,8 +474,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void k_causal_few(CausalArgs a) 
 
 // 32 NR rows, NR = 1, 2: four waves for each 32 rows, a quarter of a step's 128 keys each, so
 // that a key range of 256 keys (a 16-token block over 8192 keys on all compute units) is two
-// steps, requested at once.  With four 16-row tiles in each of four waves the same kernel took
-// 15.0 us (12.4 here): its products waited for one another, with one wave a SIMD.
+// steps, requested at once.  With four 16-row tiles in each of four waves the kernel took 15.0 us
+// in a trace (12.4 so): its products waited for one another, with one wave a SIMD.
 constexpr int kMidKeys = 128, kMidUnits = kMidKeys * kHeadDim / 8;
 
 template <int NR>

@@ -11,22 +11,23 @@
 //       uniform number in.  Without draft logits the chunks' sums follow from the statistics,
 //       and the accepted prefix is found here.
 //
-// Weights and sums are 64-bit: a running sum over a vocabulary of 10^5 has a boundary every
-// 10^-5 of it or closer, and 32-bit weights (off by up to 6e-8 each) would put a few of a
-// thousand choices on the wrong side of one.  At an error of 5e-11 it is one of 10^5.
+// Weights are 64-bit numbers with a relative error of 4.7e-11 (Pow2 below: about 34 bits), their sums
+// 64-bit: a running sum over a vocabulary of 10^5 has a boundary every 10^-5 of it or closer, and
+// 32-bit weights (off by up to 6e-8 each) would put a few of a thousand choices on the wrong
+// side of one.  At 4.7e-11 it is one of 10^5.
 // 64-bit products run at the rate of 32-bit ones here, and 32-bit exponentials at a half of
 // it, so the accuracy costs about twice the time of 32-bit weights.  A table of 2^(j/32) or
 // 2^(j/64) in LDS or lanes with a polynomial of degree 3 took 32 sequences from 84 to 81 us and
 // one from 14.3 to 14.9; not taken.
 //
-// 16 tokens over 151936: 12.4 us, of which the statistics 5.5 (one trip to memory, 38 chunks a
-// row over all compute units) and the token 6.8, a workgroup's dependent steps: decision 3.2,
-// chunk 1.2, its logits 1, token 1.  Handing the decision what it reads again later, or the
-// drafted tokens' logits with the statistics, took trips away but no time: it is the latency of
-// the instructions.  32 sequences of 16 with draft logits: 85 to 99 us on different boxes and
-// orders of memory (statistics 38 + 20, decision 4.7, sums 16, token 6.4), where the 5 TB/s of a
-// copy would read all the logits in 63; the statistics are bound by their 64-bit instructions,
-// 14 a logit.
+// 16 tokens over 151936: 11.2 to 11.6 us in a graph, of which the statistics 5.4 (one trip to memory,
+// 38 chunks a row over all compute units) and the token 6.6, a workgroup's dependent steps: decision
+// 3.2, chunk 1.2, its logits 1, token 1.  Handing the decision what it reads again later, or the
+// drafted tokens' logits with the statistics, took trips to memory away but no time: it is the
+// latency of the instructions.  32 sequences of 16 with draft logits: 80 to 103 us on different cards
+// and orders of memory (statistics 38 + 20, decision 4.6, sums 16, token 6.3), where the 5 TB/s of
+// a copy would read all the logits in 63; the statistics are bound by their 64-bit
+// instructions, 14 a logit.
 #include "device_common.h"
 #include "target_internal.h"
 
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
 }  // namespace
 
 // Few logits go to many small workgroups, many to larger ones, by the call's logits (small / large
-// form, graph replays): 2.4 million 12.3 / 13.4 us, with draft logits 3.9 million 18.2 / 20.5, 9.4
+// form, graph replays of the build that chose it): 2.4 million 12.3 / 13.4 us, with draft logits 3.9 million 18.2 / 20.5, 9.4
 // 24.1 / 26.0, 26.7 37.5 / 40.2, 37.7 48.0 / 45.8, 65.9 70.3 / 65.1.  Chunks of 8192 and 2048 tokens
 // took 14.0 and 13.6 us for the first, 22.2 and 17.6 for the second.
 hipError_t launch_verify(VerifyArgs a, int n_seq, bool many, hipStream_t st) {
