@@ -307,8 +307,9 @@ __device__ inline double probability(float x, const VerifyStat &st, double k) {
 // P and Q closer than this, relative to P, are equal: the weights of equal logits are equal, so P and
 // Q of equal rows differ by the rounding of two sums of up to 90 steps one after the other (9 in a
 // thread, 9 over a workgroup, 65 chunks in a lane, 6 over the lanes) and of two quotients, below
-// 190 2^-53.  Without it the next token would be drawn from that rounding.
-constexpr double kSame = 0x1p-44;
+// 190 2^-53.  Without it the next token would be drawn from that rounding.  Subnormal probabilities
+// are rounded more coarsely; differences of that size count as none too.
+constexpr double kSame = 0x1p-44, kNone = 0x1p-960;
 
 // A chunk whose largest weight is below this, relative to the row's, holds no token to draw.  So a
 // chunk with any mass has a token whose probability is a number: without a refused token its
@@ -350,7 +351,7 @@ struct Choice {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const double d = __builtin_fma(-we[e], inv_q, w[e]);
-                w[e] = d > kSame * w[e] ? d : 0.0;
+                w[e] = d > __builtin_fma(kSame, w[e], kNone) ? d : 0.0;
             }
         } else {
 #pragma unroll

@@ -147,3 +147,19 @@ def test_every_token_is_one_of_the_vocabulary(seed):
         assert 0 <= acc[b] <= drafts
         nxt = tok[b][acc[b]]
         assert 0 <= nxt < V and float(target[b, acc[b], nxt]) > float("-inf"), (b, acc[b], nxt)
+
+
+@pytest.mark.parametrize("low", [-709.0, -716.0, -720.0, -732.0, -740.0])
+def test_equal_rows_with_tokens_of_vanishing_weight(low):
+    """Probabilities that are subnormal numbers differ by their rounding too: no part of the rest."""
+    V, n = 700, 6
+    target = rand(5, (n, 2, V), 1.0)
+    target[:, :, 3:400] = (low + 8 * torch.rand((n, 2, 397), generator=torch.Generator().manual_seed(6))).to(torch.bfloat16)
+    draft = target[:, :1].clone()
+    for u in (0.0, 0.3, 0.9):
+        acc, tok = decide(target, draft, [[-1]] * n, [[0.5, u]] * n, T=[1.0, 0.9, 1.1, 1.0, 0.95, 1.05])
+        for b in range(n):
+            assert acc[b] == 0 and 0 <= tok[b][0] < V
+            assert u == 0.0 or not 3 <= tok[b][0] < 400                  # from P, where those have no weight to speak of
+        if u > 0.0:
+            check_verify(target, draft, [[-1]] * n, [[0.5, u]] * n, T=[1.0, 0.9, 1.1, 1.0, 0.95, 1.05])
