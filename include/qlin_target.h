@@ -97,7 +97,8 @@ typedef struct qlin_kv_cache {
  *               apart; q itself (same stride), or elements apart from every input
  *               and the cache
  * All pointers 16-byte aligned (norm weights and inv_freq: 8).  k and v must not
- * overlap the cache, and the batch's arrays neither q_out nor the cache.  Two new tokens must not share a slot (sequences sharing
+ * overlap the cache, and neither the batch's arrays nor the weights and inv_freq may
+ * overlap q_out or the cache.  Two new tokens must not share a slot (sequences sharing
  * slots: which of them is stored is not defined).
  * Errors: INVALID (NULL, sizes, strides, overlap, eps), UNSUPPORTED (head_dim !=
  * 128, limits), ALIGN, HIP.
@@ -129,9 +130,10 @@ int qlin_causal_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads,
  *   out[m][h] = RNE_bf16( sum_j softmax_j(s) v[g][j] )
  * A token that sees no key (p < 0, or a sequence without cached tokens) gives
  * zeros; one whose visible scores are all -infinity gives NaN (its softmax is 0 / 0),
- * as does one with a score of +infinity or NaN.  Keys and values behind p, infinities and NaN among them, have no
- * influence.  Softmax statistics and sums are fp32; each weight is rounded to bf16
- * once (the matrix cores' operand) and the sum adds the rounded weights.
+ * as does one with a score of +infinity or NaN.  Keys and values behind p, infinities
+ * and NaN among them, have no influence.  Scores, softmax statistics and sums are
+ * fp32; each weight is rounded to bf16 once (the matrix cores' operand) and the sum
+ * adds the rounded weights.
  *
  *   q, out      DEVICE bf16 rows of q_heads x 128, q_stride / out_stride elements
  *               apart (multiples of 8), 16-byte aligned; out must not share elements

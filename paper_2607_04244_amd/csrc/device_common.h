@@ -310,9 +310,9 @@ __device__ inline void valu_dequant(uint32_t P, const ValuDeq &d, const ExtractC
 // load before each later LDS read.  The caller waits for it explicitly
 // (s_waitcnt vmcnt) before the barrier that publishes the data; loads the
 // compiler does track and issues later are younger, so its own waits stay
-// sufficient.  A load to LDS needs one wait state after a scalar write of m0, which nobody
-// adds inside inline assembly: s_nop 0.  These statements set m0 themselves and list it as clobbered;
-// the compiler warns that it may not preserve a reserved register across
+// sufficient.  A load to LDS needs one wait state after a scalar write of m0, which the
+// compiler does not add inside inline assembly: s_nop 0.  These statements set m0
+// themselves and list it as clobbered; the compiler warns that it may not preserve a reserved register across
 // them, which matters only if it kept a value of its own in m0: the
 // generated code of every kernel here has no other m0 access.
 __device__ inline void load_lds_x16(const void *src, const uint4 *lds_dst) {

@@ -581,7 +581,7 @@ __global__ __launch_bounds__(kPickThreads) void k_verify_pick(VerifyArgs a) {
 }  // namespace
 
 // Few logits go to many small workgroups, many to larger ones, by the call's logits (small / large
-// form, graph replays of the build that chose it): 2.4 million 12.3 / 13.4 us, with draft logits 3.9 million 18.2 / 20.5, 9.4
+// form, graph replays when the rule was chosen): 2.4 million 12.3 / 13.4 us, with draft logits 3.9 million 18.2 / 20.5, 9.4
 // 24.1 / 26.0, 26.7 37.5 / 40.2, 37.7 48.0 / 45.8, 65.9 70.3 / 65.1.  Chunks of 8192 and 2048 tokens
 // took 14.0 and 13.6 us for the first, 22.2 and 17.6 for the second.
 hipError_t launch_verify(VerifyArgs a, int n_seq, bool many, hipStream_t st) {
