@@ -1,5 +1,6 @@
 // Norms and rotation of queries and keys with the append to the key/value cache
-// (qlin_norm_rope_append in include/qlin_target.h).
+// (qlin_norm_rope_append in include/qlin_target.h; qlin_norm_rope_append_four_bit in
+// include/qlin_lowbit.h, whose rows of keys and values are laid on 4-bit grids).
 //
 // Bound by memory: every head row of 256 bytes is read and written once.  A group of
 // 16 lanes holds one head row, 16 bytes a lane; a workgroup takes R tokens and as
@@ -12,6 +13,7 @@
 // (in the last-level cache 5.7 / 7.6, 7.8 / 7.8, 16.6 / 11.1).  Two and eight tokens: 54.8
 // and 51.2 us against 49.8 of four (8192 tokens, without the hint below).
 #include "target_common.h"
+#include "lowbit_internal.h"
 
 #include <type_traits>
 
@@ -23,17 +25,35 @@ constexpr int kGroupLanes = 16;          // lanes of a head row
 constexpr int kAppendThreads = 1024;
 constexpr int kManyRows = 640;           // R = 4 from here on
 
-// Sum over the 16 lanes of a DPP row, in every lane.
-__device__ inline float row_sum(float v) {
-    auto ror = [](float x, auto n) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + decltype(n)::value, 0xF, 0xF, false));
-    };
-    v += ror(v, std::integral_constant<int, 8>{});
-    v += ror(v, std::integral_constant<int, 4>{});
-    v += ror(v, std::integral_constant<int, 2>{});
-    v += ror(v, std::integral_constant<int, 1>{});
+// v of the lane N to the right within 16 lanes (a DPP row), around its end.
+template <int N>
+__device__ inline float rotated(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xF, 0xF, false));
+}
+template <int N>
+__device__ inline double rotated(double v) {
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), 0x120 + N, 0xF, 0xF, false),
+                            __builtin_amdgcn_update_dpp(0, __double2loint(v), 0x120 + N, 0xF, 0xF, false));
+}
+// f over the 16 lanes, in every lane.
+template <typename T, typename F>
+__device__ inline T row_reduce(T v, F f) {
+    v = f(v, rotated<8>(v));
+    v = f(v, rotated<4>(v));
+    v = f(v, rotated<2>(v));
+    v = f(v, rotated<1>(v));
     return v;
 }
+template <typename T>
+__device__ inline T row_sum(T v) {
+    return row_reduce(v, [](T x, T y) { return x + y; });
+}
+
+// Written out, so that a build's choice of what to fuse cannot change an output's last bit.
+__device__ inline float fused(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ inline double fused(double a, double b, double c) { return __builtin_fma(a, b, c); }
+__device__ inline float inverse_root(float x) { return 1.0f / sqrtf(x); }
+__device__ inline double inverse_root(double x) { return 1.0 / sqrt(x); }
 
 // Many tokens stream through: with the non-temporal hint both ways 8192 tokens from and to
 // memory that no cache holds take 43.0 us against 49.8, 1500 tokens 12.3 against 14.7 (with
@@ -50,11 +70,110 @@ __device__ inline void store_row(uint16_t *p, const uint4 &y) {
     else *(uint4 *)p = y;
 }
 
-template <int R>
-__global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(AppendArgs a) {
+// Eight dimensions (8 l .. 8 l + 7) of a head row: norm with the weights w (none: null), and the
+// rotation by the token's angles cs = (cos, sin).
+template <typename T, typename T2>
+__device__ inline void norm_rotate(const AppendArgs &a, const uint4 &x, const uint16_t *w, const uint2 &w0, const uint2 &w1, const T2 *cs,
+                                   int lane, T o[8]) {
+    const int l = lane & 15;
+    T f[8];
+    const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, ww[4] = {w0.x, w0.y, w1.x, w1.y};
+    T ss = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = bf16_lo_to_f32(xw[i]);
+        f[2 * i + 1] = bf16_hi_to_f32(xw[i]);
+        ss += f[2 * i] * f[2 * i] + f[2 * i + 1] * f[2 * i + 1];
+    }
+    if (w) {
+        const T inv = inverse_root(row_sum(ss) * (T)(1.0f / kHeadDim) + (T)a.eps);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = f[2 * i] * inv * (T)bf16_lo_to_f32(ww[i]);
+            f[2 * i + 1] = f[2 * i + 1] * inv * (T)bf16_hi_to_f32(ww[i]);
+        }
+    }
+    if (a.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool in = 4 * l + i < a.half;
+            const T2 t = cs[in ? 4 * l + i : 0];
+            o[2 * i] = in ? fused(f[2 * i], t.x, -(f[2 * i + 1] * t.y)) : f[2 * i];
+            o[2 * i + 1] = in ? fused(f[2 * i], t.y, f[2 * i + 1] * t.x) : f[2 * i + 1];
+        }
+    } else {
+        // the partner of a dimension is half / 8 lanes away
+        const int hl = a.half >> 3;
+        const bool lo = l < hl, in = l < 2 * hl;
+        const int from = (lane & 48) | (in ? lo ? l + hl : l - hl : l);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const T other = __shfl(f[i], from);
+            const T2 t = cs[in ? (lo ? 8 * l : 8 * (l - hl)) + i : 0];
+            o[i] = in ? fused(f[i], t.x, lo ? -(other * t.y) : other * t.y) : f[i];
+        }
+    }
+}
+
+__device__ inline uint4 pack8(const float o[8]) {
+    return make_uint4(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]), cvt_pk_bf16(o[4], o[5]), cvt_pk_bf16(o[6], o[7]));
+}
+
+// A row of bf16 values on its 4-bit grid: this lane's word of codes, and the row's (step, offset).
+// Divisions are correctly rounded, so a code is that of the exact quotient, ties included: the
+// quotient by the step from the step's reciprocal and one remainder (Markstein).
+__device__ inline uint32_t lay_on_grid(const uint4 &y, uint32_t &grid) {
+    const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+    float f[8];
+    uint32_t top = 0;                        // bits of the largest |x|: infinities and NaN are past all numbers
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = bf16_lo_to_f32(w[i]);
+        f[2 * i + 1] = bf16_hi_to_f32(w[i]);
+        top = max(top, max(w[i] << 16 & 0x7FFFFFFFu, w[i] & 0x7FFF0000u));
+    }
+    float low = f[0], high = f[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        low = fminf(low, f[i]);
+        high = fmaxf(high, f[i]);
+    }
+    low = row_reduce(low, [](float x, float y) { return fminf(x, y); });
+    high = row_reduce(high, [](float x, float y) { return fmaxf(x, y); });
+    const float most = row_reduce(__uint_as_float(top), [](float x, float y) { return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y))); });
+    const float range = high - low;
+    if (!(__float_as_uint(most) < 0x7F800000u) || __float_as_uint(range) >= 0x7F800000u) {
+        grid = 0x7FC07FC0u;
+        return 0;
+    }
+    const uint16_t sb = cvt_bf16(range / 15.0f);
+    const float step = __uint_as_float((uint32_t)sb << 16);
+    grid = __float_as_uint(low);             // bf16 in the high half: the offset
+    if (sb < 0x0080) return 0;               // below 2^-126
+    grid |= sb;
+    const float inv = 1.0f / step;
+    uint32_t codes = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = f[i] - low, q = x * inv;
+        const float c = rintf(__builtin_fmaf(__builtin_fmaf(-q, step, x), inv, q));
+        codes |= (uint32_t)fminf(c, 15.0f) << 4 * i;
+    }
+    return codes;
+}
+
+// KV4: the keys in 64 bits, so that their codes are those of the definition and not those of
+// its rounding errors; rows of keys and values as codes and grids.
+template <int R, bool KV4>
+__global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(std::conditional_t<KV4, AppendKv4Args, AppendArgs> args) {
     __shared__ float2 cs[R][kHeadDim / 2];   // (cos, sin) of each token's angles
+    __shared__ double2 cs64[KV4 ? R : 1][KV4 ? kHeadDim / 2 : 1];
     __shared__ int64_t slot[R];              // cache slot of each token, -1: not stored
     __shared__ int live[R];                  // a new token of some sequence
+    const AppendArgs &a = [&]() -> const AppendArgs & {
+        if constexpr (KV4) return args.a;
+        else return args;
+    }();
     const int lane = threadIdx.x & 63, l = threadIdx.x & 15;
     const int groups = blockDim.x / kGroupLanes, grp = threadIdx.x / kGroupLanes;
     const int m0 = blockIdx.x * R;
@@ -77,9 +196,16 @@ __global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(AppendArgs 
         }
         if (lane < a.half) {
             const double t = (double)p * (a.inv_freq[lane] * 0.15915494309189535);   // turns
-            float sn, cn;
-            sincospif(2.0f * (float)(t - rint(t)), &sn, &cn);
-            cs[r][lane] = make_float2(cn, sn);
+            if constexpr (KV4) {
+                double sn, cn;
+                sincospi(2.0 * (t - rint(t)), &sn, &cn);
+                cs64[r][lane] = make_double2(cn, sn);
+                cs[r][lane] = make_float2((float)cn, (float)sn);
+            } else {
+                float sn, cn;
+                sincospif(2.0f * (float)(t - rint(t)), &sn, &cn);
+                cs[r][lane] = make_float2(cn, sn);
+            }
         }
     }
     __syncthreads();
@@ -104,63 +230,61 @@ __global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(AppendArgs 
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            uint16_t *dst = is_q ? a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim
-                                 : (is_k ? a.kc : a.vc) + slot[r] * a.b.tok + hh * a.b.head;
             uint4 y = x[r];
-            if (is_q || is_k) {
-                float f[8];
-                const uint32_t xw[4] = {x[r].x, x[r].y, x[r].z, x[r].w}, ww[4] = {w0.x, w0.y, w1.x, w1.y};
-                float ss = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    f[2 * i] = bf16_lo_to_f32(xw[i]);
-                    f[2 * i + 1] = bf16_hi_to_f32(xw[i]);
-                    ss += f[2 * i] * f[2 * i] + f[2 * i + 1] * f[2 * i + 1];
-                }
-                if (w) {
-                    const float inv = 1.0f / sqrtf(row_sum(ss) * (1.0f / kHeadDim) + a.eps);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        f[2 * i] = f[2 * i] * inv * bf16_lo_to_f32(ww[i]);
-                        f[2 * i + 1] = f[2 * i + 1] * inv * bf16_hi_to_f32(ww[i]);
-                    }
-                }
+            if (is_q || (is_k && !KV4)) {
                 float o[8];
-                if (a.interleaved) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const bool in = 4 * l + i < a.half;
-                        const float2 t = cs[r][in ? 4 * l + i : 0];
-                        o[2 * i] = in ? f[2 * i] * t.x - f[2 * i + 1] * t.y : f[2 * i];
-                        o[2 * i + 1] = in ? f[2 * i] * t.y + f[2 * i + 1] * t.x : f[2 * i + 1];
-                    }
-                } else {
-                    // the partner of a dimension is half / 8 lanes away
-                    const int hl = a.half >> 3;
-                    const bool lo = l < hl, in = l < 2 * hl;
-                    const int from = (lane & 48) | (in ? lo ? l + hl : l - hl : l);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float other = __shfl(f[i], from);
-                        const float2 t = cs[r][in ? (lo ? 8 * l : 8 * (l - hl)) + i : 0];
-                        o[i] = !in ? f[i] : lo ? f[i] * t.x - other * t.y : other * t.y + f[i] * t.x;
-                    }
-                }
-                y = make_uint4(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]), cvt_pk_bf16(o[4], o[5]), cvt_pk_bf16(o[6], o[7]));
+                norm_rotate(a, x[r], w, w0, w1, cs[r], lane, o);
+                y = pack8(o);
             }
-            if (is_q ? live[r] : slot[r] >= 0) store_row<R>(dst + 8 * l, y);
+            if constexpr (KV4) {
+                if (is_q) {
+                    if (live[r]) store_row<R>(a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim + 8 * l, y);
+                    continue;
+                }
+                if (is_k) {
+                    double o[8];
+                    float f[8];
+                    norm_rotate(a, x[r], w, w0, w1, cs64[r], lane, o);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] = (float)o[i];
+                    y = pack8(f);
+                }
+                uint32_t grid;
+                const uint32_t codes = lay_on_grid(y, grid);
+                if (slot[r] < 0) continue;
+                const int64_t row = slot[r] * a.b.tok + hh * a.b.head;
+                (is_k ? args.c.k : args.c.v)[16 * row + l] = codes;
+                if (l == 0) (is_k ? args.c.k_grid : args.c.v_grid)[row] = grid;
+            } else {
+                uint16_t *dst = is_q ? a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim
+                                     : (is_k ? a.kc : a.vc) + slot[r] * a.b.tok + hh * a.b.head;
+                if (is_q ? live[r] : slot[r] >= 0) store_row<R>(dst + 8 * l, y);
+            }
         }
     }
+}
+
+// Heads of a token, in threads.
+int append_threads(const AppendArgs &a) {
+    const int heads = a.Hq + 2 * a.Hkv;
+    return heads * kGroupLanes > kAppendThreads ? kAppendThreads : (heads * kGroupLanes + 63) / 64 * 64;
 }
 
 }  // namespace
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st) {
-    const int heads = a.Hq + 2 * a.Hkv;
-    const int threads = heads * kGroupLanes > kAppendThreads ? kAppendThreads : (heads * kGroupLanes + 63) / 64 * 64;
     if (a.b.rows == 0) return hipSuccess;
-    if (a.b.rows < kManyRows) hipLaunchKernelGGL(k_norm_rope_append<1>, dim3(a.b.rows), dim3(threads), 0, st, a);
-    else hipLaunchKernelGGL(k_norm_rope_append<4>, dim3((a.b.rows + 3) / 4), dim3(threads), 0, st, a);
+    const dim3 threads(append_threads(a));
+    if (a.b.rows < kManyRows) hipLaunchKernelGGL((k_norm_rope_append<1, false>), dim3(a.b.rows), threads, 0, st, a);
+    else hipLaunchKernelGGL((k_norm_rope_append<4, false>), dim3((a.b.rows + 3) / 4), threads, 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_append_kv4(const AppendKv4Args &args, hipStream_t st) {
+    if (args.a.b.rows == 0) return hipSuccess;
+    const dim3 threads(append_threads(args.a));
+    if (args.a.b.rows < kManyRows) hipLaunchKernelGGL((k_norm_rope_append<1, true>), dim3(args.a.b.rows), threads, 0, st, args);
+    else hipLaunchKernelGGL((k_norm_rope_append<4, true>), dim3((args.a.b.rows + 3) / 4), threads, 0, st, args);
     return hipGetLastError();
 }
 

@@ -37,7 +37,7 @@
 // NaN among them survives.  A pass whose sums come out not finite is therefore repeated
 // with every row's own keys only (`careful`): the values of later keys as zeros, one token
 // of the tile at a time.  The usual pass pays a test of its sums at the end.
-#include "target_common.h"
+#include "causal_common.h"
 
 #include <type_traits>
 
@@ -45,30 +45,8 @@ namespace qlin {
 
 namespace {
 
-typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s_t lds_v4s;
-
-constexpr float kNegInf = -__builtin_huge_valf();
-constexpr uint32_t kBf16OnePair = 0x3F803F80u;       // bf16 (1.0, 1.0)
-
-// Both lanes of the pair {l, l ^ 16} (l ^ 32) get the same result.
-__device__ inline float pair16_max(float v) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ inline float pair32_max(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ inline float pair16_sum(float v) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ inline float pair32_sum(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 
 // Transposing LDS read: within 16 lanes, lane i receives element i & 3 of the 8-byte
 // chunks that lanes 4 j + (i >> 2), j = 0 .. 3, address.
@@ -84,157 +62,23 @@ __device__ inline int key_unit(int kk, int c) { return kk * 16 + (c ^ (kk & 15))
 __device__ inline int few_value_unit(int kk, int c) { return kk * 16 + (c ^ (2 * (kk & 7))); }
 __device__ inline int value_unit(int kk, int c) { return kk * 16 + (c ^ (4 * (kk & 3))); }
 
-// As load_lds_x16 (device_common.h) from a scalar address plus a 32-bit offset in bytes, to an
-// LDS byte address.
-__device__ inline void load_lds_s16(const uint16_t *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
-}
-__device__ inline void load_lds_v16(const uint16_t *src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds), "v"(src) : "memory", "m0");
-}
-__device__ inline void load_lds_s16_nt(const uint16_t *base, uint32_t off, uint32_t lds) {      // for data a call reads once
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
-}
-
-__device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// The row tile (of R packed rows) that work item idx is, among all sequences' tiles: its
-// sequence and its number in it; false past the last.  The tiles that see the most keys come
-// first, in kClasses classes of equal steps of keys up to max_len (a tile with the longest
-// walk that starts late ends late: packed prompts of 1 to 2048 tokens 125 us in the order of
-// the rows, 113 in this one).  By the whole wave: a class's tiles of 64 sequences at a time are
-// summed up.
-constexpr int kClasses = 8;
-
-// Inclusive sum over the lanes by DPP: within rows of 16, then across them.
-__device__ inline int lanes_upto(int v) {
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // row_shr 1, 2, 4, 8
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // lane 15 to the next row: rows 1, 3
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);     // lane 31 to rows 2, 3
-    return v;
-}
-__device__ inline bool find_tile(const CausalArgs &a, int idx, int R, int lane, Seq &s, int &tile) {
-    if (a.b.n_seq == 1) {                                // no order to find out
-        s = load_seq(a.b, 0);
-        tile = (s.rows * a.G + R - 1) / R - 1 - idx;
-        return tile >= 0;
-    }
-    for (int i = 0; i < a.b.n_seq; i += 64) {
-        Seq own{};
-        int tiles = 0;
-        if (i + lane < a.b.n_seq) {                      // the sequences' data, a lane each
-            own = load_seq(a.b, i + lane);
-            tiles = (own.rows * a.G + R - 1) / R;
-        }
-        // tiles whose first token is at class c's lower bound or later, and not in class c + 1
-        int upper = tiles;
-        const float per_token = (float)a.G / (float)R, step = (float)a.max_len / kClasses;
-        for (int c = kClasses - 1; c >= 0; --c) {
-            const float at = ((float)c * step - (float)own.p0) * per_token;
-            const int lower = c == 0 ? 0 : min(max((int)fminf(at, 1e9f), 0), upper);
-            const int sum = lanes_upto(upper - lower), total = __builtin_amdgcn_readlane(sum, 63);
-            if (idx < total) {
-                const int l = __popcll(__ballot(sum <= idx));
-                // the class's last tile of the sequence first
-                tile = __builtin_amdgcn_readlane(upper, l) - 1 - (idx - __builtin_amdgcn_readlane(sum - (upper - lower), l));
-                s = lane_value(own, l);
-                return true;
-            }
-            idx -= total;
-            upper = lower;
-        }
-    }
-    return false;
-}
-
-// A row tile's part of the work, the same in every kernel.
-struct Work {
-    Seq s;
-    int h, split;
-    int r0, rows;               // packed rows [r0, r0 + rows) of the sequence
-    int i0, rem;                // r0 = i0 G + rem
-    int hi;                     // keys [0, hi) that some row of the tile sees
-    const uint16_t *k, *v;      // token 0 of head h
+// The two 16-bit types of a cache: bf16, or f16 as a 4-bit cache is unpacked to.
+struct InBf16 {
+    typedef v8bf v8;
+    static constexpr uint32_t kOnes = kBf16OnePair;
+    static __device__ inline v16f product(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ inline uint32_t pair(float lo, float hi) { return cvt_pk_bf16(lo, hi); }
+    static __device__ inline float add(uint32_t p, float s) { return dot2(p, kOnes, s); }
 };
-
-// x / G for the x < 64 + 128 that a tile's rows reach (exact for x G < 2^32)
-__device__ inline int token_of(const CausalArgs &a, int x) { return a.G == 1 ? x : (int)__umulhi((uint32_t)x, a.inv_g); }
-
-__device__ inline int64_t uniform(int64_t v) {
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-    return (int64_t)((uint64_t)hi << 32 | lo);
-}
-
-// Workgroup (x, y): key range y of item x = tile number * heads + head.  Workgroups go to the 8 XCDs
-// in turn, x first: with a multiple of 8 heads all work on one head is on one XCD, and its
-// keys are shared in that XCD's L2.
-template <int R>
-__device__ inline bool find_work(const CausalArgs &a, int lane, int split, Work &w) {
-    const int item = gn_chunk(blockIdx.x, a.Hkv, a.inv_heads, a.heads_shift);
-    w.h = blockIdx.x - item * a.Hkv;
-    w.split = split;
-    int tile = 0;
-    if (a.one_tile) {
-        if (item >= a.b.n_seq) return false;
-        w.s = load_seq(a.b, item);
-    } else {
-        // where all workgroups run at once, two a compute unit, a long one goes with a short one
-        const int half = (a.tiles + 1) / 2, idx = a.pairs && item >= half ? a.tiles - 1 - (item - half) : item;
-        if (!find_tile(a, idx, R, lane, w.s, tile)) return false;
+struct InF16 {
+    typedef v8h v8;
+    static constexpr uint32_t kOnes = 0x3C003C00u;
+    static __device__ inline v16f product(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ inline uint32_t pair(float lo, float hi) { return cvt_pk_f16(lo, hi); }
+    static __device__ inline float add(uint32_t p, float s) {
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, p), __builtin_bit_cast(v2h, kOnes), s, false);
     }
-    w.r0 = tile * R;
-    w.rows = min(R, w.s.rows * a.G - w.r0);
-    if (w.rows <= 0) return false;
-    w.i0 = w.r0 / a.G;
-    w.rem = w.r0 - w.i0 * a.G;
-    w.hi = w.s.L > 0 ? max(w.s.p0 + w.i0 + token_of(a, w.rem + w.rows - 1) + 1, 0) : 0;
-    // the same in every lane: scalars
-    w.s.slot0 = uniform(w.s.slot0);
-    w.s.row0 = __builtin_amdgcn_readfirstlane(w.s.row0);
-    w.s.p0 = __builtin_amdgcn_readfirstlane(w.s.p0);
-    w.s.L = __builtin_amdgcn_readfirstlane(w.s.L);
-    w.r0 = __builtin_amdgcn_readfirstlane(w.r0);
-    w.rows = __builtin_amdgcn_readfirstlane(w.rows);
-    w.hi = __builtin_amdgcn_readfirstlane(w.hi);
-    w.i0 = __builtin_amdgcn_readfirstlane(w.i0);
-    w.rem = __builtin_amdgcn_readfirstlane(w.rem);
-    const int64_t at = w.s.slot0 * a.b.tok + (int64_t)w.h * a.b.head;
-    w.k = a.k + at;
-    w.v = a.v + at;
-    return true;
-}
-
-// Packed row x of the tile: its token in the sequence and its query head.
-struct RowOf { int i, hq; };
-__device__ inline RowOf row_of(const CausalArgs &a, const Work &w, int x) {
-    const int t = token_of(a, w.rem + x);
-    return RowOf{w.i0 + t, w.h * a.G + w.rem + x - t * a.G};
-}
-__device__ inline int64_t row_at(const Work &w, const RowOf &r, int64_t stride) {
-    return (int64_t)(w.s.row0 + r.i) * stride + r.hq * kHeadDim;
-}
-// The steps [first, end) of a key range, of `all` steps in ranges of at least a.least: as few
-// ranges as hold them (used), the last ones of a.S empty.
-struct Range { int first, end, used; };
-__device__ inline Range range_of(const CausalArgs &a, int all, int split) {
-    const int per = max((all + a.S - 1) / a.S, a.least);
-    return Range{split * per, min((split + 1) * per, all), (all + per - 1) / per};
-}
-
-// Partial results: for each item and range the tile's sums as the matrix cores leave them, in
-// units of 64 lanes x 4 values (1 KiB, one store of a wave), and (maximum, sum of weights) of
-// its rows.
-template <int R>
-__device__ inline float *unit_at(const CausalArgs &a, int split, int unit) {
-    return a.ws_o + (((int64_t)blockIdx.x * a.S + split) * (R / 2) + unit) * 256;
-}
-template <int R>
-__device__ inline float2 *row_ml(const CausalArgs &a, int split, int row) {
-    return (float2 *)a.ws_ml + ((int64_t)blockIdx.x * a.S + split) * R + row;
-}
+};
 
 // The values of keys [key, key + 4) and [key2, key2 + 4), without those behind `last`.
 __device__ inline v8bf values_up_to(v4s_t lo, v4s_t hi, int key, int key2, int last) {
@@ -259,12 +103,6 @@ __device__ inline bool all_finite(const V (&o)[N]) {
     return (z[0] + z[1]) + (z[2] + z[3]) == 0.0f;
 }
 
-// A row's sums are rescaled only when its maximum has grown by more than a factor 2^kLazy of
-// the weights: up to there the weights just exceed 1, with the same relative rounding.  Each row
-// goes by its own maximum, and a careful pass by the same steps, so that not a bit of a row
-// depends on what lies behind its token.
-constexpr float kLazy = 8.0f;
-
 // The weights' exponents s c - m c are fused products less a rounded m c: its rounding is in all of a
 // row's weights alike and cancels, while |m c| is at most kFar and it is at most 1.  Above, where it
 // could take all weights past their range, a careful pass takes (s - m) c, at the steps of the rows
@@ -273,36 +111,6 @@ constexpr float kFar = 16777216.0f;
 
 __device__ inline float exponent(float s, float c, float mu, float muc, bool far) {
     return far ? (s - mu) * c : __builtin_fmaf(s, c, -muc);
-}
-
-// The sums of W waves, each relative to its own maximum, as one: returns (maximum, sum of
-// weights) and the values in acc.
-template <int W>
-__device__ inline float2 merged(const float2 *ml, int ml_stride, const v4f *sums, int stride, float c, v4f &acc) {
-    float M = kNegInf;
-#pragma unroll
-    for (int i = 0; i < W; ++i) M = fmaxf(M, ml[i * ml_stride].x);
-    const float mu = M == kNegInf ? 0.0f : M;
-    float l = 0.0f;
-    acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        const float2 e = ml[i * ml_stride];
-        const float f = exp2_hw((e.x - mu) * c);
-        l += e.y * f;
-        acc += sums[i * stride] * f;
-    }
-    return make_float2(M, l);
-}
-
-// Four dimensions of an output row from their sums and the sum of weights.
-__device__ inline void store_out(const CausalArgs &a, const Work &w, const RowOf &row, int d, const v4f &acc, float l) {
-    uint2 y = {};
-    if (w.s.L > 0 && w.s.p0 + row.i >= 0) {
-        const float inv = 1.0f / l;
-        y = make_uint2(cvt_pk_bf16(acc[0] * inv, acc[1] * inv), cvt_pk_bf16(acc[2] * inv, acc[3] * inv));
-    }
-    *(uint2 *)(a.out + row_at(w, row, a.out_stride) + d) = y;
 }
 
 // ---------------------------------------------------------------- few rows
@@ -660,10 +468,35 @@ __global__ __launch_bounds__(NR * 256, NR) void k_causal_mid(CausalArgs a) {
 // One step after the other, a barrier each: 567 us; as here 539, and 521 with the searches and
 // divisions before the first step shortened.  Other orders of products, vector instructions
 // and LDS reads, and raised wave priorities, were equal or slower.
+// InF16: the cache is the workspace that a 4-bit one was unpacked to, each head of a sequence
+// times a power of two of its own (shifts), and the queries' rows times one of theirs.  A head
+// whose rows are too far apart for one power has one for each key, and its tiles go through
+// the careful pass.
 constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves, kStepKeys = 32, kStepSlots = 4;
 constexpr int kStepUnits = kStepKeys * kHeadDim / 8;          // 16-byte units of a step's K or V (512)
 
-template <int HALVES>
+// A row's queries (its lanes: l, l ^ 32) from bf16 to f16 times a power of two, and that power's inverse.
+__device__ inline float row_in_f16(v8h *qf) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const v4u x = __builtin_bit_cast(v4u, qf[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(bf16_lo_to_f32(x[j])), fabsf(bf16_hi_to_f32(x[j]))));
+    }
+    const int e = f16_exponent(pair32_max(top));
+    const float f = power_of_two(14 - e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v4u x = __builtin_bit_cast(v4u, qf[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = cvt_pk_f16(bf16_lo_to_f32(x[j]) * f, bf16_hi_to_f32(x[j]) * f);
+        qf[i] = __builtin_bit_cast(v8h, x);
+    }
+    return power_of_two(e - 14);
+}
+
+template <int HALVES, typename E>
 __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_causal_prompt(CausalArgs a) {
     __shared__ __attribute__((aligned(16))) uint4 rings[HALVES][2][kStepSlots][kStepUnits];    // K, V
     __shared__ int not_finite[HALVES * kPromptWaves];
@@ -711,11 +544,23 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
     const int last = min(w.s.p0 + row.i, most);                            // last key this row sees
     const int wave_first = __builtin_amdgcn_readfirstlane(min(w.s.p0 + row_of(a, w, min(32 * wave, w.rows - 1)).i, most));
     const int wave_last = __builtin_amdgcn_readfirstlane(min(w.s.p0 + row_of(a, w, min(32 * wave + 31, w.rows - 1)).i, most));
-    v8bf qf[8];
+    typedef typename E::v8 v8;
+    constexpr bool kScaled = std::is_same<E, InF16>::value;
+    v8 qf[8];
+    float c = a.c, back = 1.0f, v_back = 1.0f;                    // f16: scores come out over `back`, sums over v_back
+    const short2 *row_shifts = nullptr;                           // or besides over a power of two of each key
     {
         const uint16_t *qp = a.q + row_at(w, row, a.q_stride) + 8 * hi;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const v8bf *)(qp + 16 * ks);
+        for (int ks = 0; ks < 8; ++ks) qf[ks] = *(const v8 *)(qp + 16 * ks);
+        if constexpr (kScaled) {
+            const int64_t head = w.s.slot0 / a.b.seq_slots * a.Hkv + w.h;
+            const HeadShift shift = a.shifts[head];
+            back = row_in_f16(qf) * power_of_two(shift.k);
+            v_back = power_of_two(shift.v);
+            c *= back;
+            if (shift.by_row) row_shifts = a.row_shifts + head * a.b.capacity;
+        }
     }
 
     // operands from LDS: row r of the scores' A operand; of V, what the transposing read needs.
@@ -728,10 +573,10 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) vat[dt] = 16u * value_unit(vk, 4 * dt + vc) + 8 * (vq & 1);
     }
-    auto k_frag = [&](int slot, int ks) { return *(const v8bf *)((const char *)kring + kat[ks] + slot * 8192); };
+    auto k_frag = [&](int slot, int ks) { return *(const v8 *)((const char *)kring + kat[ks] + slot * 8192); };
     auto v_half = [&](int slot, int key, int dt) { return lds_read_tr((const char *)vring + vat[dt] + slot * 8192 + key * 256); };
     auto v_frag = [&](int slot, int h, int dt) {
-        return __builtin_bit_cast(v8bf, __builtin_shufflevector(v_half(slot, 16 * h, dt), v_half(slot, 16 * h + 8, dt), 0, 1, 2, 3, 4, 5, 6, 7));
+        return __builtin_bit_cast(v8, __builtin_shufflevector(v_half(slot, 16 * h, dt), v_half(slot, 16 * h + 8, dt), 0, 1, 2, 3, 4, 5, 6, 7));
     };
     auto zero = [](v16f &x) {
 #pragma unroll
@@ -747,7 +592,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
         for (int i = 0; i < 16; ++i) x = fmaxf(x, s[i]);
         return pair32_max(x);
     };
-    auto operand = [](const uint32_t *p) { return __builtin_bit_cast(v8bf, v4u{p[0], p[1], p[2], p[3]}); };
+    auto operand = [](const uint32_t *p) { return __builtin_bit_cast(v8, v4u{p[0], p[1], p[2], p[3]}); };
 
     float m = kNegInf, l = 0.0f;
     uint64_t gone_far = 0;
@@ -770,12 +615,12 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
         lds_barrier();
         zero(s0);
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(0, ks), qf[ks], s0, 0, 0, 0);
+        for (int ks = 0; ks < 8; ++ks) s0 = E::product(k_frag(0, ks), qf[ks], s0);
 
         // step u (u mod 4 = SLOT): softmax of s into p; scores of u + 1 into sn; sums of u - 1 with pp
         auto step = [&](auto slot, int u, v16f &s, v16f &sn, uint32_t *p, const uint32_t *pp) {
             constexpr int SLOT = decltype(slot)::value, KS = (SLOT + 1) & 3, VS = (SLOT + 3) & 3;
-            v8bf kf[4], vf[4];
+            v8 kf[4], vf[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) kf[i] = k_frag(KS, i);
 #pragma unroll
@@ -783,20 +628,20 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
             const int key0 = first_key + u * kStepKeys;
             if (key0 + kStepKeys - 1 > wave_first) mask(s, key0);
             const float mt = row_max(s);
-            const bool own = (mt - m) * a.c > kLazy, grown = __ballot(own) != 0;
+            const bool own = (mt - m) * c > kLazy, grown = __ballot(own) != 0;
             const float mn = own ? mt : m;
-            const float mu = mn == kNegInf ? 0.0f : mn, muc = mu * a.c;
+            const float mu = mn == kNegInf ? 0.0f : mn, muc = mu * c;
             float ls = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if (i == 0) zero(sn);
-                sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i & 3], qf[i], sn, 0, 0, 0);
+                sn = E::product(kf[i & 3], qf[i], sn);
                 if (i < 4) kf[i] = k_frag(KS, i + 4);
-                o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i & 3], operand(pp + 4 * (i >> 2)), o[i & 3], 0, 0, 0);
+                o[i & 3] = E::product(vf[i & 3], operand(pp + 4 * (i >> 2)), o[i & 3]);
                 if (i < 4) vf[i] = v_frag(VS, 1, i);
-                const float e0 = exp2_hw(__builtin_fmaf(s[2 * i], a.c, -muc)), e1 = exp2_hw(__builtin_fmaf(s[2 * i + 1], a.c, -muc));
-                p[i] = cvt_pk_bf16(e0, e1);
-                ls = dot2(p[i], kBf16OnePair, ls);
+                const float e0 = exp2_hw(__builtin_fmaf(s[2 * i], c, -muc)), e1 = exp2_hw(__builtin_fmaf(s[2 * i + 1], c, -muc));
+                p[i] = E::pair(e0, e1);
+                ls = E::add(p[i], ls);
             }
             // the weights here, between the products, not behind the branch below
 #pragma unroll
@@ -817,7 +662,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
                 __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
             }
             if (grown) {                                             // the sums so far, up to step u - 1
-                const float alpha = exp2_hw((m - mu) * a.c);
+                const float alpha = exp2_hw((m - mu) * c);
                 m = mn;
                 l *= alpha;
 #pragma unroll
@@ -852,8 +697,8 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
         lds_barrier();
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_frag((n - 1) & 3, i >> 2, i & 3), operand((n & 1 ? p0 : p1) + 4 * (i >> 2)),
-                                                               o[i & 3], 0, 0, 0);
+            o[i & 3] = E::product(v_frag((n - 1) & 3, i >> 2, i & 3), operand((n & 1 ? p0 : p1) + 4 * (i >> 2)),
+                                                               o[i & 3]);
     }
     const uint64_t bad = __ballot(!all_finite(o)) | gone_far;
     if (lane == 0) not_finite[part * kPromptWaves + wave] = bad != 0;
@@ -861,8 +706,9 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
     int any = 0;
 #pragma unroll
     for (int i = 0; i < HALVES * kPromptWaves; ++i) any |= not_finite[i];
-    if (any) {
+    if (any || row_shifts) {
         // careful: once more, step by step, every row with the values of its own keys only
+        StepScale scale;                                             // of the values' own powers
         m = kNegInf;
         l = 0.0f;
         kn = kp + 4 * wave * a.b.tok;
@@ -880,13 +726,29 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
             v16f s;
             zero(s);
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(slot, ks), qf[ks], s, 0, 0, 0);
+            for (int ks = 0; ks < 8; ++ks) s = E::product(k_frag(slot, ks), qf[ks], s);
+            float value[16];                                         // the values' powers
+            if (row_shifts) {
+                float most = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = key0 + 8 * (i >> 2) + 4 * hi + (i & 3);
+                    const short2 shift = row_shifts[min(key, w.hi - 1)];
+                    s[i] *= power_of_two(shift.x);
+                    value[i] = power_of_two(shift.y);
+                    most = fmaxf(most, key <= last ? value[i] : 0.0f);
+                }
+                const float by = scale.raise(pair32_max(most));
+                l *= by;
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) o[dt] *= by;
+            }
             mask(s, key0);
             const float mt = row_max(s);
-            const bool own = (mt - m) * a.c > kLazy;
-            const float mn = own ? mt : m, mu = mn == kNegInf ? 0.0f : mn, muc = mu * a.c;
+            const bool own = (mt - m) * c > kLazy;
+            const float mn = own ? mt : m, mu = mn == kNegInf ? 0.0f : mn, muc = mu * c;
             if (__ballot(own)) {
-                const float alpha = exp2_hw((m - mu) * a.c);
+                const float alpha = exp2_hw((m - mu) * c);
                 m = mn;
                 l *= alpha;
 #pragma unroll
@@ -897,8 +759,14 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
             uint32_t p[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                p[i] = cvt_pk_bf16(exp2_hw(exponent(s[2 * i], a.c, mu, muc, far)), exp2_hw(exponent(s[2 * i + 1], a.c, mu, muc, far)));
-                ls = dot2(p[i], kBf16OnePair, ls);
+                const float e0 = exp2_hw(exponent(s[2 * i], c, mu, muc, far) - scale.e), e1 = exp2_hw(exponent(s[2 * i + 1], c, mu, muc, far) - scale.e);
+                if (row_shifts) {
+                    p[i] = E::pair(e0 * value[2 * i], e1 * value[2 * i + 1]);
+                    ls += e0 + e1;
+                } else {
+                    p[i] = E::pair(e0, e1);
+                    ls = E::add(p[i], ls);
+                }
             }
             l += ls;
             const int t0 = min(wave_first, key0 + kStepKeys - 1), t1 = min(wave_last, key0 + kStepKeys - 1);   // later tokens see all
@@ -910,15 +778,21 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
                     v16f x = before;
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            values_up_to(v_half(slot, 16 * h, dt), v_half(slot, 16 * h + 8, dt), key0 + 16 * h + 4 * hi, key0 + 16 * h + 8 + 4 * hi, t),
-                            operand(p + 4 * h), x, 0, 0, 0);
+                        x = E::product(
+                            __builtin_bit_cast(v8, values_up_to(v_half(slot, 16 * h, dt), v_half(slot, 16 * h + 8, dt), key0 + 16 * h + 4 * hi, key0 + 16 * h + 8 + 4 * hi, t)),
+                            operand(p + 4 * h), x);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[dt][i] = min(last, key0 + kStepKeys - 1) == t ? x[i] : o[dt][i];
                 }
             }
         }
         lds_barrier();                                               // the rings are free
+        if (row_shifts) {
+            const float up = power_of_two((int)scale.e);
+            l *= up;
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) o[dt] *= up;
+        }
     }
     l = pair32_sum(l);
     if constexpr (HALVES == 2) {
@@ -936,7 +810,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
         if (part == 1) return;
         const float2 e = second[32 * wave + r];
         const float M = fmaxf(m, e.x), mu = M == kNegInf ? 0.0f : M;
-        const float f1 = exp2_hw((m - mu) * a.c), f2 = exp2_hw((e.x - mu) * a.c);
+        const float f1 = exp2_hw((m - mu) * c), f2 = exp2_hw((e.x - mu) * c);
         m = M;
         l = l * f1 + e.y * f2;
 #pragma unroll
@@ -954,7 +828,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
         // 4 dt + i has dimensions 32 dt + 8 i .. + 7, 4 of them a lane
         char *const rows = (char *)kring + wave * 8192;
         const bool sees = w.s.L > 0 && last >= 0;
-        const float inv = 1.0f / l;
+        const float inv = kScaled ? v_back / l : 1.0f / l;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -971,13 +845,17 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
             *(uint4 *)(a.out + row_at(w, row_of(a, w, 32 * wave + x), a.out_stride) + 8 * c) = *(const uint4 *)(rows + 16 * key_unit(x, c));
         }
     } else if (32 * wave + r < w.rows) {
+        if constexpr (kScaled) {
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) o[dt] *= v_back;
+        }
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 *(v4f *)(unit_at<kPromptRows>(a, w.split, (4 * wave + dt) * 4 + i) + 4 * lane) =
                     v4f{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-        if (hi == 0) *row_ml<kPromptRows>(a, w.split, 32 * wave + r) = make_float2(m, l);
+        if (hi == 0) *row_ml<kPromptRows>(a, w.split, 32 * wave + r) = make_float2(kScaled ? m * back : m, l);
     }
 }
 
@@ -1005,8 +883,7 @@ __global__ __launch_bounds__(256) void k_causal_join(CausalArgs a) {
         row = 32 * (unit >> 4) + (lane & 31);
         d = 8 * (unit & 15) + 4 * (lane >> 5);
     }
-    const int keys = RT == 0 ? kStepKeys : RT == 1 ? kFewKeys : kMidKeys;
-    const int used = w.hi > 0 ? range_of(a, (w.hi + keys - 1) / keys, 0).used : 0;
+    const int used = w.hi > 0 ? range_of(a, (w.hi + a.step_keys - 1) / a.step_keys, 0).used : 0;
     const bool on = row < w.rows;
     float m = kNegInf, ls = 0.0f;
     v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1061,20 +938,27 @@ const char *causal_kernel_name(int rt, int halves) {
     return rt == 1 ? "k_causal_few" : rt == 2 ? "k_causal_mid<1>" : rt == 4 ? "k_causal_mid<2>" : halves == 2 ? "k_causal_prompt<2>" : "k_causal_prompt<1>";
 }
 
-hipError_t launch_causal(const CausalArgs &a, int rt, int halves, hipStream_t st) {
-    const dim3 grid((unsigned)(a.tiles * a.Hkv), (unsigned)a.S);
-    if (rt == 1) hipLaunchKernelGGL(k_causal_few, grid, dim3(kFewWaves * 64), 0, st, a);
-    else if (rt == 2) hipLaunchKernelGGL(k_causal_mid<1>, grid, dim3(256), 0, st, a);
-    else if (rt == 4) hipLaunchKernelGGL(k_causal_mid<2>, grid, dim3(512), 0, st, a);
-    else if (halves == 2) hipLaunchKernelGGL(k_causal_prompt<2>, grid, dim3(2 * kPromptWaves * 64), 0, st, a);
-    else hipLaunchKernelGGL(k_causal_prompt<1>, grid, dim3(kPromptWaves * 64), 0, st, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.S == 1) return e;
+hipError_t launch_causal_join(const CausalArgs &a, int rt, hipStream_t st) {
     if (rt == 1) launch_join<1>(a, st);
     else if (rt == 2) launch_join<2>(a, st);
     else if (rt == 4) launch_join<4>(a, st);
     else launch_join<0>(a, st);
     return hipGetLastError();
+}
+
+hipError_t launch_causal(const CausalArgs &args, int rt, int halves, hipStream_t st) {
+    CausalArgs a = args;
+    a.step_keys = rt == 1 ? kFewKeys : rt ? kMidKeys : kStepKeys;
+    const dim3 grid((unsigned)(a.tiles * a.Hkv), (unsigned)a.S);
+    if (rt == 1) hipLaunchKernelGGL(k_causal_few, grid, dim3(kFewWaves * 64), 0, st, a);
+    else if (rt == 2) hipLaunchKernelGGL(k_causal_mid<1>, grid, dim3(256), 0, st, a);
+    else if (rt == 4) hipLaunchKernelGGL(k_causal_mid<2>, grid, dim3(512), 0, st, a);
+    else if (a.shifts && halves == 2) hipLaunchKernelGGL((k_causal_prompt<2, InF16>), grid, dim3(2 * kPromptWaves * 64), 0, st, a);
+    else if (a.shifts) hipLaunchKernelGGL((k_causal_prompt<1, InF16>), grid, dim3(kPromptWaves * 64), 0, st, a);
+    else if (halves == 2) hipLaunchKernelGGL((k_causal_prompt<2, InBf16>), grid, dim3(2 * kPromptWaves * 64), 0, st, a);
+    else hipLaunchKernelGGL((k_causal_prompt<1, InBf16>), grid, dim3(kPromptWaves * 64), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || a.S == 1 ? e : launch_causal_join(a, rt, st);
 }
 
 }  // namespace qlin

@@ -6,118 +6,18 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
 
-#include "qlin_internal.h"
-#include "target_internal.h"
+#include "target_checks.h"
 
 using namespace qlin;
 
 namespace {
 
-constexpr int64_t kMaxSeq = 65536, kMaxRows = (int64_t)1 << 22, kMaxLen = (int64_t)1 << 28, kMaxSlots = (int64_t)1 << 40;
-constexpr int64_t kMaxHeads = 4096, kMaxGroup = 64, kMaxSplits = 256, kMaxStride = (int64_t)1 << 40;
 constexpr int64_t kMaxDraft = kVerifyMaxDraft, kMaxVocab = (int64_t)1 << 24, kMaxVerifySeq = 65535;   // sequences: a grid's y
-constexpr int64_t kMaxTokenStride = (int64_t)1 << 28;       // 32-bit byte offsets over four tokens
-constexpr int64_t kMaxRowStride = (int64_t)1 << 32;
 constexpr int64_t kVerifyTwoParts = (int64_t)1 << 26, kVerifyMany = (int64_t)1 << 25;     // logits of a call: see qlin_verify_draft
-constexpr int64_t kMaxExtent = (int64_t)1 << 60;      // elements of one strided array
-
-// An address range, in bytes.
-struct Range { uintptr_t lo; size_t bytes; };
-
-bool overlap(const Range &a, const Range &b) { return a.bytes && b.bytes && a.lo < b.lo + b.bytes && b.lo < a.lo + a.bytes; }
-
-Range rows_range(const void *p, int64_t rows, int64_t stride, int64_t width) {
-    return Range{(uintptr_t)p, rows > 0 ? (size_t)((rows - 1) * stride + width) * 2 : 0};
-}
-
-// Whether two arrays of rows share an element.  Slices of the rows of one array do not, though
-// their ranges overlap.
-bool rows_meet(const void *p, int64_t stride, int64_t width, const void *q, int64_t q_stride, int64_t q_width, int64_t rows) {
-    if (!overlap(rows_range(p, rows, stride, width), rows_range(q, rows, q_stride, q_width))) return false;
-    if (stride != q_stride) return true;
-    const int64_t d = ((int64_t)((uintptr_t)q - (uintptr_t)p) / 2 % stride + stride) % stride;   // 16-byte aligned both
-    return d < width || d + q_width > stride;
-}
-
-Range cache_range(const void *p, const qlin_kv_cache *c) {
-    return Range{(uintptr_t)p, (size_t)((c->slots - 1) * c->token_stride + (c->heads - 1) * c->head_stride + kHeadDim) * 2};
-}
-
-bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-
-int check_batch(const qlin_batch *b) {
-    if (!b) return fail(QLIN_ERR_INVALID, "NULL batch");
-    if (b->n_seq < 1 || b->rows < 0 || b->max_new < 0 || b->max_new > b->rows || b->max_len < 0)
-        return fail(QLIN_ERR_INVALID, "n_seq must be positive, rows >= 0, max_new in [0, rows], max_len >= 0");
-    if (b->n_seq > kMaxSeq || b->rows > kMaxRows || b->max_len > kMaxLen)
-        return fail(QLIN_ERR_UNSUPPORTED, "at most 65536 sequences, 2^22 rows and 2^28 cached tokens");
-    return QLIN_OK;
-}
-
-int check_batch_arrays(const qlin_batch *b) {
-    if (!b->new_start || !b->length) return fail(QLIN_ERR_INVALID, "NULL new_start or length");
-    if (!aligned(b->new_start, 4) || !aligned(b->length, 4) || !aligned(b->cache_start, 8))
-        return fail(QLIN_ERR_ALIGN, "new_start and length must be 4-byte aligned, cache_start 8");
-    return QLIN_OK;
-}
-
-int check_heads(int64_t q_heads, int64_t kv_heads, int64_t head_dim) {
-    if (q_heads <= 0 || kv_heads <= 0 || q_heads % kv_heads)
-        return fail(QLIN_ERR_INVALID, "query and key/value heads must be positive, the first a multiple of the second");
-    if (head_dim != kHeadDim) return fail(QLIN_ERR_UNSUPPORTED, "head_dim must be 128 (got %lld)", (long long)head_dim);
-    if (q_heads > kMaxHeads) return fail(QLIN_ERR_UNSUPPORTED, "at most 4096 query heads");
-    if (q_heads / kv_heads > kMaxGroup) return fail(QLIN_ERR_UNSUPPORTED, "at most 64 query heads per key/value head");
-    return QLIN_OK;
-}
-
-int check_cache(const qlin_kv_cache *c) {
-    if (!c) return fail(QLIN_ERR_INVALID, "NULL cache");
-    if (c->slots < 1 || c->seq_slots < 0 || c->capacity < 0 || c->token_stride < kHeadDim || c->head_stride < kHeadDim)
-        return fail(QLIN_ERR_INVALID, "cache: slots must be positive, seq_slots and capacity >= 0, strides >= 128");
-    if (c->token_stride % 8 || c->head_stride % 8) return fail(QLIN_ERR_ALIGN, "cache strides must be multiples of 8");
-    if (c->slots > kMaxSlots || c->seq_slots > kMaxSlots || c->capacity > kMaxSlots || c->token_stride > kMaxTokenStride || c->head_stride > kMaxStride ||
-        (double)c->slots * (double)c->token_stride + (double)c->heads * (double)c->head_stride > (double)kMaxExtent)
-        return fail(QLIN_ERR_UNSUPPORTED, "cache too large");
-    if (!c->k || !c->v) return fail(QLIN_ERR_INVALID, "NULL cache");
-    if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(QLIN_ERR_ALIGN, "the cache must be 16-byte aligned");
-    return QLIN_OK;
-}
-
-// Whether the arrays that describe a batch share an element with a range.
-bool batch_meets(const qlin_batch *b, const Range &r) {
-    const size_t n = (size_t)b->n_seq;
-    return overlap(r, Range{(uintptr_t)b->new_start, (n + 1) * 4}) || overlap(r, Range{(uintptr_t)b->length, n * 4}) ||
-           overlap(r, Range{(uintptr_t)b->cache_start, b->cache_start ? n * 8 : 0});
-}
-
-// Row arrays of `width` elements: stride and alignment.
-int check_rows(const void *p, int64_t stride, int64_t width, const char *name) {
-    if (!p) return fail(QLIN_ERR_INVALID, "NULL %s", name);
-    if (stride < width || stride > kMaxRowStride) return fail(QLIN_ERR_INVALID, "%s: stride must be at least %lld", name, (long long)width);
-    if (stride % 8 || !aligned(p, 16)) return fail(QLIN_ERR_ALIGN, "%s must be 16-byte aligned, its stride a multiple of 8", name);
-    return QLIN_OK;
-}
-
-BatchArgs batch_args(const qlin_batch *b, const qlin_kv_cache *c) {
-    BatchArgs a;
-    a.new_start = b->new_start;
-    a.length = b->length;
-    a.cache_start = b->cache_start;
-    a.slots = c->slots;
-    a.seq_slots = c->seq_slots;
-    a.capacity = c->capacity;
-    a.tok = c->token_stride;
-    a.head = c->head_stride;
-    a.n_seq = (int)b->n_seq;
-    a.rows = (int)b->rows;
-    a.max_new = (int)b->max_new;
-    return a;
-}
 
 // The kernel and split of one causal attention, from the host's bounds.
 struct CausalPlan { int rt = 0, halves = 1, tiles = 0, one_tile = 0, pairs = 0, S = 1, least = 1; int64_t ws_bytes = 0; };
@@ -195,22 +95,6 @@ int make_causal_plan(const CausalKey &k, CausalPlan *p) {
     return QLIN_OK;
 }
 
-// Compute units of the current device.
-int compute_units(int64_t *cus) {
-    constexpr int kDevices = 64;
-    static std::atomic<int> known[kDevices];
-    int dev = 0, n = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e == hipSuccess && dev >= 0 && dev < kDevices) n = known[dev].load(std::memory_order_relaxed);
-    if (e == hipSuccess && n == 0) {
-        e = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev);
-        if (e == hipSuccess && dev >= 0 && dev < kDevices) known[dev].store(n, std::memory_order_relaxed);
-    }
-    if (e != hipSuccess) return hip_fail(e, "device query");
-    *cus = n;
-    return QLIN_OK;
-}
-
 // The plan of a call.  Each thread remembers 64, directly mapped: the layers of a model ask for
 // the same one, and weighing the choices takes longer than all the checks.
 int causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, CausalPlan *p) {
@@ -231,6 +115,38 @@ int causal_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, Ca
     return QLIN_OK;
 }
 
+// The launches of a checked call.
+int launch_attention(const qlin_batch *batch, const qlin_kv_cache *cache, const HeadShift *shifts, const short2 *row_shifts,
+                     const CausalPlan &p, int64_t q_heads, float factor, const uint16_t *q, int64_t q_stride, uint16_t *out, int64_t out_stride, void *workspace,
+                     hipStream_t stream) {
+    CausalArgs a;
+    a.b = batch_args(batch, cache);
+    a.q = q;
+    a.k = cache->k;
+    a.v = cache->v;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.Hq = (int)q_heads;
+    a.Hkv = (int)cache->heads;
+    a.G = (int)(q_heads / cache->heads);
+    a.ws_o = (float *)workspace;
+    a.ws_ml = a.ws_o + (size_t)p.tiles * a.Hkv * p.S * causal_tile_rows(p.rt) * kHeadDim;
+    a.tiles = p.tiles;
+    a.one_tile = p.one_tile;
+    a.pairs = p.pairs;
+    a.least = p.least;
+    a.S = p.S;
+    a.max_len = (int)batch->max_len;
+    gn_reciprocal(a.Hkv, &a.inv_heads, &a.heads_shift);
+    a.inv_g = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
+    a.c = factor;
+    a.shifts = shifts;
+    a.row_shifts = row_shifts;
+    const hipError_t e = launch_causal(a, p.rt, p.halves, stream);
+    return e == hipSuccess ? QLIN_OK : hip_fail(e, "causal attention launch");
+}
+
 // Workspace of the verification: the rows' statistics, then the chunks' sums, then the decisions.
 struct VerifyLayout { int64_t chunks, rows, sums, decisions, bytes; };
 
@@ -246,6 +162,18 @@ VerifyLayout verify_layout(int64_t n_seq, int64_t n_draft, int64_t vocab) {
 
 }  // namespace
 
+namespace qlin {
+
+int attend_in_f16(const qlin_batch *batch, const qlin_kv_cache *cache, const HeadShift *shifts, const short2 *row_shifts,
+                  int64_t q_heads, float factor, int64_t splits, const uint16_t *q, int64_t q_stride, uint16_t *out,
+                  int64_t out_stride, void *workspace, hipStream_t stream) {
+    CausalPlan p;
+    if (causal_plan(batch, q_heads, cache->heads, splits, &p) != QLIN_OK) return last_status();
+    return launch_attention(batch, cache, shifts, row_shifts, p, q_heads, factor, q, q_stride, out, out_stride, workspace, stream);
+}
+
+}  // namespace qlin
+
 extern "C" {
 
 int qlin_norm_rope_append(const qlin_batch *batch, const qlin_kv_cache *cache, int64_t q_heads, int64_t head_dim,
@@ -258,55 +186,15 @@ int qlin_norm_rope_append(const qlin_batch *batch, const qlin_kv_cache *cache, i
     if (!cache) return fail(QLIN_ERR_INVALID, "NULL cache");
     if (check_heads(q_heads, cache->heads, head_dim) != QLIN_OK) return last_status();
     if (check_cache(cache) != QLIN_OK) return last_status();
-    if (rotary_dim < 0 || rotary_dim > kHeadDim || rotary_dim % 16)
-        return fail(QLIN_ERR_INVALID, "rotary_dim must be a multiple of 16 in [0, 128]");
-    if (!(eps >= 0.0f) || std::isinf(eps)) return fail(QLIN_ERR_INVALID, "eps must be >= 0");
+    const AppendRows r{q, q_stride, k, k_stride, v, v_stride, q_norm, k_norm, eps, inv_freq, rotary_dim, q_out, q_out_stride};
+    if (check_append_values(r) != QLIN_OK) return last_status();
     if (batch->rows == 0) return QLIN_OK;
-    if (check_batch_arrays(batch) != QLIN_OK) return last_status();
-    const int64_t wq = q_heads * kHeadDim, wk = cache->heads * kHeadDim, M = batch->rows;
-    if (check_rows(q, q_stride, wq, "q") != QLIN_OK || check_rows(k, k_stride, wk, "k") != QLIN_OK ||
-        check_rows(v, v_stride, wk, "v") != QLIN_OK || check_rows(q_out, q_out_stride, wq, "q_out") != QLIN_OK)
-        return last_status();
-    if (rotary_dim && !inv_freq) return fail(QLIN_ERR_INVALID, "NULL inv_freq");
-    if (!aligned(q_norm, 8) || !aligned(k_norm, 8) || !aligned(inv_freq, 8))
-        return fail(QLIN_ERR_ALIGN, "norm weights and inv_freq must be 8-byte aligned");
-    const Range rq = rows_range(q, M, q_stride, wq), rk = rows_range(k, M, k_stride, wk), rv = rows_range(v, M, v_stride, wk);
-    const Range ro = rows_range(q_out, M, q_out_stride, wq), ck = cache_range(cache->k, cache), cv = cache_range(cache->v, cache);
-    if (!(q_out == q && q_out_stride == q_stride) && rows_meet(q, q_stride, wq, q_out, q_out_stride, wq, M))
-        return fail(QLIN_ERR_INVALID, "q_out overlaps q without being it");
-    if (rows_meet(k, k_stride, wk, q_out, q_out_stride, wq, M) || rows_meet(v, v_stride, wk, q_out, q_out_stride, wq, M))
-        return fail(QLIN_ERR_INVALID, "q_out overlaps k or v");
-    if (overlap(ro, ck) || overlap(ro, cv)) return fail(QLIN_ERR_INVALID, "q_out overlaps the cache");
-    for (const Range &r : {rq, rk, rv})
-        if (overlap(r, ck) || overlap(r, cv)) return fail(QLIN_ERR_INVALID, "q, k or v overlaps the cache");
-    const Range small[] = {{(uintptr_t)q_norm, q_norm ? (size_t)kHeadDim * 2 : 0}, {(uintptr_t)k_norm, k_norm ? (size_t)kHeadDim * 2 : 0},
-                           {(uintptr_t)inv_freq, (size_t)rotary_dim / 2 * 8}};
-    for (const Range &w : {ro, ck, cv}) {
-        if (batch_meets(batch, w)) return fail(QLIN_ERR_INVALID, "q_out or the cache overlaps new_start, length or cache_start");
-        for (const Range &r : small)
-            if (overlap(w, r)) return fail(QLIN_ERR_INVALID, "q_out or the cache overlaps norm weights or inv_freq");
-    }
+    const Range c[] = {cache_range(cache->k, cache), cache_range(cache->v, cache)};
+    if (check_append_arrays(batch, q_heads, cache->heads, r, c, 2) != QLIN_OK) return last_status();
 
-    AppendArgs a;
-    a.b = batch_args(batch, cache);
-    a.q = q;
-    a.k = k;
-    a.v = v;
-    a.q_norm = q_norm;
-    a.k_norm = k_norm;
-    a.inv_freq = inv_freq;
-    a.q_out = q_out;
+    AppendArgs a = append_args(batch_args(batch, cache), q_heads, cache->heads, r, interleaved);
     a.kc = cache->k;
     a.vc = cache->v;
-    a.q_stride = q_stride;
-    a.k_stride = k_stride;
-    a.v_stride = v_stride;
-    a.q_out_stride = q_out_stride;
-    a.eps = eps;
-    a.Hq = (int)q_heads;
-    a.Hkv = (int)cache->heads;
-    a.half = (int)rotary_dim / 2;
-    a.interleaved = interleaved != 0;
     const hipError_t e = launch_append(a, (hipStream_t)stream);
     return e == hipSuccess ? QLIN_OK : hip_fail(e, "append launch");
 }
@@ -334,11 +222,8 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     if (!cache) return fail(QLIN_ERR_INVALID, "NULL cache");
     if (check_heads(q_heads, cache->heads, head_dim) != QLIN_OK) return last_status();
     if (check_cache(cache) != QLIN_OK) return last_status();
-    if (splits < 0 || splits > kMaxSplits) return fail(QLIN_ERR_INVALID, "splits must be in [0, 256]");
-    // scores to base-2 exponents
-    const float factor = (float)(1.4426950408889634 * (scale > 0.0f ? (double)scale : 1.0 / std::sqrt((double)kHeadDim)));
-    if (!(scale >= 0.0f) || std::isinf(factor)) return fail(QLIN_ERR_INVALID, "scale must be positive (or 0), scale log2(e) a finite float");
-    if (workspace_bytes < 0) return fail(QLIN_ERR_INVALID, "workspace_bytes must be >= 0");
+    float factor;
+    if (check_attention_values(scale, splits, workspace_bytes, &factor) != QLIN_OK) return last_status();
     if (batch->rows == 0) return QLIN_OK;
     if (check_batch_arrays(batch) != QLIN_OK) return last_status();
     const int64_t w = q_heads * kHeadDim, M = batch->rows;
@@ -359,30 +244,7 @@ int qlin_causal_attention(const qlin_batch *batch, const qlin_kv_cache *cache, i
     if (batch_meets(batch, ws)) return fail(QLIN_ERR_INVALID, "the workspace overlaps new_start, length or cache_start");
     if (batch->max_new == 0) return QLIN_OK;
 
-    CausalArgs a;
-    a.b = batch_args(batch, cache);
-    a.q = q;
-    a.k = cache->k;
-    a.v = cache->v;
-    a.out = out;
-    a.q_stride = q_stride;
-    a.out_stride = out_stride;
-    a.Hq = (int)q_heads;
-    a.Hkv = (int)cache->heads;
-    a.G = (int)(q_heads / cache->heads);
-    a.ws_o = (float *)workspace;
-    a.ws_ml = a.ws_o + (size_t)p.tiles * a.Hkv * p.S * causal_tile_rows(p.rt) * kHeadDim;
-    a.tiles = p.tiles;
-    a.one_tile = p.one_tile;
-    a.pairs = p.pairs;
-    a.least = p.least;
-    a.S = p.S;
-    a.max_len = (int)batch->max_len;
-    gn_reciprocal(a.Hkv, &a.inv_heads, &a.heads_shift);
-    a.inv_g = a.G > 1 ? (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G) : 0u;
-    a.c = factor;
-    const hipError_t e = launch_causal(a, p.rt, p.halves, (hipStream_t)stream);
-    return e == hipSuccess ? QLIN_OK : hip_fail(e, "causal attention launch");
+    return launch_attention(batch, cache, nullptr, nullptr, p, q_heads, factor, q, q_stride, out, out_stride, workspace, (hipStream_t)stream);
 }
 
 int qlin_verify_plan(int64_t n_seq, int64_t n_draft, int64_t vocab, int64_t *workspace_bytes) {

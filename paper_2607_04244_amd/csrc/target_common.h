@@ -26,7 +26,7 @@ __device__ inline Seq load_seq(const BatchArgs &a, int b) {
     s.slot0 = a.cache_start ? a.cache_start[b] : (int64_t)b * a.seq_slots;
     int64_t room = a.capacity ? a.capacity : a.slots;
     if (a.capacity && a.cache_start && a.seq_slots) room -= s.slot0 % a.seq_slots;
-    s.L = s.slot0 >= 0 && s.slot0 <= a.slots - L && L <= room ? L : 0;
+    s.L = s.slot0 >= 0 && s.slot0 <= a.slots - L && L <= room && L <= a.longest ? L : 0;
     return s;
 }
 

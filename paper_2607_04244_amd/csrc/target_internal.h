@@ -18,6 +18,7 @@ struct BatchArgs {
     int64_t slots, seq_slots, capacity;
     int64_t tok, head;              // elements between slots, between heads
     int n_seq, rows, max_new;
+    int longest;                    // a longer sequence counts as one without cached tokens
 };
 
 struct AppendArgs {
@@ -31,6 +32,8 @@ struct AppendArgs {
     int Hq, Hkv, half, interleaved;
 };
 
+struct HeadShift { short k, v; int by_row; };
+
 struct CausalArgs {
     BatchArgs b;
     const uint16_t *q, *k, *v;
@@ -42,10 +45,13 @@ struct CausalArgs {
     int one_tile;                   // one tile a sequence: tile i is sequence i
     int pairs;                      // at most two workgroups a compute unit
     int S, least;                   // key ranges; least steps of one
+    int step_keys;                  // keys of a step (set by the launch)
     int max_len;                    // bound of the sequences' lengths (orders the tiles)
     uint32_t inv_heads, inv_g;      // x / Hkv by gn_chunk; ceil(2^32 / G) (0: G = 1)
     int heads_shift;
     float c;                        // scale log2(e): scores to base-2 exponents
+    const HeadShift *shifts;        // k and v are f16 times 2^-shift, of each sequence and head; null: bf16
+    const short2 *row_shifts;       // where it is by_row: (k's, v's) shift of each sequence, head and token
 };
 
 // Rows (tokens x heads of a group) of a tile of k_causal_few (rt = 1), of k_causal_mid (2, 4) or
@@ -76,6 +82,7 @@ struct VerifyArgs {
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st);
 hipError_t launch_causal(const CausalArgs &a, int rt, int halves, hipStream_t st);
+hipError_t launch_causal_join(const CausalArgs &a, int rt, hipStream_t st);   // a.step_keys as the ranges' kernel
 const char *causal_kernel_name(int rt, int halves);
 hipError_t launch_verify(VerifyArgs a, int n_seq, bool many, hipStream_t st);
 

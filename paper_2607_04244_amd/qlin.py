@@ -32,7 +32,9 @@ EXPORTS = ("qlin_create", "qlin_create_symmetric", "qlin_forward", "qlin_forward
            "qlin_dequantize", "qlin_shape", "qlin_last_status", "qlin_stream_read", "qlin_quantize",
            "qlin_swa_plan", "qlin_swa_attention", "qlin_forward_group", "qlin_group_plan",
            "qlin_workspace_bytes", "qlin_forward_group_noalloc", "qlin_norm_rope_append", "qlin_causal_plan",
-           "qlin_causal_attention", "qlin_verify_plan", "qlin_verify_draft")
+           "qlin_causal_attention", "qlin_verify_plan", "qlin_verify_draft", "qlin_block_norm", "qlin_quantize_tokens",
+           "qlin_eight_bit_plan", "qlin_eight_bit_linear", "qlin_norm_rope_append_four_bit", "qlin_unpack_four_bit", "qlin_causal_four_bit_plan",
+           "qlin_causal_attention_four_bit")
 
 _lib = None
 
@@ -58,7 +60,15 @@ class KVCache(_Room):
         super().__init__(capacity, *fields)
 
 
+class KV4Cache(ctypes.Structure):
+    """struct qlin_kv4_cache (include/qlin_lowbit.h); strides in rows."""
+    _fields_ = [("capacity", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_grid", ctypes.c_void_p),
+                ("v_grid", ctypes.c_void_p), ("heads", ctypes.c_int64), ("slots", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("seq_slots", ctypes.c_int64)]
+
+
 _cache_members = struct.Struct("=8q").pack
+_kv4_members = struct.Struct("=10q").pack
 
 
 class QlinError(RuntimeError):
@@ -126,6 +136,23 @@ def lib():
     L.qlin_verify_plan.argtypes = [I64, I64, I64, ctypes.POINTER(I64)]
     L.qlin_verify_draft.restype = I32
     L.qlin_verify_draft.argtypes = [I64, I64, I64, VP, I64, VP, I64, VP, VP, VP, VP, VP, VP, VP, I64, VP]
+    QP, PI64 = ctypes.POINTER(KV4Cache), ctypes.POINTER(I64)
+    L.qlin_block_norm.restype = I32
+    L.qlin_block_norm.argtypes = [I64, I64, VP, I64, VP, I64, VP, VP, I64, I32, F32, VP, F32, VP, I64, VP, I64, VP]
+    L.qlin_quantize_tokens.restype = I32
+    L.qlin_quantize_tokens.argtypes = [I64, I64, VP, I64, I32, VP, I64, VP, VP]
+    L.qlin_eight_bit_plan.restype = I32
+    L.qlin_eight_bit_plan.argtypes = [I64, I64, I64, I64, PI64, PI64, ctypes.c_char_p, I64]
+    L.qlin_eight_bit_linear.restype = I32
+    L.qlin_eight_bit_linear.argtypes = [I64, I64, I64, I64, VP, I64, VP, VP, I64, VP, VP, I64, VP, I64, VP]
+    L.qlin_norm_rope_append_four_bit.restype = I32
+    L.qlin_norm_rope_append_four_bit.argtypes = [BP, QP, *L.qlin_norm_rope_append.argtypes[2:]]
+    L.qlin_unpack_four_bit.restype = I32
+    L.qlin_unpack_four_bit.argtypes = [BP, QP, CP, I64, I32, VP]
+    L.qlin_causal_four_bit_plan.restype = I32
+    L.qlin_causal_four_bit_plan.argtypes = L.qlin_causal_plan.argtypes
+    L.qlin_causal_attention_four_bit.restype = I32
+    L.qlin_causal_attention_four_bit.argtypes = [BP, QP, *L.qlin_causal_attention.argtypes[2:]]
     L.qlin_shape.restype = I32
     L.qlin_shape.argtypes = [P, ctypes.POINTER(I64), ctypes.POINTER(I64)]
     _lib = L
@@ -321,6 +348,55 @@ def qlin_verify_draft(n_seq, n_draft, vocab, target_ptr, target_stride, draft_pt
                                    ws_ptr, ws_bytes, stream)
 
 
+def qlin_block_norm(rows, width, y_ptr, y_stride, residual_ptr, residual_stride, post_norm_ptr, gate_ptr, gate_stride,
+                    gate_sigmoid, scale, pre_norm_ptr, eps, residual_out_ptr, residual_out_stride, out_ptr, out_stride, stream):
+    return lib().qlin_block_norm(rows, width, y_ptr, y_stride, residual_ptr, residual_stride, post_norm_ptr, gate_ptr,
+                                 gate_stride, gate_sigmoid, scale, pre_norm_ptr, eps, residual_out_ptr,
+                                 residual_out_stride, out_ptr, out_stride, stream)
+
+
+def qlin_quantize_tokens(rows, width, x_ptr, x_stride, gated, codes_ptr, codes_stride, scale_ptr, stream):
+    return lib().qlin_quantize_tokens(rows, width, x_ptr, x_stride, gated, codes_ptr, codes_stride, scale_ptr, stream)
+
+
+def _plan(call, *args):
+    S, ws = ctypes.c_int64(), ctypes.c_int64()
+    buf = ctypes.create_string_buffer(256)
+    _check(call(*args, ctypes.byref(S), ctypes.byref(ws), buf, len(buf)))
+    return S.value, ws.value, buf.value.decode()
+
+
+def qlin_eight_bit_plan(M, N, K, splits=0):
+    """(splits, workspace_bytes, text) of the 8-bit linear's plan."""
+    return _plan(lib().qlin_eight_bit_plan, M, N, K, splits)
+
+
+def qlin_eight_bit_linear(M, N, K, splits, x_ptr, x_stride, x_scale_ptr, w_ptr, w_stride, w_scale_ptr, y_ptr, y_stride, ws_ptr,
+                   ws_bytes, stream):
+    return lib().qlin_eight_bit_linear(M, N, K, splits, x_ptr, x_stride, x_scale_ptr, w_ptr, w_stride, w_scale_ptr, y_ptr,
+                                y_stride, ws_ptr, ws_bytes, stream)
+
+
+def qlin_norm_rope_append_four_bit(batch, cache, *args):
+    """batch: Batch, cache: KV4Cache (or None: NULL); the others as qlin_norm_rope_append."""
+    return lib().qlin_norm_rope_append_four_bit(batch, cache, *args)
+
+
+def qlin_unpack_four_bit(batch, cache, to, head_dim, new_only, stream):
+    """batch: Batch, cache: KV4Cache, to: KVCache (or None: NULL)."""
+    return lib().qlin_unpack_four_bit(batch, cache, to, head_dim, new_only, stream)
+
+
+def qlin_causal_four_bit_plan(batch, q_heads, kv_heads, head_dim, splits=0):
+    """(splits, workspace_bytes, text) of the plan of the causal attention over a 4-bit cache."""
+    return _plan(lib().qlin_causal_four_bit_plan, batch, q_heads, kv_heads, head_dim, splits)
+
+
+def qlin_causal_attention_four_bit(batch, cache, *args):
+    """batch: Batch, cache: KV4Cache (or None: NULL); the others as qlin_causal_attention."""
+    return lib().qlin_causal_attention_four_bit(batch, cache, *args)
+
+
 # ---------------------------------------------------------------- torch wrappers
 
 _raw_stream = _current_device = None
@@ -474,8 +550,13 @@ def norm_rope_append(q, k, v, k_cache, v_cache, new_start, length, max_new=None,
     q heads, 128]; rows of no sequence are left as they are.
     """
     dev = _device()
+    return _append(lib().qlin_norm_rope_append, dev, _kv_cache(k_cache, v_cache, dev), k_cache, q, k, v, new_start, length,
+                   max_new, max_len, cache_start, q_norm, k_norm, eps, inv_freq, interleaved, out)
+
+
+def _append(call, dev, cache, k_cache, q, k, v, new_start, length, max_new, max_len, cache_start, q_norm, k_norm, eps,
+            inv_freq, interleaved, out):
     bf16 = _torch.bfloat16
-    cache = _kv_cache(k_cache, v_cache, dev)
     at, strides, widths = [], [], []
     for name, t in (("q", q), ("k", k), ("v", v)):
         at.append(_address(name, t, bf16, dev))
@@ -503,10 +584,10 @@ def norm_rope_append(q, k, v, k_cache, v_cache, new_start, length, max_new=None,
         if out.shape != (rows, Hq, 128):
             raise ValueError(f"out must have shape {(rows, Hq, 128)}")
         out_stride = _row_stride("out", out, Hq)
-    _check(lib().qlin_norm_rope_append(batch, cache, Hq, 128, at[0], strides[0], at[1], strides[1], at[2], strides[2],
-                                       _vector("q_norm", q_norm, bf16, dev, 128),
-                                       _vector("k_norm", k_norm, bf16, dev, 128), eps, freq, rotary,
-                                       1 if interleaved else 0, out_at, out_stride, _raw_stream(dev)))
+    _check(call(batch, cache, Hq, 128, at[0], strides[0], at[1], strides[1], at[2], strides[2],
+                _vector("q_norm", q_norm, bf16, dev, 128),
+                _vector("k_norm", k_norm, bf16, dev, 128), eps, freq, rotary,
+                1 if interleaved else 0, out_at, out_stride, _raw_stream(dev)))
     return out
 
 
@@ -524,20 +605,25 @@ def causal_attention(q, k_cache, v_cache, new_start, length, max_new=None, max_l
     they are.
     """
     dev = _device()
+    return _attend(lib().qlin_causal_attention, lib().qlin_causal_plan, dev, _kv_cache(k_cache, v_cache, dev), k_cache, q,
+                   new_start, length, max_new, max_len, cache_start, scale, splits, out, workspace)
+
+
+def _attend(call, plan, dev, cache, k_cache, q, new_start, length, max_new, max_len, cache_start, scale, splits, out,
+            workspace):
     bf16 = _torch.bfloat16
     q_at = _address("q", q, bf16, dev)
     if q.dim() != 3:
         raise ValueError("q must have rank 3")
     rows, Hq, D = shape = q.shape
     q_stride = _row_stride("q", q, Hq)
-    cache = _kv_cache(k_cache, v_cache, dev)
     batch = _batch(dev, rows, new_start, length, max_new, max_len, cache_start, k_cache)
     if workspace is None:
-        size = batch.n_seq, rows, batch.max_new, batch.max_len, Hq, cache.heads, D, splits, dev
+        size = plan.__name__, batch.n_seq, rows, batch.max_new, batch.max_len, Hq, cache.heads, D, splits, dev
         need = _scratch_bytes.get(size)
         if need is None:
             need = ctypes.c_int64()
-            _check(lib().qlin_causal_plan(batch, Hq, cache.heads, D, splits, None, ctypes.byref(need), None, 0))
+            _check(plan(batch, Hq, cache.heads, D, splits, None, ctypes.byref(need), None, 0))
             need = _remember(size, need.value)
         if need:
             workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device)
@@ -552,8 +638,7 @@ def causal_attention(q, k_cache, v_cache, new_start, length, max_new=None, max_l
         if out.shape != shape:
             raise ValueError(f"out must have shape {tuple(shape)}")
         out_stride = _row_stride("out", out, Hq)
-    _check(lib().qlin_causal_attention(batch, cache, Hq, D, scale, splits, q_at, q_stride, out_at, out_stride,
-                                       *_scratch(workspace), _raw_stream(dev)))
+    _check(call(batch, cache, Hq, D, scale, splits, q_at, q_stride, out_at, out_stride, *_scratch(workspace), _raw_stream(dev)))
     return out
 
 
@@ -584,6 +669,207 @@ def _logit_rows(name, t, n, rows, vocab):
     if (one != 1 and vocab > 1) or (n > 1 and seq != rows * row):
         raise ValueError(f"{name} must have contiguous rows at one distance")
     return row if n * rows > 1 else vocab
+
+
+def new_kv4_cache(*shape, device=None):
+    """A 4-bit cache of rows of 128 values, all zeros: (key words, key grids, value words, value
+    grids), int32 [*shape, 16] and bf16 [*shape, 2] tensors.  shape: sequences, heads, capacity;
+    or tokens, heads."""
+    import torch
+    dev = device or "cuda"
+    return tuple(torch.zeros((*shape, n), dtype=t, device=dev) for _ in "kv" for n, t in ((16, torch.int32), (2, torch.bfloat16)))
+
+
+def _kv4_cache(cache, dev):
+    """KV4Cache of (key words, key grids, value words, value grids)."""
+    k, kg, v, vg = cache
+    at = (_address("key words", k, _torch.int32, dev), _address("value words", v, _torch.int32, dev),
+          _address("key grids", kg, _torch.bfloat16, dev), _address("value grids", vg, _torch.bfloat16, dev))
+    shape, stride = k.shape, k.stride()
+    rank = len(shape)
+    if (rank not in (3, 4) or shape[-1] != 16 or 0 in shape or v.shape != shape or kg.shape != (*shape[:-1], 2) or vg.shape != kg.shape
+            or v.stride() != stride or stride[-1] != 1 or kg.stride() != vg.stride()):
+        raise ValueError("a 4-bit cache is int32 words [sequences, heads, capacity, 16] or [tokens, heads, 16] and bf16 "
+                         "grids [..., 2] of keys and of values")
+    for n, words, grid in zip(shape[:-1], stride, kg.stride()):
+        if n > 1 and (words % 16 or grid * 8 != words):
+            raise ValueError("the cache's rows must be whole, words and grids alike")
+    if kg.stride()[-1] != 1:
+        raise ValueError("the cache's grids must be contiguous pairs")
+    rows = [n // 16 for n in stride[:-1]]
+    if rank == 3:
+        return KV4Cache.from_buffer_copy(_kv4_members(0, *at, shape[1], shape[0], max(rows[0], 1), max(rows[1], 1), 0))
+    n, heads, capacity, _ = shape
+    seq, head, token = rows
+    token, head = max(token, 1), max(head, 1)
+    if n == 1:
+        seq = 0
+    if seq % token:
+        raise ValueError("the cache's sequences must lie whole tokens apart")
+    seq //= token
+    return KV4Cache.from_buffer_copy(_kv4_members(capacity, *at, heads, (n - 1) * seq + capacity, token, head, seq))
+
+
+def norm_rope_append_kv4(q, k, v, cache, new_start, length, max_new=None, max_len=None, cache_start=None, q_norm=None,
+                         k_norm=None, eps=1e-6, inv_freq=None, interleaved=False, out=None):
+    """norm_rope_append into a 4-bit cache (qlin_norm_rope_append_four_bit in include/qlin_lowbit.h).
+
+    cache: the four tensors of ``new_kv4_cache``; the other arguments as for
+    ``norm_rope_append``.  Returns ``out`` [rows, q heads, 128].
+    """
+    dev = _device()
+    return _append(lib().qlin_norm_rope_append_four_bit, dev, _kv4_cache(cache, dev), cache[0], q, k, v, new_start, length,
+                   max_new, max_len, cache_start, q_norm, k_norm, eps, inv_freq, interleaved, out)
+
+
+def unpack_kv4(cache, k_cache, v_cache, new_start, length, max_new=None, max_len=None, cache_start=None, new_only=False):
+    """The batch's cached tokens (with ``new_only`` its new ones) of a 4-bit cache into the same slots
+    of a bf16 cache of as many sequences or tokens (qlin_unpack_four_bit in include/qlin_lowbit.h).
+    Batches are described as for ``norm_rope_append``; max_new bounds a sequence's new tokens
+    (default: the tokens it can have in the cache).  Returns (k_cache, v_cache)."""
+    dev = _device()
+    src, to = _kv4_cache(cache, dev), _kv_cache(k_cache, v_cache, dev)
+    if k_cache.dim() != cache[0].dim() or k_cache.shape[:-1] != cache[0].shape[:-1]:
+        raise ValueError("the caches must have the same sequences, heads and capacity (or tokens and heads)")
+    if cache_start is None and length.numel() > 1 and src.seq_slots != to.seq_slots:
+        raise ValueError("the caches' sequences must lie as many slots apart, or cache_start be given")
+    if max_new is None:
+        max_new = cache[0].shape[-2 if cache[0].dim() == 4 else 0]
+    batch = _batch(dev, 1 << 22, new_start, length, max_new, max_len, cache_start, cache[0])     # no row arrays: any rows
+    _check(lib().qlin_unpack_four_bit(batch, src, to, 128, 1 if new_only else 0, _raw_stream(dev)))
+    return k_cache, v_cache
+
+
+def causal_attention_kv4(q, cache, new_start, length, max_new=None, max_len=None, cache_start=None, scale=0.0, splits=0,
+                         out=None, workspace=None):
+    """Causal attention over a 4-bit cache (qlin_causal_attention_four_bit in include/qlin_lowbit.h).
+
+    cache: the four tensors of ``new_kv4_cache``; the other arguments as for
+    ``causal_attention``, where max_len also bounds what is computed: rows of longer
+    sequences are zeros.  Returns ``out`` [rows, q heads, 128].
+    """
+    dev = _device()
+    return _attend(lib().qlin_causal_attention_four_bit, lib().qlin_causal_four_bit_plan, dev, _kv4_cache(cache, dev), cache[0], q,
+                   new_start, length, max_new, max_len, cache_start, scale, splits, out, workspace)
+
+
+def _rows_of(name, t, dtype, dev, rows=None, width=None):
+    """(address, elements between rows) of a tensor [rows, width] with contiguous rows."""
+    at = _address(name, t, dtype, dev)
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (width is not None and t.shape[1] != width):
+        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {'width' if width is None else width}]")
+    row, one = t.stride()
+    if one != 1 and t.shape[1] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return at, row if t.shape[0] > 1 else t.shape[1]
+
+
+def block_norm(y, residual, norm=None, post_norm=None, gate=None, sigmoid=False, scale=1.0, eps=1e-6, out=None,
+               residual_out=None):
+    """The norms around a block with its gate and the residual (qlin_block_norm in
+    include/qlin_lowbit.h): residual + scale * norm(y, post_norm) * gate, and its norm.
+
+    y, residual: CUDA bf16 [rows, width], row slices allowed; y None: the residual as it is.
+    norm, post_norm: bf16 [width] or None; gate: bf16 [rows, width] or [width], or None
+    (``sigmoid``: its logistic function).  Returns (out, residual_out): the second norm (None
+    without ``norm``) and the new residual; either may be given, also y or residual themselves.
+    """
+    dev = _device()
+    bf16 = _torch.bfloat16
+    res_at, res_stride = _rows_of("residual", residual, bf16, dev)
+    rows, width = residual.shape
+    y_at = out_at = new_at = gate_at = None
+    y_stride = out_stride = new_stride = gate_stride = 0
+    if y is None:
+        if residual_out is not None:
+            raise ValueError("without y there is no new residual")
+        residual_out = residual
+    else:
+        y_at, y_stride = _rows_of("y", y, bf16, dev, rows, width)
+        if residual_out is None:
+            residual_out = _torch.empty((rows, width), dtype=bf16, device=residual.device)
+            new_at, new_stride = residual_out.data_ptr(), width
+        else:
+            new_at, new_stride = _rows_of("residual_out", residual_out, bf16, dev, rows, width)
+    if norm is not None:
+        if out is None:
+            out = _torch.empty((rows, width), dtype=bf16, device=residual.device)
+            out_at, out_stride = out.data_ptr(), width
+        else:
+            out_at, out_stride = _rows_of("out", out, bf16, dev, rows, width)
+    elif out is not None:
+        raise ValueError("out needs norm")
+    if gate is not None:
+        if gate.dim() == 1:
+            gate_at = _vector("gate", gate, bf16, dev, width)
+        else:
+            gate_at, gate_stride = _rows_of("gate", gate, bf16, dev, rows, width)
+    _check(lib().qlin_block_norm(rows, width, y_at, y_stride, res_at, res_stride, _vector("post_norm", post_norm, bf16, dev, width),
+                                 gate_at, gate_stride, 1 if sigmoid else 0, scale, _vector("norm", norm, bf16, dev, width), eps,
+                                 new_at, new_stride, out_at, out_stride, _raw_stream(dev)))
+    return out, residual_out
+
+
+def quantize_tokens(x, gated=False, codes=None, scale=None):
+    """8-bit integers with one scale a row (qlin_quantize_tokens in include/qlin_lowbit.h).
+
+    x: CUDA bf16 [rows, width], row slices allowed; ``gated``: [rows, 2 width], whose halves a, b
+    give silu(a) b.  Returns (codes int8 [rows, width], scale float32 [rows]).
+    """
+    dev = _device()
+    x_at, x_stride = _rows_of("x", x, _torch.bfloat16, dev)
+    rows, width = x.shape
+    if gated:
+        if width % 2:
+            raise ValueError("x must be [rows, 2 width]")
+        width //= 2
+    if codes is None:
+        codes = _torch.empty((rows, width), dtype=_torch.int8, device=x.device)
+        codes_at, codes_stride = codes.data_ptr(), width
+    else:
+        codes_at, codes_stride = _rows_of("codes", codes, _torch.int8, dev, rows, width)
+    if scale is None:
+        scale = _torch.empty(rows, dtype=_torch.float32, device=x.device)
+    _check(lib().qlin_quantize_tokens(rows, width, x_at, x_stride, 1 if gated else 0, codes_at, codes_stride,
+                                      _vector("scale", scale, _torch.float32, dev, rows), _raw_stream(dev)))
+    return codes, scale
+
+
+def linear_i8(x, x_scale, w, w_scale, splits=0, out=None, workspace=None):
+    """y = (x . w^T) x_scale w_scale in 8-bit integers (qlin_eight_bit_linear in include/qlin_lowbit.h).
+
+    x: CUDA int8 [M, K] and x_scale float32 [M] (``quantize_tokens``); w: int8 [N, K] and
+    w_scale float32 [N], a scale for each channel; row slices allowed.  ``workspace`` (a CUDA
+    tensor of at least the planned bytes) is allocated when needed and not given.  Returns bf16
+    [M, N].
+    """
+    dev = _device()
+    i8, f32 = _torch.int8, _torch.float32
+    x_at, x_stride = _rows_of("x", x, i8, dev)
+    M, K = x.shape
+    w_at, w_stride = _rows_of("w", w, i8, dev, None, K)
+    N = w.shape[0]
+    if workspace is None:
+        size = M, N, K, splits, dev, i8
+        need = _scratch_bytes.get(size)
+        if need is None:
+            need = _remember(size, qlin_eight_bit_plan(M, N, K, splits)[1])
+        if need:
+            workspace = _torch.empty(need, dtype=_torch.uint8, device=x.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
+    if out is None:
+        # rows a multiple of 8 elements apart
+        out = _torch.empty((M, (N + 7) // 8 * 8), dtype=_torch.bfloat16, device=x.device)[:, :N]
+        out_at, out_stride = out.data_ptr(), (N + 7) // 8 * 8
+    else:
+        out_at, out_stride = _rows_of("out", out, _torch.bfloat16, dev, M, N)
+        if M == 1:
+            out_stride = (N + 7) // 8 * 8
+    _check(lib().qlin_eight_bit_linear(M, N, K, splits, x_at, x_stride, _vector("x_scale", x_scale, f32, dev, M), w_at, w_stride,
+                                _vector("w_scale", w_scale, f32, dev, N), out_at, out_stride, *_scratch(workspace),
+                                _raw_stream(dev)))
+    return out
 
 
 def verify_draft(target, drafted, uniform, draft=None, n_draft=None, temperature=None, accepted=None, tokens=None,

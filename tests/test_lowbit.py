@@ -1,0 +1,285 @@
+"""GPU tests of block norms, 8-bit tokens and the 8-bit linear (include/qlin_lowbit.h)
+against the oracle, through the Python entry points.
+
+Tolerances, derived (bf16 rounds by at most half a step, 2^-8 of the value; fp32 by 2^-24):
+* norms: a squares' sum of up to 8192 values is at most 64 additions a lane and 16 across
+  them, 80 x 2^-24 < 2^-17, half of that in its root; with square root, division and three
+  products 2^-17 of the value.  The logistic function takes e^-g from the base-2
+  exponential of a rounded product: 2^-24 |g| log2(e) ln 2 and 2 ulp, so (|g| + 8) 2^-23.
+* tokens and the linear's outputs of given tokens are whole numbers and roundings of exact
+  sums: equal, bit for bit.
+* gated tokens: v has a relative error of 2^-21 (exponential, sum, quotient, product), so
+  scale too, and codes differ from v / scale by half and 127 (2^-21 + 2^-21 + 2^-23).
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import lowbit_ref as ref
+from paper_2607_04244_amd import qlin
+
+pytestmark = pytest.mark.gpu
+
+
+def rand(seed, shape, sigma=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (sigma * torch.randn(shape, generator=g)).to(torch.bfloat16)
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def strided(t, pad):
+    """A device copy of rows with `pad` more elements between them."""
+    wide = torch.full((t.shape[0], t.shape[1] + pad), 5, dtype=t.dtype)
+    wide[:, :t.shape[1]] = t
+    return wide.cuda()[:, :t.shape[1]]
+
+
+# ---------------------------------------------------------------- block norms
+
+
+def check_norm(rows, width, post=True, pre=True, gate=None, sigmoid=False, scale=1.0, eps=1e-6, pad=0, into="new", seed=0, y=None, sigma=1.5):
+    y = rand(seed, (rows, width), sigma) if y is None else y
+    res = rand(seed + 1, (rows, width), 3.0)
+    wp, w = 1 + rand(seed + 2, (width,), 0.2), 1 + rand(seed + 3, (width,), 0.2)
+    g = None if gate is None else rand(seed + 4, (rows, width) if gate == "rows" else (width,), 2.0)
+    dy, dr = strided(y, pad), strided(res, pad)
+    dg = None if g is None else strided(g, pad) if g.dim() == 2 else g.cuda()
+    kw = {}
+    if into == "inputs":                       # the new residual on the old one, the norm on y
+        kw = dict(residual_out=dr, **(dict(out=dy) if pre else {}))
+    elif into == "crossed":
+        kw = dict(residual_out=dy, **(dict(out=dr) if pre else {}))
+    out, h = qlin.block_norm(dy, dr, w.cuda() if pre else None, post_norm=wp.cuda() if post else None, gate=dg, sigmoid=sigmoid,
+                             scale=scale, eps=eps, **kw)
+    torch.cuda.synchronize()
+    want, t = ref.block_norm(f64(y), f64(res), f64(wp) if post else None, None if g is None else f64(g), sigmoid, scale, eps)
+    rel = 2.0 ** -17 + ((np.abs(f64(g)) + 8) * 2.0 ** -23 if sigmoid else 0.0)
+    tol = 2.0 ** -8 * np.abs(want) + 2 * rel * np.abs(t) + 2.0 ** -23 * np.abs(f64(res)) + 1e-38
+    assert np.all(np.abs(f64(h) - want) <= tol)
+    if not pre:
+        assert out is None
+        return
+    want = ref.norm(f64(h), f64(w), eps)       # of the residual stream as it is stored
+    assert np.all(np.abs(f64(out) - want) <= (2.0 ** -8 + 2.0 ** -17) * np.abs(want) + 1e-38)
+
+
+@pytest.mark.parametrize("rows,width", [(1, 2560), (1, 8), (3, 64), (16, 2560), (7, 2568), (5, 520), (2, 9728), (1, 16384), (2047, 512), (2048, 512),
+                                        (2049, 2560), (2051, 1032), (2050, 8), (2048, 4096), (2049, 4104), (1, 65536), (3, 20480)])
+def test_norm_sizes(rows, width):
+    check_norm(rows, width, gate="rows", sigmoid=True, scale=0.5, seed=width)
+
+
+@pytest.mark.parametrize("rows,width", [(9, 2560), (2100, 640)])
+@pytest.mark.parametrize("kw", [dict(post=False), dict(pre=False), dict(post=False, pre=False), dict(gate="rows"), dict(gate="channel"),
+                                dict(gate="channel", sigmoid=True), dict(scale=0.0), dict(scale=-0.25), dict(eps=0.0), dict(eps=3.0), dict(pad=8),
+                                dict(pad=24, gate="rows"), dict(into="inputs"), dict(into="inputs", pad=16, gate="rows"), dict(into="crossed"),
+                                dict(into="inputs", pre=False)])
+def test_norm_forms(rows, width, kw):
+    check_norm(rows, width, seed=11, **kw)
+
+
+def test_norm_of_the_residual_alone():
+    res, w = rand(0, (5, 2560), 3.0), 1 + rand(1, (2560,), 0.2)
+    d = res.cuda()
+    out, h = qlin.block_norm(None, d, w.cuda())
+    torch.cuda.synchronize()
+    assert h is d and torch.equal(d.cpu(), res)
+    want = ref.norm(f64(res), f64(w), 1e-6)
+    assert np.all(np.abs(f64(out) - want) <= (2.0 ** -8 + 2.0 ** -17) * np.abs(want))
+
+
+@pytest.mark.parametrize("rows", [4, 2050])
+def test_norm_rows_are_apart(rows):
+    """Zero rows stay zero, an infinity or NaN stays in its row."""
+    y, res = torch.zeros((rows, 512), dtype=torch.bfloat16), torch.zeros((rows, 512), dtype=torch.bfloat16)
+    y[1, 3], y[2, 5], res[3, 7] = float("inf"), float("nan"), float("inf")
+    w = torch.ones(512, dtype=torch.bfloat16, device="cuda")
+    out, h = qlin.block_norm(y.cuda(), res.cuda(), w, post_norm=w)
+    torch.cuda.synchronize()
+    assert torch.all(out[0] == 0) and torch.all(h[0] == 0) and torch.all(out[4:] == 0)
+    for m in (1, 2, 3):
+        assert not torch.isfinite(out[m]).all()
+
+
+def test_norm_no_rows():
+    e = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
+    out, h = qlin.block_norm(e, e, torch.ones(64, dtype=torch.bfloat16, device="cuda"))
+    assert out.shape == h.shape == (0, 64)
+
+
+# ---------------------------------------------------------------- tokens
+
+
+@pytest.mark.parametrize("rows,width", [(1, 16), (1, 2560), (16, 9728), (5, 48), (3, 65536), (2048, 4096), (2049, 528), (2050, 16), (2048, 4112)])
+@pytest.mark.parametrize("pad", [0, 16])
+def test_tokens(rows, width, pad):
+    x = rand(width + rows, (rows, width), 2.0)
+    x[:, ::37] *= 16
+    codes, scale = qlin.quantize_tokens(strided(x, pad), codes=strided(torch.zeros((rows, width), dtype=torch.int8), pad))
+    torch.cuda.synchronize()
+    want, sw = ref.quantize_tokens(f64(x))
+    assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scale.cpu().numpy(), sw)
+
+
+@pytest.mark.parametrize("rows,width", [(1, 16), (7, 9728), (2050, 528), (333, 2560)])
+def test_gated_tokens(rows, width):
+    x = rand(width, (rows, 2 * width), 3.0)
+    x[0, :4] = torch.tensor([-120.0, 60.0, -2e4, 90.0])
+    codes, scale = qlin.quantize_tokens(x.cuda(), gated=True)
+    torch.cuda.synchronize()
+    v = ref.silu_product(f64(x))
+    sw = np.abs(v).max(axis=1) / 127
+    s = f64(scale)
+    assert np.all(np.abs(s - sw) <= 2.0 ** -20 * sw)
+    assert np.all(np.abs(codes.cpu().numpy() - v / sw[:, None]) <= 0.5 + 127 * (2.0 ** -20 + 2.0 ** -23))
+    assert np.all(np.abs(codes.cpu().numpy()).max(axis=1) == 127)
+
+
+def test_tokens_at_the_ends_of_the_range():
+    x = torch.zeros((10, 32), dtype=torch.bfloat16)
+    x[1, 2], x[2, 3], x[3, 4] = float("inf"), float("nan"), float("-inf")
+    x[4, 0], x[4, 1] = 3.3e38, -3.3e38
+    x[5, 0], x[5, 1] = 2.0 ** -100, 2.0 ** -107
+    x[6, 0] = 2.0 ** -101
+    x[7] = torch.arange(32).to(torch.bfloat16) - 16
+    x[8, 0], x[8, 1:] = 127.0, torch.arange(31).to(torch.bfloat16) + 0.5            # ties
+    x[9, 0] = -1e-20
+    codes, scale = qlin.quantize_tokens(x.cuda())
+    torch.cuda.synchronize()
+    want, sw = ref.quantize_tokens(f64(x))
+    assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scale.cpu().numpy(), sw, equal_nan=True)
+
+
+# ---------------------------------------------------------------- the linear
+
+
+def check_linear(M, N, K, splits=0, pad=0, seed=0, edge=False):
+    g = torch.Generator().manual_seed(seed + M + N + K)
+    x, w = (torch.randint(-127, 128, (n, K), generator=g, dtype=torch.int8) for n in (M, N))
+    if edge:                                   # the largest sums
+        x.fill_(-128)
+        w.fill_(-128)
+        w[::2] = 127
+    sx, sw = (0.001 + torch.rand(n, generator=g) for n in (M, N))
+    out = torch.full((M, (N + 7) // 8 * 8 + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = qlin.linear_i8(strided(x, pad), sx.cuda(), strided(w, pad), sw.cuda(), splits=splits, out=out[:, :N])
+    torch.cuda.synchronize()
+    assert got.shape == (M, N) and torch.all(out[:, N:] == 7.0)
+    assert np.array_equal(f64(got), ref.linear_i8(x.numpy(), sx.numpy(), w.numpy(), sw.numpy()))
+
+
+@pytest.mark.parametrize("M", [1, 2, 15, 16, 17, 31, 33, 64, 65, 100, 128, 129, 257])
+@pytest.mark.parametrize("N,K", [(1, 16), (16, 64), (7, 80), (130, 1008), (257, 560), (1000, 144)])
+def test_linear_sizes(M, N, K):
+    check_linear(M, N, K)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 2560, 4096), (16, 2560, 2560), (5, 4100, 9728), (48, 1024, 2560), (300, 520, 9728), (512, 2560, 2560)])
+def test_linear_of_layers(M, N, K):
+    check_linear(M, N, K, pad=16)
+
+
+@pytest.mark.parametrize("splits", [1, 2, 3, 7, 64])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 2560), (20, 100, 528), (130, 140, 1040), (300, 129, 4096), (70, 16, 16)])
+def test_linear_forced_splits(M, N, K, splits):
+    check_linear(M, N, K, splits=splits, pad=32)
+
+
+@pytest.mark.parametrize("M", [3, 40, 70])
+def test_linear_largest_sums(M):
+    check_linear(M, 33, 131056, edge=True)
+
+
+def test_linear_default_output_and_no_rows():
+    x, w = torch.ones((3, 32), dtype=torch.int8, device="cuda"), torch.ones((5, 32), dtype=torch.int8, device="cuda")
+    sx, sw = torch.ones(3, device="cuda"), torch.full((5,), 0.5, device="cuda")
+    y = qlin.linear_i8(x, sx, w, sw)
+    assert y.shape == (3, 5) and torch.all(y == 16.0)
+    assert qlin.linear_i8(x[:0], sx[:0], w, sw).shape == (0, 5)
+
+
+def test_linear_of_a_row_without_numbers():
+    """A token with scale NaN gives NaN, its neighbours do not see it."""
+    x = rand(0, (3, 64))
+    x[1, 5] = float("nan")
+    codes, scale = qlin.quantize_tokens(x.cuda())
+    w = torch.randint(-127, 128, (20, 64), dtype=torch.int8, device="cuda")
+    y = qlin.linear_i8(codes, scale, w, torch.ones(20, device="cuda"))
+    assert torch.isnan(y[1]).all() and torch.isfinite(y[[0, 2]]).all()
+
+
+def test_linear_forced_workspace():
+    M, N, K, S = 70, 96, 1024, 4
+    need = qlin.qlin_eight_bit_plan(M, N, K, S)[1]
+    assert need == S * M * N * 4
+    x, w = torch.ones((M, K), dtype=torch.int8, device="cuda"), torch.ones((N, K), dtype=torch.int8, device="cuda")
+    one = torch.ones(max(M, N), device="cuda")
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    assert torch.all(qlin.linear_i8(x, one[:M], w, one[:N], splits=S, workspace=ws) == K)
+    with pytest.raises(qlin.QlinError):
+        qlin.linear_i8(x, one[:M], w, one[:N], splits=S, workspace=ws[:-16])
+
+
+def test_binding_checks():
+    x, w, s = torch.ones((2, 32), dtype=torch.int8, device="cuda"), torch.ones((4, 32), dtype=torch.int8, device="cuda"), torch.ones(4, device="cuda")
+    for args in [(x.cpu(), s[:2], w, s), (x.float(), s[:2], w, s), (x, s, w, s), (x, s[:2], w[:, :16], s), (x, s[:2], w, s.double()), (x[0], s[:2], w, s),
+                 (x.t(), s[:2], w, s)]:
+        with pytest.raises(ValueError):
+            qlin.linear_i8(*args)
+    b = torch.ones((2, 32), dtype=torch.bfloat16, device="cuda")
+    n = torch.ones(32, dtype=torch.bfloat16, device="cuda")
+    for kw in [dict(out=b[:1]), dict(residual_out=b.float()), dict(gate=b[:, :16]), dict(post_norm=n[:16]), dict(gate=n.cpu())]:
+        with pytest.raises(ValueError):
+            qlin.block_norm(b, b.clone(), n, **kw)
+    with pytest.raises(ValueError):
+        qlin.block_norm(b, b.clone(), out=b)
+    with pytest.raises(ValueError):
+        qlin.quantize_tokens(b[:, :15], gated=True)
+    with pytest.raises(ValueError):
+        qlin.quantize_tokens(b, scale=s.double()[:2])
+
+
+def test_in_graphs_and_on_streams():
+    """A block's end, quantization and a linear with K ranges: captured and replayed on new inputs
+    with eager work between, two graphs sharing a workspace, and eager on two streams at once."""
+    M, K, N, S = 70, 2560, 200, 3
+    y, res = rand(0, (M, K)).cuda(), rand(1, (M, K)).cuda()
+    w, wn = torch.randint(-127, 128, (N, K), dtype=torch.int8, device="cuda"), torch.ones(K, dtype=torch.bfloat16, device="cuda")
+    sw = torch.rand(N, device="cuda")
+    ws = torch.empty(qlin.qlin_eight_bit_plan(M, N, K, S)[1], dtype=torch.uint8, device="cuda")
+
+    def step(y, workspace):
+        x, h = qlin.block_norm(y, res, wn, post_norm=wn)
+        codes, scale = qlin.quantize_tokens(x)
+        return qlin.linear_i8(codes, scale, w, sw, splits=S, workspace=workspace), h
+
+    other = rand(2, (M, K)).cuda()
+    step(y, ws)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for src in (y, other):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(src, ws))
+        graphs.append(g)
+    for i in range(4):
+        y.copy_(rand(10 + i, (M, K)))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for src, got in zip((y, other), outs):
+            want = step(src, None)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    results = []
+    torch.cuda.synchronize()
+    for s, src in zip(streams * 3, [y, other] * 3):
+        with torch.cuda.stream(s):
+            results.append(step(src, None))
+    torch.cuda.synchronize()
+    for got, src in zip(results, [y, other] * 3):
+        assert torch.equal(got[0], step(src, None)[0])
