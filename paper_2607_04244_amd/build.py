@@ -21,7 +21,7 @@ LIB = os.path.join(HERE, "libqlin.so")
 SOURCES = [("kernels.hip", []), ("tiled.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]),
            ("mid.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]), ("attn.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]),
            ("append.hip", []), ("causal.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]), ("verify.hip", []),
-           ("norm.hip", []), ("linear8.hip", []), ("kv4.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]),
+           ("norm.hip", []), ("linear8.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]), ("kv4.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]),
            ("qlin.cpp", []), ("attn_abi.cpp", []), ("target_abi.cpp", []), ("lowbit_abi.cpp", [])]
 HOST_SOURCES = ("qlin.cpp", "attn_abi.cpp", "target_abi.cpp", "lowbit_abi.cpp")       # no device code: plain C++ against the HIP headers
 LIB_ASAN = os.path.join(HERE, "libqlin_asan.so")

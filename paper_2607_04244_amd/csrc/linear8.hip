@@ -5,12 +5,19 @@
 // cores, exact in any order, so K is cut freely over waves and workgroups.  The weights are
 // the A operand, the tokens B: a lane's results are four channels of one token at a time.
 //
-//   k_i8_few<MT>   up to 16 MT rows: bound by the weights' bytes.  A workgroup has 16 channels,
-//       its waves a part of K each, read straight into the operands' registers.
-//   k_i8_tile      128 x 128 outputs, K 128 at a time through LDS: bound by the matrix cores.
-//   k_i8_join      adds K ranges' sums and scales them.
+//   k_i8_few<MT, NS>  up to 16 MT rows: bound by the weights' bytes.  Eight waves share K, each
+//       reads its part of 16 channels straight into the operand's registers.  16 x 2560 x 19456
+//       (rows, K, channels) 14.2 us, 3.55 TB/s, where a plain read of the weights takes 11.0;
+//       1 x 4096 x 2560 4.9 us, the launch and one trip to memory.
+//   k_i8_tile      tiles of 64 x 128 to 256 x 320 outputs through LDS: bound by the matrix cores and
+//       LDS reads between them, and by the clock, which falls under them.  8192 x 8192 x 8192 532
+//       us, 2065 TOP/s (the library's product 2050); 2048 x 2560 x 19456 136.5 us, 1495 TOP/s
+//       (122): 488 tiles on 256 units.
+//   k_i8_tile_join, k_i8_join   add K ranges' sums and scale them.
 #include "target_common.h"
 #include "lowbit_internal.h"
+
+#include <type_traits>
 
 namespace qlin {
 
@@ -19,154 +26,266 @@ namespace {
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
 
+__device__ inline void load_lds_a16(const int8_t *src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds), "v"(src) : "memory", "m0");
+}
+
 __device__ inline v4i load16(const int8_t *p) { return *(const v4i *)p; }
-__device__ inline v4i load16_nt(const int8_t *p) { return __builtin_nontemporal_load((const v4i *)p); }
 
 __device__ inline float scaled(int sum, float sx, float sw) { return (float)sum * (sx * sw); }
 
+// Four channels of a token.
+__device__ inline void store4(const I8Args &a, int m, int n, float sx, const v4i &sum) {
+    uint16_t *y = a.y + (int64_t)m * a.y_stride + n;
+    if (n + 3 < a.N) {
+        *(uint2 *)y = make_uint2(cvt_pk_bf16(scaled(sum[0], sx, a.w_scale[n]), scaled(sum[1], sx, a.w_scale[n + 1])),
+                                 cvt_pk_bf16(scaled(sum[2], sx, a.w_scale[n + 2]), scaled(sum[3], sx, a.w_scale[n + 3])));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (n + e < a.N) y[e] = cvt_bf16(scaled(sum[e], sx, a.w_scale[n + e]));
+}
+
 // ---------------------------------------------------------------- few rows
 
-constexpr int kFewWaves = 8, kFewBatch = 8;          // steps of 64 bytes requested together
+constexpr int kFewWaves = kI8FewWaves, kFewBatch = 8;          // steps of 64 bytes requested together
+constexpr int kFewGroups = 256;                      // one a compute unit
 
-template <int MT>
+// Not read with the hint that data is read once: 15.3 us with it, 14.2 without, as the 64 bytes of a
+// row that a load takes are half a cache line.  One workgroup a compute unit walks several
+// channel tiles: two units' worth 16.1 us, each tile its own workgroup 18.2.
+// NS > 0: a wave's part of K is at most NS steps; its part of the tokens stays in registers
+// while the workgroup walks channel tiles, whose weights are requested a tile ahead.  NS = 0:
+// any K, both operands in batches.
+template <int MT, int NS>
 __global__ __launch_bounds__(kFewWaves * 64) void k_i8_few(I8Args a) {
-    __shared__ v4i part[kFewWaves][MT][64];
+    __shared__ v4i part[2][kFewWaves][MT][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int g = lane >> 4, r = lane & 15;
-    const int n0 = blockIdx.x * 16, all = (a.K + kI8FewStep - 1) / kI8FewStep;
+    const int all = (a.K + kI8Step - 1) / kI8Step;
     const int first = blockIdx.y * a.steps, end = min(first + a.steps, all);
     const int per = (end - first + kFewWaves - 1) / kFewWaves;
     const int s0 = first + wave * per, s1 = min(s0 + per, end);
 
-    const int8_t *wp = a.w + (int64_t)min(n0 + r, a.N - 1) * a.w_stride + 16 * g;
     const int8_t *xp[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) xp[t] = a.x + (int64_t)min(16 * t + r, a.M - 1) * a.x_stride + 16 * g;
-    v4i acc[MT];
+    auto w_at = [&](int tile) { return a.w + (int64_t)min(16 * tile + r, a.N - 1) * a.w_stride + 16 * g; };
+    auto inside = [&](int s) { return s < s1 && s * kI8Step + 16 * g < a.K; };
+    constexpr int B = NS ? NS : kFewBatch;
+    v4i wv[B], xv[B][MT];
+    auto load_w = [&](const int8_t *wp, int s) {
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = v4i{0, 0, 0, 0};
-    for (int s = s0; s < s1; s += kFewBatch) {
-        v4i wv[kFewBatch], xv[kFewBatch][MT];
+        for (int i = 0; i < B; ++i) wv[i] = inside(s + i) ? load16(wp + (s + i) * kI8Step) : v4i{0, 0, 0, 0};
+    };
+    auto load_x = [&](int s) {
 #pragma unroll
-        for (int i = 0; i < kFewBatch; ++i) {
-            const int k = (s + i) * kI8FewStep;
-            wv[i] = v4i{0, 0, 0, 0};                 // past the range or K
-            if (s + i < s1 && k + 16 * g < a.K) {
-                wv[i] = load16_nt(wp + k);
+        for (int i = 0; i < B; ++i)
 #pragma unroll
-                for (int t = 0; t < MT; ++t) xv[i][t] = load16(xp[t] + k);
-            } else {
+            for (int t = 0; t < MT; ++t) xv[i][t] = inside(s + i) ? load16(xp[t] + (s + i) * kI8Step) : v4i{0, 0, 0, 0};
+    };
+    int buffer = 0;
+    if (NS) {
+        load_w(w_at(blockIdx.x), s0);
+        load_x(s0);
+    }
+    for (int tile = blockIdx.x; tile < a.tiles_n; tile += gridDim.x, buffer ^= 1) {
+        v4i acc[MT];
 #pragma unroll
-                for (int t = 0; t < MT; ++t) xv[i][t] = v4i{0, 0, 0, 0};
+        for (int t = 0; t < MT; ++t) acc[t] = v4i{0, 0, 0, 0};
+        auto multiply = [&](const v4i *w) {
+#pragma unroll
+            for (int i = 0; i < B; ++i)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], xv[i][t], acc[t], 0, 0, 0);
+        };
+        if constexpr (NS > 0) {
+            v4i now[B];
+#pragma unroll
+            for (int i = 0; i < B; ++i) now[i] = wv[i];
+            if (tile + (int)gridDim.x < a.tiles_n) load_w(w_at(tile + gridDim.x), s0);
+            multiply(now);
+        } else {
+            for (int s = s0; s < s1; s += B) {
+                load_w(w_at(tile), s);
+                load_x(s);
+                multiply(wv);
             }
         }
 #pragma unroll
-        for (int i = 0; i < kFewBatch; ++i)
+        for (int t = 0; t < MT; ++t) part[buffer][wave][t][lane] = acc[t];
+        lds_barrier();
+        // an output a thread: channel fastest
+        for (int e = threadIdx.x; e < 256 * MT; e += kFewWaves * 64) {
+            const int n = 16 * tile + (e & 15), m = e >> 4;
+            int sum = 0;
 #pragma unroll
-            for (int t = 0; t < MT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[i], xv[i][t], acc[t], 0, 0, 0);
+            for (int i = 0; i < kFewWaves; ++i) sum += ((const int *)&part[buffer][i][m >> 4][(m & 15) + 16 * ((e & 15) >> 2)])[e & 3];
+            if (m >= a.M || n >= a.N) continue;
+            if (a.S > 1) a.parts[((int64_t)blockIdx.y * a.M + m) * a.N + n] = sum;
+            else a.y[(int64_t)m * a.y_stride + n] = cvt_bf16(scaled(sum, a.x_scale[m], a.w_scale[n]));
+        }
     }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
-    __syncthreads();
-    // an output a thread: channel fastest
-    for (int e = threadIdx.x; e < 256 * MT; e += kFewWaves * 64) {
-        const int n = e & 15, m = e >> 4;
-        int sum = 0;
-#pragma unroll
-        for (int i = 0; i < kFewWaves; ++i) sum += ((const int *)&part[i][m >> 4][(m & 15) + 16 * (n >> 2)])[n & 3];
-        if (m >= a.M || n0 + n >= a.N) continue;
-        if (a.S > 1) a.parts[((int64_t)blockIdx.y * a.M + m) * a.N + n0 + n] = sum;
-        else a.y[(int64_t)m * a.y_stride + n0 + n] = cvt_bf16(scaled(sum, a.x_scale[m], a.w_scale[n0 + n]));
-    }
+}
+
+template <int MT>
+void launch_few(const I8Args &a, int per_wave, hipStream_t st) {
+    const dim3 threads(kFewWaves * 64);
+    const int rounds = (a.tiles_n * a.S + kFewGroups - 1) / kFewGroups;
+    const dim3 grid((a.tiles_n + rounds - 1) / rounds, a.S), each(a.tiles_n, a.S);
+    constexpr int most = i8_few_steps(16 * MT);
+    if (per_wave <= 5) hipLaunchKernelGGL((k_i8_few<MT, 5>), grid, threads, 0, st, a);
+    else if (most >= 8 && per_wave <= 8) hipLaunchKernelGGL((k_i8_few<MT, most >= 8 ? 8 : 0>), grid, threads, 0, st, a);
+    else if (per_wave <= most) hipLaunchKernelGGL((k_i8_few<MT, most>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((k_i8_few<MT, 0>), each, threads, 0, st, a);
 }
 
 // ---------------------------------------------------------------- many rows
 
-constexpr int kTileThreads = 256;
-
-// Rows of 128 bytes in LDS, their 16-byte units in an order that changes every two rows: one
+// 64-byte steps of K through a ring of ST stages in LDS, filled ST - 1 steps ahead by
+// direct-to-LDS loads; one barrier a step.  WN x WM products of 32 x 32 a wave, GN x GM waves: at
+// 256 x 256 outputs LDS reads and products of a step take about as long, 4 waves of 128 x 128
+// instead of 8 of 128 x 64 read less and wait more (602 us for 8192 x 8192 x 8192 against 572).
+// A step's first fragments are read during the last products of the step before, so that a
+// wave alone on its SIMD does not wait for them.
+// Rows of 64 bytes in LDS, their 16-byte units in an order that changes every four rows: one
 // unit of 16 rows, which lanes read together, meets different banks.
-__device__ inline int tile_unit(int row, int u) { return row * 8 + (u ^ ((row >> 1) & 7)); }
+__device__ inline int tile_unit(int row, int u) { return row * 4 + (u ^ ((row >> 2) & 3)); }
 
-__global__ __launch_bounds__(kTileThreads, 2) void k_i8_tile(I8Args a) {
-    constexpr int T = kI8Tile, U = T * kI8TileStep / 16;                       // units of one operand's stage
-    __shared__ __attribute__((aligned(16))) uint4 ring[2][2][U];                // [stage][w, x]
+// Workgroup b's tile.  Workgroups go to the 8 XCDs in turn; each XCD takes a contiguous part of
+// the tiles, eight of the tokens' by all of the channels', tokens fastest: what runs at once on
+// an XCD shares rows of both operands in its L2.
+__device__ inline void tile_of(const I8Args &a, int b, int &tm, int &tn) {
+    const int tiles = a.tiles_m * a.tiles_n, x = b & 7, whole = tiles >> 3, rest = tiles & 7;
+    const int t = x * whole + min(x, rest) + (b >> 3), band = t / (8 * a.tiles_n), in = t - band * 8 * a.tiles_n;
+    const int rows = min(8, a.tiles_m - 8 * band);
+    tn = in / rows;
+    tm = 8 * band + in - tn * rows;
+}
+
+template <int WN, int WM, int GN, int GM, int ST, int PER_CU>
+__global__ __launch_bounds__(GN * GM * 64, GN * GM * PER_CU / 4) void k_i8_tile(I8Args a) {
+    constexpr int TN = 32 * WN * GN, TM = 32 * WM * GM, W = GN * GM;
+    constexpr int L = ((TN + TM) / 16 + W - 1) / W;                                 // loads of a wave a step
+    __shared__ __attribute__((aligned(16))) uint4 ring[ST][L * W * 64];             // rows of w, then of x (the last one again)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int hi = lane >> 5, r = lane & 31;
-    const int n0 = (int)(blockIdx.x % (unsigned)a.tiles_n) * T, m0 = (int)(blockIdx.x / (unsigned)a.tiles_n) * T;
-    const int all = (a.K + kI8TileStep - 1) / kI8TileStep;
+    int tm, tn;
+    tile_of(a, blockIdx.x, tm, tn);
+    const int n0 = tn * TN, m0 = tm * TM;
+    const int all = (a.K + kI8Step - 1) / kI8Step;
     const int first = blockIdx.y * a.steps, end = min(first + a.steps, all);
 
-    // a wave loads 8 rows at a time, 4 times, of each operand
-    const int lr = lane >> 3, lu = lane & 7;
-    const int8_t *src[2][4];
-    int unit[4];
+    // load i of a wave: rows 16 (wave + W i) .. + 15 of the stage, four lanes a row
+    const int8_t *src[L];
+    const int unit = (lane & 3) ^ ((lane >> 4) & 3);                                // its place's unit: rows are multiples of 16
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int row = 8 * (4 * wave + j) + lr;
-        unit[j] = lu ^ ((row >> 1) & 7);
-        src[0][j] = a.w + (int64_t)min(n0 + row, a.N - 1) * a.w_stride;
-        src[1][j] = a.x + (int64_t)min(m0 + row, a.M - 1) * a.x_stride;
+    for (int i = 0; i < L; ++i) {
+        const int row = 16 * (wave + W * i) + (lane >> 2);
+        src[i] = row < TN ? a.w + (int64_t)min(n0 + row, a.N - 1) * a.w_stride : a.x + (int64_t)min(m0 + row - TN, a.M - 1) * a.x_stride;
     }
+    const uint32_t lds = lds_addr(ring) + wave * 1024;
     auto issue = [&](int s) {
-        const int k = s * kI8TileStep, st = s & 1;
+        const int at = s * kI8Step + 16 * unit;                                     // past K: the row's first unit, left out below
+        const uint32_t to = lds + (uint32_t)((s - first) % ST) * (uint32_t)sizeof(ring[0]);
 #pragma unroll
-        for (int o = 0; o < 2; ++o)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int at = k + 16 * unit[j];                                // past K: its first unit, left out below
-                load_lds_x16(src[o][j] + (at < a.K ? at : 0), &ring[st][o][64 * (4 * wave + j)]);
-            }
+        for (int i = 0; i < L; ++i) load_lds_a16(src[i] + (at < a.K ? at : 0), to + i * W * 1024);
     };
-    const int wn = 64 * (wave & 1), wm = 64 * (wave >> 1);
-    v16i acc[2][2];
+    const int wn = 32 * WN * (wave % GN), wm = TN + 32 * WM * (wave / GN);
+    v16i acc[WN][WM];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < WN; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < WM; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    if (first < end) issue(first);
-    for (int s = first; s < end; ++s) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        lds_barrier();                                                         // this stage is there, the other one read
-        if (s + 1 < end) issue(s + 1);
-        const uint4 *ws = ring[s & 1][0], *xs = ring[s & 1][1];
-        const bool partial = (s + 1) * kI8TileStep > a.K;
+    v4i wf[2][WN], xf[2][WM];
+    auto fragments = [&](int s, auto half) {                                        // 32 bytes of K
+        constexpr int h = decltype(half)::value;
+        const uint4 *st = ring[(s - first) % ST];
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            v4i wf[2], xf[2];
+        for (int i = 0; i < WN; ++i) wf[h][i] = __builtin_bit_cast(v4i, st[tile_unit(wn + 32 * i + r, 2 * h + hi)]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                wf[i] = __builtin_bit_cast(v4i, ws[tile_unit(wn + 32 * i + r, 2 * ks + hi)]);
-                xf[i] = __builtin_bit_cast(v4i, xs[tile_unit(wm + 32 * i + r, 2 * ks + hi)]);
-                if (partial && s * kI8TileStep + 16 * (2 * ks + hi) >= a.K) wf[i] = v4i{0, 0, 0, 0};
+        for (int j = 0; j < WM; ++j) xf[h][j] = __builtin_bit_cast(v4i, st[tile_unit(wm + 32 * j + r, 2 * h + hi)]);
+        if (s * kI8Step + 16 * (2 * h + 1) >= a.K) {                                // the last, partial step
+            const bool in = s * kI8Step + 16 * (2 * h + hi) < a.K;
+#pragma unroll
+            for (int i = 0; i < WN; ++i) wf[h][i] = in ? wf[h][i] : v4i{0, 0, 0, 0};
+        }
+    };
+    auto products = [&](auto half) {
+        constexpr int h = decltype(half)::value;
+#pragma unroll
+        for (int i = 0; i < WN; ++i)
+#pragma unroll
+            for (int j = 0; j < WM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[h][i], xf[h][j], acc[i][j], 0, 0, 0);
+    };
+    // step s has landed: the loads of the ST - 2 steps behind it may be in flight
+    auto landed = [&](int s) {
+        if (s + ST - 2 < end) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((ST - 2) * L) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+    };
+    typedef std::integral_constant<int, 0> Low;
+    typedef std::integral_constant<int, 1> High;
+    if (first < end) {
+#pragma unroll
+        for (int i = 0; i < ST - 1; ++i)
+            if (first + i < end) issue(first + i);
+        landed(first);
+        fragments(first, Low{});
+        for (int s = first; s < end; ++s) {
+            if (s + ST - 1 < end) issue(s + ST - 1);                                // where step s - 1 was, which every wave has read
+            fragments(s, High{});
+            products(Low{});
+            if (s + 1 < end) {
+                landed(s + 1);
+                fragments(s + 1, Low{});
             }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[i], xf[j], acc[i][j], 0, 0, 0);
+            products(High{});
         }
     }
+    if (a.S > 1) {                                          // in the matrix cores' order
+        v4i *to = (v4i *)a.parts + ((int64_t)(blockIdx.y * gridDim.x + blockIdx.x) * W + wave) * (WN * WM * 256) + lane;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int m = m0 + wm + 32 * j + r;
-        if (m >= a.M) continue;
-        const float sx = a.S > 1 ? 0.0f : a.x_scale[m];
+        for (int i = 0; i < WN; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < WM; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = n0 + wn + 32 * i + 8 * q + 4 * hi;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (n + e >= a.N) continue;
-                    const int sum = acc[i][j][4 * q + e];
-                    if (a.S > 1) a.parts[((int64_t)blockIdx.y * a.M + m) * a.N + n + e] = sum;
-                    else a.y[(int64_t)m * a.y_stride + n + e] = cvt_bf16(scaled(sum, sx, a.w_scale[n + e]));
-                }
-            }
+                for (int q = 0; q < 4; ++q)
+                    to[((i * WM + j) * 4 + q) * 64] = v4i{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        return;
     }
+#pragma unroll
+    for (int j = 0; j < WM; ++j) {
+        const int m = m0 + wm - TN + 32 * j + r;
+        if (m >= a.M) continue;
+        const float sx = a.x_scale[m];
+#pragma unroll
+        for (int i = 0; i < WN; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                store4(a, m, n0 + wn + 32 * i + 8 * q + 4 * hi, sx, v4i{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+    }
+}
+
+// A wave a 32 x 32 product's quarter (1 KiB of each range's sums), four channels of a token a lane.
+template <int WN, int WM, int GN, int GM>
+__global__ __launch_bounds__(256) void k_i8_tile_join(I8Args a) {
+    constexpr int W = GN * GM, P = W * WN * WM * 4;         // quarters of a tile
+    const int lane = threadIdx.x & 63, at = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int tile = at / P, p = at - tile * P, wave = p / (WN * WM * 4), ij = p / 4 % (WN * WM), q = p & 3;
+    int tm, tn;
+    tile_of(a, tile, tm, tn);
+    const int n = tn * (32 * WN * GN) + 32 * WN * (wave % GN) + 32 * (ij / WM) + 8 * q + 4 * (lane >> 5);
+    const int m = tm * (32 * WM * GM) + 32 * WM * (wave / GN) + 32 * (ij % WM) + (lane & 31);
+    if (m >= a.M || n >= a.N) return;
+    const v4i *from = (const v4i *)a.parts + (int64_t)at * 64 + lane;
+    const int64_t range = (int64_t)a.tiles_m * a.tiles_n * P * 64;
+    v4i sum = from[0];
+    for (int s = 1; s < a.S; ++s) sum += from[s * range];
+    store4(a, m, n, a.x_scale[m], sum);
 }
 
 __global__ __launch_bounds__(256) void k_i8_join(I8Args a) {
@@ -179,14 +298,30 @@ __global__ __launch_bounds__(256) void k_i8_join(I8Args a) {
     }
 }
 
+template <int WN, int WM, int GN, int GM, int ST, int PER_CU>
+hipError_t launch_tile(const I8Args &a, hipStream_t st) {
+    const unsigned tiles = (unsigned)(a.tiles_m * a.tiles_n);
+    hipLaunchKernelGGL((k_i8_tile<WN, WM, GN, GM, ST, PER_CU>), dim3(tiles, a.S), dim3(GN * GM * 64), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.S == 1) return e;
+    hipLaunchKernelGGL((k_i8_tile_join<WN, WM, GN, GM>), dim3(tiles * (GN * GM * WN * WM)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_i8_linear(const I8Args &a, hipStream_t st) {
-    const dim3 few((a.N + 15) / 16, a.S), threads(kFewWaves * 64);
-    if (a.M <= 16) hipLaunchKernelGGL(k_i8_few<1>, few, threads, 0, st, a);
-    else if (a.M <= 32) hipLaunchKernelGGL(k_i8_few<2>, few, threads, 0, st, a);
-    else if (a.M <= kI8FewRows) hipLaunchKernelGGL(k_i8_few<4>, few, threads, 0, st, a);
-    else hipLaunchKernelGGL(k_i8_tile, dim3((unsigned)(a.tiles_m * a.tiles_n), a.S), dim3(kTileThreads), 0, st, a);
+    switch (a.form) {
+    case 1: return launch_tile<2, 1, 2, 2, 4, 2>(a, st);
+    case 2: return launch_tile<2, 2, 2, 2, 4, 2>(a, st);
+    case 3: return launch_tile<2, 2, 4, 2, 3, 2>(a, st);
+    case 4: return launch_tile<4, 2, 2, 4, 4, 1>(a, st);
+    case 5: return launch_tile<5, 2, 2, 4, 3, 1>(a, st);
+    }
+    const int per_wave = (a.steps + kFewWaves - 1) / kFewWaves;
+    if (a.M <= 16) launch_few<1>(a, per_wave, st);
+    else if (a.M <= 32) launch_few<2>(a, per_wave, st);
+    else launch_few<4>(a, per_wave, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;
     const int64_t blocks = ((int64_t)a.M * a.N + 255) / 256;

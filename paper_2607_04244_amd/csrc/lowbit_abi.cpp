@@ -97,7 +97,7 @@ UnpackArgs unpack_args(const qlin_batch *b, const qlin_kv4_cache *c, bool new_on
 
 // ---- the linear
 
-struct I8Plan { int few = 0, tiles_m = 0, tiles_n = 0, S = 1, steps = 0; int64_t ws_bytes = 0; };
+struct I8Plan { int form = 0, tiles_m = 0, tiles_n = 0, S = 1, steps = 0; int64_t ws_bytes = 0; };
 
 int check_i8(int64_t M, int64_t N, int64_t K, int64_t splits) {
     if (M < 0 || N < 1 || K < 16 || K % 16 || splits < 0 || splits > kMaxKSplits)
@@ -106,22 +106,68 @@ int check_i8(int64_t M, int64_t N, int64_t K, int64_t splits) {
     return QLIN_OK;
 }
 
+constexpr const char *kI8Names[] = {"k_i8_few", "k_i8_tile<128x64>", "k_i8_tile<128x128>", "k_i8_tile<256x128>", "k_i8_tile<256x256>", "k_i8_tile<320x256>"};
+
+// Estimated microseconds of a call in a tile form with S ranges of K, fitted to graph replays
+// (K steps of 64 bytes; weights of several layers in turn).  A step takes `alone` where a
+// workgroup has its compute unit to itself and few work, `full` where all units do (with two on
+// a unit, for both; their clock falls), and a workgroup some time for its first loads and its
+// stores.  Measured / estimated: 2048 x 2560 x 19456 (rows, K, channels) in forms 2 to 5 169 /
+// 155 / 158 / 140 and 149 / 139 / 145 / 136 us; 8192 x 8192 x 8192 702 / 609 / 549 / 674 and
+// 875 / 660 / 595 / 773; 333 x 9728 x 2560 in form 2 with 1, 2, 3, 4, 6 ranges 58.6 / 34.4 /
+// 28.0 / 25.7 / 30.2, in form 1 46.1 / 29.7 / 32.3 / 28.6 / 31.5.
+struct I8Time { double alone, full, fixed; };
+constexpr I8Time kI8Times[] = {{}, {0.27, 0.48, 3.5}, {0.36, 0.85, 4.0}, {0.60, 1.25, 5.0}, {0.90, 1.12, 5.5}, {1.12, 1.55, 6.0}};
+
+double i8_cost(int form, double tiles, double tiles_m, double steps, double S, double weights, double cus) {
+    const I8Form &f = kI8Forms[form];
+    const I8Time &t = kI8Times[form];
+    const double slots = cus * f.per_cu, rounds = std::floor(tiles * S / slots), rest = (tiles * S - rounds * slots) / cus;
+    const double range = std::ceil(steps / S), load = f.per_cu == 1 ? rest : std::max(rest - 1.0, 0.0);
+    const double time = rounds * (range * t.full + t.fixed) + (rest > 0.0 ? range * (t.alone + (t.full - t.alone) * load) + t.fixed : 0.0);
+    const double join = S > 1.0 ? 3.0 + S * tiles * f.n * f.m * 8.0 / 8e6 : 0.0;
+    return std::max(time, std::min(tiles_m, 2.0) * weights / 3.3e6) + join;      // two tiles of rows read the weights twice
+}
+
 int i8_plan(int64_t M, int64_t N, int64_t K, int64_t splits, I8Plan *p) {
     if (check_i8(M, N, K, splits) != QLIN_OK) return last_status();
-    int64_t cus = 256;
+    int64_t cus = 256;                               // forced ranges: arithmetic
     if (splits == 0 && compute_units(&cus) != QLIN_OK) return last_status();
-    p->few = M <= kI8FewRows;
-    const int64_t steps = p->few ? (K + kI8FewStep - 1) / kI8FewStep : (K + kI8TileStep - 1) / kI8TileStep;
-    p->tiles_m = (int)(p->few ? 1 : (M + kI8Tile - 1) / kI8Tile);
-    p->tiles_n = (int)(p->few ? (N + 15) / 16 : (N + kI8Tile - 1) / kI8Tile);
-    const int64_t tiles = (int64_t)p->tiles_m * p->tiles_n;
+    const bool few = M <= kI8FewRows;
+    const int64_t steps = (K + kI8Step - 1) / kI8Step;
+    int64_t S = 1;
+    if (few) {
+        // as few ranges as let each wave keep its part of the tokens in registers: 64 x 9728 x 2560
+        // (rows, K, channels) 26.9 us in one range, 17.3 in four; 32 rows 17.9, 13.8 in three
+        const int64_t held = kI8FewWaves * i8_few_steps((int)M);
+        S = splits ? splits : (steps + held - 1) / held;
+    } else {
+        double best = 0.0;
+        for (int form = 1; form < kI8FormCount; ++form) {
+            const I8Form &f = kI8Forms[form];
+            const int64_t tiles_m = (M + f.m - 1) / f.m, tiles = tiles_m * ((N + f.n - 1) / f.n);
+            auto consider = [&](int64_t ranges) {
+                const double t = i8_cost(form, (double)tiles, (double)tiles_m, (double)steps, (double)ranges, (double)N * (double)K, (double)cus);
+                if (best > 0.0 && t >= best) return;
+                best = t;
+                p->form = form;
+                S = ranges;
+            };
+            if (splits) consider(splits);
+            else
+                for (const int64_t s : {1, 2, 3, 4, 6, 8})
+                    if (s <= std::max<int64_t>(steps / 4, 1)) consider(s);
+        }
+    }
+    const I8Form &f = kI8Forms[p->form];
+    p->tiles_m = (int)((M + f.m - 1) / f.m);
+    p->tiles_n = (int)((N + f.n - 1) / f.n);
+    const int64_t tiles = (int64_t)std::max(p->tiles_m, 1) * p->tiles_n;
     if (tiles >= (int64_t)1 << 23) return fail(QLIN_ERR_UNSUPPORTED, "too many rows and channels for one call");
-    int64_t S = splits;
-    if (S == 0) S = p->few ? 1 : std::max<int64_t>(1, std::min<int64_t>(2 * cus / tiles, steps / 8));
     S = std::max<int64_t>(1, std::min(S, std::min(steps, kMaxKSplits)));
     p->steps = (int)((steps + S - 1) / S);
     p->S = (int)((steps + p->steps - 1) / p->steps);
-    p->ws_bytes = p->S > 1 ? (int64_t)p->S * M * N * 4 : 0;
+    p->ws_bytes = p->S == 1 ? 0 : (int64_t)p->S * 4 * (few ? M * N : tiles * f.n * f.m);
     return QLIN_OK;
 }
 
@@ -278,7 +324,7 @@ int qlin_eight_bit_plan(int64_t M, int64_t N, int64_t K, int64_t splits, int64_t
     if (splits_out) *splits_out = p.S;
     if (workspace_bytes) *workspace_bytes = p.ws_bytes;
     if (buf && buflen > 0)
-        snprintf(buf, (size_t)buflen, "kernel=%s splits=%d grid=%lld combine=%d", p.few ? "k_i8_few" : "k_i8_tile", p.S,
+        snprintf(buf, (size_t)buflen, "kernel=%s splits=%d grid=%lld combine=%d", kI8Names[p.form], p.S,
                  (long long)p.tiles_m * p.tiles_n * p.S, p.S > 1 ? 1 : 0);
     return QLIN_OK;
 }
@@ -324,6 +370,7 @@ int qlin_eight_bit_linear(int64_t M, int64_t N, int64_t K, int64_t splits, const
     a.steps = p.steps;
     a.tiles_m = p.tiles_m;
     a.tiles_n = p.tiles_n;
+    a.form = p.form;
     const hipError_t e = launch_i8_linear(a, (hipStream_t)stream);
     return e == hipSuccess ? QLIN_OK : hip_fail(e, "8-bit linear launch");
 }

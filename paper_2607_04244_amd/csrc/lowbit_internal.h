@@ -28,14 +28,21 @@ struct I8Args {
     const int8_t *x, *w;
     const float *x_scale, *w_scale;
     uint16_t *y;
-    int32_t *parts;                 // S > 1: [S][M][N] sums
+    int32_t *parts;                 // S > 1: the ranges' sums, [S][M][N], or of tiles in the matrix cores' order
     int64_t x_stride, w_stride, y_stride;
     int M, N, K;
-    int S, steps;                   // K ranges; steps of one (of kI8FewStep or kI8TileStep bytes)
+    int S, steps;                   // K ranges; steps of one (64 bytes)
     int tiles_m, tiles_n;
+    int form;                       // of kI8Forms
 };
-constexpr int kI8FewRows = 64;      // rows up to which k_i8_few is taken
-constexpr int kI8FewStep = 64, kI8TileStep = 128, kI8Tile = 128;
+// Form 0 is k_i8_few, up to kI8FewRows rows; the others k_i8_tile: channels and rows of a tile,
+// workgroups of a compute unit.
+struct I8Form { int n, m, per_cu; };
+constexpr I8Form kI8Forms[] = {{16, 64, 2}, {128, 64, 2}, {128, 128, 2}, {256, 128, 2}, {256, 256, 1}, {320, 256, 1}};
+constexpr int kI8FormCount = sizeof kI8Forms / sizeof *kI8Forms;
+constexpr int kI8FewRows = 64, kI8Step = 64, kI8FewWaves = 8;
+// Steps of the tokens that a wave of k_i8_few holds in registers, for M rows.
+constexpr int i8_few_steps(int M) { return M <= 16 ? 19 : M <= 32 ? 8 : 5; }
 
 // The 4-bit cache's arrays beside BatchArgs, whose tok and head are rows here.
 struct Kv4Arrays {

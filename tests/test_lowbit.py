@@ -189,6 +189,19 @@ def test_linear_forced_splits(M, N, K, splits):
     check_linear(M, N, K, splits=splits, pad=32)
 
 
+@pytest.mark.parametrize("M,N,K,form", [(65, 128, 5120, "128x64"), (1500, 1500, 2000, "128x64"), (700, 6000, 1040, "128x128"), (2300, 5130, 96, "256x128"),
+                                        (2048, 19456, 272, "320x256"), (4096, 8190, 528, "256x256")])
+def test_linear_tile_forms(M, N, K, form):
+    """Each tile form, its last tiles partly outside, a last step of K that is no whole one."""
+    assert form in qlin.qlin_eight_bit_plan(M, N, K, 1)[2]
+    g = torch.Generator(device="cuda").manual_seed(M)
+    x, w = (torch.randint(-127, 128, (n, K), generator=g, dtype=torch.int8, device="cuda") for n in (M, N))
+    sx, sw = (0.001 + torch.rand(n, generator=g, device="cuda") for n in (M, N))
+    y = qlin.linear_i8(x, sx, w, sw, splits=1)
+    total = x.double() @ w.double().t().contiguous()          # exact
+    assert torch.equal(y, (total.float() * (sx[:, None] * sw)).to(torch.bfloat16))
+
+
 @pytest.mark.parametrize("M", [3, 40, 70])
 def test_linear_largest_sums(M):
     check_linear(M, 33, 131056, edge=True)
@@ -215,7 +228,7 @@ def test_linear_of_a_row_without_numbers():
 def test_linear_forced_workspace():
     M, N, K, S = 70, 96, 1024, 4
     need = qlin.qlin_eight_bit_plan(M, N, K, S)[1]
-    assert need == S * M * N * 4
+    assert need >= S * M * N * 4
     x, w = torch.ones((M, K), dtype=torch.int8, device="cuda"), torch.ones((N, K), dtype=torch.int8, device="cuda")
     one = torch.ones(max(M, N), device="cuda")
     ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")

@@ -80,7 +80,7 @@ BAD_SIZES = [(dict(M=-1), INVALID), (dict(M=(1 << 22) + 1), UNSUPPORTED), (dict(
     (dict(S=1, y=None), INVALID), (dict(S=1, xs=1008), INVALID), (dict(S=1, ws=1032), ALIGN), (dict(S=1, ws=1 << 33), INVALID),
     (dict(S=1, x=A + 8), ALIGN), (dict(S=1, w=A + 4), ALIGN), (dict(S=1, sx=A + 2), ALIGN), (dict(S=1, sw=A + 1), ALIGN),
     (dict(S=1, y=A + 8), ALIGN), (dict(S=1, ys=500), ALIGN), (dict(S=1, ys=496), INVALID), (dict(S=1, wb=-1), INVALID),
-    (dict(S=1, wsp=A + 8), ALIGN), (dict(S=2, wsp=None), INVALID), (dict(S=2, wb=2 * 100 * 500 * 4 - 1), INVALID),
+    (dict(S=1, wsp=A + 8), ALIGN), (dict(S=2, wsp=None), INVALID), (dict(S=2, wb=2 * 100 * 500 * 4 - 1), INVALID), (dict(S=2, M=10, wb=2 * 10 * 500 * 4 - 1), INVALID),
     (dict(S=1, y=A + 1024), INVALID), (dict(S=1, y=A + 2 * STEP + 16), INVALID), (dict(S=1, y=A + STEP), INVALID), (dict(S=1, y=A + 3 * STEP), INVALID),
     (dict(S=2, wsp=A), INVALID), (dict(S=2, wsp=A + 4 * STEP + 1024), INVALID), (dict(S=2, wsp=A + 3 * STEP), INVALID),
 ])
@@ -98,13 +98,13 @@ def test_linear_no_rows_and_plans():
         assert e.value.code == code
     assert qlin.qlin_eight_bit_plan(100, 500, 1024, 1)[:2] == (1, 0)
     splits, need, text = qlin.qlin_eight_bit_plan(100, 500, 1024, 4)
-    assert splits == 4 and need == 4 * 100 * 500 * 4 and "splits=4" in text
+    assert splits == 4 and need >= 4 * 100 * 500 * 4 and "splits=4" in text       # whole tiles
     # no more ranges than steps, and none without a step
     for M in (1, 20, 100):
         for K in (16, 272, 1040):
             for S in (1, 2, 3, 5, 64):
                 splits, need, _ = qlin.qlin_eight_bit_plan(M, 64, K, S)
-                assert 1 <= splits <= S and need == (splits * M * 64 * 4 if splits > 1 else 0)
+                assert 1 <= splits <= S and (need >= splits * M * 64 * 4 if splits > 1 else need == 0)
     assert qlin.lib().qlin_eight_bit_plan(1, 16, 16, 1, None, None, None, 0) == OK
 
 
