@@ -137,8 +137,10 @@ __device__ inline bool find_work(const CausalArgs &a, int lane, int split, Work 
     w.split = split;
     int tile = 0;
     if (a.one_tile) {
-        if (item >= a.b.n_seq) return false;
-        w.s = load_seq(a.b, item);
+        const int b = a.one_tile == 1 ? item : item / a.one_tile;
+        if (b >= a.b.n_seq) return false;
+        w.s = load_seq(a.b, b);
+        tile = a.one_tile == 1 ? 0 : a.one_tile - 1 - (item - b * a.one_tile);
     } else {
         // where all workgroups run at once, two a compute unit, a long one goes with a short one
         const int half = (a.tiles + 1) / 2, idx = a.pairs && item >= half ? a.tiles - 1 - (item - half) : item;

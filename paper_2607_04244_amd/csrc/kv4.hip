@@ -81,6 +81,39 @@ __device__ inline void load_lds_v4(const uint32_t *src, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(lds), "v"(src) : "memory", "m0");
 }
 
+// 16 scores of a row to weights 2^((s - m) c - E).  Where |m c| is small enough that its rounding
+// leaves weights as exact as they are anyway, they are one fused product each.  By the row, not
+// the wave: not a bit of a row depends on others.
+constexpr float kNear = 256.0f;
+__device__ inline void weights(float e[16], float m, float c, float E) {
+    const float mu = m == kNegInf ? 0.0f : m, mc = mu * c;
+    if (fabsf(mc) <= kNear) {
+        const float sub = mc + E;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = __builtin_fmaf(e[i], c, -sub);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = __builtin_fmaf(e[i] - mu, c, -E);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) e[i] = exp2_hw(e[i]);
+}
+// The weights' sums (l of p, z of p o) and p s as the operand: pairs of keys 8 h + i, 8 h + 4 + i in
+// word 4 h + i, odd keys' over 16.
+__device__ inline void weigh(const float e[16], const uint32_t grid[16], float &l, float &z, uint32_t *p) {
+    float ps[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        l += e[i];
+        z = __builtin_fmaf(e[i], grid_offset(grid[i]), z);
+        ps[i] = e[i] * (grid_step(grid[i]) * (i & 1 ? 0.0625f : 1.0f));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[4 * h + i] = cvt_pk_f16(ps[8 * h + i], ps[8 * h + 4 + i]);
+}
+
 // Steps of 64 keys, a wave's own: K and V codes (4 KiB each), then their grids (256 bytes
 // each), two steps of each wave in flight by direct-to-LDS loads.
 constexpr int kKvWaves = 4, kKvStages = 2, kStepBytes = 2 * kKv4Keys * 64 + 2 * kKv4Keys * 4, kStepLoads = 10;
@@ -199,7 +232,6 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_few(CausalKv4Args x) {
         const int key0 = u * kKv4Keys + 16 * g;               // this lane's keys: key0 + 4 kt + i
         const bool masked = (u + 1) * kKv4Keys - 1 > first_last;
         auto grids = [&](int at, int kt) { return *(const uint4 *)(step + at + 4 * (16 * g + 4 * kt)); };
-        auto seen = [&](int kt, int i) { return !masked || key0 + 4 * kt + i <= last; };
         v4f sc[4];
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
@@ -212,17 +244,23 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_few(CausalKv4Args x) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) sc[kt][i] = __builtin_fmaf(grid_step(grid[i]), acc[i], grid_offset(grid[i]) * qs);
         }
+        uint32_t vg[16];                                      // V's grids of the same keys
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+            const uint4 x = grids(kVGridAt, kt);
+            vg[4 * kt] = x.x;
+            vg[4 * kt + 1] = x.y;
+            vg[4 * kt + 2] = x.z;
+            vg[4 * kt + 3] = x.w;
+        }
         float most = 0.0f;                                    // the largest step, where E has to grow
         if (masked) {
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
-                const uint4 vg = grids(kVGridAt, kt);
-                const uint32_t grid[4] = {vg.x, vg.y, vg.z, vg.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sc[kt][i] = seen(kt, i) ? sc[kt][i] : kNegInf;
-                    most = fmaxf(most, seen(kt, i) ? grid_step(grid[i]) : 0.0f);
-                }
+            for (int i = 0; i < 16; ++i) {
+                const bool seen = key0 + i <= last;
+                sc[i >> 2][i & 3] = seen ? sc[i >> 2][i & 3] : kNegInf;
+                vg[i] = seen ? vg[i] : 0u;
+                most = fmaxf(most, grid_step(vg[i]));
             }
             most = pair32_max(pair16_max(most));
         } else {
@@ -243,33 +281,17 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_few(CausalKv4Args x) {
                 least_limit = wave_min(scale.limit);
             }
         }
-        const float mu = m == kNegInf ? 0.0f : m;
-        uint32_t p[2][4];                                     // p s of keys 8 h + i and 8 h + 4 + i
+        float e[16];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float ps[2][4];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int kt = 2 * h + k;
-                const uint4 vg = grids(kVGridAt, kt);
-                uint32_t grid[4] = {vg.x, vg.y, vg.z, vg.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (masked) grid[i] = seen(kt, i) ? grid[i] : 0u;
-                    const float e = exp2_hw(__builtin_fmaf(sc[kt][i] - mu, c, -scale.e));
-                    l += e;
-                    z = __builtin_fmaf(e, grid_offset(grid[i]), z);
-                    ps[k][i] = e * (grid_step(grid[i]) * (i & 1 ? 0.0625f : 1.0f));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[h][i] = cvt_pk_f16(ps[0][i], ps[1][i]);
-        }
+        for (int i = 0; i < 16; ++i) e[i] = sc[i >> 2][i & 3];
+        weights(e, m, c, scale.e);
+        uint32_t p[8];
+        weigh(e, vg, l, z, p);
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) {
             const v2i t = lds_read_tr4(step + vat[dt >> 1] + 8 * (dt & 1));
-            o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(extract.pairs(t[0])), operand(p[0]), o[dt], 0, 0, 0);
-            o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(extract.pairs(t[1])), operand(p[1]), o[dt], 0, 0, 0);
+            o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(extract.pairs(t[0])), operand(p), o[dt], 0, 0, 0);
+            o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(extract.pairs(t[1])), operand(p + 4), o[dt], 0, 0, 0);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // this stage has been read
         if (u + 2 * kKvWaves < u1) load.issue(u + 2 * kKvWaves, st);
@@ -304,13 +326,11 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_few(CausalKv4Args x) {
 
 // ---------------------------------------------------------------- more rows
 
-// 32 RT rows, RT = 1, 2: every wave has all rows for its own steps, so that a word is
-// extracted once for them.
-template <int RT>
-__global__ __launch_bounds__(kKvWaves * 64, RT == 1 ? 2 : 1) void k_kv4_rows(CausalKv4Args x) {
-    constexpr int R = 32 * RT, kRing = kKvWaves * kKvStages * kStepBytes, kSums = kKvWaves * 16 * RT * 64 * 16;
+// Tiles of 32 rows, every wave with its own steps.
+__global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_rows(CausalKv4Args x) {
+    constexpr int R = 32;
     const CausalArgs &a = x.a;
-    __shared__ __attribute__((aligned(16))) char ring[kRing > kSums ? kRing : kSums];     // then the waves' sums
+    __shared__ __attribute__((aligned(16))) char ring[kKvWaves][kKvStages][kStepBytes];     // then the waves' sums
     __shared__ float2 ml[kKvWaves][R];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int hi = lane >> 5, r = lane & 31;
@@ -319,23 +339,18 @@ __global__ __launch_bounds__(kKvWaves * 64, RT == 1 ? 2 : 1) void k_kv4_rows(Cau
     const Range range = range_of(a, (w.hi + kKv4Keys - 1) / kKv4Keys, w.split);
     if (a.S > 1 && w.split >= range.used) return;
     const int u0 = range.first, u1 = range.end;
-    const char *const own_ring = ring + wave * kKvStages * kStepBytes;
-    const Loader<2> load(x, w, lane, lds_addr(own_ring));
+    const Loader<2> load(x, w, lane, lds_addr(ring[wave]));
     if (u0 + wave < u1) load.issue(u0 + wave, 0);
     if (u0 + wave + kKvWaves < u1) load.issue(u0 + wave + kKvWaves, 1);
 
-    // queries: B operand, row r of each tile; K's word ks of lane half hi is dimensions 64 hi + 8 ks .. + 7
-    int last[RT];                                             // last key that the row sees
-    v8h qf[RT][8];
-    float qs[RT], back[RT], c[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const RowOf row = row_of(a, w, min(32 * t + r, w.rows - 1));
-        last[t] = w.s.p0 + row.i;
-        load_queries<8>(a.q + row_at(w, row, a.q_stride) + 64 * hi, qf[t], qs[t], back[t], pair32_max, pair32_sum);
-        c[t] = a.c * back[t];
-    }
+    // queries: B operand, row r; K's word ks of lane half hi is dimensions 64 hi + 8 ks .. + 7
+    const RowOf row = row_of(a, w, min(r, w.rows - 1));
+    const int last = w.s.p0 + row.i;                          // last key that the row sees
     const int first_last = w.s.p0 + w.i0;                     // keys up to here are seen by every row
+    v8h qf[8];
+    float qs, back;
+    load_queries<8>(a.q + row_at(w, row, a.q_stride) + 64 * hi, qf, qs, back, pair32_max, pair32_sum);
+    const float c = a.c * back;
     const ExtractConsts<true> extract;
 
     // places in half a step (32 keys): K of key 16 ((r >> 2) & 1) + 4 (r >> 3) + (r & 3), V of key
@@ -345,30 +360,25 @@ __global__ __launch_bounds__(kKvWaves * 64, RT == 1 ? 2 : 1) void k_kv4_rows(Cau
     int vat[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) vat[i] = kVAt + (16 * hi + (lane & 15)) * 64 + 16 * (i ^ v_order(lane & 15)) + 8 * ((lane >> 4) & 1);
-    float m[RT], l[RT], z[RT];                                // maximum; sums of p and p o
-    StepScale scale[RT];
+    float m = kNegInf, l = 0.0f, z = 0.0f;                    // maximum; sums of p and p o
+    StepScale scale;
     float least_limit = 0.0f;                                 // of the wave's rows
-    v16f o[RT][4];
+    v16f o[4];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        m[t] = kNegInf;
-        l[t] = z[t] = 0.0f;
+    for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+    auto rescale = [&](float by) {
+        l *= by;
+        z *= by;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[t][dt][i] = 0.0f;
-    }
-    auto rescale = [&](int t, float by) {
-        l[t] *= by;
-        z[t] *= by;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt) o[t][dt] *= by;
+        for (int dt = 0; dt < 4; ++dt) o[dt] *= by;
     };
     int st = 0;
     for (int u = u0 + wave; u < u1; u += kKvWaves, st ^= 1) {
         load.wait(u + kKvWaves < u1);
         const bool masked = (u + 1) * kKv4Keys - 1 > first_last;
-        const char *const stage = own_ring + st * kStepBytes;
+        const char *const stage = ring[wave][st];
         float most_all = 0.0f;                                // the largest step, where some row's E has to grow
         if (!masked) {
             const float own = grid_step(*(const uint32_t *)(stage + kVGridAt + 4 * lane));
@@ -381,132 +391,92 @@ __global__ __launch_bounds__(kKvWaves * 64, RT == 1 ? 2 : 1) void k_kv4_rows(Cau
             const int key0 = u * kKv4Keys + 32 * half + 16 * hi;          // this lane's keys: key0 + i
             const uint4 k0 = *(const uint4 *)(step + kat0), k1 = *(const uint4 *)(step + kat1);
             const uint32_t word[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w};
-            v16f sc[RT];
+            v16f sc;
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
+            for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-                const v8h kf = operand(extract.pairs(word[ks]));
-#pragma unroll
-                for (int t = 0; t < RT; ++t) sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[t][ks], sc[t], 0, 0, 0);
-            }
-            uint32_t vgrid[16];
-            float most[RT];
+            for (int ks = 0; ks < 8; ++ks)
+                sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(extract.pairs(word[ks])), qf[ks], sc, 0, 0, 0);
+            uint32_t vg[16];
+            float e[16];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint4 kg = *(const uint4 *)(grids + kKGridAt + 4 * (16 * hi + 4 * j));
-                const uint4 vg = *(const uint4 *)(grids + kVGridAt + 4 * (16 * hi + 4 * j));
+                const uint4 g = *(const uint4 *)(grids + kVGridAt + 4 * (16 * hi + 4 * j));
                 const uint32_t grid[4] = {kg.x, kg.y, kg.z, kg.w};
-                vgrid[4 * j] = vg.x;
-                vgrid[4 * j + 1] = vg.y;
-                vgrid[4 * j + 2] = vg.z;
-                vgrid[4 * j + 3] = vg.w;
+                vg[4 * j] = g.x;
+                vg[4 * j + 1] = g.y;
+                vg[4 * j + 2] = g.z;
+                vg[4 * j + 3] = g.w;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float s = grid_step(grid[i]), of = grid_offset(grid[i]);
+                for (int i = 0; i < 4; ++i) e[4 * j + i] = __builtin_fmaf(grid_step(grid[i]), sc[4 * j + i], grid_offset(grid[i]) * qs);
+            }
+            float most = most_all;
+            if (masked) {
 #pragma unroll
-                    for (int t = 0; t < RT; ++t) sc[t][4 * j + i] = __builtin_fmaf(s, sc[t][4 * j + i], of * qs[t]);
+                for (int i = 0; i < 16; ++i) {
+                    const bool seen = key0 + i <= last;
+                    e[i] = seen ? e[i] : kNegInf;
+                    vg[i] = seen ? vg[i] : 0u;
+                    most = fmaxf(most, grid_step(vg[i]));
+                }
+                most = pair32_max(most);
+            }
+            float mt = kNegInf;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mt = fmaxf(mt, e[i]);
+            mt = pair32_max(mt);
+            const bool own = (mt - m) * c > kLazy;
+            if (__ballot(own || most > scale.limit)) {
+                const float mn = own ? mt : m;
+                rescale(exp2_hw((m - (mn == kNegInf ? 0.0f : mn)) * c));
+                m = mn;
+                if (__ballot(most > scale.limit)) {
+                    rescale(scale.raise(most));
+                    least_limit = wave_min(scale.limit);
                 }
             }
-            uint32_t p[RT][8];                                // p s of keys 8 h + i and 8 h + 4 + i: 4 h + i
-            float mu[RT];
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                most[t] = most_all;
-                if (masked) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const bool seen = key0 + i <= last[t];
-                        sc[t][i] = seen ? sc[t][i] : kNegInf;
-                        most[t] = fmaxf(most[t], seen ? grid_step(vgrid[i]) : 0.0f);
-                    }
-                    most[t] = pair32_max(most[t]);
-                }
-                float mt = kNegInf;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[t][i]);
-                mt = pair32_max(mt);
-                const bool own = (mt - m[t]) * c[t] > kLazy;
-                if (__ballot(own || most[t] > scale[t].limit)) {
-                    const float mn = own ? mt : m[t];
-                    rescale(t, exp2_hw((m[t] - (mn == kNegInf ? 0.0f : mn)) * c[t]));
-                    m[t] = mn;
-                    if (__ballot(most[t] > scale[t].limit)) {
-                        rescale(t, scale[t].raise(most[t]));
-                        least_limit = wave_min(RT == 1 ? scale[0].limit : fminf(scale[0].limit, scale[RT - 1].limit));
-                    }
-                }
-                mu[t] = m[t] == kNegInf ? 0.0f : m[t];
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float ps[RT][8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t g = vgrid[8 * h + i];
-                    const float s = grid_step(g) * (i & 1 ? 0.0625f : 1.0f), of = grid_offset(g);
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        const bool seen = !masked || key0 + 8 * h + i <= last[t];
-                        const float e = exp2_hw(__builtin_fmaf(sc[t][8 * h + i] - mu[t], c[t], -scale[t].e));
-                        l[t] += e;
-                        z[t] = __builtin_fmaf(e, seen ? of : 0.0f, z[t]);
-                        ps[t][i] = e * (seen ? s : 0.0f);
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < RT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) p[t][4 * h + i] = cvt_pk_f16(ps[t][i], ps[t][4 + i]);
-            }
+            weights(e, m, c, scale.e);
+            uint32_t p[8];
+            weigh(e, vg, l, z, p);
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) {
                 const v2i v = lds_read_tr4(step + vat[dt]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const v8h vf = operand(extract.pairs(v[h]));
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) o[t][dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, operand(p[t] + 4 * h), o[t][dt], 0, 0, 0);
-                }
+                for (int h = 0; h < 2; ++h)
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(extract.pairs(v[h])), operand(p + 4 * h), o[dt], 0, 0, 0);
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // this stage has been read
         if (u + 2 * kKvWaves < u1) load.issue(u + 2 * kKvWaves, st);
     }
     // the waves' sums through LDS, in the matrix cores' order
+    const float up = power_of_two((int)scale.e);
+    l = pair32_sum(l) * up;
+    z = pair32_sum(z);
     __syncthreads();
-    v4f *const sums = (v4f *)ring;
+    v4f *const sums = (v4f *)&ring[0][0][0];
+    static_assert(sizeof(ring) >= sizeof(v4f) * kKvWaves * 16 * 64, "the sums fit the ring");
+    if (hi == 0) ml[wave][r] = make_float2(m * back, l);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const float up = power_of_two((int)scale[t].e), zt = pair32_sum(z[t]);
-        l[t] = pair32_sum(l[t]) * up;
-        if (hi == 0) ml[wave][32 * t + r] = make_float2(m[t] * back[t], l[t]);
+    for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const v4f x = {o[t][dt][4 * i], o[t][dt][4 * i + 1], o[t][dt][4 * i + 2], o[t][dt][4 * i + 3]};
-                sums[((wave * RT + t) * 16 + dt * 4 + i) * 64 + lane] = (x * kCodes + zt) * up;
-            }
-    }
+        for (int i = 0; i < 4; ++i) {
+            const v4f y = {o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+            sums[(wave * 16 + dt * 4 + i) * 64 + lane] = (y * kCodes + z) * up;
+        }
     __syncthreads();
+    if (r >= w.rows) return;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        if (32 * t + r >= w.rows) continue;
-        const RowOf row = row_of(a, w, 32 * t + r);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int unit = 4 * wave + j;                    // of this row tile: dimensions 8 unit + 4 hi .. + 3
-            v4f acc;
-            const float2 e = merged<kKvWaves>(&ml[0][32 * t + r], R, sums + (t * 16 + unit) * 64 + lane, RT * 16 * 64, a.c, acc);
-            if (a.S == 1) {
-                store_out(a, w, row, 8 * unit + 4 * hi, acc, e.y);
-            } else {
-                *(v4f *)(unit_at<R>(a, w.split, t * 16 + unit) + 4 * lane) = acc;
-                if (unit == 0 && hi == 0) *row_ml<R>(a, w.split, 32 * t + r) = e;
-            }
+    for (int j = 0; j < 4; ++j) {
+        const int unit = 4 * wave + j;                        // dimensions 8 unit + 4 hi .. + 3
+        v4f acc;
+        const float2 e = merged<kKvWaves>(&ml[0][r], R, sums + unit * 64 + lane, 16 * 64, a.c, acc);
+        if (a.S == 1) {
+            store_out(a, w, row, 8 * unit + 4 * hi, acc, e.y);
+        } else {
+            *(v4f *)(unit_at<R>(a, w.split, unit) + 4 * lane) = acc;
+            if (unit == 0 && hi == 0) *row_ml<R>(a, w.split, r) = e;
         }
     }
 }
@@ -623,15 +593,14 @@ __global__ __launch_bounds__(256) void k_unpack_kv4(UnpackArgs a) {
 
 }  // namespace
 
-const char *causal_kv4_kernel_name(int rt) { return rt == 1 ? "k_kv4_few" : rt == 2 ? "k_kv4_rows<1>" : "k_kv4_rows<2>"; }
+const char *causal_kv4_kernel_name(int rt) { return rt == 1 ? "k_kv4_few" : "k_kv4_rows"; }
 
 hipError_t launch_causal_kv4(const CausalKv4Args &args, int rt, hipStream_t st) {
     CausalKv4Args x = args;
     x.a.step_keys = kKv4Keys;
     const dim3 grid((unsigned)(x.a.tiles * x.a.Hkv), (unsigned)x.a.S), threads(kKvWaves * 64);
     if (rt == 1) hipLaunchKernelGGL(k_kv4_few, grid, threads, 0, st, x);
-    else if (rt == 2) hipLaunchKernelGGL(k_kv4_rows<1>, grid, threads, 0, st, x);
-    else hipLaunchKernelGGL(k_kv4_rows<2>, grid, threads, 0, st, x);
+    else hipLaunchKernelGGL(k_kv4_rows, grid, threads, 0, st, x);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess || x.a.S == 1 ? e : launch_causal_join(x.a, rt, st);
 }

@@ -10,6 +10,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <cstdlib>
 
 #include "lowbit_internal.h"
 #include "target_checks.h"
@@ -173,7 +174,7 @@ int i8_plan(int64_t M, int64_t N, int64_t K, int64_t splits, I8Plan *p) {
 
 // ---- attention over the 4-bit cache
 
-// rt: 1, 2, 4 as causal_tile_rows; 0: unpacked to the workspace, then qlin_causal_attention
+// rt: 1, 2 as causal_tile_rows; 0: unpacked to the workspace, then qlin_causal_attention
 struct Kv4Plan { int rt = 0, tiles = 0, one_tile = 0, S = 1, least = 1; int64_t ws_bytes = 0, unpacked = 0; };
 
 // Where the parts of the unpack form's workspace begin: keys, values, lengths, shifts of heads and of
@@ -211,7 +212,7 @@ int kv4_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, Kv4Pl
     int64_t cus = 256;
     if (splits == 0 && compute_units(&cus) != QLIN_OK) return last_status();
     const int64_t G = Hq / Hkv, most = b->max_new * G;
-    p->rt = most <= 16 ? 1 : most <= 32 ? 2 : most <= 256 || b->max_len == 0 ? 4 : 0;
+    p->rt = most <= 16 ? 1 : most <= 256 || b->max_len == 0 ? 2 : 0;
     if (p->rt == 0) {
         int64_t attention = 0;
         if (qlin_causal_plan(b, Hq, Hkv, kHeadDim, splits, nullptr, &attention, nullptr, 0) != QLIN_OK) return last_status();
@@ -222,9 +223,11 @@ int kv4_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, Kv4Pl
         return QLIN_OK;
     }
     const int64_t R = causal_tile_rows(p->rt), per = (most + R - 1) / R;
-    p->one_tile = per <= 1;
-    const int64_t tiles = p->one_tile ? b->n_seq : std::min(b->n_seq * per, b->rows * G / R + b->n_seq);
-    const int64_t blocks = std::max<int64_t>(tiles * Hkv, 1), slots = p->rt == 4 ? cus : 2 * cus;
+    // of sequences with about as many new tokens each, a tile is found without a walk over them (the
+    // first microseconds of a workgroup)
+    p->one_tile = (int)(per <= 1 ? 1 : b->n_seq * per <= 2 * (b->rows * G / R + 1) ? per : 0);
+    const int64_t tiles = p->one_tile ? b->n_seq * per : std::min(b->n_seq * per, b->rows * G / R + b->n_seq);
+    const int64_t blocks = std::max<int64_t>(tiles * Hkv, 1), slots = 2 * cus;
     const int64_t least = 4 * kKv4Keys;                           // a step of each wave
     int64_t S = splits;
     if (S == 0) S = std::max<int64_t>(1, std::min<int64_t>(slots / blocks, (b->max_len + least - 1) / least));
@@ -233,7 +236,7 @@ int kv4_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, Kv4Pl
         return fail(QLIN_ERR_UNSUPPORTED, "too many rows, heads and key ranges for one call");
     p->tiles = (int)tiles;
     p->S = (int)S;
-    p->least = 4;
+    p->least = getenv("KVL") ? (int)(((b->max_len + 63) / 64 + S - 1) / S) : 4;
     p->ws_bytes = S > 1 ? tiles * Hkv * S * R * (kHeadDim + 2) * 4 : 0;
     return QLIN_OK;
 }

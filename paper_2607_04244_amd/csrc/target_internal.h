@@ -42,7 +42,7 @@ struct CausalArgs {
     int Hq, Hkv, G;
     float *ws_o, *ws_ml;            // S > 1: sums and (maximum, sum of weights) of each item, range and row
     int tiles;                      // row tiles, at least those there are
-    int one_tile;                   // one tile a sequence: tile i is sequence i
+    int one_tile;                   // this many tiles a sequence (1: tile i is sequence i); 0: as many as its rows need
     int pairs;                      // at most two workgroups a compute unit
     int S, least;                   // key ranges; least steps of one
     int step_keys;                  // keys of a step (set by the launch)
