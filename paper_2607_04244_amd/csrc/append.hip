@@ -49,12 +49,6 @@ __device__ inline T row_sum(T v) {
     return row_reduce(v, [](T x, T y) { return x + y; });
 }
 
-// Written out, so that a build's choice of what to fuse cannot change an output's last bit.
-__device__ inline float fused(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
-__device__ inline double fused(double a, double b, double c) { return __builtin_fma(a, b, c); }
-__device__ inline float inverse_root(float x) { return 1.0f / sqrtf(x); }
-__device__ inline double inverse_root(double x) { return 1.0 / sqrt(x); }
-
 // Many tokens stream through: with the non-temporal hint both ways 8192 tokens from and to
 // memory that no cache holds take 43.0 us against 49.8, 1500 tokens 12.3 against 14.7 (with
 // it on the loads alone 47.7 and 13.1; where the last-level cache holds all, 41.6 against
@@ -70,15 +64,18 @@ __device__ inline void store_row(uint16_t *p, const uint4 &y) {
     else *(uint4 *)p = y;
 }
 
+__device__ inline uint4 pack8(const float o[8]) {
+    return make_uint4(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]), cvt_pk_bf16(o[4], o[5]), cvt_pk_bf16(o[6], o[7]));
+}
+
 // Eight dimensions (8 l .. 8 l + 7) of a head row: norm with the weights w (none: null), and the
 // rotation by the token's angles cs = (cos, sin).
-template <typename T, typename T2>
-__device__ inline void norm_rotate(const AppendArgs &a, const uint4 &x, const uint16_t *w, const uint2 &w0, const uint2 &w1, const T2 *cs,
-                                   int lane, T o[8]) {
+__device__ inline void norm_rotate(const AppendArgs &a, const uint4 &x, const uint16_t *w, const uint2 &w0, const uint2 &w1, const float2 *cs,
+                                   int lane, float o[8]) {
     const int l = lane & 15;
-    T f[8];
+    float f[8];
     const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, ww[4] = {w0.x, w0.y, w1.x, w1.y};
-    T ss = 0;
+    float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         f[2 * i] = bf16_lo_to_f32(xw[i]);
@@ -86,20 +83,21 @@ __device__ inline void norm_rotate(const AppendArgs &a, const uint4 &x, const ui
         ss += f[2 * i] * f[2 * i] + f[2 * i + 1] * f[2 * i + 1];
     }
     if (w) {
-        const T inv = inverse_root(row_sum(ss) * (T)(1.0f / kHeadDim) + (T)a.eps);
+        const float inv = 1.0f / sqrtf(row_sum(ss) * (1.0f / kHeadDim) + a.eps);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            f[2 * i] = f[2 * i] * inv * (T)bf16_lo_to_f32(ww[i]);
-            f[2 * i + 1] = f[2 * i + 1] * inv * (T)bf16_hi_to_f32(ww[i]);
+            f[2 * i] = f[2 * i] * inv * bf16_lo_to_f32(ww[i]);
+            f[2 * i + 1] = f[2 * i + 1] * inv * bf16_hi_to_f32(ww[i]);
         }
     }
+    // fused products written out, so that a build's choice cannot change an output's last bit
     if (a.interleaved) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool in = 4 * l + i < a.half;
-            const T2 t = cs[in ? 4 * l + i : 0];
-            o[2 * i] = in ? fused(f[2 * i], t.x, -(f[2 * i + 1] * t.y)) : f[2 * i];
-            o[2 * i + 1] = in ? fused(f[2 * i], t.y, f[2 * i + 1] * t.x) : f[2 * i + 1];
+            const float2 t = cs[in ? 4 * l + i : 0];
+            o[2 * i] = in ? __builtin_fmaf(f[2 * i], t.x, -(f[2 * i + 1] * t.y)) : f[2 * i];
+            o[2 * i + 1] = in ? __builtin_fmaf(f[2 * i], t.y, f[2 * i + 1] * t.x) : f[2 * i + 1];
         }
     } else {
         // the partner of a dimension is half / 8 lanes away
@@ -108,30 +106,88 @@ __device__ inline void norm_rotate(const AppendArgs &a, const uint4 &x, const ui
         const int from = (lane & 48) | (in ? lo ? l + hl : l - hl : l);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const T other = __shfl(f[i], from);
-            const T2 t = cs[in ? (lo ? 8 * l : 8 * (l - hl)) + i : 0];
-            o[i] = in ? fused(f[i], t.x, lo ? -(other * t.y) : other * t.y) : f[i];
+            const float other = __shfl(f[i], from);
+            const float2 t = cs[in ? (lo ? 8 * l : 8 * (l - hl)) + i : 0];
+            o[i] = in ? __builtin_fmaf(f[i], t.x, lo ? -(other * t.y) : other * t.y) : f[i];
         }
     }
 }
 
-__device__ inline uint4 pack8(const float o[8]) {
-    return make_uint4(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]), cvt_pk_bf16(o[4], o[5]), cvt_pk_bf16(o[6], o[7]));
+// Place of angle i among a token's angles in 64 bits: what 8 lanes read together, angles 8 apart,
+// lies side by side.
+__device__ inline int angle_at(int i) { return (i & 7) * 8 + (i >> 3); }
+
+// The same in 64 bits, rounded to fp32 and bf16 at the end.  x w is exact in fp32, so the row is
+// rotated before it is divided by its root, and partners travel in 32 bits.
+__device__ inline uint4 norm_rotate_64(const AppendArgs &a, const uint4 &x, const uint16_t *w, const uint2 &w0, const uint2 &w1,
+                                       const double2 *cs, int lane) {
+    const int l = lane & 15;
+    float f[8], y[8];
+    const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, ww[4] = {w0.x, w0.y, w1.x, w1.y};
+    double ss = 0.0, inv = 1.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = bf16_lo_to_f32(xw[i]);
+        f[2 * i + 1] = bf16_hi_to_f32(xw[i]);
+    }
+    if (w) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)f[i], (double)f[i], ss);
+        const double mean = row_sum(ss) * (1.0 / kHeadDim) + (double)a.eps;
+        // the hardware's estimate of 1 / sqrt(mean), twice by Newton's rule: past 2^-50
+        inv = __builtin_amdgcn_rsq(mean);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) inv = __builtin_fma(0.5 * inv, __builtin_fma(-mean * inv, inv, 1.0), inv);
+        if (!(mean > 0.0)) inv = 1.0 / sqrt(mean);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] *= bf16_lo_to_f32(ww[i]);
+            f[2 * i + 1] *= bf16_hi_to_f32(ww[i]);
+        }
+    }
+    if (a.interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool in = 4 * l + i < a.half;
+            const double2 t = cs[in ? angle_at(4 * l + i) : 0];
+            const double x0 = f[2 * i], x1 = f[2 * i + 1];
+            y[2 * i] = (float)((in ? __builtin_fma(x0, t.x, -(x1 * t.y)) : x0) * inv);
+            y[2 * i + 1] = (float)((in ? __builtin_fma(x0, t.y, x1 * t.x) : x1) * inv);
+        }
+    } else {
+        const int hl = a.half >> 3;
+        const bool lo = l < hl, in = l < 2 * hl;
+        const int from = (lane & 48) | (in ? lo ? l + hl : l - hl : l);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const double x0 = f[i], other = __shfl(lo ? f[i] : -f[i], from);       // what the upper half gets has its sign, what the lower gets the other
+            const double2 t = cs[in ? angle_at((lo ? 8 * l : 8 * (l - hl)) + i) : 0];
+            y[i] = (float)((in ? __builtin_fma(x0, t.x, other * t.y) : x0) * inv);
+        }
+    }
+    return pack8(y);
+}
+
+// x / d, correctly rounded, from d's correctly rounded reciprocal (Markstein): the remainder of the
+// first quotient is exact in a fused product.
+__device__ inline float quotient(float x, float d, float inverse) {
+    const float q = x * inverse;
+    return __builtin_fmaf(__builtin_fmaf(-q, d, x), inverse, q);
 }
 
 // A row of bf16 values on its 4-bit grid: this lane's word of codes, and the row's (step, offset).
-// Divisions are correctly rounded, so a code is that of the exact quotient, ties included: the
-// quotient by the step from the step's reciprocal and one remainder (Markstein).
-__device__ inline uint32_t lay_on_grid(const uint4 &y, uint32_t &grid) {
+// Quotients are correctly rounded, so a code is that of the exact one, ties included.
+__device__ inline uint32_t lay_on_grid(const uint4 &y, int lane, uint32_t &grid) {
     const uint32_t w[4] = {y.x, y.y, y.z, y.w};
     float f[8];
-    uint32_t top = 0;                        // bits of the largest |x|: infinities and NaN are past all numbers
+    uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         f[2 * i] = bf16_lo_to_f32(w[i]);
         f[2 * i + 1] = bf16_hi_to_f32(w[i]);
         top = max(top, max(w[i] << 16 & 0x7FFFFFFFu, w[i] & 0x7FFF0000u));
     }
+    const uint64_t without_number = __ballot(top >= 0x7F800000u) >> (lane & 48) & 0xFFFFu;      // in the row's 16 lanes
     float low = f[0], high = f[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) {
@@ -140,24 +196,27 @@ __device__ inline uint32_t lay_on_grid(const uint4 &y, uint32_t &grid) {
     }
     low = row_reduce(low, [](float x, float y) { return fminf(x, y); });
     high = row_reduce(high, [](float x, float y) { return fmaxf(x, y); });
-    const float most = row_reduce(__uint_as_float(top), [](float x, float y) { return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y))); });
     const float range = high - low;
-    if (!(__float_as_uint(most) < 0x7F800000u) || __float_as_uint(range) >= 0x7F800000u) {
+    if (without_number || !(range < __builtin_huge_valf())) {
         grid = 0x7FC07FC0u;
         return 0;
     }
-    const uint16_t sb = cvt_bf16(range / 15.0f);
+    const uint16_t sb = cvt_bf16(quotient(range, 15.0f, 1.0f / 15.0f));
     const float step = __uint_as_float((uint32_t)sb << 16);
     grid = __float_as_uint(low);             // bf16 in the high half: the offset
     if (sb < 0x0080) return 0;               // below 2^-126
     grid |= sb;
-    const float inv = 1.0f / step;
+    // of a number of 8 bits, the hardware's estimate (off by one unit at most) and Newton's rule give
+    // the correctly rounded reciprocal: so for each of the 128 significands and each estimate
+    float inverse = __builtin_amdgcn_rcpf(step);
+    inverse = __builtin_fmaf(__builtin_fmaf(-step, inverse, 1.0f), inverse, inverse);
+    // added to 1.5 2^23 a quotient is rounded to a whole number, in the sum's low bits
+    constexpr uint32_t kWhole = 0x4B400000u;
     uint32_t codes = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float x = f[i] - low, q = x * inv;
-        const float c = rintf(__builtin_fmaf(__builtin_fmaf(-q, step, x), inv, q));
-        codes |= (uint32_t)fminf(c, 15.0f) << 4 * i;
+        const uint32_t c = __float_as_uint(quotient(f[i] - low, step, inverse) + __uint_as_float(kWhole));
+        codes += (min(c, kWhole + 15u) - kWhole) << 4 * i;
     }
     return codes;
 }
@@ -165,7 +224,7 @@ __device__ inline uint32_t lay_on_grid(const uint4 &y, uint32_t &grid) {
 // KV4: the keys in 64 bits, so that their codes are those of the definition and not those of
 // its rounding errors; rows of keys and values as codes and grids.
 template <int R, bool KV4>
-__global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(std::conditional_t<KV4, AppendKv4Args, AppendArgs> args) {
+__global__ __launch_bounds__(kAppendThreads, KV4 ? 6 : 4) void k_norm_rope_append(std::conditional_t<KV4, AppendKv4Args, AppendArgs> args) {
     __shared__ float2 cs[R][kHeadDim / 2];   // (cos, sin) of each token's angles
     __shared__ double2 cs64[KV4 ? R : 1][KV4 ? kHeadDim / 2 : 1];
     __shared__ int64_t slot[R];              // cache slot of each token, -1: not stored
@@ -178,6 +237,7 @@ __global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(std::condit
     const int groups = blockDim.x / kGroupLanes, grp = threadIdx.x / kGroupLanes;
     const int m0 = blockIdx.x * R;
 
+#pragma unroll 1
     for (int r = threadIdx.x >> 6; r < R; r += blockDim.x >> 6) {      // a wave a token
         const int m = m0 + r;
         const int b = m < a.b.rows ? find_seq(a.b, m, lane) : a.b.n_seq;
@@ -199,7 +259,7 @@ __global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(std::condit
             if constexpr (KV4) {
                 double sn, cn;
                 sincospi(2.0 * (t - rint(t)), &sn, &cn);
-                cs64[r][lane] = make_double2(cn, sn);
+                cs64[r][angle_at(lane)] = make_double2(cn, sn);
                 cs[r][lane] = make_float2((float)cn, (float)sn);
             } else {
                 float sn, cn;
@@ -228,36 +288,39 @@ __global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(std::condit
             w0 = *(const uint2 *)(w + 8 * l);
             w1 = *(const uint2 *)(w + 8 * l + 4);
         }
+        if constexpr (KV4) {
+            // one token after the other, so that two workgroups' registers fit a compute unit
+#pragma unroll 1
+            for (int r = 0; r < R; ++r) {
+                const uint4 now = x[0];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            uint4 y = x[r];
-            if (is_q || (is_k && !KV4)) {
-                float o[8];
-                norm_rotate(a, x[r], w, w0, w1, cs[r], lane, o);
-                y = pack8(o);
-            }
-            if constexpr (KV4) {
+                for (int i = 0; i + 1 < R; ++i) x[i] = x[i + 1];
+                int at = lane;               // opaque: places in LDS worked out for each token take fewer registers
+                asm volatile("" : "+v"(at), "+v"(w0.x), "+v"(w0.y), "+v"(w1.x), "+v"(w1.y));
                 if (is_q) {
-                    if (live[r]) store_row<R>(a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim + 8 * l, y);
+                    float o[8];
+                    norm_rotate(a, now, w, w0, w1, cs[r], at, o);
+                    if (live[r]) store_row<R>(a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim + 8 * l, pack8(o));
                     continue;
                 }
-                if (is_k) {
-                    double o[8];
-                    float f[8];
-                    norm_rotate(a, x[r], w, w0, w1, cs64[r], lane, o);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] = (float)o[i];
-                    y = pack8(f);
-                }
                 uint32_t grid;
-                const uint32_t codes = lay_on_grid(y, grid);
+                const uint32_t codes = lay_on_grid(is_k ? norm_rotate_64(a, now, w, w0, w1, cs64[r], at) : now, lane, grid);
                 if (slot[r] < 0) continue;
                 const int64_t row = slot[r] * a.b.tok + hh * a.b.head;
                 (is_k ? args.c.k : args.c.v)[16 * row + l] = codes;
                 if (l == 0) (is_k ? args.c.k_grid : args.c.v_grid)[row] = grid;
-            } else {
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
                 uint16_t *dst = is_q ? a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim
                                      : (is_k ? a.kc : a.vc) + slot[r] * a.b.tok + hh * a.b.head;
+                uint4 y = x[r];
+                if (is_q || is_k) {
+                    float o[8];
+                    norm_rotate(a, x[r], w, w0, w1, cs[r], lane, o);
+                    y = pack8(o);
+                }
                 if (is_q ? live[r] : slot[r] >= 0) store_row<R>(dst + 8 * l, y);
             }
         }

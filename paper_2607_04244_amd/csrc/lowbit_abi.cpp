@@ -10,7 +10,6 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
-#include <cstdlib>
 
 #include "lowbit_internal.h"
 #include "target_checks.h"
@@ -23,6 +22,7 @@ constexpr int64_t kMaxWidth = 65536, kMaxChannels = (int64_t)1 << 22, kMaxK = 13
 constexpr int64_t kMaxRowTokens = (int64_t)1 << 20;          // 32-bit byte offsets over 64 tokens
 constexpr int64_t kMaxRowHeads = (int64_t)1 << 36;
 constexpr int64_t kMaxCacheRows = (int64_t)1 << 53;          // 64-bit byte offsets
+constexpr int64_t kKv4FewRows = 64;                        // a sequence's rows from which unpacking is weighed
 constexpr int64_t kMaxUnpacked = (int64_t)1 << 38;           // bytes of a workspace in bf16
 
 Range bytes_range(const void *p, int64_t rows, int64_t stride, int64_t width) {
@@ -208,35 +208,66 @@ qlin_kv_cache unpacked_cache(const qlin_batch *b, int64_t heads, void *workspace
     return c;
 }
 
+// Estimated microseconds of the kernels that read codes (rt 1, 2): `blocks` (tile, head) items,
+// sequences of up to `most` keys, in S ranges of equal size.  Fitted to graph replays of 32 / 8
+// heads.  A workgroup has some time without keys, then a step of 64 keys a wave takes `alone` where
+// it has its compute unit to itself and `paired` where two share one; ranges of several sequences
+// are assumed half as many as of the longest in each.  Measured / estimated: 32 tokens of 4096
+// keys in 1 and 2 ranges 31.3, 32.3 / 31.7, 36.4; 8 of 4000 in 2, 4, 8 20.5, 16.5, 17.5 / 21.2, 14.5, 11.5;
+// 16 tokens over 8192 in 8, 16, 32 18.2, 15.3, 16.7 / 17.2, 13.3, 13.4; 5 x 16 over 517 to 8192 in 4, 8, 12
+// 26.8, 27.3, 25.0 / 27.5, 24.9, 25.6.
+double kv4_cost(int rt, double blocks, double most, double S, bool several, double cus) {
+    const double fixed = rt == 1 ? 4.5 : 6.0, alone = rt == 1 ? 1.7 : 2.0, paired = rt == 1 ? 2.8 : 3.6;
+    const double W = blocks * (several ? 0.5 * (S + 1.0) : S), slots = 2.0 * cus;
+    const double load = std::min(std::max(W / cus - 1.0, 0.0), 1.0), steps = std::ceil(most / S / (4.0 * kKv4Keys));
+    const double one = fixed + steps * (alone + (paired - alone) * load);
+    return (W <= slots ? one : W * one / slots + 0.5 * one) + (S > 1.0 ? 3.0 + W * causal_tile_rows(rt) * (kHeadDim + 2) * 4 / 8e6 : 0.0);
+}
+
+// The same of the unpack form: two kernels that write the cache in 16 bits, then tiles of 128 rows.
+// Measured / estimated: 300 tokens behind 3700 51.9 / 46, 500 behind 7400 99 / 102, 16 x 128 behind 2872
+// 169 / 190 us.
+double unpack_cost(double tiles, double rows, double mean, double cus) { return 18.0 + rows * 1.5e-4 + 1.15 * tiles * mean * 0.033 / (2.0 * cus); }
+
 int kv4_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, Kv4Plan *p) {
-    int64_t cus = 256;
+    int64_t cus = 256;                                            // forced ranges: arithmetic
     if (splits == 0 && compute_units(&cus) != QLIN_OK) return last_status();
     const int64_t G = Hq / Hkv, most = b->max_new * G;
-    p->rt = most <= 16 ? 1 : most <= 256 || b->max_len == 0 ? 2 : 0;
-    if (p->rt == 0) {
-        int64_t attention = 0;
-        if (qlin_causal_plan(b, Hq, Hkv, kHeadDim, splits, nullptr, &attention, nullptr, 0) != QLIN_OK) return last_status();
-        if ((double)b->n_seq * (double)Hkv * (double)b->max_len * 4.0 * kHeadDim > (double)kMaxUnpacked)
-            return fail(QLIN_ERR_UNSUPPORTED, "n_seq, heads and max_len too large for long chunks in one call");
-        p->unpacked = Unpacked(b->n_seq, Hkv, b->max_len).attention;
-        p->ws_bytes = p->unpacked + attention;
-        return QLIN_OK;
-    }
+    p->rt = most <= 16 ? 1 : 2;
     const int64_t R = causal_tile_rows(p->rt), per = (most + R - 1) / R;
     // of sequences with about as many new tokens each, a tile is found without a walk over them (the
     // first microseconds of a workgroup)
     p->one_tile = (int)(per <= 1 ? 1 : b->n_seq * per <= 2 * (b->rows * G / R + 1) ? per : 0);
     const int64_t tiles = p->one_tile ? b->n_seq * per : std::min(b->n_seq * per, b->rows * G / R + b->n_seq);
-    const int64_t blocks = std::max<int64_t>(tiles * Hkv, 1), slots = 2 * cus;
-    const int64_t least = 4 * kKv4Keys;                           // a step of each wave
-    int64_t S = splits;
-    if (S == 0) S = std::max<int64_t>(1, std::min<int64_t>(slots / blocks, (b->max_len + least - 1) / least));
-    S = std::min(S, kMaxSplits);
+    const int64_t blocks = std::max<int64_t>(tiles * Hkv, 1), steps = (b->max_len + kKv4Keys - 1) / kKv4Keys;
+    // a tile's keys: of a prompt's tiles half of it on average
+    const double mean = (double)b->max_len - 0.5 * (double)std::min(b->max_new, b->max_len);
+    int64_t S = std::max<int64_t>(splits, 1);
+    double best = kv4_cost(p->rt, (double)blocks, mean, (double)S, b->n_seq > 1, (double)cus);
+    if (splits == 0 && blocks < 2 * cus)                          // more ranges of them cost more than late tails
+        for (const int64_t s : {(int64_t)2, (int64_t)3, (int64_t)4, (int64_t)6, (int64_t)8, (int64_t)12, (int64_t)16, (int64_t)24, cus / blocks, 2 * cus / blocks}) {
+            if (s < 2 || s > std::min((steps + 3) / 4, kMaxSplits)) continue;      // a step of each wave
+            const double t = kv4_cost(p->rt, (double)blocks, mean, (double)s, b->n_seq > 1, (double)cus);
+            if (t >= best) continue;
+            best = t;
+            S = s;
+        }
+    const int64_t tiles128 = std::min(b->n_seq * ((most + 127) / 128), b->rows * G / 128 + b->n_seq);
+    const double rows16 = (double)b->n_seq * (double)Hkv * (double)b->max_len;
+    if (most > kKv4FewRows && b->max_len > 0 && unpack_cost((double)(tiles128 * Hkv), rows16, mean, (double)cus) < best &&
+        rows16 * 4.0 * kHeadDim <= (double)kMaxUnpacked) {
+        int64_t attention = 0;
+        if (qlin_causal_plan(b, Hq, Hkv, kHeadDim, splits, nullptr, &attention, nullptr, 0) != QLIN_OK) return last_status();
+        p->rt = 0;
+        p->unpacked = Unpacked(b->n_seq, Hkv, b->max_len).attention;
+        p->ws_bytes = p->unpacked + attention;
+        return QLIN_OK;
+    }
     if (tiles * Hkv * std::max(S, S > 1 ? R / 2 : 0) >= (int64_t)1 << 23)
         return fail(QLIN_ERR_UNSUPPORTED, "too many rows, heads and key ranges for one call");
     p->tiles = (int)tiles;
     p->S = (int)S;
-    p->least = getenv("KVL") ? (int)(((b->max_len + 63) / 64 + S - 1) / S) : 4;
+    p->least = (int)std::max<int64_t>(splits ? 4 : (steps + S - 1) / S, 4);        // ranges of one size: short sequences stay whole
     p->ws_bytes = S > 1 ? tiles * Hkv * S * R * (kHeadDim + 2) * 4 : 0;
     return QLIN_OK;
 }

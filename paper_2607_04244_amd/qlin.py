@@ -643,12 +643,13 @@ def _attend(call, plan, dev, cache, k_cache, q, new_start, length, max_new, max_
 
 
 _scratch_bytes = {}                 # of a call's sizes
+_linear_bytes = {}
 
 
-def _remember(size, need):
-    if len(_scratch_bytes) >= 1024:
-        _scratch_bytes.clear()
-    _scratch_bytes[size] = need
+def _remember(size, need, memory=_scratch_bytes):
+    if len(memory) >= 1024:
+        memory.clear()
+    memory[size] = need
     return need
 
 
@@ -685,23 +686,27 @@ def _kv4_cache(cache, dev):
     k, kg, v, vg = cache
     at = (_address("key words", k, _torch.int32, dev), _address("value words", v, _torch.int32, dev),
           _address("key grids", kg, _torch.bfloat16, dev), _address("value grids", vg, _torch.bfloat16, dev))
-    shape, stride = k.shape, k.stride()
+    shape = k.shape
     rank = len(shape)
-    if (rank not in (3, 4) or shape[-1] != 16 or 0 in shape or v.shape != shape or kg.shape != (*shape[:-1], 2) or vg.shape != kg.shape
-            or v.stride() != stride or stride[-1] != 1 or kg.stride() != vg.stride()):
+    if rank not in (3, 4) or shape[-1] != 16 or 0 in shape or v.shape != shape or kg.shape != (*shape[:-1], 2) or vg.shape != kg.shape:
         raise ValueError("a 4-bit cache is int32 words [sequences, heads, capacity, 16] or [tokens, heads, 16] and bf16 "
                          "grids [..., 2] of keys and of values")
-    for n, words, grid in zip(shape[:-1], stride, kg.stride()):
-        if n > 1 and (words % 16 or grid * 8 != words):
-            raise ValueError("the cache's rows must be whole, words and grids alike")
-    if kg.stride()[-1] != 1:
-        raise ValueError("the cache's grids must be contiguous pairs")
-    rows = [n // 16 for n in stride[:-1]]
+    if k.is_contiguous() and v.is_contiguous() and kg.is_contiguous() and vg.is_contiguous():
+        if rank == 3:
+            return KV4Cache.from_buffer_copy(_kv4_members(0, *at, shape[1], shape[0], shape[1], 1, 0))
+        n, heads, capacity, _ = shape
+        return KV4Cache.from_buffer_copy(_kv4_members(capacity, *at, heads, (n - 1) * heads * capacity + capacity, 1, capacity,
+                                                      heads * capacity if n > 1 else 0))
+    stride, pairs = k.stride(), kg.stride()
+    if v.stride() != stride or vg.stride() != pairs or stride[-1] != 1 or pairs[-1] != 1:
+        raise ValueError("keys and values must have the same strides, words and grids be contiguous")
+    if any(n > 1 and (words % 16 or pair * 8 != words) for n, words, pair in zip(shape[:-1], stride, pairs)):
+        raise ValueError("the cache's rows must be whole, words and grids alike")
+    rows = [max(n // 16, 1) for n in stride[:-1]]
     if rank == 3:
-        return KV4Cache.from_buffer_copy(_kv4_members(0, *at, shape[1], shape[0], max(rows[0], 1), max(rows[1], 1), 0))
+        return KV4Cache.from_buffer_copy(_kv4_members(0, *at, shape[1], shape[0], rows[0], rows[1], 0))
     n, heads, capacity, _ = shape
     seq, head, token = rows
-    token, head = max(token, 1), max(head, 1)
     if n == 1:
         seq = 0
     if seq % token:
@@ -753,15 +758,23 @@ def causal_attention_kv4(q, cache, new_start, length, max_new=None, max_len=None
                    new_start, length, max_new, max_len, cache_start, scale, splits, out, workspace)
 
 
-def _rows_of(name, t, dtype, dev, rows=None, width=None):
+def _rows_of(name, t, dtype, dev, shape=None):
     """(address, elements between rows) of a tensor [rows, width] with contiguous rows."""
     at = _address(name, t, dtype, dev)
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (width is not None and t.shape[1] != width):
-        raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {'width' if width is None else width}]")
+    own = t.shape
+    if len(own) != 2 or (shape is not None and own != shape):
+        raise ValueError(f"{name} must be [rows, width]" + ("" if shape is None else f", {tuple(shape)}"))
+    if t.is_contiguous():
+        return at, own[1]
     row, one = t.stride()
-    if one != 1 and t.shape[1] > 1:
+    if one != 1 and own[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    return at, row if t.shape[0] > 1 else t.shape[1]
+    return at, row if own[0] > 1 else own[1]
+
+
+def _new_like(t, rows, width):
+    """An uninitialised bf16 tensor [rows, width] beside t (which is one)."""
+    return _torch.empty_like(t) if t.is_contiguous() else _torch.empty((rows, width), dtype=t.dtype, device=t.device)
 
 
 def block_norm(y, residual, norm=None, post_norm=None, gate=None, sigmoid=False, scale=1.0, eps=1e-6, out=None,
@@ -777,36 +790,39 @@ def block_norm(y, residual, norm=None, post_norm=None, gate=None, sigmoid=False,
     dev = _device()
     bf16 = _torch.bfloat16
     res_at, res_stride = _rows_of("residual", residual, bf16, dev)
-    rows, width = residual.shape
-    y_at = out_at = new_at = gate_at = None
+    rows, width = shape = residual.shape
+    y_at = out_at = new_at = gate_at = norm_at = post_at = None
     y_stride = out_stride = new_stride = gate_stride = 0
     if y is None:
         if residual_out is not None:
             raise ValueError("without y there is no new residual")
         residual_out = residual
     else:
-        y_at, y_stride = _rows_of("y", y, bf16, dev, rows, width)
+        y_at, y_stride = _rows_of("y", y, bf16, dev, shape)
         if residual_out is None:
-            residual_out = _torch.empty((rows, width), dtype=bf16, device=residual.device)
+            residual_out = _new_like(residual, rows, width)
             new_at, new_stride = residual_out.data_ptr(), width
         else:
-            new_at, new_stride = _rows_of("residual_out", residual_out, bf16, dev, rows, width)
+            new_at, new_stride = _rows_of("residual_out", residual_out, bf16, dev, shape)
     if norm is not None:
+        norm_at = _vector("norm", norm, bf16, dev, width)
         if out is None:
-            out = _torch.empty((rows, width), dtype=bf16, device=residual.device)
+            out = _new_like(residual, rows, width)
             out_at, out_stride = out.data_ptr(), width
         else:
-            out_at, out_stride = _rows_of("out", out, bf16, dev, rows, width)
+            out_at, out_stride = _rows_of("out", out, bf16, dev, shape)
     elif out is not None:
         raise ValueError("out needs norm")
+    if post_norm is not None:
+        post_at = _vector("post_norm", post_norm, bf16, dev, width)
     if gate is not None:
         if gate.dim() == 1:
             gate_at = _vector("gate", gate, bf16, dev, width)
         else:
-            gate_at, gate_stride = _rows_of("gate", gate, bf16, dev, rows, width)
-    _check(lib().qlin_block_norm(rows, width, y_at, y_stride, res_at, res_stride, _vector("post_norm", post_norm, bf16, dev, width),
-                                 gate_at, gate_stride, 1 if sigmoid else 0, scale, _vector("norm", norm, bf16, dev, width), eps,
-                                 new_at, new_stride, out_at, out_stride, _raw_stream(dev)))
+            gate_at, gate_stride = _rows_of("gate", gate, bf16, dev, shape)
+    _check((_lib or lib()).qlin_block_norm(rows, width, y_at, y_stride, res_at, res_stride, post_at, gate_at, gate_stride,
+                                           1 if sigmoid else 0, scale, norm_at, eps, new_at, new_stride, out_at, out_stride,
+                                           _raw_stream(dev)))
     return out, residual_out
 
 
@@ -827,48 +843,57 @@ def quantize_tokens(x, gated=False, codes=None, scale=None):
         codes = _torch.empty((rows, width), dtype=_torch.int8, device=x.device)
         codes_at, codes_stride = codes.data_ptr(), width
     else:
-        codes_at, codes_stride = _rows_of("codes", codes, _torch.int8, dev, rows, width)
+        codes_at, codes_stride = _rows_of("codes", codes, _torch.int8, dev, (rows, width))
     if scale is None:
         scale = _torch.empty(rows, dtype=_torch.float32, device=x.device)
-    _check(lib().qlin_quantize_tokens(rows, width, x_at, x_stride, 1 if gated else 0, codes_at, codes_stride,
-                                      _vector("scale", scale, _torch.float32, dev, rows), _raw_stream(dev)))
+        scale_at = scale.data_ptr()
+    else:
+        scale_at = _vector("scale", scale, _torch.float32, dev, rows)
+    _check((_lib or lib()).qlin_quantize_tokens(rows, width, x_at, x_stride, 1 if gated else 0, codes_at, codes_stride, scale_at,
+                                                _raw_stream(dev)))
     return codes, scale
 
 
 def linear_i8(x, x_scale, w, w_scale, splits=0, out=None, workspace=None):
-    """y = (x . w^T) x_scale w_scale in 8-bit integers (qlin_eight_bit_linear in include/qlin_lowbit.h).
+    """y = (x . w^T) x_scale w_scale in 8-bit integers (qlin_eight_bit_linear in
+    include/qlin_lowbit.h).
 
     x: CUDA int8 [M, K] and x_scale float32 [M] (``quantize_tokens``); w: int8 [N, K] and
     w_scale float32 [N], a scale for each channel; row slices allowed.  ``workspace`` (a CUDA
     tensor of at least the planned bytes) is allocated when needed and not given.  Returns bf16
-    [M, N].
+    [M, N], its rows a multiple of 8 elements apart.
     """
     dev = _device()
     i8, f32 = _torch.int8, _torch.float32
     x_at, x_stride = _rows_of("x", x, i8, dev)
     M, K = x.shape
-    w_at, w_stride = _rows_of("w", w, i8, dev, None, K)
+    w_at, w_stride = _rows_of("w", w, i8, dev)
     N = w.shape[0]
+    if w.shape[1] != K:
+        raise ValueError(f"w must be [channels, {K}]")
     if workspace is None:
-        size = M, N, K, splits, dev, i8
-        need = _scratch_bytes.get(size)
+        size = M, N, K, splits, dev
+        need = _linear_bytes.get(size)
         if need is None:
-            need = _remember(size, qlin_eight_bit_plan(M, N, K, splits)[1])
+            need = _remember(size, qlin_eight_bit_plan(M, N, K, splits)[1], _linear_bytes)
         if need:
             workspace = _torch.empty(need, dtype=_torch.uint8, device=x.device)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
     if out is None:
-        # rows a multiple of 8 elements apart
-        out = _torch.empty((M, (N + 7) // 8 * 8), dtype=_torch.bfloat16, device=x.device)[:, :N]
-        out_at, out_stride = out.data_ptr(), (N + 7) // 8 * 8
+        out_stride = (N + 7) // 8 * 8
+        out = _torch.empty((M, out_stride), dtype=_torch.bfloat16, device=x.device)
+        out_at = out.data_ptr()
+        if out_stride != N:
+            out = out[:, :N]
     else:
-        out_at, out_stride = _rows_of("out", out, _torch.bfloat16, dev, M, N)
+        out_at, out_stride = _rows_of("out", out, _torch.bfloat16, dev, (M, N))
         if M == 1:
             out_stride = (N + 7) // 8 * 8
-    _check(lib().qlin_eight_bit_linear(M, N, K, splits, x_at, x_stride, _vector("x_scale", x_scale, f32, dev, M), w_at, w_stride,
-                                _vector("w_scale", w_scale, f32, dev, N), out_at, out_stride, *_scratch(workspace),
-                                _raw_stream(dev)))
+    ws_at, ws_bytes = (None, 0) if workspace is None else _scratch(workspace)
+    _check((_lib or lib()).qlin_eight_bit_linear(M, N, K, splits, x_at, x_stride, _vector("x_scale", x_scale, f32, dev, M), w_at,
+                                                 w_stride, _vector("w_scale", w_scale, f32, dev, N), out_at, out_stride, ws_at,
+                                                 ws_bytes, _raw_stream(dev)))
     return out
 
 

@@ -318,6 +318,17 @@ def check_attention(new, length, layout="heads", Hq=4, Hkv=2, splits=0, seed=0, 
     return out
 
 
+# Many queries over what might be many keys take the form that unpacks the cache.
+UNPACKED = dict(Hq=64, Hkv=1, max_len=100000)
+
+
+def test_which_form_a_call_takes():
+    assert "k_kv4_few" in plan_text([1], [300], 4, 1) and "k_kv4_rows" in plan_text([16], [300], 4, 1) and "k_kv4_rows" in plan_text([300], [333], 4, 2)
+    for new in (70, 35, 200):
+        assert plan_text([new], [300], 64, 1, max_len=100000).startswith("unpack")
+    assert plan_text([80, 5], [300, 40], 128, 2, max_len=400000).startswith("unpack")
+
+
 BATCHES = [([1], [1]), ([1, 1, 1], [65, 1, 200]), ([16], [16]), ([16, 0, 7], [300, 8, 131]), ([70], [70]), ([200, 3, 1, 64], [200, 3, 150, 190]),
            ([5, 9], [3, 0]), ([1, 1], [64, 128]), ([33, 40], [333, 64]), ([1], [63])]
 
@@ -326,6 +337,18 @@ BATCHES = [([1], [1]), ([1, 1, 1], [65, 1, 200]), ([16], [16]), ([16, 0, 7], [30
 @pytest.mark.parametrize("new,length", BATCHES)
 def test_attention_batches(layout, new, length):
     check_attention(new, length, layout, seed=sum(new))
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("new,length", [([70], [70]), ([40, 1, 33], [190, 65, 140]), ([50, 9], [3, 0]), ([100], [333])])
+@pytest.mark.parametrize("splits", [0, 3])
+def test_attention_unpacked(layout, new, length, splits):
+    check_attention(new, length, layout, seed=sum(new), splits=splits, pad=2, **UNPACKED)
+
+
+def test_attention_unpacked_heads():
+    check_attention([80, 5], [300, 40], Hq=128, Hkv=2, max_len=400000, seed=3)
+    check_attention([80, 5], [300, 40], Hq=128, Hkv=2, max_len=400000, seed=3, spread=3.0, max_new=78)
 
 
 @pytest.mark.parametrize("Hq,Hkv", [(1, 1), (8, 8), (6, 2), (10, 2), (7, 1), (16, 2), (64, 1), (24, 8), (3, 3), (40, 8)])
@@ -358,8 +381,8 @@ def test_attention_every_length_up_to_two_steps():
     check_attention([1] * n, list(range(n)), Hq=4, Hkv=1, seed=8)
 
 
-@pytest.mark.parametrize("new", [1, 16, 300])
-def test_attention_weights_over_steps_of_all_sizes(new):
+@pytest.mark.parametrize("new,kw", [(1, dict(Hq=4, Hkv=1)), (16, dict(Hq=4, Hkv=1)), (300, dict(Hq=4, Hkv=1)), (60, UNPACKED)])
+def test_attention_weights_over_steps_of_all_sizes(new, kw):
     """Steps from 2^-40 to 2^20 in growing and falling order; a row of zeros among the values."""
     L = 400
     for order in (1, -1):
@@ -369,21 +392,30 @@ def test_attention_weights_over_steps_of_all_sizes(new):
         grid[17] = 0
         c.host[3][0, 0, :L] = grid
         c.dev[3][0, 0, :L] = grid.cuda()
-        check_attention([new], [L], Hq=4, Hkv=1, cache=c, seed=order + 5)
+        check_attention([new], [L], cache=c, seed=order + 5, **kw)
+
+
+def test_attention_unpacked_keys_of_all_sizes():
+    """Keys whose rows are far apart, against queries that bring their scores into range."""
+    c = Cache("heads", [200], 1, 6)
+    grid = torch.stack([2.0 ** torch.linspace(-30, 0, 200), -7 * 2.0 ** torch.linspace(-30, 0, 200)], -1).to(torch.bfloat16)
+    c.host[1][0, 0, :200] = grid
+    c.dev[1][0, 0, :200] = grid.cuda()
+    check_attention([60], [200], cache=c, seed=5, **UNPACKED)
 
 
 @pytest.mark.parametrize("power", [-60, -20, 20, 40])
-@pytest.mark.parametrize("new", [1, 12, 300])
-def test_attention_queries_of_all_sizes(new, power):
-    q = (rand(3, (new, 4, HEAD)).double() * 2.0 ** power).to(torch.bfloat16)
-    check_attention([new], [320], Hq=4, Hkv=2, q=q, scale=2.0 ** -power * 0.1, seed=power + 100)
+@pytest.mark.parametrize("new,kw", [(1, dict(Hq=4, Hkv=2)), (12, dict(Hq=4, Hkv=2)), (300, dict(Hq=4, Hkv=2)), (40, UNPACKED)])
+def test_attention_queries_of_all_sizes(new, power, kw):
+    q = (rand(3, (new, kw["Hq"], HEAD)).double() * 2.0 ** power).to(torch.bfloat16)
+    check_attention([new], [320], q=q, scale=2.0 ** -power * 0.1, seed=power + 100, **kw)
 
 
-@pytest.mark.parametrize("new,length", [([1, 1], [70, 300]), ([16, 4], [40, 200]), ([60], [60]), ([300, 20], [300, 120])])
-def test_attention_what_is_hidden_has_no_influence(new, length):
+@pytest.mark.parametrize("new,length,Hq,Hkv,max_len", [([1, 1], [70, 300], 8, 2, None), ([16, 4], [40, 200], 8, 2, None), ([60], [60], 8, 2, None),
+                                                       ([300, 20], [300, 120], 8, 2, None), ([70, 20], [70, 120], 64, 1, 100000)])
+def test_attention_what_is_hidden_has_no_influence(new, length, Hq, Hkv, max_len):
     """Codes, steps and offsets behind a token's position, infinities and NaN among them: the rows
     of earlier tokens keep every bit."""
-    Hq, Hkv = 8, 2
     q = rand(1, (sum(new), Hq, HEAD))
     c = Cache("heads", length, Hkv, 4)
     outs = []
@@ -394,7 +426,7 @@ def test_attention_what_is_hidden_has_no_influence(new, length):
                 cut = L - n + n // 2 + 1              # hidden from the first half of the new tokens
                 for part in range(4):
                     dev[part][b, :, cut:] = -1 if part % 2 == 0 else junk
-        outs.append(qlin.causal_attention_kv4(q.cuda(), dev, i32(starts(new)), i32(length), max_new=max(new)))
+        outs.append(qlin.causal_attention_kv4(q.cuda(), dev, i32(starts(new)), i32(length), max_new=max(new), max_len=max_len))
     torch.cuda.synchronize()
     m = 0
     for n in new:
@@ -403,32 +435,32 @@ def test_attention_what_is_hidden_has_no_influence(new, length):
         m += n
 
 
-@pytest.mark.parametrize("new", [1, 12, 300])
-def test_attention_rows_without_numbers(new):
+@pytest.mark.parametrize("new,G,max_len", [(1, 3, None), (12, 3, None), (300, 3, None), (100, 64, 400000)])
+def test_attention_rows_without_numbers(new, G, max_len):
     """A visible NaN row of the cache, and a query of NaN, give NaN; other heads do not see them."""
     L = new + 50
     c = Cache("heads", [L], 2, 1)
     c.dev[1][0, 0, 3] = float("nan")
-    q = rand(0, (new, 6, HEAD))
-    q[0, 4, 7] = float("nan")
-    out = qlin.causal_attention_kv4(q.cuda(), c.dev, i32([0, new]), i32([L]), max_new=new)
+    q = rand(0, (new, 2 * G, HEAD))
+    q[0, G + 1, 7] = float("nan")
+    out = qlin.causal_attention_kv4(q.cuda(), c.dev, i32([0, new]), i32([L]), max_new=new, max_len=max_len)
     torch.cuda.synchronize()
-    assert torch.isnan(out[:, :3]).all() and torch.isnan(out[0, 4]).all()
-    assert torch.isfinite(out[:, [3, 5]]).all() and torch.isfinite(out[1:, 4]).all()
+    assert torch.isnan(out[:, :G]).all() and torch.isnan(out[0, G + 1]).all()
+    assert torch.isfinite(out[:, [G, G + 2]]).all() and torch.isfinite(out[1:, G + 1]).all()
 
 
-@pytest.mark.parametrize("new", [1, 16, 300])
-def test_attention_sequences_that_count_as_empty(new):
+@pytest.mark.parametrize("new,Hq,max_len", [(1, 4, None), (16, 4, None), (300, 4, None), (50, 128, 400000)])
+def test_attention_sequences_that_count_as_empty(new, Hq, max_len):
     """Outside the cache, past the room, longer than max_len: zeros."""
     c = Cache("heads", [400] * 4, 2, 2, capacity=400)
-    q = rand(0, (4 * new, 4, HEAD)).cuda()
+    q = rand(0, (4 * new, Hq, HEAD)).cuda()
     at = starts([new] * 4)
-    out = qlin.causal_attention_kv4(q, c.dev, i32(at), i32([401, 400, 1 << 30, -5]), max_new=new)
+    out = qlin.causal_attention_kv4(q, c.dev, i32(at), i32([401, 400, 1 << 30, -5]), max_new=new, max_len=max_len)
     assert not out[:new].any() and out[new:2 * new].any() and not out[2 * new:].any()
     out = qlin.causal_attention_kv4(q, c.dev, i32(at), i32([399, 350, 351, 0]), max_new=new, max_len=350)
     assert not out[:new].any() and out[new:2 * new].any() and not out[2 * new:].any()
     start = torch.tensor([-1, 0, 3200, 2801], dtype=torch.int64, device="cuda")
-    out = qlin.causal_attention_kv4(q, c.dev, i32(at), i32([400] * 4), max_new=new, cache_start=start)
+    out = qlin.causal_attention_kv4(q, c.dev, i32(at), i32([400] * 4), max_new=new, max_len=max_len, cache_start=start)
     assert not out[:new].any() and out[new:2 * new].any() and not out[2 * new:].any()
 
 
@@ -441,10 +473,10 @@ def test_attention_and_append_past_32_bits_of_offset():
     for part in range(4):
         dev[part][at:at + 600, 0] = c.dev[part][0, 0, :600]
     start = torch.tensor([at], dtype=torch.int64, device="cuda")
-    for new in (1, 16, 300):
-        q = rand(new, (new, 2, HEAD)).cuda()
-        far = qlin.causal_attention_kv4(q, dev, i32([0, new]), i32([600]), max_new=new, max_len=600, cache_start=start)
-        near = qlin.causal_attention_kv4(q, c.dev, i32([0, new]), i32([600]), max_new=new, max_len=600)
+    for new, Hq, max_len in ((1, 2, 600), (16, 2, 600), (300, 2, 600), (100, 64, 100000)):
+        q = rand(new, (new, Hq, HEAD)).cuda()
+        far = qlin.causal_attention_kv4(q, dev, i32([0, new]), i32([600]), max_new=new, max_len=max_len, cache_start=start)
+        near = qlin.causal_attention_kv4(q, c.dev, i32([0, new]), i32([600]), max_new=new, max_len=max_len)
         assert torch.equal(far, near)
     x = [rand(i, (4, HEAD)).cuda() for i in range(3)]
     qlin.norm_rope_append_kv4(*x, dev, i32([0, 4]), i32([640]), cache_start=start)
@@ -493,15 +525,15 @@ def test_append_and_attention_together():
         assert torch.equal(got, step(x, at, length, 1)[1])
 
 
-@pytest.mark.parametrize("new", [1, 300])
-def test_graphs_that_share_a_workspace_and_streams(new):
-    Hq, Hkv, L = 8, 2, 600
+@pytest.mark.parametrize("new,Hq,Hkv,max_len", [(1, 8, 2, 603), (40, 8, 2, 603), (100, 64, 1, 100000)])
+def test_graphs_that_share_a_workspace_and_streams(new, Hq, Hkv, max_len):
+    L = 600
     c = Cache("heads", [L], Hkv, 1)
-    b = qlin.Batch(1, new, new, 603, None, None, None)
+    b = qlin.Batch(1, new, new, max_len, None, None, None)
     ws = torch.empty(qlin.qlin_causal_four_bit_plan(b, Hq, Hkv, HEAD)[1], dtype=torch.uint8, device="cuda")
     assert ws.numel() > 0
     qs, at, length = [rand(i, (new, Hq, HEAD)).cuda() for i in range(2)], i32([0, new]), i32([L])
-    run = lambda q, w: qlin.causal_attention_kv4(q, c.dev, at, length, max_new=new, workspace=w)
+    run = lambda q, w: qlin.causal_attention_kv4(q, c.dev, at, length, max_new=new, max_len=max_len, workspace=w)
     want = [run(q, None).clone() for q in qs]
     torch.cuda.synchronize()
     graphs, outs = [], []
