@@ -221,24 +221,13 @@ __device__ inline uint32_t lay_on_grid(const uint4 &y, int lane, uint32_t &grid)
     return codes;
 }
 
-// KV4: the keys in 64 bits, so that their codes are those of the definition and not those of
-// its rounding errors; rows of keys and values as codes and grids.
-template <int R, bool KV4>
-__global__ __launch_bounds__(kAppendThreads, KV4 ? 6 : 4) void k_norm_rope_append(std::conditional_t<KV4, AppendKv4Args, AppendArgs> args) {
-    __shared__ float2 cs[R][kHeadDim / 2];   // (cos, sin) of each token's angles
-    __shared__ double2 cs64[KV4 ? R : 1][KV4 ? kHeadDim / 2 : 1];
-    __shared__ int64_t slot[R];              // cache slot of each token, -1: not stored
-    __shared__ int live[R];                  // a new token of some sequence
-    const AppendArgs &a = [&]() -> const AppendArgs & {
-        if constexpr (KV4) return args.a;
-        else return args;
-    }();
-    const int lane = threadIdx.x & 63, l = threadIdx.x & 15;
-    const int groups = blockDim.x / kGroupLanes, grp = threadIdx.x / kGroupLanes;
-    const int m0 = blockIdx.x * R;
-
-#pragma unroll 1
-    for (int r = threadIdx.x >> 6; r < R; r += blockDim.x >> 6) {      // a wave a token
+// The workgroup's tokens m0 .. m0 + R - 1, a wave each: their cache slots (-1: not stored), whether
+// they are new tokens of some sequence, and (cos, sin) of their angles, in 64 bits too where
+// cs64 is given.
+template <int R>
+__device__ inline void find_tokens(const AppendArgs &a, int m0, int64_t *slot, int *live, float2 (*cs)[kHeadDim / 2], double2 (*cs64)[kHeadDim / 2]) {
+    const int lane = threadIdx.x & 63;
+    for (int r = threadIdx.x >> 6; r < R; r += blockDim.x >> 6) {
         const int m = m0 + r;
         const int b = m < a.b.rows ? find_seq(a.b, m, lane) : a.b.n_seq;
         int p = 0;
@@ -256,7 +245,7 @@ __global__ __launch_bounds__(kAppendThreads, KV4 ? 6 : 4) void k_norm_rope_appen
         }
         if (lane < a.half) {
             const double t = (double)p * (a.inv_freq[lane] * 0.15915494309189535);   // turns
-            if constexpr (KV4) {
+            if (cs64) {
                 double sn, cn;
                 sincospi(2.0 * (t - rint(t)), &sn, &cn);
                 cs64[r][angle_at(lane)] = make_double2(cn, sn);
@@ -268,6 +257,17 @@ __global__ __launch_bounds__(kAppendThreads, KV4 ? 6 : 4) void k_norm_rope_appen
             }
         }
     }
+}
+
+template <int R>
+__global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(AppendArgs a) {
+    __shared__ float2 cs[R][kHeadDim / 2];
+    __shared__ int64_t slot[R];
+    __shared__ int live[R];
+    const int lane = threadIdx.x & 63, l = threadIdx.x & 15;
+    const int groups = blockDim.x / kGroupLanes, grp = threadIdx.x / kGroupLanes;
+    const int m0 = blockIdx.x * R;
+    find_tokens<R>(a, m0, slot, live, cs, nullptr);
     __syncthreads();
 
     const int heads = a.Hq + 2 * a.Hkv;
@@ -288,41 +288,94 @@ __global__ __launch_bounds__(kAppendThreads, KV4 ? 6 : 4) void k_norm_rope_appen
             w0 = *(const uint2 *)(w + 8 * l);
             w1 = *(const uint2 *)(w + 8 * l + 4);
         }
-        if constexpr (KV4) {
-            // one token after the other, so that two workgroups' registers fit a compute unit
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            uint16_t *dst = is_q ? a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim
+                                 : (is_k ? a.kc : a.vc) + slot[r] * a.b.tok + hh * a.b.head;
+            uint4 y = x[r];
+            if (is_q || is_k) {
+                float o[8];
+                norm_rotate(a, x[r], w, w0, w1, cs[r], lane, o);
+                y = pack8(o);
+            }
+            if (is_q ? live[r] : slot[r] >= 0) store_row<R>(dst + 8 * l, y);
+        }
+    }
+}
+
+// Into the 4-bit cache.  The keys in 64 bits, so that their codes are those of the definition and
+// not those of its rounding errors: several times the instructions of a query's row, so rows
+// are dealt out keys first and few waves have those of more than one token.  8192 tokens 51 to
+// 52 us; a wave a head for all four tokens 58.3, of which the keys' 64 bits 17 (the bf16 cache
+// 40.6).  80 registers, so that two workgroups of 48 heads share a compute unit: with 88, and
+// one, 63.6.  One token a workgroup keeps the order of its heads (368 rows 7.05 us; 7.44 dealt).
+template <int R>
+__global__ __launch_bounds__(kAppendThreads, 6) void k_norm_rope_append_kv4(AppendKv4Args args) {
+    __shared__ float2 cs[R][kHeadDim / 2];
+    __shared__ double2 cs64[R][kHeadDim / 2];
+    __shared__ int64_t slot[R];
+    __shared__ int live[R];
+    const AppendArgs &a = args.a;
+    const int lane = threadIdx.x & 63, l = threadIdx.x & 15;
+    const int groups = blockDim.x / kGroupLanes, grp = threadIdx.x / kGroupLanes;
+    const int m0 = blockIdx.x * R;
+    find_tokens<R>(a, m0, slot, live, cs, cs64);
+    __syncthreads();
+
+    const int keys = R * a.Hkv, all = R * (a.Hq + 2 * a.Hkv);
+    // row i: keys of all tokens, then values, then queries
+    struct Row { bool is_k, is_q; int r, h; };
+    auto row_of = [&](int i) {
+        if constexpr (R == 1) {                          // one token: its queries, keys, values
+            const int h = i - a.Hq;
+            return Row{h >= 0 && h < a.Hkv, h < 0, 0, h < 0 ? i : h < a.Hkv ? h : h - a.Hkv};
+        }
+        Row t{i < keys, i >= 2 * keys, 0, 0};
+        const int in = t.is_q ? i - 2 * keys : t.is_k ? i : i - keys, heads = t.is_q ? a.Hq : a.Hkv;
+        const uint32_t inverse = t.is_q ? args.inv_q : args.inv_kv;
+        t.r = inverse ? (int)__umulhi((uint32_t)in, inverse) : in;
+        t.h = in - t.r * heads;
+        return t;
+    };
+    for (int i0 = grp; i0 < all; i0 += R * groups) {
+        uint4 x[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int at = i0 + i * groups;
+            x[i] = uint4{};
+            if (at >= all) continue;
+            const Row t = row_of(at);
+            if (!live[t.r]) continue;
+            const uint16_t *src = t.is_q ? a.q + (int64_t)(m0 + t.r) * a.q_stride : t.is_k ? a.k + (int64_t)(m0 + t.r) * a.k_stride : a.v + (int64_t)(m0 + t.r) * a.v_stride;
+            x[i] = load_row<R>(src + t.h * kHeadDim + 8 * l);
+        }
+        // one row after the other, so that two workgroups' registers fit a compute unit
 #pragma unroll 1
-            for (int r = 0; r < R; ++r) {
-                const uint4 now = x[0];
+        for (int i = i0; i < min(i0 + R * groups, all); i += groups) {
+            const uint4 now = x[0];
 #pragma unroll
-                for (int i = 0; i + 1 < R; ++i) x[i] = x[i + 1];
-                int at = lane;               // opaque: places in LDS worked out for each token take fewer registers
-                asm volatile("" : "+v"(at), "+v"(w0.x), "+v"(w0.y), "+v"(w1.x), "+v"(w1.y));
-                if (is_q) {
-                    float o[8];
-                    norm_rotate(a, now, w, w0, w1, cs[r], at, o);
-                    if (live[r]) store_row<R>(a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim + 8 * l, pack8(o));
-                    continue;
-                }
-                uint32_t grid;
-                const uint32_t codes = lay_on_grid(is_k ? norm_rotate_64(a, now, w, w0, w1, cs64[r], at) : now, lane, grid);
-                if (slot[r] < 0) continue;
-                const int64_t row = slot[r] * a.b.tok + hh * a.b.head;
-                (is_k ? args.c.k : args.c.v)[16 * row + l] = codes;
-                if (l == 0) (is_k ? args.c.k_grid : args.c.v_grid)[row] = grid;
+            for (int k = 0; k + 1 < R; ++k) x[k] = x[k + 1];
+            int at = lane;                   // opaque: places in LDS worked out for each row take fewer registers
+            asm volatile("" : "+v"(at));
+            const Row t = row_of(i);
+            const uint16_t *w = t.is_q ? a.q_norm : t.is_k ? a.k_norm : nullptr;
+            uint2 w0 = {}, w1 = {};
+            if (w) {
+                w0 = *(const uint2 *)(w + 8 * l);
+                w1 = *(const uint2 *)(w + 8 * l + 4);
             }
-        } else {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                uint16_t *dst = is_q ? a.q_out + (int64_t)(m0 + r) * a.q_out_stride + hh * kHeadDim
-                                     : (is_k ? a.kc : a.vc) + slot[r] * a.b.tok + hh * a.b.head;
-                uint4 y = x[r];
-                if (is_q || is_k) {
-                    float o[8];
-                    norm_rotate(a, x[r], w, w0, w1, cs[r], lane, o);
-                    y = pack8(o);
-                }
-                if (is_q ? live[r] : slot[r] >= 0) store_row<R>(dst + 8 * l, y);
+            if (t.is_q) {
+                float o[8];
+                norm_rotate(a, now, w, w0, w1, cs[t.r], at, o);
+                if (live[t.r]) store_row<R>(a.q_out + (int64_t)(m0 + t.r) * a.q_out_stride + t.h * kHeadDim + 8 * l, pack8(o));
+                continue;
             }
+            uint32_t grid;
+            const uint32_t codes = lay_on_grid(t.is_k ? norm_rotate_64(a, now, w, w0, w1, cs64[t.r], at) : now, lane, grid);
+            if (slot[t.r] < 0) continue;
+            const int64_t row = slot[t.r] * a.b.tok + t.h * a.b.head;
+            (t.is_k ? args.c.k : args.c.v)[16 * row + l] = codes;
+            if (l == 0) (t.is_k ? args.c.k_grid : args.c.v_grid)[row] = grid;
         }
     }
 }
@@ -338,16 +391,21 @@ int append_threads(const AppendArgs &a) {
 hipError_t launch_append(const AppendArgs &a, hipStream_t st) {
     if (a.b.rows == 0) return hipSuccess;
     const dim3 threads(append_threads(a));
-    if (a.b.rows < kManyRows) hipLaunchKernelGGL((k_norm_rope_append<1, false>), dim3(a.b.rows), threads, 0, st, a);
-    else hipLaunchKernelGGL((k_norm_rope_append<4, false>), dim3((a.b.rows + 3) / 4), threads, 0, st, a);
+    if (a.b.rows < kManyRows) hipLaunchKernelGGL(k_norm_rope_append<1>, dim3(a.b.rows), threads, 0, st, a);
+    else hipLaunchKernelGGL(k_norm_rope_append<4>, dim3((a.b.rows + 3) / 4), threads, 0, st, a);
     return hipGetLastError();
 }
 
 hipError_t launch_append_kv4(const AppendKv4Args &args, hipStream_t st) {
-    if (args.a.b.rows == 0) return hipSuccess;
-    const dim3 threads(append_threads(args.a));
-    if (args.a.b.rows < kManyRows) hipLaunchKernelGGL((k_norm_rope_append<1, true>), dim3(args.a.b.rows), threads, 0, st, args);
-    else hipLaunchKernelGGL((k_norm_rope_append<4, true>), dim3((args.a.b.rows + 3) / 4), threads, 0, st, args);
+    const AppendArgs &a = args.a;
+    if (a.b.rows == 0) return hipSuccess;
+    AppendKv4Args x = args;
+    auto inverse = [](int n) { return n > 1 ? (uint32_t)((((uint64_t)1 << 32) + n - 1) / n) : 0u; };
+    x.inv_q = inverse(a.Hq);
+    x.inv_kv = inverse(a.Hkv);
+    const dim3 threads(append_threads(a));
+    if (a.b.rows < kManyRows) hipLaunchKernelGGL(k_norm_rope_append_kv4<1>, dim3(a.b.rows), threads, 0, st, x);
+    else hipLaunchKernelGGL(k_norm_rope_append_kv4<4>, dim3((a.b.rows + 3) / 4), threads, 0, st, x);
     return hipGetLastError();
 }
 

@@ -548,41 +548,55 @@ __global__ __launch_bounds__(256) void k_unpack_kv4(UnpackArgs a) {
         float f[2] = {1.0f, 1.0f};
         bool by_row = false;
         if constexpr (SCALED) {
+            // the same in every lane: scalar loads, and no exchange across lanes while there are few
             float4 p = make_float4(0.0f, 0.0f, __builtin_huge_valf(), __builtin_huge_valf());
             const float4 *peaks = a.peaks + ((int64_t)b * a.heads + h) * a.peak_tiles;
-            for (int i = lane; i < (end + kPeakTokens - 1) / kPeakTokens; i += 64) {
-                const float4 x = peaks[i];
-                p = make_float4(fmaxf(p.x, x.x), fmaxf(p.y, x.y), fminf(p.z, x.z), fminf(p.w, x.w));
+            const int n = (end + kPeakTokens - 1) / kPeakTokens;
+            auto add = [&](const float4 &x) { p = make_float4(fmaxf(p.x, x.x), fmaxf(p.y, x.y), fminf(p.z, x.z), fminf(p.w, x.w)); };
+            if (n <= 8) {
+                for (int i = 0; i < n; ++i) add(peaks[i]);
+            } else {
+                for (int i = lane; i < n; i += 64) add(peaks[i]);
+                p = make_float4(-wave_min(-p.x), -wave_min(-p.y), wave_min(p.z), wave_min(p.w));
             }
-            p = make_float4(-wave_min(-p.x), -wave_min(-p.y), wave_min(p.z), wave_min(p.w));
             by_row = p.z < p.x * (1.0f / 4096.0f) || p.w < p.y * (1.0f / 4096.0f);
             const int k = by_row ? 0 : f16_exponent(p.x) - 14, v = by_row ? 0 : f16_exponent(p.y) - 14;
             if (tile == 0 && threadIdx.x == 0) a.shifts[(int64_t)b * a.heads + h] = HeadShift{(short)k, (short)v, by_row};
             f[0] = power_of_two(-k);
             f[1] = power_of_two(-v);
         }
-        for (int i = grp; i < kUnpackTokens; i += 16) {
-            const int j = first + tile * kUnpackTokens + i;
+        constexpr int kRows = kUnpackTokens / 16;             // of a group of 16 lanes, requested together
+        uint32_t w[kRows][2], g[kRows][2];
+        const int j0 = first + tile * kUnpackTokens + grp;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int64_t row = (s.slot0 + min(j0 + 16 * i, end - 1)) * a.b.tok + (int64_t)h * a.b.head;
+            w[i][0] = a.c.k[16 * row + l];
+            w[i][1] = a.c.v[16 * row + l];
+            g[i][0] = a.c.k_grid[row];
+            g[i][1] = a.c.v_grid[row];
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int j = j0 + 16 * i;
             if (j >= end) break;
-            const int64_t row = (s.slot0 + j) * a.b.tok + (int64_t)h * a.b.head;
             const int64_t to = (to0 + j) * a.to_tok + (int64_t)h * a.to_head + 8 * l;
             if (SCALED && by_row) {
                 auto shift = [](uint32_t g) {
                     return f16_exponent(fmaxf(fabsf(grid_offset(g)), fabsf(__builtin_fmaf(15.0f, grid_step(g), grid_offset(g))))) - 14;
                 };
-                const int k = shift(a.c.k_grid[row]), v = shift(a.c.v_grid[row]);
+                const int k = shift(g[i][0]), v = shift(g[i][1]);
                 if (l == 0) a.row_shifts[((int64_t)b * a.heads + h) * a.to_capacity + j] = make_short2((short)k, (short)v);
                 f[0] = power_of_two(-k);
                 f[1] = power_of_two(-v);
             }
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
-                const uint32_t w = (kv ? a.c.v : a.c.k)[16 * row + l], g = (kv ? a.c.v_grid : a.c.k_grid)[row];
-                const float st = grid_step(g) * f[kv], of = grid_offset(g) * f[kv];
+                const float st = grid_step(g[i][kv]) * f[kv], of = grid_offset(g[i][kv]) * f[kv];
                 uint32_t y[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x0 = __builtin_fmaf(st, (float)(w >> 8 * e & 15u), of), x1 = __builtin_fmaf(st, (float)(w >> (8 * e + 4) & 15u), of);
+                    const float x0 = __builtin_fmaf(st, (float)(w[i][kv] >> 8 * e & 15u), of), x1 = __builtin_fmaf(st, (float)(w[i][kv] >> (8 * e + 4) & 15u), of);
                     y[e] = SCALED ? cvt_pk_f16(x0, x1) : cvt_pk_bf16(x0, x1);
                 }
                 *(uint4 *)((kv ? a.v : a.k) + to) = make_uint4(y[0], y[1], y[2], y[3]);

@@ -53,6 +53,7 @@ struct Kv4Arrays {
 struct AppendKv4Args {
     AppendArgs a;                   // a.kc and a.vc unused
     Kv4Arrays c;
+    uint32_t inv_q, inv_kv;         // ceil(2^32 / heads), 0: one head (set by the launch)
 };
 
 struct UnpackArgs {
