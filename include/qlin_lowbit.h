@@ -44,7 +44,7 @@ extern "C" {
  *   post_norm, pre_norm   DEVICE bf16 [width]
  *   gate        DEVICE bf16 rows gate_stride apart, or [width] for all rows with
  *               gate_stride 0
- *   width       a multiple of 8, 8 .. 65536;  rows 0 .. 2^22 (0 is a no-op)
+ *   width       a multiple of 8, 8 .. 65536;  rows 0 .. 2^22 - 1 (0 is a no-op)
  *   scale       finite;  eps >= 0
  * All pointers 16-byte aligned.
  * Errors: INVALID, UNSUPPORTED (limits), ALIGN, HIP.
@@ -64,7 +64,7 @@ int qlin_block_norm(int64_t rows, int64_t width, const uint16_t *y, int64_t y_st
  *   x           DEVICE bf16 rows x_stride elements apart (a multiple of 8)
  *   codes       DEVICE int8 rows codes_stride apart (a multiple of 16)
  *   scale       DEVICE float [rows]
- *   width       a multiple of 16, 16 .. 65536;  rows 0 .. 2^22 (0 is a no-op)
+ *   width       a multiple of 16, 16 .. 65536;  rows 0 .. 2^22 - 1 (0 is a no-op)
  * x and codes 16-byte aligned; the outputs must not overlap x or each other.
  * Errors: INVALID, UNSUPPORTED, ALIGN, HIP.
  */

@@ -168,6 +168,8 @@ int i8_plan(int64_t M, int64_t N, int64_t K, int64_t splits, I8Plan *p) {
     S = std::max<int64_t>(1, std::min(S, std::min(steps, kMaxKSplits)));
     p->steps = (int)((steps + S - 1) / S);
     p->S = (int)((steps + p->steps - 1) / p->steps);
+    if (p->S > 1 && !few && tiles * f.n * f.m >= (int64_t)1 << 34)       // the joining kernel's grid
+        return fail(QLIN_ERR_UNSUPPORTED, "too many rows and channels for K ranges");
     p->ws_bytes = p->S == 1 ? 0 : (int64_t)p->S * 4 * (few ? M * N : tiles * f.n * f.m);
     return QLIN_OK;
 }
@@ -282,7 +284,7 @@ int qlin_block_norm(int64_t rows, int64_t width, const uint16_t *y, int64_t y_st
                     int64_t residual_out_stride, uint16_t *out, int64_t out_stride, void *stream) {
     clear_err();
     if (rows < 0 || width < 8 || width % 8) return fail(QLIN_ERR_INVALID, "rows must be >= 0, width a positive multiple of 8");
-    if (rows > kMaxRows || width > kMaxWidth) return fail(QLIN_ERR_UNSUPPORTED, "at most 2^22 rows of 65536");
+    if (rows >= kMaxRows || width > kMaxWidth) return fail(QLIN_ERR_UNSUPPORTED, "fewer than 2^22 rows of up to 65536");
     if (!(eps >= 0.0f) || std::isinf(eps)) return fail(QLIN_ERR_INVALID, "eps must be >= 0");
     if (!std::isfinite(scale)) return fail(QLIN_ERR_INVALID, "scale must be finite");
     if (rows == 0) return QLIN_OK;
@@ -337,7 +339,7 @@ int qlin_quantize_tokens(int64_t rows, int64_t width, const uint16_t *x, int64_t
                          int64_t codes_stride, float *scale, void *stream) {
     clear_err();
     if (rows < 0 || width < 16 || width % 16) return fail(QLIN_ERR_INVALID, "rows must be >= 0, width a positive multiple of 16");
-    if (rows > kMaxRows || width > kMaxWidth) return fail(QLIN_ERR_UNSUPPORTED, "at most 2^22 rows of 65536");
+    if (rows >= kMaxRows || width > kMaxWidth) return fail(QLIN_ERR_UNSUPPORTED, "fewer than 2^22 rows of up to 65536");
     if (rows == 0) return QLIN_OK;
     const int64_t in = gated ? 2 * width : width;
     if (check_rows(x, x_stride, in, "x") != QLIN_OK) return last_status();

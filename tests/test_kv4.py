@@ -10,8 +10,8 @@ Tolerances, derived (a rounding is off by at most half a step: bf16 2^-8 of the 
   error is e = scale (c 2^-24 (15 s + |o|) sum|q|), c = 140 for 128 products, their scaling
   and the exponent's rounding, and 2^-20 for the exponential; a weight over their sum moves by
   a factor of at most exp(2 (e + 2^-20)) either way, the result by that less 1 times B.  Each weight times step is rounded to f16,
-  2^-12 of 15 p s; below f16's normal range by 2^-25 of the unit 2^E <= s_max / 16, n 15
-  s_max 2^-29 for n keys.  fp32 sums over n keys: 2 n 2^-24 B.  The output's rounding 2^-8.
+  2^-12 of 15 p s; below f16's normal range by 2^-25 of the unit 2^E <= s_max / 16, or for odd
+  keys, whose operands are over 16, by 2^-21 of it: n 15 s_max 2^-25 for n keys.  fp32 sums over n keys: 2 n 2^-24 B.  The output's rounding 2^-8.
 * in the forms that unpack, keys and values are f16: 2^-12 of each, so e has scale 2^-12
   sum|q||k| more, and the result 2^-11 sum_j p_j |v_j| for values and weights.  A row's values
   below f16's normal range are off by 2^-25 where its largest is at least 2^2: 2^-24 of B.
@@ -285,7 +285,7 @@ def bound(qb, c, b, Hq, Hkv, scale, unpacked):
                 e += scale * 2.0 ** -12 * float((np.abs(k[:seen, g]) @ q1).max())
                 extra = 2.0 ** -11 * A[i, h] + 2.0 ** -24 * B
             x = e + 2.0 ** -20
-            tol[i, h] = np.expm1(2 * x) * B + 2.0 ** -12 * 15 * float(p @ vs[:seen, g]) + seen * 15 * vs[:seen, g].max() * 2.0 ** -29 \
+            tol[i, h] = np.expm1(2 * x) * B + 2.0 ** -12 * 15 * float(p @ vs[:seen, g]) + seen * 15 * vs[:seen, g].max() * 2.0 ** -25 \
                 + 2 * seen * 2.0 ** -24 * B + 2.0 ** -8 * np.abs(want[i, h]) + extra + 1e-38
     return want, tol
 

@@ -21,7 +21,7 @@ def norm(**kw):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(rows=-1), INVALID), (dict(rows=(1 << 22) + 1), UNSUPPORTED), (dict(width=0), INVALID), (dict(width=252), INVALID),
+    (dict(rows=-1), INVALID), (dict(rows=1 << 22), UNSUPPORTED), (dict(width=0), INVALID), (dict(width=252), INVALID),
     (dict(width=65544, ys=65544), UNSUPPORTED), (dict(eps=-1.0), INVALID), (dict(eps=NAN), INVALID), (dict(eps=INF), INVALID),
     (dict(scale=NAN), INVALID), (dict(scale=INF), INVALID), (dict(res=None), INVALID), (dict(new=None), INVALID), (dict(y=None), INVALID),
     (dict(y=None, post=None, gate=None), INVALID), (dict(y=None, post=None, gate=None, new=None, pre=None, out=None), INVALID),
@@ -49,7 +49,7 @@ def tokens(**kw):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(rows=-1), INVALID), (dict(rows=(1 << 22) + 1), UNSUPPORTED), (dict(width=0), INVALID), (dict(width=8), INVALID), (dict(width=264), INVALID),
+    (dict(rows=-1), INVALID), (dict(rows=1 << 22), UNSUPPORTED), (dict(width=0), INVALID), (dict(width=8), INVALID), (dict(width=264), INVALID),
     (dict(width=65552, xs=65552), UNSUPPORTED), (dict(x=None), INVALID), (dict(c=None), INVALID), (dict(s=None), INVALID), (dict(xs=248), INVALID),
     (dict(xs=504, gated=1), INVALID), (dict(xs=516), ALIGN), (dict(cs=240), INVALID), (dict(cs=264), ALIGN), (dict(cs=1 << 33), INVALID),
     (dict(x=A + 8), ALIGN), (dict(c=A + STEP + 8), ALIGN), (dict(s=A + 2), ALIGN), (dict(c=A + 16), INVALID), (dict(s=A + 512), INVALID),
@@ -72,7 +72,7 @@ def linear(**kw):
 
 BAD_SIZES = [(dict(M=-1), INVALID), (dict(M=(1 << 22) + 1), UNSUPPORTED), (dict(N=0), INVALID), (dict(N=(1 << 22) + 1), UNSUPPORTED),
              (dict(K=0), INVALID), (dict(K=8), INVALID), (dict(K=1000), INVALID), (dict(K=131072), UNSUPPORTED), (dict(S=-1), INVALID),
-             (dict(S=65), INVALID), (dict(M=1 << 22, N=1 << 22, S=1), UNSUPPORTED)]
+             (dict(S=65), INVALID), (dict(M=1 << 22, N=1 << 22, S=1), UNSUPPORTED), (dict(M=1 << 18, N=1 << 18, S=2), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_SIZES + [
