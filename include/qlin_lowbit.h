@@ -80,8 +80,8 @@ int qlin_quantize_tokens(int64_t rows, int64_t width, const uint16_t *x, int64_t
  * buf (at most buflen bytes).
  * Errors: INVALID, UNSUPPORTED, HIP (device query).
  */
-int qlin_eight_bit_plan(int64_t M, int64_t N, int64_t K, int64_t splits, int64_t *splits_out, int64_t *workspace_bytes, char *buf,
-                 int64_t buflen);
+int qlin_eight_bit_plan(int64_t M, int64_t N, int64_t K, int64_t splits, int64_t *splits_out,
+                        int64_t *workspace_bytes, char *buf, int64_t buflen);
 
 /*
  * qlin_eight_bit_linear -- y[m][n] = RNE_bf16( float(sum_k x[m][k] w[n][k]) * (x_scale[m] * w_scale[n]) )
@@ -99,9 +99,9 @@ int qlin_eight_bit_plan(int64_t M, int64_t N, int64_t K, int64_t splits, int64_t
  * Calls sharing a workspace must be ordered on one stream.
  * Errors: INVALID, UNSUPPORTED, ALIGN, HIP.
  */
-int qlin_eight_bit_linear(int64_t M, int64_t N, int64_t K, int64_t splits, const int8_t *x, int64_t x_stride, const float *x_scale,
-                   const int8_t *w, int64_t w_stride, const float *w_scale, uint16_t *y, int64_t y_stride, void *workspace,
-                   int64_t workspace_bytes, void *stream);
+int qlin_eight_bit_linear(int64_t M, int64_t N, int64_t K, int64_t splits, const int8_t *x, int64_t x_stride,
+                          const float *x_scale, const int8_t *w, int64_t w_stride, const float *w_scale, uint16_t *y,
+                          int64_t y_stride, void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
  * The key/value cache in 4 bits: slot s of key/value head h is row s * token_stride +
@@ -134,33 +134,35 @@ typedef struct qlin_kv4_cache {
  * Arguments, sequences and errors as qlin_norm_rope_append; two new tokens must not
  * share a slot.
  */
-int qlin_norm_rope_append_four_bit(const qlin_batch *batch, const qlin_kv4_cache *cache, int64_t q_heads, int64_t head_dim,
-                              const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride, const uint16_t *v,
-                              int64_t v_stride, const uint16_t *q_norm, const uint16_t *k_norm, float eps,
-                              const double *inv_freq, int64_t rotary_dim, int interleaved, uint16_t *q_out,
-                              int64_t q_out_stride, void *stream);
+int qlin_norm_rope_append_four_bit(const qlin_batch *batch, const qlin_kv4_cache *cache, int64_t q_heads,
+                                   int64_t head_dim, const uint16_t *q, int64_t q_stride, const uint16_t *k,
+                                   int64_t k_stride, const uint16_t *v, int64_t v_stride, const uint16_t *q_norm,
+                                   const uint16_t *k_norm, float eps, const double *inv_freq, int64_t rotary_dim,
+                                   int interleaved, uint16_t *q_out, int64_t q_out_stride, void *stream);
 
 /*
  * qlin_unpack_four_bit -- RNE_bf16(step * c + offset) (one fp32 fused product) of the batch's
  * cached tokens into a bf16 cache of as many heads: token j of sequence b goes from its
  * slot of `cache` to the same slot of `to`.  new_only: the new tokens (the first max_new of
  * the last new_start[b + 1] - new_start[b]), else all, those of sequences without new
- * tokens too.  batch->rows only bounds new_start.  A sequence whose slots are not inside both caches and their rooms, or that is longer
- * than max_len, counts as one without cached tokens.  Sequences sharing slots store the
- * same values there.
+ * tokens too.  batch->rows only bounds new_start.  A sequence whose slots are not inside
+ * both caches and their rooms, or that is longer than max_len, counts as one without
+ * cached tokens.  Sequences sharing slots store the same values there.
  * Errors: INVALID (NULL, sizes, the caches overlap, different heads), UNSUPPORTED, ALIGN, HIP.
  */
-int qlin_unpack_four_bit(const qlin_batch *batch, const qlin_kv4_cache *cache, const qlin_kv_cache *to, int64_t head_dim,
-                    int new_only, void *stream);
+int qlin_unpack_four_bit(const qlin_batch *batch, const qlin_kv4_cache *cache, const qlin_kv_cache *to,
+                         int64_t head_dim, int new_only, void *stream);
 
 /*
  * qlin_causal_four_bit_plan -- as qlin_causal_plan, for qlin_causal_attention_four_bit.  Long
- * chunks take "unpack" forms: the workspace then holds the batch's cache in bf16,
- * n_seq * heads * max_len * 512 bytes, and what qlin_causal_attention needs.
+ * chunks take "unpack" forms where that is estimated faster and at most 16 GiB: the
+ * workspace then holds the batch's cache in f16 (512 bytes a slot and head of n_seq *
+ * heads * max_len, and 4 for powers of two of its rows) and what qlin_causal_attention
+ * needs.  max_len is best kept near the longest length.
  * Errors: INVALID, UNSUPPORTED, HIP (device query).
  */
-int qlin_causal_four_bit_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t splits,
-                         int64_t *splits_out, int64_t *workspace_bytes, char *buf, int64_t buflen);
+int qlin_causal_four_bit_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                              int64_t splits, int64_t *splits_out, int64_t *workspace_bytes, char *buf, int64_t buflen);
 
 /*
  * qlin_causal_attention_four_bit -- qlin_causal_attention over a 4-bit cache: the keys and
@@ -170,15 +172,19 @@ int qlin_causal_four_bit_plan(const qlin_batch *batch, int64_t q_heads, int64_t 
  *   - the products of q with codes are scaled afterwards, in fp32, so the sum of a
  *     row's |q| and the cache's steps and offsets should be below 2^56, where nothing
  *     overflows; beyond, rows may come out as NaN;
- *   - each weight times its value's step is rounded to bf16 once, and the offsets are
- *     added in fp32; in the unpack forms keys and values are rounded to bf16 instead.
+ *   - products run in f16: q, taken to f16's range by a power of two a row, and each
+ *     weight times its value's step are rounded to 11 bits once, codes are exact, and
+ *     offsets are added in fp32; in the unpack forms keys and values are rounded to 11
+ *     bits instead, and weights as well.  The powers of two go by a sequence's rows and
+ *     change what is rounded away, nothing else.
  * A token that sees no key gives zeros; codes, steps and offsets behind a token's
  * position, infinities and NaN among them, have no influence.
  * Errors: as qlin_causal_attention.
  */
-int qlin_causal_attention_four_bit(const qlin_batch *batch, const qlin_kv4_cache *cache, int64_t q_heads, int64_t head_dim,
-                              float scale, int64_t splits, const uint16_t *q, int64_t q_stride, uint16_t *out,
-                              int64_t out_stride, void *workspace, int64_t workspace_bytes, void *stream);
+int qlin_causal_attention_four_bit(const qlin_batch *batch, const qlin_kv4_cache *cache, int64_t q_heads,
+                                   int64_t head_dim, float scale, int64_t splits, const uint16_t *q, int64_t q_stride,
+                                   uint16_t *out, int64_t out_stride, void *workspace, int64_t workspace_bytes,
+                                   void *stream);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,7 @@ constexpr int64_t kMaxRowTokens = (int64_t)1 << 20;          // 32-bit byte offs
 constexpr int64_t kMaxRowHeads = (int64_t)1 << 36;
 constexpr int64_t kMaxCacheRows = (int64_t)1 << 53;          // 64-bit byte offsets
 constexpr int64_t kKv4FewRows = 64;                        // a sequence's rows from which unpacking is weighed
-constexpr int64_t kMaxUnpacked = (int64_t)1 << 38;           // bytes of a workspace in bf16
+constexpr int64_t kMaxUnpacked = (int64_t)1 << 34;           // bytes of an unpacked cache: beyond, codes are read, which takes no such scratch
 
 Range bytes_range(const void *p, int64_t rows, int64_t stride, int64_t width) {
     return Range{(uintptr_t)p, p && rows > 0 ? (size_t)((rows - 1) * stride + width) : 0};
@@ -516,7 +516,7 @@ int qlin_causal_attention_four_bit(const qlin_batch *batch, const qlin_kv4_cache
     if (batch->max_new == 0) return QLIN_OK;
 
     if (p.rt == 0) {
-        // the cache in bf16 first; sequences that count as without cached tokens have length 0 there
+        // the cache in f16 first; sequences that count as without cached tokens have length 0 there
         const qlin_kv_cache to = unpacked_cache(batch, cache->heads, workspace);
         const Unpacked at(batch->n_seq, cache->heads, batch->max_len);
         UnpackArgs a = unpack_args(batch, cache, false);

@@ -33,8 +33,8 @@ EXPORTS = ("qlin_create", "qlin_create_symmetric", "qlin_forward", "qlin_forward
            "qlin_swa_plan", "qlin_swa_attention", "qlin_forward_group", "qlin_group_plan",
            "qlin_workspace_bytes", "qlin_forward_group_noalloc", "qlin_norm_rope_append", "qlin_causal_plan",
            "qlin_causal_attention", "qlin_verify_plan", "qlin_verify_draft", "qlin_block_norm", "qlin_quantize_tokens",
-           "qlin_eight_bit_plan", "qlin_eight_bit_linear", "qlin_norm_rope_append_four_bit", "qlin_unpack_four_bit", "qlin_causal_four_bit_plan",
-           "qlin_causal_attention_four_bit")
+           "qlin_eight_bit_plan", "qlin_eight_bit_linear", "qlin_norm_rope_append_four_bit", "qlin_unpack_four_bit",
+           "qlin_causal_four_bit_plan", "qlin_causal_attention_four_bit")
 
 _lib = None
 

@@ -227,7 +227,10 @@ def test_attention_plans():
     splits, need, text = qlin.qlin_causal_four_bit_plan(b, 32, 8, 128, 1)
     assert text.startswith("unpack=") and need >= 3 * 8 * 5000 * 512
     assert attend(b=b, wb=need - 1) == INVALID
-    # too large for that: the codes themselves; too many tiles for one grid
+    # too large for that, past 16 GiB: the codes themselves; too many tiles for one grid
+    for n, kind in ((32, "unpack="), (33, "kernel=k_kv4_rows")):
+        text = qlin.qlin_causal_four_bit_plan(batch(n_seq=n, rows=2000 * n, max_new=2000, max_len=1 << 17), 32, 8, 128, 1)[2]
+        assert text.startswith(kind)
     text = qlin.qlin_causal_four_bit_plan(batch(n_seq=65536, rows=1 << 22, max_new=1 << 22, max_len=1 << 20), 32, 8, 128, 1)[2]
     assert text.startswith("kernel=k_kv4_rows")
     with pytest.raises(qlin.QlinError) as e:
