@@ -10,9 +10,9 @@
 //       (rows, K, channels) 14.2 us, 3.55 TB/s, where a plain read of the weights takes 11.0;
 //       1 x 4096 x 2560 4.9 us, the launch and one trip to memory.
 //   k_i8_tile      tiles of 64 x 128 to 256 x 320 outputs through LDS: bound by the matrix cores and
-//       LDS reads between them, and by the clock, which falls under them.  8192 x 8192 x 8192 532
-//       us, 2065 TOP/s (the library's product 2050); 2048 x 2560 x 19456 136.5 us, 1495 TOP/s
-//       (122): 488 tiles on 256 units.
+//       LDS reads between them, and by the clock, which falls under them.  8192 x 8192 x 8192 501 to 518
+//       us, 2120 to 2195 TOP/s (the library's product 2050); 2048 x 2560 x 19456 122 to 124 us,
+//       1650 TOP/s (122): 488 tiles on 256 units.
 //   k_i8_tile_join, k_i8_join   add K ranges' sums and scale them.
 #include "target_common.h"
 #include "lowbit_internal.h"
@@ -143,15 +143,23 @@ void launch_few(const I8Args &a, int per_wave, hipStream_t st) {
 
 // ---------------------------------------------------------------- many rows
 
-// 64-byte steps of K through a ring of ST stages in LDS, filled ST - 1 steps ahead by
-// direct-to-LDS loads; one barrier a step.  WN x WM products of 32 x 32 a wave, GN x GM waves: at
-// 256 x 256 outputs LDS reads and products of a step take about as long, 4 waves of 128 x 128
-// instead of 8 of 128 x 64 read less and wait more (602 us for 8192 x 8192 x 8192 against 572).
-// A step's first fragments are read during the last products of the step before, so that a
-// wave alone on its SIMD does not wait for them.
-// Rows of 64 bytes in LDS, their 16-byte units in an order that changes every four rows: one
-// unit of 16 rows, which lanes read together, meets different banks.
-__device__ inline int tile_unit(int row, int u) { return row * 4 + (u ^ ((row >> 2) & 3)); }
+// Steps of 64 KS bytes of K through a ring of ST stages in LDS, filled ST - 1 steps ahead by
+// direct-to-LDS loads; one barrier a step.  WN x WM products of 32 x 32 a wave, GN x GM waves: 4
+// waves of 128 x 128 instead of 8 of 128 x 64 read less and wait more (602 us for 8192 x 8192 x 8192
+// against 572).  A step's first fragments are read during the last products of the step before, so
+// that a wave alone on its SIMD does not wait for them.
+// KS = 2: half the barriers, and loads of whole cache lines.  2048 x 2560 x 19456 122 to 124 us in two
+// stages against 139 in three of 64 bytes, 8192 x 8192 x 8192 501 to 518 against 542; 128 x 64 outputs 24.4 against
+// 28.1 (256 x 2560 x 9728).  128 x 128, where two stages are all that fits two workgroups, 28.4
+// against 24.8 (333 x 9728 x 2560).
+// The matrix cores alone, operands of random bits in registers, run at 3256 TOP/s on all units (4673
+// with zeros: power); with the LDS reads and a barrier beside them 2853, this kernel without its
+// loads 2659.  Loads dealt out between the products, a raised priority for them and tiles in bands
+// of 4 were equal.
+// LDS rows hold their 16-byte units in an order that changes with the row, so that one unit of 16
+// rows, which lanes read together, meets different banks.
+template <int KS>
+__device__ inline int tile_unit(int row, int u) { return KS == 1 ? row * 4 + (u ^ ((row >> 2) & 3)) : row * 8 + (u ^ ((row >> 1) & 7)); }
 
 // Workgroup b's tile.  Workgroups go to the 8 XCDs in turn; each XCD takes a contiguous part of
 // the tiles, eight of the tokens' by all of the channels', tokens fastest: what runs at once on
@@ -164,33 +172,34 @@ __device__ inline void tile_of(const I8Args &a, int b, int &tm, int &tn) {
     tm = 8 * band + in - tn * rows;
 }
 
-template <int WN, int WM, int GN, int GM, int ST, int PER_CU>
+template <int WN, int WM, int GN, int GM, int KS, int ST, int PER_CU>
 __global__ __launch_bounds__(GN * GM * 64, GN * GM * PER_CU / 4) void k_i8_tile(I8Args a) {
     constexpr int TN = 32 * WN * GN, TM = 32 * WM * GM, W = GN * GM;
-    constexpr int L = ((TN + TM) / 16 + W - 1) / W;                                 // loads of a wave a step
+    constexpr int U = 4 * KS, R = 64 / U, Q = 2 * KS, Step = KS * kI8Step;          // units of a row, rows of a load, products' parts of a step
+    constexpr int L = ((TN + TM) / R + W - 1) / W;                                  // loads of a wave a step
+    static_assert(KS == 1 || (KS == 2 && W % 2 == 0), "a place's unit is the same in each of a wave's loads");
     __shared__ __attribute__((aligned(16))) uint4 ring[ST][L * W * 64];             // rows of w, then of x (the last one again)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int hi = lane >> 5, r = lane & 31;
     int tm, tn;
     tile_of(a, blockIdx.x, tm, tn);
     const int n0 = tn * TN, m0 = tm * TM;
-    const int all = (a.K + kI8Step - 1) / kI8Step;
-    const int first = blockIdx.y * a.steps, end = min(first + a.steps, all);
+    const int k0 = blockIdx.y * a.steps * kI8Step, k1 = min(k0 + a.steps * kI8Step, a.K), end = (k1 - k0 + Step - 1) / Step;
 
-    // load i of a wave: rows 16 (wave + W i) .. + 15 of the stage, four lanes a row
+    // load i of a wave: rows R (wave + W i) .. + R - 1 of the stage, U lanes a row
     const int8_t *src[L];
-    const int unit = (lane & 3) ^ ((lane >> 4) & 3);                                // its place's unit: rows are multiples of 16
+    const int unit = KS == 1 ? (lane & 3) ^ ((lane >> 4) & 3) : (lane & 7) ^ (4 * (wave & 1) + (lane >> 4));    // its place's unit
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-        const int row = 16 * (wave + W * i) + (lane >> 2);
+        const int row = R * (wave + W * i) + lane / U;
         src[i] = row < TN ? a.w + (int64_t)min(n0 + row, a.N - 1) * a.w_stride : a.x + (int64_t)min(m0 + row - TN, a.M - 1) * a.x_stride;
     }
     const uint32_t lds = lds_addr(ring) + wave * 1024;
     auto issue = [&](int s) {
-        const int at = s * kI8Step + 16 * unit;                                     // past K: the row's first unit, left out below
-        const uint32_t to = lds + (uint32_t)((s - first) % ST) * (uint32_t)sizeof(ring[0]);
+        const int at = k0 + s * Step + 16 * unit;                                   // past the range: the row's first unit, left out below
+        const uint32_t to = lds + (uint32_t)(s % ST) * (uint32_t)sizeof(ring[0]);
 #pragma unroll
-        for (int i = 0; i < L; ++i) load_lds_a16(src[i] + (at < a.K ? at : 0), to + i * W * 1024);
+        for (int i = 0; i < L; ++i) load_lds_a16(src[i] + (at < k1 ? at : 0), to + i * W * 1024);
     };
     const int wn = 32 * WN * (wave % GN), wm = TN + 32 * WM * (wave / GN);
     v16i acc[WN][WM];
@@ -201,21 +210,21 @@ __global__ __launch_bounds__(GN * GM * 64, GN * GM * PER_CU / 4) void k_i8_tile(
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
     v4i wf[2][WN], xf[2][WM];
-    auto fragments = [&](int s, auto half) {                                        // 32 bytes of K
-        constexpr int h = decltype(half)::value;
-        const uint4 *st = ring[(s - first) % ST];
+    auto fragments = [&](int s, auto part) {                                        // 32 bytes of K
+        constexpr int q = decltype(part)::value, h = q & 1;
+        const uint4 *st = ring[s % ST];
 #pragma unroll
-        for (int i = 0; i < WN; ++i) wf[h][i] = __builtin_bit_cast(v4i, st[tile_unit(wn + 32 * i + r, 2 * h + hi)]);
+        for (int i = 0; i < WN; ++i) wf[h][i] = __builtin_bit_cast(v4i, st[tile_unit<KS>(wn + 32 * i + r, 2 * q + hi)]);
 #pragma unroll
-        for (int j = 0; j < WM; ++j) xf[h][j] = __builtin_bit_cast(v4i, st[tile_unit(wm + 32 * j + r, 2 * h + hi)]);
-        if (s * kI8Step + 16 * (2 * h + 1) >= a.K) {                                // the last, partial step
-            const bool in = s * kI8Step + 16 * (2 * h + hi) < a.K;
+        for (int j = 0; j < WM; ++j) xf[h][j] = __builtin_bit_cast(v4i, st[tile_unit<KS>(wm + 32 * j + r, 2 * q + hi)]);
+        if (k0 + s * Step + 16 * (2 * q + 1) >= k1) {                               // the last, partial step
+            const bool in = k0 + s * Step + 16 * (2 * q + hi) < k1;
 #pragma unroll
             for (int i = 0; i < WN; ++i) wf[h][i] = in ? wf[h][i] : v4i{0, 0, 0, 0};
         }
     };
-    auto products = [&](auto half) {
-        constexpr int h = decltype(half)::value;
+    auto products = [&](auto part) {
+        constexpr int h = decltype(part)::value & 1;
 #pragma unroll
         for (int i = 0; i < WN; ++i)
 #pragma unroll
@@ -227,23 +236,29 @@ __global__ __launch_bounds__(GN * GM * 64, GN * GM * PER_CU / 4) void k_i8_tile(
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
     };
-    typedef std::integral_constant<int, 0> Low;
-    typedef std::integral_constant<int, 1> High;
-    if (first < end) {
+    typedef std::integral_constant<int, 0> First;
+    typedef std::integral_constant<int, Q - 1> Last;
+    if (end > 0) {
 #pragma unroll
         for (int i = 0; i < ST - 1; ++i)
-            if (first + i < end) issue(first + i);
-        landed(first);
-        fragments(first, Low{});
-        for (int s = first; s < end; ++s) {
+            if (i < end) issue(i);
+        landed(0);
+        fragments(0, First{});
+        for (int s = 0; s < end; ++s) {
             if (s + ST - 1 < end) issue(s + ST - 1);                                // where step s - 1 was, which every wave has read
-            fragments(s, High{});
-            products(Low{});
+            fragments(s, std::integral_constant<int, 1>{});
+            products(First{});
+            if constexpr (KS == 2) {
+                fragments(s, std::integral_constant<int, 2>{});
+                products(std::integral_constant<int, 1>{});
+                fragments(s, Last{});
+                products(std::integral_constant<int, 2>{});
+            }
             if (s + 1 < end) {
                 landed(s + 1);
-                fragments(s + 1, Low{});
+                fragments(s + 1, First{});
             }
-            products(High{});
+            products(Last{});
         }
     }
     if (a.S > 1) {                                          // in the matrix cores' order
@@ -298,10 +313,10 @@ __global__ __launch_bounds__(256) void k_i8_join(I8Args a) {
     }
 }
 
-template <int WN, int WM, int GN, int GM, int ST, int PER_CU>
+template <int WN, int WM, int GN, int GM, int KS, int ST, int PER_CU>
 hipError_t launch_tile(const I8Args &a, hipStream_t st) {
     const unsigned tiles = (unsigned)(a.tiles_m * a.tiles_n);
-    hipLaunchKernelGGL((k_i8_tile<WN, WM, GN, GM, ST, PER_CU>), dim3(tiles, a.S), dim3(GN * GM * 64), 0, st, a);
+    hipLaunchKernelGGL((k_i8_tile<WN, WM, GN, GM, KS, ST, PER_CU>), dim3(tiles, a.S), dim3(GN * GM * 64), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;
     hipLaunchKernelGGL((k_i8_tile_join<WN, WM, GN, GM>), dim3(tiles * (GN * GM * WN * WM)), dim3(256), 0, st, a);
@@ -312,11 +327,11 @@ hipError_t launch_tile(const I8Args &a, hipStream_t st) {
 
 hipError_t launch_i8_linear(const I8Args &a, hipStream_t st) {
     switch (a.form) {
-    case 1: return launch_tile<2, 1, 2, 2, 4, 2>(a, st);
-    case 2: return launch_tile<2, 2, 2, 2, 4, 2>(a, st);
-    case 3: return launch_tile<2, 2, 4, 2, 3, 2>(a, st);
-    case 4: return launch_tile<4, 2, 2, 4, 4, 1>(a, st);
-    case 5: return launch_tile<5, 2, 2, 4, 3, 1>(a, st);
+    case 1: return launch_tile<2, 1, 2, 2, 2, 3, 2>(a, st);
+    case 2: return launch_tile<2, 2, 2, 2, 1, 4, 2>(a, st);
+    case 3: return launch_tile<2, 2, 4, 2, 1, 3, 2>(a, st);
+    case 4: return launch_tile<4, 2, 2, 4, 2, 2, 1>(a, st);
+    case 5: return launch_tile<5, 2, 2, 4, 2, 2, 1>(a, st);
     }
     const int per_wave = (a.steps + kFewWaves - 1) / kFewWaves;
     if (a.M <= 16) launch_few<1>(a, per_wave, st);

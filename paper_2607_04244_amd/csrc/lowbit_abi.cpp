@@ -111,23 +111,25 @@ constexpr const char *kI8Names[] = {"k_i8_few", "k_i8_tile<128x64>", "k_i8_tile<
 
 // Estimated microseconds of a call in a tile form with S ranges of K, fitted to graph replays
 // (K steps of 64 bytes; weights of several layers in turn).  A step takes `alone` where a
-// workgroup has its compute unit to itself and few work, `full` where all units do (with two on
-// a unit, for both; their clock falls), and a workgroup some time for its first loads and its
-// stores.  Measured / estimated: 2048 x 2560 x 19456 (rows, K, channels) in forms 2 to 5 169 /
-// 155 / 158 / 140 and 149 / 139 / 145 / 136 us; 8192 x 8192 x 8192 702 / 609 / 549 / 674 and
-// 875 / 660 / 595 / 773; 333 x 9728 x 2560 in form 2 with 1, 2, 3, 4, 6 ranges 58.6 / 34.4 /
-// 28.0 / 25.7 / 30.2, in form 1 46.1 / 29.7 / 32.3 / 28.6 / 31.5.
+// workgroup has its compute unit to itself and few work, `full` where all units do or it shares
+// one (for both; their clock falls), and a workgroup some time for its first loads and its
+// stores.  Measured / estimated, forms 1 to 5: 512 x 19456 x 2560 (rows, channels, K) 55.6 / 56.3 /
+// 60.0 / 49.5 / 56.9 and 52.0 / 59.2 / 55.8 / 45.5 / 52.0 us; 1500 x 2560 x 2560 18.1 / 19.8 / 26.8 /
+// 40.0 / 48.8 and 20.7 / 19.4 / 33.4 / 42.8 / 45.8; 333 x 2560 x 9728 in form 2 with 1, 2, 3, 4 ranges
+// 57.0 / 33.7 / 26.5 / 23.5 and 54.1 / 33.7 / 26.5 / 23.1.  Over 14 sizes that times of all forms were
+// taken of, its choice is the fastest measured or up to 9 % slower.
 struct I8Time { double alone, full, fixed; };
-constexpr I8Time kI8Times[] = {{}, {0.27, 0.48, 3.5}, {0.36, 0.85, 4.0}, {0.60, 1.25, 5.0}, {0.90, 1.12, 5.5}, {1.12, 1.55, 6.0}};
+constexpr I8Time kI8Times[] = {{}, {0.22, 0.38, 5.5}, {0.31, 0.62, 7.0}, {0.61, 1.17, 9.0}, {0.80, 0.99, 9.0}, {0.82, 1.35, 9.0}};
 
 double i8_cost(int form, double tiles, double tiles_m, double steps, double S, double weights, double cus) {
     const I8Form &f = kI8Forms[form];
     const I8Time &t = kI8Times[form];
     const double slots = cus * f.per_cu, rounds = std::floor(tiles * S / slots), rest = (tiles * S - rounds * slots) / cus;
-    const double range = std::ceil(steps / S), load = f.per_cu == 1 ? rest : std::max(rest - 1.0, 0.0);
+    // of two workgroups a unit, the units that have both end last, however few
+    const double range = std::ceil(steps / S), load = f.per_cu == 1 ? rest : std::min(std::max(rest - 1.0, 0.0) * 5.0, 1.0);
     const double time = rounds * (range * t.full + t.fixed) + (rest > 0.0 ? range * (t.alone + (t.full - t.alone) * load) + t.fixed : 0.0);
-    const double join = S > 1.0 ? 3.0 + S * tiles * f.n * f.m * 8.0 / 8e6 : 0.0;
-    return std::max(time, std::min(tiles_m, 2.0) * weights / 3.3e6) + join;      // two tiles of rows read the weights twice
+    const double join = S > 1.0 ? 1.8 + S * tiles * f.n * f.m * 8.0 / 1.2e7 : 0.0;
+    return std::max(time, std::min(tiles_m, 2.0) * weights / 4e6) + join;        // two tiles of rows read the weights twice
 }
 
 int i8_plan(int64_t M, int64_t N, int64_t K, int64_t splits, I8Plan *p) {

@@ -189,15 +189,18 @@ def test_linear_forced_splits(M, N, K, splits):
     check_linear(M, N, K, splits=splits, pad=32)
 
 
-@pytest.mark.parametrize("M,N,K,form", [(65, 128, 5120, "128x64"), (1500, 1500, 2000, "128x64"), (700, 6000, 1040, "128x128"), (2300, 5130, 96, "256x128"),
-                                        (2048, 19456, 272, "320x256"), (4096, 8190, 528, "256x256")])
-def test_linear_tile_forms(M, N, K, form):
-    """Each tile form, its last tiles partly outside, a last step of K that is no whole one."""
-    assert form in qlin.qlin_eight_bit_plan(M, N, K, 1)[2]
+@pytest.mark.parametrize("M,N,K,splits,form", [
+    (65, 128, 5120, 1, "128x64"), (1500, 1500, 2000, 1, "128x64"), (700, 6000, 1040, 1, "128x128"), (2300, 5130, 96, 1, "256x256"), (1600, 5100, 208, 1, "256x128"),
+    (2048, 19456, 272, 1, "320x256"), (4096, 8190, 528, 1, "256x256"), (2300, 5130, 1040, 2, "256x128"), (700, 6000, 1040, 2, "256x256"),
+    (3000, 2600, 1040, 2, "320x256"), (65, 128, 1088, 2, "128x64"), (2300, 5130, 80, 2, None), (2048, 19456, 80, 1, "320x256"), (2048, 19456, 16, 1, None)])
+def test_linear_tile_forms(M, N, K, splits, form):
+    """Each tile form, its last tiles partly outside, a last step of K that is no whole one, K ranges that
+    end inside a step."""
+    assert form is None or form in qlin.qlin_eight_bit_plan(M, N, K, splits)[2]
     g = torch.Generator(device="cuda").manual_seed(M)
     x, w = (torch.randint(-127, 128, (n, K), generator=g, dtype=torch.int8, device="cuda") for n in (M, N))
     sx, sw = (0.001 + torch.rand(n, generator=g, device="cuda") for n in (M, N))
-    y = qlin.linear_i8(x, sx, w, sw, splits=1)
+    y = qlin.linear_i8(x, sx, w, sw, splits=splits)
     total = x.double() @ w.double().t().contiguous()          # exact
     assert torch.equal(y, (total.float() * (sx[:, None] * sw)).to(torch.bfloat16))
 
