@@ -700,15 +700,16 @@ def _kv4_cache(cache, dev):
     stride, pairs = k.stride(), kg.stride()
     if v.stride() != stride or vg.stride() != pairs or stride[-1] != 1 or pairs[-1] != 1:
         raise ValueError("keys and values must have the same strides, words and grids be contiguous")
-    if any(n > 1 and (words % 16 or pair * 8 != words) for n, words, pair in zip(shape[:-1], stride, pairs)):
-        raise ValueError("the cache's rows must be whole, words and grids alike")
-    rows = [max(n // 16, 1) for n in stride[:-1]]
+    if any(n > 1 and (words % 16 or pair * 8 != words or (words == 0 and i != rank - 4))
+           for i, (n, words, pair) in enumerate(zip(shape[:-1], stride, pairs))):
+        raise ValueError("the cache's rows must be whole, each its own, words and grids alike")
+    rows = [n // 16 if many > 1 else 1 for many, n in zip(shape, stride[:-1])]
     if rank == 3:
         return KV4Cache.from_buffer_copy(_kv4_members(0, *at, shape[1], shape[0], rows[0], rows[1], 0))
     n, heads, capacity, _ = shape
     seq, head, token = rows
     if n == 1:
-        seq = 0
+        seq = 0                                              # as of sequences that share a room
     if seq % token:
         raise ValueError("the cache's sequences must lie whole tokens apart")
     seq //= token
