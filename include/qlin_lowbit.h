@@ -107,7 +107,7 @@ int qlin_eight_bit_linear(int64_t M, int64_t N, int64_t K, int64_t splits, const
  * The key/value cache in 4 bits: slot s of key/value head h is row s * token_stride +
  * h * head_stride.  A row stands for 128 values step * c[d] + offset: 16 words of eight
  * codes, that of dimension d in bits 4 (d % 8) .. + 3 of word d / 8, and a pair of bf16
- * (step, offset).  Layouts, rooms, capacity and cache_start as for qlin_kv_cache, in
+ * (step, offset), either of any sign.  Layouts, rooms, capacity and cache_start as for qlin_kv_cache, in
  * rows: [sequences][heads][capacity] has token_stride 1, head_stride capacity, seq_slots
  * heads * capacity; [tokens][heads] has token_stride heads, head_stride 1.
  */

@@ -78,6 +78,8 @@ __device__ inline void load_queries(const uint16_t *qp, v8h *qf, float &qs, floa
 }
 __device__ inline float grid_step(uint32_t g) { return bf16_lo_to_f32(g); }
 __device__ inline float grid_offset(uint32_t g) { return bf16_hi_to_f32(g); }
+// What StepScale goes by: steps of either sign.
+__device__ inline float grid_size(uint32_t g) { return fabsf(grid_step(g)); }
 
 // Smallest value over the wave.
 __device__ inline float wave_min(float v) {
@@ -272,11 +274,11 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_few(CausalKv4Args x) {
                 const bool seen = key0 + i <= last;
                 sc[i >> 2][i & 3] = seen ? sc[i >> 2][i & 3] : kNegInf;
                 vg[i] = seen ? vg[i] : 0u;
-                most = fmaxf(most, grid_step(vg[i]));
+                most = fmaxf(most, grid_size(vg[i]));
             }
             most = pair32_max(pair16_max(most));
         } else {
-            const float own = grid_step(*(const uint32_t *)(step + kVGridAt + 4 * lane));
+            const float own = grid_size(*(const uint32_t *)(step + kVGridAt + 4 * lane));
             if (__ballot(own > least_limit)) most = -wave_min(-own);
         }
         float mt = kNegInf;
@@ -393,7 +395,7 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_rows(CausalKv4Args x) 
         const char *const stage = ring[wave][st];
         float most_all = 0.0f;                                // the largest step, where some row's E has to grow
         if (!masked) {
-            const float own = grid_step(*(const uint32_t *)(stage + kVGridAt + 4 * lane));
+            const float own = grid_size(*(const uint32_t *)(stage + kVGridAt + 4 * lane));
             if (__ballot(own > least_limit)) most_all = -wave_min(-own);
         }
 #pragma unroll 1
@@ -430,7 +432,7 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_rows(CausalKv4Args x) 
                     const bool seen = key0 + i <= last;
                     e[i] = seen ? e[i] : kNegInf;
                     vg[i] = seen ? vg[i] : 0u;
-                    most = fmaxf(most, grid_step(vg[i]));
+                    most = fmaxf(most, grid_size(vg[i]));
                 }
                 most = pair32_max(most);
             }
