@@ -107,9 +107,10 @@ int qlin_eight_bit_linear(int64_t M, int64_t N, int64_t K, int64_t splits, const
  * The key/value cache in 4 bits: slot s of key/value head h is row s * token_stride +
  * h * head_stride.  A row stands for 128 values step * c[d] + offset: 16 words of eight
  * codes, that of dimension d in bits 4 (d % 8) .. + 3 of word d / 8, and a pair of bf16
- * (step, offset), either of any sign.  Layouts, rooms, capacity and cache_start as for qlin_kv_cache, in
- * rows: [sequences][heads][capacity] has token_stride 1, head_stride capacity, seq_slots
- * heads * capacity; [tokens][heads] has token_stride heads, head_stride 1.
+ * (step, offset), either of any sign.  Layouts, rooms, capacity and cache_start as for
+ * qlin_kv_cache, in rows: [sequences][heads][capacity] has token_stride 1, head_stride
+ * capacity, seq_slots heads * capacity; [tokens][heads] has token_stride heads,
+ * head_stride 1.
  */
 typedef struct qlin_kv4_cache {
     int64_t capacity;             /* slots of one sequence's room, 0 .. 2^40; 0: no bound but slots */
@@ -125,8 +126,8 @@ typedef struct qlin_kv4_cache {
 /*
  * qlin_norm_rope_append_four_bit -- qlin_norm_rope_append into a 4-bit cache: q_out is the
  * same, and the keys' and values' rows of 128 bf16 values x (keys after norm and
- * rotation, which for them run in 64 bits, rounded once to fp32 and from there to bf16)
- * are stored as
+ * rotation, which for them run in 64 bits, where no square or product of bf16 values
+ * leaves the range, rounded once to fp32 and from there to bf16) are stored as
  *   offset = min(x), step = RNE_bf16((max(x) - offset) / 15), both steps fp32
  *   c[d] = min(RNE((x[d] - offset) / step), 15), ties to even, or 0 where step is 0
  * A step below 2^-126 is 0.  A row with an infinity or NaN, or whose max - min is past

@@ -15,6 +15,7 @@
 #include "target_common.h"
 #include "lowbit_internal.h"
 
+#include <climits>
 #include <type_traits>
 
 namespace qlin {
@@ -117,12 +118,14 @@ __device__ inline void norm_rotate(const AppendArgs &a, const uint4 &x, const ui
 // lies side by side.
 __device__ inline int angle_at(int i) { return (i & 7) * 8 + (i >> 3); }
 
-// The same in 64 bits, rounded to fp32 and bf16 at the end.  x w is exact in fp32, so the row is
-// rotated before it is divided by its root, and partners travel in 32 bits.
+// The same in 64 bits, rounded to fp32 and bf16 at the end.  The row is rotated before it is divided by
+// its root: x w is exact, with 16 significant bits at most, so a double's high word holds it
+// whole, whatever its size, and partners travel in 32 bits.
 __device__ inline uint4 norm_rotate_64(const AppendArgs &a, const uint4 &x, const uint16_t *w, const uint2 &w0, const uint2 &w1,
                                        const double2 *cs, int lane) {
     const int l = lane & 15;
     float f[8], y[8];
+    int xw_hi[8];
     const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, ww[4] = {w0.x, w0.y, w1.x, w1.y};
     double ss = 0.0, inv = 1.0;
 #pragma unroll
@@ -139,28 +142,30 @@ __device__ inline uint4 norm_rotate_64(const AppendArgs &a, const uint4 &x, cons
 #pragma unroll
         for (int i = 0; i < 2; ++i) inv = __builtin_fma(0.5 * inv, __builtin_fma(-mean * inv, inv, 1.0), inv);
         if (!(mean > 0.0)) inv = 1.0 / sqrt(mean);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] *= bf16_lo_to_f32(ww[i]);
-            f[2 * i + 1] *= bf16_hi_to_f32(ww[i]);
-        }
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float by = i & 1 ? bf16_hi_to_f32(ww[i >> 1]) : bf16_lo_to_f32(ww[i >> 1]);
+        xw_hi[i] = __double2hiint(w ? (double)f[i] * (double)by : (double)f[i]);
+    }
+    auto product = [](int hi) { return __hiloint2double(hi, 0); };
     if (a.interleaved) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool in = 4 * l + i < a.half;
             const double2 t = cs[in ? angle_at(4 * l + i) : 0];
-            const double x0 = f[2 * i], x1 = f[2 * i + 1];
+            const double x0 = product(xw_hi[2 * i]), x1 = product(xw_hi[2 * i + 1]);
             y[2 * i] = (float)((in ? __builtin_fma(x0, t.x, -(x1 * t.y)) : x0) * inv);
             y[2 * i + 1] = (float)((in ? __builtin_fma(x0, t.y, x1 * t.x) : x1) * inv);
         }
     } else {
         const int hl = a.half >> 3;
         const bool lo = l < hl, in = l < 2 * hl;
-        const int from = (lane & 48) | (in ? lo ? l + hl : l - hl : l);
+        const int from = (lane & 48) | (in ? lo ? l + hl : l - hl : l), sign = lo ? 0 : INT_MIN;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const double x0 = f[i], other = __shfl(lo ? f[i] : -f[i], from);       // what the upper half gets has its sign, what the lower gets the other
+            // what the upper half gets has its sign, what the lower gets the other
+            const double x0 = product(xw_hi[i]), other = product(__shfl(xw_hi[i] ^ sign, from));
             const double2 t = cs[in ? angle_at((lo ? 8 * l : 8 * (l - hl)) + i) : 0];
             y[i] = (float)((in ? __builtin_fma(x0, t.x, other * t.y) : x0) * inv);
         }
