@@ -172,7 +172,7 @@ int qlin_causal_four_bit_plan(const qlin_batch *batch, int64_t q_heads, int64_t 
  *     are zeros): max_len sizes the workspace;
  *   - the products of q with codes are scaled afterwards, in fp32, so the sum of a
  *     row's |q| and the cache's steps and offsets should be below 2^56, where nothing
- *     overflows; beyond, rows may come out as NaN;
+ *     overflows; beyond, rows may come out as NaN.  Sizes below 2^-84 lose bits;
  *   - products run in f16: q, taken to f16's range by a power of two a row, and each
  *     weight times its value's step are rounded to 11 bits once, codes are exact, and
  *     offsets are added in fp32; in the unpack forms keys and values are rounded to 11

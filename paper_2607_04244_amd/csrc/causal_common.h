@@ -205,13 +205,14 @@ constexpr float kLazy = 8.0f;
 
 // E of a row whose weights p are multiplied by a size s of each key and rounded to f16: they are
 // held as p 2^-E, so that p s stays in range (p at most 2^kLazy, s 2^-E below 2^7).  limit: the
-// size from which E has to grow.
+// size from which E has to grow.  E is at least -80, so that the sum of 2^28 weights stays in
+// fp32; sizes below 2^-94 lose bits.
 struct StepScale {
     float e = 0.0f, limit = 0.0f;
     // What the row's sums are multiplied by for a size `most` above the limit.
     __device__ inline float raise(float most) {
         if (!(most > limit)) return 1.0f;
-        const int to = min(max(exponent_of(most) - 4, -100), 100), from = (int)e;
+        const int to = min(max(exponent_of(most) - 4, -80), 100), from = (int)e;
         e = (float)to;
         limit = power_of_two(to + 7);
         return __builtin_ldexpf(1.0f, from - to);

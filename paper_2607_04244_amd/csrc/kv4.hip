@@ -78,8 +78,9 @@ __device__ inline void load_queries(const uint16_t *qp, v8h *qf, float &qs, floa
 }
 __device__ inline float grid_step(uint32_t g) { return bf16_lo_to_f32(g); }
 __device__ inline float grid_offset(uint32_t g) { return bf16_hi_to_f32(g); }
-// What StepScale goes by: steps of either sign.
-__device__ inline float grid_size(uint32_t g) { return fabsf(grid_step(g)); }
+// What StepScale goes by: steps of either sign, and offsets, which the same weights are multiplied by
+// in fp32: p 2^-E |o| stays below 2^55.  Beside an offset a step of 2^-40 of it is nothing.
+__device__ inline float grid_size(uint32_t g) { return fmaxf(fabsf(grid_step(g)), fabsf(grid_offset(g)) * 0x1p-40f); }
 
 // Smallest value over the wave.
 __device__ inline float wave_min(float v) {
