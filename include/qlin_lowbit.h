@@ -176,10 +176,13 @@ int qlin_causal_four_bit_plan(const qlin_batch *batch, int64_t q_heads, int64_t 
  *   - products run in f16: q, taken to f16's range by a power of two a row, and each
  *     weight times its value's step are rounded to 11 bits once, codes are exact, and
  *     offsets are added in fp32; in the unpack forms keys and values are rounded to 11
- *     bits instead, and weights as well.  The powers of two go by a sequence's rows and
- *     change what is rounded away, nothing else.
+ *     bits instead, and weights as well.  The powers of two change what is rounded away,
+ *     nothing else.
  * A token that sees no key gives zeros; codes, steps and offsets behind a token's
- * position, infinities and NaN among them, have no influence.
+ * position, infinities and NaN among them, take no part in its result.  The forms that read
+ * codes keep its every bit whatever lies there; in the unpack forms the powers of two go
+ * by all finite rows of a sequence, so there finite later rows far larger or smaller than
+ * the earlier ones can change how these are rounded.
  * Errors: as qlin_causal_attention.
  */
 int qlin_causal_attention_four_bit(const qlin_batch *batch, const qlin_kv4_cache *cache, int64_t q_heads,
