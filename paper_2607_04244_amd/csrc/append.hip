@@ -65,10 +65,6 @@ __device__ inline void store_row(uint16_t *p, const uint4 &y) {
     else *(uint4 *)p = y;
 }
 
-__device__ inline uint4 pack8(const float o[8]) {
-    return make_uint4(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]), cvt_pk_bf16(o[4], o[5]), cvt_pk_bf16(o[6], o[7]));
-}
-
 // Eight dimensions (8 l .. 8 l + 7) of a head row: norm with the weights w (none: null), and the
 // rotation by the token's angles cs = (cos, sin).
 __device__ inline void norm_rotate(const AppendArgs &a, const uint4 &x, const uint16_t *w, const uint2 &w0, const uint2 &w1, const float2 *cs,
@@ -171,13 +167,6 @@ __device__ inline uint4 norm_rotate_64(const AppendArgs &a, const uint4 &x, cons
         }
     }
     return pack8(y);
-}
-
-// x / d, correctly rounded, from d's correctly rounded reciprocal (Markstein): the remainder of the
-// first quotient is exact in a fused product.
-__device__ inline float quotient(float x, float d, float inverse) {
-    const float q = x * inverse;
-    return __builtin_fmaf(__builtin_fmaf(-q, d, x), inverse, q);
 }
 
 // A row of bf16 values on its 4-bit grid: this lane's word of codes, and the row's (step, offset).

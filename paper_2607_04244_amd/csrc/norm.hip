@@ -60,9 +60,6 @@ __device__ inline void unpack8(const uint4 &x, float f[8]) {
         f[2 * i + 1] = bf16_hi_to_f32(w[i]);
     }
 }
-__device__ inline uint4 pack8(const float f[8]) {
-    return make_uint4(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]), cvt_pk_bf16(f[4], f[5]), cvt_pk_bf16(f[6], f[7]));
-}
 
 // CH units of 8 elements a thread.
 template <int CH, bool WG>
@@ -146,13 +143,6 @@ __global__ __launch_bounds__(WG ? 1024 : 64 * kWaveRows) void k_block_norm(Block
     }
 }
 
-// A quotient of fp32 numbers, correctly rounded, from the divisor's correctly rounded
-// reciprocal (Markstein): the remainder of the first quotient is exact in a fused product.
-__device__ inline float quotient(float x, float d, float inv) {
-    const float q = x * inv;
-    return __builtin_fmaf(__builtin_fmaf(-q, d, x), inv, q);
-}
-
 template <int CH, bool WG>
 __global__ __launch_bounds__(WG ? 1024 : 64 * kWaveRows) void k_quantize_tokens(QuantizeArgs a) {
     __shared__ uint32_t peaks[16];
@@ -201,17 +191,18 @@ __global__ __launch_bounds__(WG ? 1024 : 64 * kWaveRows) void k_quantize_tokens(
     }
 }
 
-// Calls run(CH, WG, grid, threads).  A wave takes rows of up to `most` units, at most 8 a lane.
-template <typename F>
-hipError_t for_rows(int rows, int width, int most, F run) {
+// Calls run(CH, WG, grid, threads).  A wave takes rows of up to Most units a lane.
+template <int Most, typename F>
+hipError_t for_rows(int rows, int width, F run) {
+    static_assert(Most == 5 || Most == 8, "the kernels that there are");
     const int units = width / 8;
-    if (rows >= 2048 && units <= most) {
+    if (rows >= 2048 && units <= 64 * Most) {
         const dim3 grid((rows + kWaveRows - 1) / kWaveRows), threads(64 * kWaveRows);
         const int per = (units + 63) / 64;
         if (per <= 1) run(std::integral_constant<int, 1>{}, std::false_type{}, grid, threads);
         else if (per <= 2) run(std::integral_constant<int, 2>{}, std::false_type{}, grid, threads);
-        else if (per <= 5) run(std::integral_constant<int, 5>{}, std::false_type{}, grid, threads);
-        else run(std::integral_constant<int, 8>{}, std::false_type{}, grid, threads);
+        else if (Most == 5 || per <= 5) run(std::integral_constant<int, 5>{}, std::false_type{}, grid, threads);
+        else run(std::integral_constant<int, Most>{}, std::false_type{}, grid, threads);
     } else {
         const int per = (units + 1023) / 1024, n = (units + per - 1) / per;
         const dim3 grid(rows), threads((n + 63) / 64 * 64);
@@ -226,13 +217,13 @@ hipError_t for_rows(int rows, int width, int most, F run) {
 }  // namespace
 
 hipError_t launch_block_norm(const BlockNormArgs &a, hipStream_t st) {
-    return for_rows(a.rows, a.width, 320, [&](auto ch, auto wg, dim3 grid, dim3 threads) {
+    return for_rows<5>(a.rows, a.width, [&](auto ch, auto wg, dim3 grid, dim3 threads) {
         hipLaunchKernelGGL((k_block_norm<decltype(ch)::value, decltype(wg)::value>), grid, threads, 0, st, a);
     });
 }
 
 hipError_t launch_quantize_tokens(const QuantizeArgs &a, hipStream_t st) {
-    return for_rows(a.rows, a.width, 512, [&](auto ch, auto wg, dim3 grid, dim3 threads) {
+    return for_rows<8>(a.rows, a.width, [&](auto ch, auto wg, dim3 grid, dim3 threads) {
         hipLaunchKernelGGL((k_quantize_tokens<decltype(ch)::value, decltype(wg)::value>), grid, threads, 0, st, a);
     });
 }

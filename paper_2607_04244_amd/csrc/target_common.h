@@ -1,5 +1,5 @@
-// Device-side helpers shared by the target's kernels (append.hip, causal.hip):
-// a sequence's rows and slots, with every bound clamped.  Header-only, inline.
+// Device-side helpers shared by the target's kernels: a sequence's rows and slots, with
+// every bound clamped, and arithmetic of rows.  Header-only, inline.
 #pragma once
 
 #include "device_common.h"
@@ -48,6 +48,18 @@ __device__ inline int find_seq(const BatchArgs &a, int m, int lane) {
     for (int i = 0; i < a.n_seq; i += 64)
         b += __popcll(__ballot(i + lane < a.n_seq && a.new_start[min(i + lane, a.n_seq - 1) + 1] <= m));
     return b;
+}
+
+// Eight values rounded to bf16.
+__device__ inline uint4 pack8(const float f[8]) {
+    return make_uint4(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]), cvt_pk_bf16(f[4], f[5]), cvt_pk_bf16(f[6], f[7]));
+}
+
+// A quotient of fp32 numbers, correctly rounded, from the divisor's correctly rounded
+// reciprocal (Markstein): the remainder of the first quotient is exact in a fused product.
+__device__ inline float quotient(float x, float d, float inv) {
+    const float q = x * inv;
+    return __builtin_fmaf(__builtin_fmaf(-q, d, x), inv, q);
 }
 
 }  // namespace qlin
