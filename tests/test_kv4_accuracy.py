@@ -153,3 +153,28 @@ def test_error_of_heads_of_different_sizes(new, length, Hq, max_len):
         parts = have[m:m + n], *errors(f64(q[m:m + n]), c, b, Hkv, HEAD ** -0.5, unpacked)
         for g in range(Hkv):
             within(*(x[:, g * G:(g + 1) * G] for x in parts), f"sequence {b} head {g}")
+
+
+# Workgroups of one and of two halves of the keys, alone and in ranges.
+SPLIT = [([130], [600], 32, 4, 8, "<1>"), ([60, 70], [300, 600], 64, 2, 12, "<1>"), ([130], [600], 128, 2, 1, "<1>"),
+         ([130], [600], 64, 2, 1, "<2>"), ([130], [600], 64, 2, 3, "<2>")]
+
+
+@pytest.mark.parametrize("new,length,Hq,Hkv,splits,kind", SPLIT)
+def test_which_workgroups_a_call_takes(new, length, Hq, Hkv, splits, kind):
+    """No launch: forced ranges are planned without a device."""
+    text = plan_text(new, length, Hq, Hkv, splits, max_len=100000 if kind == "<2>" else None)
+    assert text.startswith("unpack") and f"k_causal_prompt{kind}" in text
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("far", [False, True])
+@pytest.mark.parametrize("new,length,Hq,Hkv,splits,kind", SPLIT)
+def test_error_of_workgroups_of_one_and_two_halves(new, length, Hq, Hkv, splits, kind, far):
+    """far: rows of keys and values up to 2^16 apart, each with a power of two of its own."""
+    c = Cache("heads", length, Hkv, 9, spread=0.3)
+    if far:
+        g = torch.Generator().manual_seed(2)
+        for part in (1, 3):
+            set_grid(c, part, grid_of(0.3 * 2.0 ** (-16 * torch.rand(max(length), generator=g))))
+    check(new, length, Hq=Hq, Hkv=Hkv, cache=c, splits=splits, seed=1, max_len=100000 if kind == "<2>" else None)
