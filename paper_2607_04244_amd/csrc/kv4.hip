@@ -79,8 +79,11 @@ __device__ inline void load_queries(const uint16_t *qp, v8h *qf, float &qs, floa
 __device__ inline float grid_step(uint32_t g) { return bf16_lo_to_f32(g); }
 __device__ inline float grid_offset(uint32_t g) { return bf16_hi_to_f32(g); }
 // What StepScale goes by: steps of either sign, and offsets, which the same weights are multiplied by
-// in fp32: p 2^-E |o| stays below 2^55.  Beside an offset a step of 2^-40 of it is nothing.
-__device__ inline float grid_size(uint32_t g) { return fmaxf(fabsf(grid_step(g)), fabsf(grid_offset(g)) * 0x1p-40f); }
+// in fp32: p 2^-E |o| stays below 2^55.  Beside an offset a step of 2^-40 of it is nothing.  The
+// step's bits behind the offset's make that larger by less than a bf16 step.
+constexpr float kOffsetSize = 0x1p-40f;
+__device__ inline float offset_bound(uint32_t g) { return fabsf(__uint_as_float(g)); }
+__device__ inline float grid_size(uint32_t g) { return fmaxf(fabsf(grid_step(g)), offset_bound(g) * kOffsetSize); }
 
 // Smallest value over the wave.
 __device__ inline float wave_min(float v) {
@@ -270,14 +273,16 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_few(CausalKv4Args x) {
         }
         float most = 0.0f;                                    // the largest step, where E has to grow
         if (masked) {
+            float offset = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const bool seen = key0 + i <= last;
                 sc[i >> 2][i & 3] = seen ? sc[i >> 2][i & 3] : kNegInf;
                 vg[i] = seen ? vg[i] : 0u;
-                most = fmaxf(most, grid_size(vg[i]));
+                most = fmaxf(most, fabsf(grid_step(vg[i])));
+                offset = fmaxf(offset, offset_bound(vg[i]));
             }
-            most = pair32_max(pair16_max(most));
+            most = pair32_max(pair16_max(fmaxf(most, offset * kOffsetSize)));
         } else {
             const float own = grid_size(*(const uint32_t *)(step + kVGridAt + 4 * lane));
             if (__ballot(own > least_limit)) most = -wave_min(-own);
@@ -428,14 +433,16 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_rows(CausalKv4Args x) 
             }
             float most = most_all;
             if (masked) {
+                float offset = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const bool seen = key0 + i <= last;
                     e[i] = seen ? e[i] : kNegInf;
                     vg[i] = seen ? vg[i] : 0u;
-                    most = fmaxf(most, grid_size(vg[i]));
+                    most = fmaxf(most, fabsf(grid_step(vg[i])));
+                    offset = fmaxf(offset, offset_bound(vg[i]));
                 }
-                most = pair32_max(most);
+                most = pair32_max(fmaxf(most, offset * kOffsetSize));
             }
             float mt = kNegInf;
 #pragma unroll
