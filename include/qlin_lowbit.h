@@ -32,7 +32,8 @@ extern "C" {
  *   h = RNE_bf16(residual[m] + scale t)                          -> residual_out[m]
  *   out[m] = RNE_bf16(norm(h, pre_norm))
  *   norm(x, w)[i] = x[i] / sqrt(mean(x^2) + eps) * w[i]; the squares' sum is fp32, so
- *   a row of values above 2^60 comes out as zeros.  act is the identity, or the
+ *   a row of values above 2^60 comes out as zeros, and with eps 0 one below 2^-60 loses
+ *   bits, down to no numbers at all.  act is the identity, or the
  *   logistic function with gate_sigmoid.
  * Left out where its argument is NULL: the norm of y (post_norm), the gate, and the
  * second norm (pre_norm and out both NULL).  With y NULL the residual is normed as it
@@ -60,7 +61,8 @@ int qlin_block_norm(int64_t rows, int64_t width, const uint16_t *y, int64_t y_st
  *       gated (silu(a) = a / (1 + e^-a), in fp32)
  *   scale[m] = max |v| / 127  (fp32);  codes[m][i] = RNE(v[i] / scale[m]), -127 .. 127
  * A row with an infinity or NaN has scale NaN and codes 0; one whose largest value is
- * below 2^-100 counts as zeros (scale 0).
+ * below 2^-100 counts as zeros (scale 0).  Rows of bf16 weights, a channel each, give that
+ * linear's w and w_scale in the same way.
  *   x           DEVICE bf16 rows x_stride elements apart (a multiple of 8)
  *   codes       DEVICE int8 rows codes_stride apart (a multiple of 16)
  *   scale       DEVICE float [rows]
@@ -159,7 +161,9 @@ int qlin_unpack_four_bit(const qlin_batch *batch, const qlin_kv4_cache *cache, c
  * chunks take "unpack" forms where that is estimated faster and at most 16 GiB: the
  * workspace then holds the batch's cache in f16 (512 bytes a slot and head of n_seq *
  * heads * max_len, and 4 for powers of two of its rows) and what qlin_causal_attention
- * needs.  max_len is best kept near the longest length.
+ * needs.  Every sequence has room for max_len there, so that is as much as a bf16 cache of
+ * such rooms and more than a packed one: keep max_len near the longest length, and large
+ * chunks of a few sequences a call where memory is short.
  * Errors: INVALID, UNSUPPORTED, HIP (device query).
  */
 int qlin_causal_four_bit_plan(const qlin_batch *batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,

@@ -299,10 +299,12 @@ __global__ __launch_bounds__(kAppendThreads) void k_norm_rope_append(AppendArgs 
 
 // Into the 4-bit cache.  The keys in 64 bits, so that their codes are those of the definition and
 // not those of its rounding errors: several times the instructions of a query's row, so rows
-// are dealt out keys first and few waves have those of more than one token.  8192 tokens 51 to
-// 52 us; a wave a head for all four tokens 58.3, of which the keys' 64 bits 17 (the bf16 cache
+// are dealt out keys first and few waves have those of more than one token.  8192 tokens 52
+// us; a wave a head for all four tokens 58.3, of which the keys' 64 bits 17 (the bf16 cache
 // 40.6).  80 registers, so that two workgroups of 48 heads share a compute unit: with 88, and
-// one, 63.6.  One token a workgroup keeps the order of its heads (368 rows 7.05 us; 7.44 dealt).
+// one, 63.6.  One token a workgroup keeps the order of its heads (368 rows 7.05 us; 7.44 dealt): a launch
+// and three trips to memory one after the other, as rows are requested behind the search for
+// their sequence; and under the bound of registers meant for four tokens it keeps one in scratch.
 template <int R>
 __global__ __launch_bounds__(kAppendThreads, 6) void k_norm_rope_append_kv4(AppendKv4Args args) {
     __shared__ float2 cs[R][kHeadDim / 2];

@@ -8,10 +8,11 @@
 // and four ANDs.  What a row's step s and offset o add is one product for each key and row,
 // not one for each value:
 //   q . k = s (q . c) + o sum(q),   sum_j p_j v_j = sum_j (p_j s_j) c_j + sum_j p_j o_j
-// with p_j s_j rounded to f16 once, its operand (11 bits: the error of an output is that of
-// its own rounding to bf16).  Queries are brought into f16's range by a power of two for each
-// row; weights by 2^-E for each row, E from the largest step that the row has seen, raised
-// as the maximum is, so weights times steps keep their 11 bits down to 2^-15 of the largest.
+// with p_j s_j rounded to f16 once, its operand (11 bits: against 64 bits an output's error is 1.75e-3 in
+// the 2-norm, of which its own rounding to bf16 is 1.65e-3).  Queries are brought into f16's range by a
+// power of two for each row; weights by 2^-E for each row, E from the largest size of step that
+// the row has seen, raised as the maximum is, so weights times steps keep their 11 bits down to
+// 2^-15 of the largest.
 // The contraction's order is free: a lane's K words are 32 (64) dimensions in a row, whose
 // queries are brought into the extraction's order once, and V comes transposed from LDS, 16
 // keys of a dimension a lane.  Codes are finite whatever lies behind a row's token, and a
@@ -20,14 +21,19 @@
 //   k_kv4_few      up to 16 rows (single tokens): bound by the cache's bytes where many sequences
 //       are read, 64 of 4096 keys 48.3 to 50.4 us, 5.7 to 5.9 TB/s, and 64 of 130 to 8190 64 to 67, by
 //       the longest; one token over 8191 keys 7.2 us and 3.2 for the join, its latency.
-//   k_kv4_rows     tiles of 32 rows (blocks, chunks, short prompts): bound by vector instructions,
-//       about 300 for 16 products of 32 keys and rows, 16 exponentials among them.  32 sequences of
-//       16 tokens over 4096 keys 62 to 66 us; 16 tokens over 8192 keys 15.3, 512 without a prefix 13.0.
-//       Tiles of 64 rows with one extraction for both, alone on a compute unit: 78 and 19.0 us.
+//   k_kv4_rows     tiles of 32 rows (blocks, chunks, short prompts): about 350 vector instructions for
+//       16 products of 32 keys and rows, 16 exponentials among them.  They bound it where all units
+//       work: 32 sequences of 16 tokens over 4096 keys 65 to 69 us, the vector unit busy for 73 % of
+//       them, the matrix cores for 25.  Few blocks leave both idle: five of 517 to 8192 keys 38 and 10 %
+//       of 23 us, in which a wave has four steps at most, behind its start and before the sums of
+//       four waves are merged.  16 tokens over 8192 keys 15.6, 512 without a prefix 13.7.  Tiles of
+//       64 rows with one extraction for both, alone on a compute unit: 78 and 19.0 us.
 //   k_kv4_peaks, k_unpack_kv4   the cache in 16 bits, bf16 for a caller and f16 for
 //       k_causal_prompt, which long chunks go through (causal.hip): its 11 bits keep the result as
 //       exact as above, where bf16's 8 would take its error from 1.7e-3 to 4.1e-3.  8192 tokens of 8
-//       heads 8.2 to 9.8 us, 4.3 to 5 TB/s; packed prompts of 1 to 2048 4.9 and 13.6 of 130 in all.
+//       heads 8.2 to 9.9 us, 4.3 to 5 TB/s; packed prompts of 1 to 2048 4.9 and 13.7 of 130 in all.
+//       Heads whose rows have a power each go through that kernel's careful pass, behind a first one
+//       that is thrown away: with one row 2^13 below the others a prompt of 2048 takes 254 us for 63.
 #include "causal_common.h"
 #include "lowbit_internal.h"
 

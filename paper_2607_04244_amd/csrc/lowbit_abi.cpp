@@ -230,7 +230,8 @@ double kv4_cost(int rt, double blocks, double most, double S, bool several, doub
 
 // The same of the unpack form: two kernels that write the cache in 16 bits, then tiles of 128 rows.
 // Measured / estimated: 300 tokens behind 3700 51.9 / 46, 500 behind 7400 99 / 102, 16 x 128 behind 2872
-// 169 / 190 us.
+// 169 / 190 us.  What it cannot know: heads that go by a power for each row (cached rows more than 2^12
+// apart) take up to four times as long, 500 behind 7400 348 us.
 double unpack_cost(double tiles, double rows, double mean, double cus) { return 18.0 + rows * 1.5e-4 + 1.15 * tiles * mean * 0.033 / (2.0 * cus); }
 
 int kv4_plan(const qlin_batch *b, int64_t Hq, int64_t Hkv, int64_t splits, Kv4Plan *p) {

@@ -752,7 +752,9 @@ def causal_attention_kv4(q, cache, new_start, length, max_new=None, max_len=None
 
     cache: the four tensors of ``new_kv4_cache``; the other arguments as for
     ``causal_attention``, where max_len also bounds what is computed: rows of longer
-    sequences are zeros.  Returns ``out`` [rows, q heads, 128].
+    sequences are zeros.  It sizes the scratch of long chunks too, 512 bytes for each sequence,
+    head and token up to max_len, at most 16 GiB: over a packed cache, whose default is all of its
+    tokens, give the longest length.  Returns ``out`` [rows, q heads, 128].
     """
     dev = _device()
     return _attend(lib().qlin_causal_attention_four_bit, lib().qlin_causal_four_bit_plan, dev, _kv4_cache(cache, dev), cache[0], q,
@@ -860,7 +862,8 @@ def linear_i8(x, x_scale, w, w_scale, splits=0, out=None, workspace=None):
     include/qlin_lowbit.h).
 
     x: CUDA int8 [M, K] and x_scale float32 [M] (``quantize_tokens``); w: int8 [N, K] and
-    w_scale float32 [N], a scale for each channel; row slices allowed.  ``workspace`` (a CUDA
+    w_scale float32 [N], a scale for each channel (``quantize_tokens`` of bf16 weights [N, K], up to
+    its widths, or any other int8 rows); row slices allowed.  ``workspace`` (a CUDA
     tensor of at least the planned bytes) is allocated when needed and not given.  Returns bf16
     [M, N], its rows a multiple of 8 elements apart.
     """
