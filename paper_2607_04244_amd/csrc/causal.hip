@@ -866,7 +866,7 @@ __global__ __launch_bounds__(HALVES * kPromptWaves * 64, 2 / HALVES) void k_caus
 // with few rows by one trip to memory for the lengths and one for all ranges.
 constexpr int kJoinBatch = 8;      // ranges requested together
 
-template <int RT, int P>
+template <int RT, int P, bool SEVERAL>
 __global__ __launch_bounds__(256) void k_causal_join(CausalArgs a) {
     constexpr int R = causal_tile_rows(RT);
     __shared__ float2 gml[4][64];
@@ -874,7 +874,7 @@ __global__ __launch_bounds__(256) void k_causal_join(CausalArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = wave % P;
     const int unit = (blockIdx.y * 4 + wave) / P;
     Work w;
-    if (!find_work<R>(a, lane, 0, w)) return;
+    if (!find_work<R, SEVERAL>(a, lane, 0, w)) return;
     int row, d;                                                    // of this lane
     if (RT == 1) {
         row = 16 * (unit >> 3) + (lane & 15);
@@ -883,7 +883,7 @@ __global__ __launch_bounds__(256) void k_causal_join(CausalArgs a) {
         row = 32 * (unit >> 4) + (lane & 31);
         d = 8 * (unit & 15) + 4 * (lane >> 5);
     }
-    const int used = w.hi > 0 ? range_of(a, (w.hi + a.step_keys - 1) / a.step_keys, 0).used : 0;
+    const int used = w.hi > 0 ? range_of(a, (w.hi + (1 << a.step_shift) - 1) >> a.step_shift, 0).used : 0;
     const bool on = row < w.rows;
     float m = kNegInf, ls = 0.0f;
     v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -925,11 +925,11 @@ __global__ __launch_bounds__(256) void k_causal_join(CausalArgs a) {
     store_out(a, w, row_of(a, w, row), d, acc, ls);
 }
 
-template <int RT>
+template <int RT, bool SEVERAL = false>
 void launch_join(const CausalArgs &a, hipStream_t st) {
     constexpr int units = causal_tile_rows(RT) / 2;                // of an item
-    if (a.S > 4) hipLaunchKernelGGL((k_causal_join<RT, 4>), dim3((unsigned)(a.tiles * a.Hkv), units), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_causal_join<RT, 1>), dim3((unsigned)(a.tiles * a.Hkv), units / 4), dim3(256), 0, st, a);
+    if (a.S > 4) hipLaunchKernelGGL((k_causal_join<RT, 4, SEVERAL>), dim3((unsigned)(a.tiles * a.Hkv), units), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_causal_join<RT, 1, SEVERAL>), dim3((unsigned)(a.tiles * a.Hkv), units / 4), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -938,17 +938,15 @@ const char *causal_kernel_name(int rt, int halves) {
     return rt == 1 ? "k_causal_few" : rt == 2 ? "k_causal_mid<1>" : rt == 4 ? "k_causal_mid<2>" : halves == 2 ? "k_causal_prompt<2>" : "k_causal_prompt<1>";
 }
 
-hipError_t launch_causal_join(const CausalArgs &a, int rt, hipStream_t st) {
+hipError_t launch_kv4_join(const CausalArgs &a, int rt, hipStream_t st) {
     if (rt == 1) launch_join<1>(a, st);
-    else if (rt == 2) launch_join<2>(a, st);
-    else if (rt == 4) launch_join<4>(a, st);
-    else launch_join<0>(a, st);
+    else launch_join<2, true>(a, st);
     return hipGetLastError();
 }
 
 hipError_t launch_causal(const CausalArgs &args, int rt, int halves, hipStream_t st) {
     CausalArgs a = args;
-    a.step_keys = rt == 1 ? kFewKeys : rt ? kMidKeys : kStepKeys;
+    a.step_shift = shift_of(rt == 1 ? kFewKeys : rt ? kMidKeys : kStepKeys);
     const dim3 grid((unsigned)(a.tiles * a.Hkv), (unsigned)a.S);
     if (rt == 1) hipLaunchKernelGGL(k_causal_few, grid, dim3(kFewWaves * 64), 0, st, a);
     else if (rt == 2) hipLaunchKernelGGL(k_causal_mid<1>, grid, dim3(256), 0, st, a);
@@ -958,7 +956,12 @@ hipError_t launch_causal(const CausalArgs &args, int rt, int halves, hipStream_t
     else if (halves == 2) hipLaunchKernelGGL((k_causal_prompt<2, InBf16>), grid, dim3(2 * kPromptWaves * 64), 0, st, a);
     else hipLaunchKernelGGL((k_causal_prompt<1, InBf16>), grid, dim3(kPromptWaves * 64), 0, st, a);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess || a.S == 1 ? e : launch_causal_join(a, rt, st);
+    if (e != hipSuccess || a.S == 1) return e;
+    if (rt == 1) launch_join<1>(a, st);
+    else if (rt == 2) launch_join<2>(a, st);
+    else if (rt == 4) launch_join<4>(a, st);
+    else launch_join<0>(a, st);
+    return hipGetLastError();
 }
 
 }  // namespace qlin

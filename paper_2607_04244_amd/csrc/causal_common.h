@@ -129,18 +129,22 @@ __device__ inline int64_t uniform(int64_t v) {
 
 // Workgroup (x, y): key range y of item x = tile number * heads + head.  Workgroups go to the 8 XCDs
 // in turn, x first: with a multiple of 8 heads all work on one head is on one XCD, and its
-// keys are shared in that XCD's L2.
-template <int R>
+// keys are shared in that XCD's L2.  SEVERAL: one_tile may be more than 1 (the division takes the
+// kernels that cannot have that 0.1 to 0.2 us).
+template <int R, bool SEVERAL = false>
 __device__ inline bool find_work(const CausalArgs &a, int lane, int split, Work &w) {
     const int item = gn_chunk(blockIdx.x, a.Hkv, a.inv_heads, a.heads_shift);
     w.h = blockIdx.x - item * a.Hkv;
     w.split = split;
     int tile = 0;
     if (a.one_tile) {
-        const int b = a.one_tile == 1 ? item : item / a.one_tile;
+        int b = item;
+        if (SEVERAL && a.one_tile > 1) {
+            b = item / a.one_tile;
+            tile = a.one_tile - 1 - (item - b * a.one_tile);
+        }
         if (b >= a.b.n_seq) return false;
         w.s = load_seq(a.b, b);
-        tile = a.one_tile == 1 ? 0 : a.one_tile - 1 - (item - b * a.one_tile);
     } else {
         // where all workgroups run at once, two a compute unit, a long one goes with a short one
         const int half = (a.tiles + 1) / 2, idx = a.pairs && item >= half ? a.tiles - 1 - (item - half) : item;
@@ -184,6 +188,9 @@ __device__ inline Range range_of(const CausalArgs &a, int all, int split) {
     const int per = max((all + a.S - 1) / a.S, a.least);
     return Range{split * per, min((split + 1) * per, all), (all + per - 1) / per};
 }
+
+// log2 of a step's keys, for the join, which a division by them would take 0.15 to 0.4 us.
+constexpr int shift_of(int keys) { return keys > 1 ? 1 + shift_of(keys / 2) : 0; }
 
 // Partial results: for each item and range the tile's sums as the matrix cores leave them, in
 // units of 64 lanes x 4 values (1 KiB, one store of a wave), and (maximum, sum of weights) of

@@ -361,7 +361,7 @@ __global__ __launch_bounds__(kKvWaves * 64, 2) void k_kv4_rows(CausalKv4Args x) 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int hi = lane >> 5, r = lane & 31;
     Work w;
-    if (!find_work<R>(a, lane, blockIdx.y, w)) return;
+    if (!find_work<R, true>(a, lane, blockIdx.y, w)) return;
     const Range range = range_of(a, (w.hi + kKv4Keys - 1) / kKv4Keys, w.split);
     if (a.S > 1 && w.split >= range.used) return;
     const int u0 = range.first, u1 = range.end;
@@ -639,12 +639,12 @@ const char *causal_kv4_kernel_name(int rt) { return rt == 1 ? "k_kv4_few" : "k_k
 
 hipError_t launch_causal_kv4(const CausalKv4Args &args, int rt, hipStream_t st) {
     CausalKv4Args x = args;
-    x.a.step_keys = kKv4Keys;
+    x.a.step_shift = shift_of(kKv4Keys);
     const dim3 grid((unsigned)(x.a.tiles * x.a.Hkv), (unsigned)x.a.S), threads(kKvWaves * 64);
     if (rt == 1) hipLaunchKernelGGL(k_kv4_few, grid, threads, 0, st, x);
     else hipLaunchKernelGGL(k_kv4_rows, grid, threads, 0, st, x);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess || x.a.S == 1 ? e : launch_causal_join(x.a, rt, st);
+    return e != hipSuccess || x.a.S == 1 ? e : launch_kv4_join(x.a, rt, st);
 }
 
 hipError_t launch_unpack_kv4(const UnpackArgs &a, hipStream_t st) {

@@ -45,7 +45,7 @@ struct CausalArgs {
     int one_tile;                   // this many tiles a sequence (1: tile i is sequence i); 0: as many as its rows need
     int pairs;                      // at most two workgroups a compute unit
     int S, least;                   // key ranges; least steps of one
-    int step_keys;                  // keys of a step (set by the launch)
+    int step_shift;                 // a step has 2^step_shift keys (set by the launch)
     int max_len;                    // bound of the sequences' lengths (orders the tiles)
     uint32_t inv_heads, inv_g;      // x / Hkv by gn_chunk; ceil(2^32 / G) (0: G = 1)
     int heads_shift;
@@ -82,7 +82,7 @@ struct VerifyArgs {
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st);
 hipError_t launch_causal(const CausalArgs &a, int rt, int halves, hipStream_t st);
-hipError_t launch_causal_join(const CausalArgs &a, int rt, hipStream_t st);   // a.step_keys as the ranges' kernel
+hipError_t launch_kv4_join(const CausalArgs &a, int rt, hipStream_t st);      // rt 1, 2
 const char *causal_kernel_name(int rt, int halves);
 hipError_t launch_verify(VerifyArgs a, int n_seq, bool many, hipStream_t st);
 
