@@ -550,7 +550,7 @@ def norm_rope_append(q, k, v, k_cache, v_cache, new_start, length, max_new=None,
     q heads, 128]; rows of no sequence are left as they are.
     """
     dev = _device()
-    return _append(lib().qlin_norm_rope_append, dev, _kv_cache(k_cache, v_cache, dev), k_cache, q, k, v, new_start, length,
+    return _append((_lib or lib()).qlin_norm_rope_append, dev, _kv_cache(k_cache, v_cache, dev), k_cache, q, k, v, new_start, length,
                    max_new, max_len, cache_start, q_norm, k_norm, eps, inv_freq, interleaved, out)
 
 
@@ -605,11 +605,12 @@ def causal_attention(q, k_cache, v_cache, new_start, length, max_new=None, max_l
     they are.
     """
     dev = _device()
-    return _attend(lib().qlin_causal_attention, lib().qlin_causal_plan, dev, _kv_cache(k_cache, v_cache, dev), k_cache, q,
+    L = _lib or lib()
+    return _attend(L.qlin_causal_attention, L.qlin_causal_plan, _scratch_bytes, dev, _kv_cache(k_cache, v_cache, dev), k_cache, q,
                    new_start, length, max_new, max_len, cache_start, scale, splits, out, workspace)
 
 
-def _attend(call, plan, dev, cache, k_cache, q, new_start, length, max_new, max_len, cache_start, scale, splits, out,
+def _attend(call, plan, memory, dev, cache, k_cache, q, new_start, length, max_new, max_len, cache_start, scale, splits, out,
             workspace):
     bf16 = _torch.bfloat16
     q_at = _address("q", q, bf16, dev)
@@ -619,12 +620,12 @@ def _attend(call, plan, dev, cache, k_cache, q, new_start, length, max_new, max_
     q_stride = _row_stride("q", q, Hq)
     batch = _batch(dev, rows, new_start, length, max_new, max_len, cache_start, k_cache)
     if workspace is None:
-        size = plan.__name__, batch.n_seq, rows, batch.max_new, batch.max_len, Hq, cache.heads, D, splits, dev
-        need = _scratch_bytes.get(size)
+        size = batch.n_seq, rows, batch.max_new, batch.max_len, Hq, cache.heads, D, splits, dev
+        need = memory.get(size)
         if need is None:
             need = ctypes.c_int64()
             _check(plan(batch, Hq, cache.heads, D, splits, None, ctypes.byref(need), None, 0))
-            need = _remember(size, need.value)
+            need = _remember(size, need.value, memory)
         if need:
             workspace = _torch.empty(need, dtype=_torch.uint8, device=q.device)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
@@ -642,8 +643,7 @@ def _attend(call, plan, dev, cache, k_cache, q, new_start, length, max_new, max_
     return out
 
 
-_scratch_bytes = {}                 # of a call's sizes
-_linear_bytes = {}
+_scratch_bytes, _kv4_scratch_bytes, _linear_bytes = {}, {}, {}         # of a call's sizes
 
 
 def _remember(size, need, memory=_scratch_bytes):
@@ -724,7 +724,7 @@ def norm_rope_append_kv4(q, k, v, cache, new_start, length, max_new=None, max_le
     ``norm_rope_append``.  Returns ``out`` [rows, q heads, 128].
     """
     dev = _device()
-    return _append(lib().qlin_norm_rope_append_four_bit, dev, _kv4_cache(cache, dev), cache[0], q, k, v, new_start, length,
+    return _append((_lib or lib()).qlin_norm_rope_append_four_bit, dev, _kv4_cache(cache, dev), cache[0], q, k, v, new_start, length,
                    max_new, max_len, cache_start, q_norm, k_norm, eps, inv_freq, interleaved, out)
 
 
@@ -757,8 +757,9 @@ def causal_attention_kv4(q, cache, new_start, length, max_new=None, max_len=None
     tokens, give the longest length.  Returns ``out`` [rows, q heads, 128].
     """
     dev = _device()
-    return _attend(lib().qlin_causal_attention_four_bit, lib().qlin_causal_four_bit_plan, dev, _kv4_cache(cache, dev), cache[0], q,
-                   new_start, length, max_new, max_len, cache_start, scale, splits, out, workspace)
+    L = _lib or lib()
+    return _attend(L.qlin_causal_attention_four_bit, L.qlin_causal_four_bit_plan, _kv4_scratch_bytes, dev, _kv4_cache(cache, dev), cache[0],
+                   q, new_start, length, max_new, max_len, cache_start, scale, splits, out, workspace)
 
 
 def _rows_of(name, t, dtype, dev, shape=None):
