@@ -26,7 +26,7 @@
 //       work: 32 sequences of 16 tokens over 4096 keys 65 to 69 us, the vector unit busy for 73 % of
 //       them, the matrix cores for 25.  Few blocks leave both idle: five of 517 to 8192 keys 38 and 10 %
 //       of 23 us, in which a wave has four steps at most, behind its start and before the sums of
-//       four waves are merged.  16 tokens over 8192 keys 15.6, 512 without a prefix 13.7.  Tiles of
+//       four waves are merged.  16 tokens over 8192 keys 15.4, 512 without a prefix 13.3.  Tiles of
 //       64 rows with one extraction for both, alone on a compute unit: 78 and 19.0 us.
 //   k_kv4_peaks, k_unpack_kv4   the cache in 16 bits, bf16 for a caller and f16 for
 //       k_causal_prompt, which long chunks go through (causal.hip): its 11 bits keep the result as
